@@ -1,0 +1,528 @@
+"""Timing cases of the cache's position rotation and of the 8-bit rolling cache.
+
+A case is a dict of plain values; ``op`` says which entry point it calls:
+
+* ``rotate``  ``fkv_rotate_chunk``: the chunk's queries and keys, as the
+              projection leaves them, rotated by position and laid out for the
+              chunk attention, the values laid out beside them;
+* ``append``  ``fkv_append_frames_rotated``: a finished chunk's frames into
+              their cache slots, the keys rotated on the way;
+* ``append8`` ``fkv_append_frames_q8``: the same into a cache held in 8 bits
+              (E4M3) with a scale for each head and block of tokens;
+* ``score``   ``fkv_score_select_q8``: segment similarity and BottomK selection
+              of the dynamic heads from that cache's keys;
+* ``attend``  ``fkv_chunk_attention_q8``: attention of any number of query
+              tokens over every head's kept history in that cache and the
+              current tokens.
+
+Sizes: ``heads`` heads of ``d``, F tokens per frame in rows of ``row``, H
+history frames in ``cap`` slots, C new frames, blocks of ``block`` tokens,
+segments of L tokens; ``n_static`` heads are static (sink frame + ``recent``
+frames), the others dynamic (sink frame + the fraction ``keep`` of the
+segments).  ``layout`` is "token" for views of one [tokens][3][heads][d]
+projection, "head" for contiguous [heads][tokens][d].
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+_DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+THETA = 10000.0
+E4M3_MAX = 448.0
+EXP_MIN, EXP_MAX = -100, 119          # exponents of a block's scale
+
+
+def _case(name, op, **kw):
+    c = dict(op=op, dtype="bf16", heads=12, d=128, F=1560, row=52, H=21, cap=21, C=3, first=18, layout="token",
+             pairing="adjacent", pairs="22/21/21", linear=False, block=64, L=1560, n_static=6, recent=6, keep=0.5,
+             n_q=4680, n_cur=4680, lse=False)
+    if name:
+        c["name"] = name
+    c.update(kw)
+    return c
+
+
+def listed():
+    return [
+        # an AR step's queries, keys and values at 480P: 3 frames of 30 x 52 patches, three position axes
+        _case("rotate-480p", "rotate"),
+        # one token of a one-dimensional sequence: the smallest call, where launch and host time count
+        _case("rotate-token", "rotate", dtype="f32", heads=16, d=64, F=1, row=1, C=1, first=4097, layout="head",
+              pairing="halves", pairs="32/0/0"),
+        # a finished chunk at 1080P: the largest write
+        _case("append-1080p", "append", F=8160, row=120),
+        # odd sizes, half the channels rotated, positions that run on from token to token, fp32
+        _case("append-odd-f32", "append", dtype="f32", heads=16, d=64, F=333, row=37, C=2, first=1000, H=13, cap=16,
+              layout="head", pairing="halves", pairs="16/0/0", linear=True),
+        # a finished 480P chunk into the 8-bit cache
+        _case("append8-480p", "append8"),
+        # one token into the 8-bit cache
+        _case("append8-token", "append8", heads=16, d=64, F=1, row=1, C=1, H=200, cap=256, first=4097,
+              pairing="halves", pairs="32/0/0", block=16),
+        # scoring and selection of a 480P layer, one frame per segment
+        _case("score-480p", "score"),
+        # ragged: three segments per frame, blocks that end inside a segment
+        _case("score-small", "score", heads=16, d=64, F=333, row=37, H=13, cap=16, C=2, L=111, n_static=8, recent=3,
+              block=32),
+        # the chunk's attention of a 480P layer: the largest
+        _case("attend-480p", "attend"),
+        # one query token over a whole 480P window: the bytes of the cache bound it
+        _case("attend-one-480p", "attend", n_static=12, recent=21, n_q=1, n_cur=1, lse=True),
+        # a small model's chunk, head_dim 64 and ragged sizes
+        _case("attend-small", "attend", heads=16, d=64, F=333, row=37, H=13, cap=16, C=2, L=111, n_static=8, recent=3,
+              block=32, n_q=666, n_cur=666),
+        # a few query tokens over a short cache of odd frames: latency
+        _case("attend-few", "attend", heads=4, d=64, F=75, row=15, H=9, cap=9, C=1, L=25, n_static=2, recent=2,
+              block=16, n_q=5, n_cur=0, lse=True),
+    ]
+
+
+def draw(rng):
+    def log_int(lo, hi):
+        return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+    while True:
+        op = rng.choice(["rotate", "append", "append8", "score", "attend", "attend"])
+        d = rng.choice([64, 128, 128])
+        heads = rng.randint(1, 24)
+        C = rng.randint(1, 4)
+        row = log_int(1, 128)
+        F = row * log_int(1, 68) if rng.random() < 0.8 else rng.randint(1, 5)
+        row = min(row, F)
+        if op in ("score", "attend"):
+            seg = rng.choice(["frame", "sub", "multi"])
+            n = rng.randint(2, 12)
+            if seg == "sub":
+                F = n * log_int(1, 600)
+                L = F // n
+            else:
+                L = F if seg == "frame" else F * rng.randint(2, 4)
+            row = min(row, F)
+        else:
+            L = F
+        H = rng.randint(1, 24)
+        cap = max(H, C) + rng.randint(0, 3)
+        half = d // 2
+        if rng.random() < 0.5:
+            a = half // 3
+            pairs = "%d/%d/%d" % (half - 2 * a, a, a)
+        else:
+            pairs = "%d/0/0" % rng.choice([half, half // 2])
+        n_q = {"one": 1, "few": rng.randint(2, 16), "some": log_int(17, 600), "chunk": C * F}[
+            rng.choice(["one", "few", "some", "chunk"])]
+        n_cur = rng.choice([n_q, n_q, rng.choice([0, 1, rng.randint(1, 300)])])
+        c = _case(None, op, dtype=rng.choice(["bf16", "bf16", "f32"]) if op in ("rotate", "append", "append8") else "bf16",
+                  heads=heads, d=d, F=F, row=row, H=H, cap=cap, C=C, first=log_int(1, 100000),
+                  layout=rng.choice(["token", "token", "head"]), pairing=rng.choice(["adjacent", "halves"]), pairs=pairs,
+                  linear=pairs.endswith("/0/0") and rng.random() < 0.5, block=rng.choice([16, 32, 64, 128]), L=L,
+                  n_static=rng.randint(0, heads), recent=rng.randint(1, 6), keep=round(rng.uniform(0.15, 0.9), 2),
+                  n_q=n_q, n_cur=n_cur, lse=op == "attend" and rng.random() < 0.4)
+        if F > 8160 or -(-H * F // L) > 4096 or (op == "score" and c["n_static"] == heads):
+            continue
+        w = work(c)
+        if w["flops"] <= 5.3e11 and w["bytes"] <= 3e8 and heads * H * F * d <= 1.2e8:
+            return c
+
+
+# ------------------------------------------------------------------ budgets
+def _budgets(c):
+    """(type, sink, recent, keep_k, scope) of each head."""
+    F, H, L = c["F"], c["H"], c["L"]
+    if L < F:
+        dyn = (1, 1, 0, int(F // L * c["keep"]), 0)
+    else:
+        m = L // F
+        dyn = (1, 1, 0, int((-(-H // m) - 1) * c["keep"]), 1)
+    return [(0, 1, c["recent"], 0, 1) if h < c["n_static"] else dyn for h in range(c["heads"])]
+
+
+def _kept_tokens(c):
+    """Retained history tokens of each head (a short last segment counted as it comes out longest)."""
+    F, H, L = c["F"], c["H"], c["L"]
+    out = []
+    for kind, sink, recent, k, scope in _budgets(c):
+        if kind == 0:
+            out.append(min(H, sink + recent) * F)
+        elif scope == 0:
+            out.append(min(sink, H) * F + max(H - sink, 0) * min(k, F // L) * L)
+        else:
+            n_seg = -(-H * F // L)
+            out.append(min((1 + min(k, n_seg - 1)) * L, H * F))
+    return out
+
+
+def work(case):
+    c, es = case, 2 if case["dtype"] == "bf16" else 4
+    heads, d, F, H = c["heads"], c["d"], c["F"], c["H"]
+    new = heads * c["C"] * F * d
+    scales = 4.0 / c["block"] / d            # bytes of scales for each cached element
+    if c["op"] == "rotate":
+        return {"bytes": 6.0 * new * es, "flops": 6.0 * new}
+    if c["op"] == "append":
+        return {"bytes": 4.0 * new * es, "flops": 3.0 * new}
+    if c["op"] == "append8":
+        return {"bytes": 2.0 * new * (es + 1 + scales), "flops": 3.0 * new + 4.0 * new}
+    if c["op"] == "score":
+        n = (heads - c["n_static"]) * F * d
+        return {"bytes": n * (H * (1 + scales) + 2.0), "flops": 4.0 * n * H}
+    kept, n_cur, n_q = sum(_kept_tokens(c)), c["n_cur"], c["n_q"]
+    return {"bytes": kept * 2.0 * d * (1 + scales) + heads * (n_cur + n_q) * 4.0 * d + (4.0 * heads * n_q if c["lse"] else 0),
+            "flops": 4.0 * d * n_q * (kept + heads * n_cur)}
+
+
+# ------------------------------------------------------------------- inputs
+def _quantised(x, block):
+    """E4M3 codes and power-of-two scales of x [..., F, d], one scale for each block of tokens: the smallest
+    power of two that brings the block's largest magnitude to 448 or less."""
+    F = x.shape[-2]
+    nb = -(-F // block)
+    mag = torch.nn.functional.pad(x.abs(), (0, 0, 0, nb * block - F)).unflatten(-2, (nb, block))
+    top = torch.where(torch.isfinite(mag), mag, torch.zeros_like(mag)).amax((-1, -2))
+    m, e = torch.frexp(top)                               # top = m 2^e, 0.5 <= m < 1
+    k = torch.where(m > 0.875, e - 8, e - 9).clamp(EXP_MIN, EXP_MAX)   # 448 = 0.875 * 2^9
+    k = torch.where(top > 0, k, torch.zeros_like(k))
+    scale = ((k + 127).to(torch.int32) << 23).view(torch.float32)      # 2^k
+    y = x / scale.repeat_interleave(block, -1)[..., :F, None]
+    return y.clamp(-E4M3_MAX, E4M3_MAX).to(torch.float8_e4m3fn), scale
+
+
+def _chunk(c, g, dt):
+    """Q, K and V of C new frames as [heads][tokens][d] tensors; keys with channels of unlike size."""
+    n, heads, d = c["C"] * c["F"], c["heads"], c["d"]
+    gain = torch.exp(0.4 * torch.randn((3, heads, d), generator=g, device="cuda"))
+    x = (torch.randn((n, 3, heads, d), generator=g, device="cuda") * gain).to(dt)
+    views = [x[:, i].transpose(0, 1) for i in range(3)]
+    return views if c["layout"] == "token" else [v.contiguous() for v in views]
+
+
+def _cache(c, g):
+    """An 8-bit cache whose keys follow an AR(1) chain from frame to frame, its slots in another order than its frames."""
+    heads, d, F, H, cap = c["heads"], c["d"], c["F"], c["H"], c["cap"]
+    gain = torch.exp(0.4 * torch.randn((2, heads, 1, d), generator=g, device="cuda"))
+    slots = np.random.default_rng(int(torch.randint(0, 1 << 30, (1,), generator=g, device="cuda"))).permutation(cap)[:H]
+    K = torch.randn((heads, cap, F, d), generator=g, device="cuda")
+    V = torch.randn((heads, cap, F, d), generator=g, device="cuda") * gain[1].unsqueeze(1)
+    x = None
+    for t in range(H + 1):
+        eps = torch.randn((heads, F, d), generator=g, device="cuda")
+        x = eps if x is None else 0.9 * x + math.sqrt(1 - 0.81) * eps
+        if t < H:
+            K[:, int(slots[t])] = x * gain[0]
+    K8, ks = _quantised(K, c["block"])
+    V8, vs = _quantised(V, c["block"])
+    return dict(K8=K8, V8=V8, k_scale=ks, v_scale=vs, next_keys=x * gain[0]), [int(s) for s in slots]
+
+
+def _kept_segments(c, seed):
+    """A selection as the dynamic heads' budgets allow it: ascending ids, -1 after them, and the tokens kept."""
+    F, H, L, heads = c["F"], c["H"], c["L"], c["heads"]
+    n_seg = -(-H * F // L)
+    kept = np.full((heads, n_seg), -1, np.int32)
+    kv_len = np.zeros(heads, np.int32)
+    rng = np.random.default_rng(seed)
+    for h, (kind, sink, recent, k, scope) in enumerate(_budgets(c)):
+        if kind == 0:
+            kv_len[h] = min(H, sink + recent) * F
+            continue
+        if scope == 0:
+            per = F // L
+            ids = [list(range(per))] + [t * per + np.sort(rng.permutation(per)[:min(k, per)]) for t in range(1, H)]
+            ids = np.concatenate(ids).astype(np.int32)
+        else:
+            ids = np.concatenate([[0], 1 + np.sort(rng.permutation(n_seg - 1)[:k])]).astype(np.int32)
+        kept[h, :len(ids)] = ids
+        kv_len[h] = sum(min(L, H * F - int(g) * L) for g in ids)
+    return kept, kv_len
+
+
+def prepare(case, seed):
+    c = dict(case)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    dt = _DT[c["dtype"]]
+    heads, d, F, cap = c["heads"], c["d"], c["F"], c["cap"]
+    s = dict(c=c, pos=[c["first"] + f * (F if c["linear"] else 1) for f in range(c["C"])])
+    if c["op"] == "rotate":
+        s["Q"], s["K"], s["V"] = _chunk(c, g, dt)
+        for name in ("Qr", "Kr", "Vr"):
+            s[name] = torch.empty((heads, c["C"] * F, d), dtype=dt, device="cuda")
+    elif c["op"] in ("append", "append8"):
+        _, s["K"], s["V"] = _chunk(c, g, dt)
+        s["slots"] = [int(v) for v in np.random.default_rng(seed).permutation(cap)[:c["C"]]]
+        if c["op"] == "append":
+            s["K_hist"] = torch.zeros((heads, cap, F, d), dtype=dt, device="cuda")
+            s["V_hist"] = torch.zeros_like(s["K_hist"])
+        else:
+            nb = -(-F // c["block"])
+            s["K8"] = torch.zeros((heads, cap, F, d), dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+            s["V8"] = torch.zeros((heads, cap, F, d), dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+            s["k_scale"] = torch.ones((heads, cap, nb), device="cuda")
+            s["v_scale"] = torch.ones((heads, cap, nb), device="cuda")
+    else:
+        cache, s["slots"] = _cache(c, g)
+        next_keys = cache.pop("next_keys")
+        s.update(cache)
+        if c["op"] == "score":
+            n_seg = -(-c["H"] * F // c["L"])
+            s["K_cur"] = torch.randn((heads, c["C"] * F, d), generator=g, device="cuda").to(dt)
+            s["K_cur"][:, :F] = next_keys.to(dt)
+            s["scores"] = torch.zeros((heads, n_seg), device="cuda")
+            s["kept"] = torch.full((heads, n_seg), -1, dtype=torch.int32, device="cuda")
+            s["kv_len"] = torch.zeros(heads, dtype=torch.int32, device="cuda")
+        else:
+            kept, kv_len = _kept_segments(c, seed)
+            s["kept"], s["kv_len"] = torch.from_numpy(kept).cuda(), torch.from_numpy(kv_len).cuda()
+            rows = lambda n: torch.randn((heads, n, d), generator=g, device="cuda").to(dt)  # noqa: E731
+            s["Q"], s["K_cur"], s["V_cur"] = rows(c["n_q"]), rows(c["n_cur"]), rows(c["n_cur"])
+            s["O"] = torch.empty_like(s["Q"])
+            s["lse"] = torch.empty((heads, c["n_q"]), device="cuda") if c["lse"] else None
+    return s
+
+
+# -------------------------------------------------------------- plain forms
+def _angles(c, pos):
+    """Angle of each token and channel pair, fp64 [C*F][d/2]: the position on the pair's axis times its frequency."""
+    F, half = c["F"], c["d"] // 2
+    nt, nr, nc = (int(v) for v in c["pairs"].split("/"))
+    p = torch.arange(F, device="cuda", dtype=torch.float64)
+    t = torch.tensor(pos, device="cuda", dtype=torch.float64)[:, None] + (p if c["linear"] else 0 * p)
+    row = torch.floor(p / c["row"]).expand_as(t)
+    col = torch.remainder(p, c["row"]).expand_as(t)
+    freq = lambda n: THETA ** (-torch.arange(n, device="cuda", dtype=torch.float64) / max(n, 1))  # noqa: E731
+    ang = torch.cat([t[..., None] * freq(nt), row[..., None] * freq(nr), col[..., None] * freq(nc),
+                     t.new_zeros(t.shape + (half - nt - nr - nc,))], -1)
+    return ang.reshape(-1, half)
+
+
+def _rotated(c, x, pos):
+    """x [heads][C*F][d] with every channel pair turned by its angle, in 32 bits."""
+    ang = _angles(c, pos)
+    cos, sin = torch.cos(ang).float(), torch.sin(ang).float()
+    x = x.float()
+    if c["pairing"] == "adjacent":
+        a, b = x[..., 0::2], x[..., 1::2]
+        return torch.stack([a * cos - b * sin, a * sin + b * cos], -1).flatten(-2)
+    a, b = x.chunk(2, -1)
+    return torch.cat([a * cos - b * sin, a * sin + b * cos], -1)
+
+
+def _frames(c, x):
+    return x.reshape(c["heads"], c["C"], c["F"], c["d"])
+
+
+def _values(s, name, kind=torch.float32):
+    """The cache's values as numbers, frames in logical order: [heads][H*F][d]."""
+    c = s["c"]
+    at = torch.tensor(s["slots"], device="cuda")
+    x = s[name].view(torch.uint8)[:, at].view(torch.float8_e4m3fn).to(kind)
+    sc = s[("k" if name == "K8" else "v") + "_scale"][:, at].to(kind)
+    x = x * sc.repeat_interleave(c["block"], -1)[..., :c["F"], None]
+    return x.flatten(1, 2)
+
+
+def _plain_score(s):
+    c = s["c"]
+    heads, d, F, H, L = c["heads"], c["d"], c["F"], c["H"], c["L"]
+    x = torch.cat([_values(s, "K8"), s["K_cur"][:, :F].float()], 1)[c["n_static"]:].double()
+    a, b = x[:, :-F], x[:, F:]
+    n_seg = s["scores"].shape[1]
+    def sums(v):
+        v = torch.nn.functional.pad(v.sum(-1), (0, n_seg * L - H * F))
+        return v.unflatten(1, (n_seg, L)).sum(-1)
+    norm = sums(a * a) * sums(b * b)
+    score = torch.where(norm > 0, sums(a * b) / norm.sqrt(), torch.zeros_like(norm)).float()
+    _, sink, _, k, scope = _budgets(c)[-1]
+    first_frame = torch.arange(n_seg, device="cuda") * L // F
+    forced = (first_frame < sink).expand_as(score)
+    group = F // L if scope == 0 else n_seg
+    order = torch.where(forced, torch.full_like(score, math.inf), score).unflatten(1, (n_seg // group, group))
+    order = torch.argsort(order, dim=-1, stable=True)                      # the least similar first, ties by the lower index
+    rank = torch.empty_like(order).scatter_(-1, order, torch.arange(group, device="cuda").expand_as(order).contiguous())
+    keep = forced | (rank.flatten(1) < k)
+    ids = torch.arange(n_seg, device="cuda")
+    place = torch.where(keep, ids, n_seg).sort(-1).values
+    tokens = torch.where(keep, torch.clamp(H * F - ids * L, max=L), 0).sum(-1)
+    s["scores"][c["n_static"]:] = score
+    s["kept"][c["n_static"]:] = torch.where(place < n_seg, place, -1).int()
+    s["kv_len"][c["n_static"]:] = tokens.int()
+    return [s["scores"], s["kept"], s["kv_len"]]
+
+
+def _kept_mask(s):
+    """Which history tokens each head keeps, [heads][H*F]."""
+    c = s["c"]
+    F, H, L = c["F"], c["H"], c["L"]
+    frame = torch.arange(H * F, device="cuda") // F
+    static = (frame < 1) | (frame >= H - c["recent"])
+    seg = torch.zeros((c["heads"], s["kept"].shape[1] + 1), dtype=torch.bool, device="cuda")
+    seg.scatter_(1, torch.where(s["kept"] < 0, s["kept"].shape[1], s["kept"]).long(), True)
+    dyn = seg[:, :-1].repeat_interleave(L, 1)[:, :H * F]
+    return torch.cat([static.expand(c["n_static"], -1), dyn[c["n_static"]:]])
+
+
+def _plain_attend(s):
+    c = s["c"]
+    keep = _kept_mask(s)
+    n = max(_kept_tokens(c))
+    at = torch.argsort(keep.to(torch.int8), dim=1, descending=True, stable=True)[:, :n]     # each head's kept tokens, then others
+    here = torch.nn.functional.pad(keep.gather(1, at), (0, c["n_cur"]), value=True)
+    rows = at[..., None].expand(-1, -1, c["d"])
+    K = torch.cat([_values(s, "K8").gather(1, rows), s["K_cur"].float()], 1)
+    V = torch.cat([_values(s, "V8").gather(1, rows), s["V_cur"].float()], 1)
+    z = torch.bmm(s["Q"].float(), K.transpose(1, 2).contiguous()) / math.sqrt(c["d"])
+    z.masked_fill_(~here[:, None], -math.inf)
+    top = z.amax(-1, keepdim=True)
+    p = z.sub_(top).exp_()
+    total = p.sum(-1, keepdim=True)
+    s["O"].copy_(torch.bmm(p, V) / total)
+    if s["lse"] is None:
+        return [s["O"]]
+    s["lse"].copy_((top + total.log())[..., 0])
+    return [s["O"], s["lse"]]
+
+
+# -------------------------------------------------------------------- passes
+def _shape(c):
+    import paper_2605_09681_amd as fkv
+    return fkv.make_shape(c["heads"], c["d"], c["F"], c["H"], c["cap"], c["C"], c["L"], c["dtype"])
+
+
+def _rope(c):
+    import paper_2605_09681_amd as fkv
+    nt, nr, nc = (int(v) for v in c["pairs"].split("/"))
+    return fkv.make_rope(nt, nr, nc, row_tokens=c["row"], token_step=int(c["linear"]), theta=THETA,
+                         pairing=fkv.FKV_PAIR_ADJACENT if c["pairing"] == "adjacent" else fkv.FKV_PAIR_HALVES)
+
+
+def _call(s):
+    """The calls that a program makes, with the plan and the workspace that it keeps from pass to pass."""
+    import paper_2605_09681_amd as fkv
+    c, op = s["c"], s["c"]["op"]
+    if "shape" not in s:
+        s["shape"], s["rope"], s["heads"] = _shape(c), _rope(c), fkv.make_heads(_budgets(c))
+        if "K8" in s:
+            s["cache"] = fkv.Cache8(s["K8"], s["V8"], s["k_scale"], s["v_scale"], c["block"])
+        if op in ("score", "attend"):
+            n = (fkv.fkv_score_workspace_size(s["shape"], s["heads"]) if op == "score" else
+                 fkv.fkv_chunk_attention_q8_workspace_size(s["shape"], s["heads"], c["n_q"], c["n_cur"]))
+            s["ws"] = torch.zeros(max(n, 1), dtype=torch.uint8, device="cuda")
+    if op == "rotate":
+        fkv.fkv_rotate_chunk(s["shape"], s["rope"], s["pos"], s["Q"], s["K"], s["V"], s["Qr"], s["Kr"], s["Vr"])
+        return [s["Qr"], s["Kr"], s["Vr"]]
+    if op == "append":
+        fkv.fkv_append_frames_rotated(s["shape"], s["rope"], s["pos"], s["K"], s["V"], s["slots"], s["K_hist"], s["V_hist"])
+        return [s["K_hist"], s["V_hist"]]
+    if op == "append8":
+        fkv.fkv_append_frames_q8(s["shape"], s["rope"], s["pos"], s["K"], s["V"], s["slots"], s["cache"])
+        return [s["K8"], s["V8"], s["k_scale"], s["v_scale"]]
+    if op == "score":
+        fkv.fkv_score_select_q8(s["shape"], s["heads"], s["cache"], s["slots"], s["K_cur"], s["scores"], s["kept"],
+                                s["kv_len"], s["ws"])
+        return [s["scores"], s["kept"], s["kv_len"]]
+    fkv.fkv_chunk_attention_q8(s["shape"], s["heads"], s["cache"], s["slots"], s["kept"], s["kv_len"], s["Q"],
+                               s["K_cur"], s["V_cur"], 1 / math.sqrt(c["d"]), s["O"], s["lse"], s["ws"])
+    return [s["O"]] if s["lse"] is None else [s["O"], s["lse"]]
+
+
+def run(state):
+    s, c = state, state["c"]
+    if own:
+        return _call(s)
+    if c["op"] == "rotate":
+        s["Qr"].copy_(_rotated(c, s["Q"], s["pos"]))
+        s["Kr"].copy_(_rotated(c, s["K"], s["pos"]))
+        s["Vr"].copy_(s["V"])
+        return [s["Qr"], s["Kr"], s["Vr"]]
+    if c["op"] == "append":
+        at = torch.tensor(s["slots"], device="cuda")
+        s["K_hist"][:, at] = _frames(c, _rotated(c, s["K"], s["pos"])).to(s["K_hist"].dtype)
+        s["V_hist"][:, at] = _frames(c, s["V"])
+        return [s["K_hist"], s["V_hist"]]
+    if c["op"] == "append8":
+        at = torch.tensor(s["slots"], device="cuda")
+        k8, ks = _quantised(_frames(c, _rotated(c, s["K"], s["pos"])), c["block"])
+        v8, vs = _quantised(_frames(c, s["V"].float()), c["block"])
+        s["K8"].view(torch.uint8)[:, at] = k8.view(torch.uint8)
+        s["V8"].view(torch.uint8)[:, at] = v8.view(torch.uint8)
+        s["k_scale"][:, at], s["v_scale"][:, at] = ks, vs
+        return [s["K8"], s["V8"], s["k_scale"], s["v_scale"]]
+    return _plain_score(s) if c["op"] == "score" else _plain_attend(s)
+
+
+# --------------------------------------------------------------------- exact
+def _turned64(c, x, pos):
+    """The rotation in 64 bits as products of complex numbers, frame by frame."""
+    F, half = c["F"], c["d"] // 2
+    counts = [int(v) for v in c["pairs"].split("/")]
+    out = []
+    for f, t0 in enumerate(pos):
+        y = x[:, f * F:(f + 1) * F].double()
+        z = torch.complex(y[..., 0::2], y[..., 1::2]) if c["pairing"] == "adjacent" else torch.complex(y[..., :half], y[..., half:])
+        p = np.arange(F)
+        axes = [t0 + (p if c["linear"] else 0 * p), p // c["row"], p % c["row"]]
+        turn = np.ones((F, half), np.complex128)
+        j0 = 0
+        for n, at in zip(counts, axes):
+            for j in range(n):
+                turn[:, j0 + j] = np.exp(1j * (at * THETA ** (-j / n)))
+            j0 += n
+        z = z * torch.from_numpy(turn).cuda()
+        out.append(torch.stack([z.real, z.imag], -1).flatten(-2) if c["pairing"] == "adjacent" else torch.cat([z.real, z.imag], -1))
+    return torch.cat(out, 1)
+
+
+def _blocks64(x, block):
+    """x over its block's scale, not rounded, and the scales: x [heads][frames][F][d] in 64 bits."""
+    y, scales = torch.empty_like(x), []
+    power = lambda k: ((k.long() + 1023) << 52).view(torch.float64)  # noqa: E731
+    for b0 in range(0, x.shape[2], block):
+        part = x[:, :, b0:b0 + block]
+        top = part.abs().amax((2, 3))
+        k = torch.ceil(torch.log2(top / E4M3_MAX))
+        k = k.clamp(EXP_MIN, EXP_MAX)
+        k = torch.where(top <= E4M3_MAX * power(k - 1), k - 1, torch.where(top > E4M3_MAX * power(k), k + 1, k))
+        sc = torch.where(top > 0, power(k.clamp(EXP_MIN, EXP_MAX)), torch.ones_like(top))
+        y[:, :, b0:b0 + block] = part / sc[..., None, None]
+        scales.append(sc)
+    return y, torch.stack(scales, -1)
+
+
+def _into(full, part, slots):
+    out = full.double()
+    for f, sl in enumerate(slots):
+        out[:, sl] = part[:, f]
+    return out
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    c, H, F, L, d = s["c"], s["c"]["H"], s["c"]["F"], s["c"]["L"], s["c"]["d"]
+    if c["op"] == "rotate":
+        return [_turned64(c, s["Q"], s["pos"]), _turned64(c, s["K"], s["pos"]), s["V"].double()]
+    if c["op"] in ("append", "append8"):
+        K, V = _frames(c, _turned64(c, s["K"], s["pos"])), _frames(c, s["V"].double())
+        if c["op"] == "append":
+            return [_into(s["K_hist"], K, s["slots"]), _into(s["V_hist"], V, s["slots"])]
+        (k, ks), (v, vs) = _blocks64(K, c["block"]), _blocks64(V, c["block"])
+        return [_into(s["K8"], k, s["slots"]), _into(s["V8"], v, s["slots"]), _into(s["k_scale"], ks, s["slots"]),
+                _into(s["v_scale"], vs, s["slots"])]
+    K = _values(s, "K8", torch.float64)
+    if c["op"] == "score":
+        out = s["scores"].double()
+        K = torch.cat([K, s["K_cur"][:, :F].double()], 1)
+        for g in range(out.shape[1]):
+            lo, hi = g * L, min(g * L + L, H * F)
+            a, b = K[c["n_static"]:, lo:hi].flatten(1), K[c["n_static"]:, lo + F:hi + F].flatten(1)
+            out[c["n_static"]:, g] = (a * b).sum(1) / ((a * a).sum(1) * (b * b).sum(1)).sqrt()
+        return [out, None, None]
+    V = _values(s, "V8", torch.float64)
+    O, lse, keep = [], [], _kept_mask(s)
+    for h in range(c["heads"]):
+        k = torch.cat([K[h][keep[h]], s["K_cur"][h].double()])
+        v = torch.cat([V[h][keep[h]], s["V_cur"][h].double()])
+        z = s["Q"][h].double() @ k.T.contiguous() / math.sqrt(d)
+        lse.append(torch.logsumexp(z, 1))
+        O.append(torch.softmax(z, 1) @ v)
+    return [torch.stack(O)] if s["lse"] is None else [torch.stack(O), torch.stack(lse)]
