@@ -386,7 +386,8 @@ def _plain_attend(s):
 # -------------------------------------------------------------------- passes
 def _shape(c):
     import paper_2605_09681_amd as fkv
-    return fkv.make_shape(c["heads"], c["d"], c["F"], c["H"], c["cap"], c["C"], c["L"], c["dtype"])
+    L = c["L"] if c["op"] in ("score", "attend") else c["F"]          # (no segments otherwise)
+    return fkv.make_shape(c["heads"], c["d"], c["F"], c["H"], c["cap"], c["C"], L, c["dtype"])
 
 
 def _rope(c):
