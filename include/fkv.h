@@ -506,6 +506,138 @@ fkv_status fkv_chunk_attention_fp8(const fkv_shape *shape, const void *Q8,
                                    void *workspace, size_t workspace_bytes,
                                    void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Position rotation and the 8-bit rolling cache.
+ *
+ * Rotation (rotary position embedding over up to three axes, as video
+ * transformers use it): channel pair j of a query or key, (x, y), becomes
+ *   (x cos a - y sin a, x sin a + y cos a),  a = position * theta^(-i / n),
+ * where the pairs are dealt to the axes in order: the first frame_pairs turn
+ * by the frame position, the next row_pairs by the token's row, the next
+ * col_pairs by its column (i = index within the axis' n pairs), the others stay
+ * as they are.  Token p of a frame is at row p / row_tokens, column p %
+ * row_tokens; its frame position is frame_pos[f] + p * token_step (token_step
+ * 1 with frame_pos[f] = the position of the frame's first token is the
+ * one-dimensional order of a token sequence; 0 gives a whole frame one
+ * position).  frame_pos is a HOST array, |frame_pos[f]| <= FKV_MAX_POSITION.
+ * Pair j is channels (2j, 2j + 1) (FKV_PAIR_ADJACENT) or (j, j + d/2)
+ * (FKV_PAIR_HALVES).  Angles are reduced in fp64; the products are fp32, and
+ * each result is rounded once to the output's type. */
+#define FKV_MAX_POSITION (1 << 24)
+typedef enum { FKV_PAIR_ADJACENT = 0, FKV_PAIR_HALVES = 1 } fkv_pairing;
+typedef struct {
+    int32_t frame_pairs, row_pairs, col_pairs; /* >= 0, their sum <= d/2 */
+    int32_t row_tokens;  /* 1..F */
+    int32_t token_step;  /* 0 or 1 */
+    int32_t pairing;     /* fkv_pairing */
+    double theta;        /* >= 1, finite */
+} fkv_rope;
+
+/* Rows of new tokens as a projection leaves them: row r of head h starts at
+ * element h * head_stride + r * token_stride of data (device memory, element
+ * type shape->dtype; the d channels of a row are adjacent).  data and both
+ * strides (>= 0) are multiples of 16 bytes.  Contiguous [n_heads][n][d] is
+ * {data, n * d, d}; one third of a projection [n][3][n_heads][d] is
+ * {data + third * n_heads * d, d, 3 * n_heads * d}. */
+typedef struct {
+    const void *data;
+    int64_t head_stride, token_stride; /* elements */
+} fkv_rows;
+
+/* The chunk's queries and keys, rotated, and its values, as the chunk
+ * attention takes them: Qr, Kr, Vr [n_heads][C*F][d] contiguous receive Q and K
+ * rotated (frame f at frame_pos[f], C entries) and V as it is.  A pair
+ * (Q, Qr), (K, Kr) or (V, Vr) of NULLs is left out; FKV_ERR_ARG if all are, or
+ * one of a pair is.  An output may be its own input when that is contiguous
+ * (in place); otherwise outputs overlap no input. */
+fkv_status fkv_rotate_chunk(const fkv_shape *shape, const fkv_rope *rope, const int32_t *frame_pos,
+                            const fkv_rows *Q, const fkv_rows *K, const fkv_rows *V, void *Qr,
+                            void *Kr, void *Vr, void *stream);
+
+/* fkv_append_frames with the keys rotated on the way: the n_frames frames of
+ * K_new / V_new (n_frames * F rows per head) are written to the slots
+ * dst_slot[f] of K_hist / V_hist, the keys of frame f rotated at frame_pos[f].
+ * Slots that are not listed keep their bytes.  dst_slot and its errors as in
+ * fkv_append_frames. */
+fkv_status fkv_append_frames_rotated(const fkv_shape *shape, const fkv_rope *rope,
+                                     const int32_t *frame_pos, const fkv_rows *K_new,
+                                     const fkv_rows *V_new, int32_t n_frames,
+                                     const int32_t *dst_slot, void *K_hist, void *V_hist,
+                                     void *stream);
+
+/* A rolling cache held in 8 bits (device memory, 16-byte aligned):
+ *   K8, V8           uint8 [n_heads][cap_frames][F][d]   E4M3 codes (OCP: no
+ *                    infinity, 0x7f / 0xff is NaN)
+ *   k_scale, v_scale float [n_heads][cap_frames][ceil(F / block_tokens)]
+ * Token p of a frame belongs to block p / block_tokens, and a cached element
+ * stands for code * scale of its block.  Scales are powers of two in [2^-100,
+ * 2^119] (readers use a scale's exponent alone): a scale moves a block into the
+ * range of E4M3 without a rounding of its own, and code * scale is exact in
+ * bf16, so reading the cache is reading the bf16 cache of the values it stands
+ * for.  block_tokens: 16, 32, 64 or 128. */
+typedef struct {
+    void *K8, *V8;
+    float *k_scale, *v_scale;
+    int32_t block_tokens;
+} fkv_cache8;
+
+/* fkv_append_frames into an 8-bit cache, the keys rotated on the way (rope
+ * NULL: as they are; frame_pos is then not read).  For every head, listed
+ * frame and block, for keys and for values: with amax the largest finite
+ * magnitude of the block's (rotated) elements, the block's scale is the
+ * smallest power of two 2^k with amax <= 448 * 2^k, k held to [-100, 119] (1
+ * where amax is 0), and its codes are the elements / 2^k rounded to nearest
+ * even, at most 448 in magnitude; an infinity or a NaN becomes NaN and leaves
+ * the other elements alone.  Elements are rotated in fp32 and rounded once,
+ * to 8 bits.  Slots that are not listed keep their codes and scales.  bf16 and
+ * fp32 rows; dst_slot and its errors as in fkv_append_frames. */
+fkv_status fkv_append_frames_q8(const fkv_shape *shape, const fkv_rope *rope,
+                                const int32_t *frame_pos, const fkv_rows *K_new,
+                                const fkv_rows *V_new, int32_t n_frames, const int32_t *dst_slot,
+                                const fkv_cache8 *cache, void *stream);
+
+/* fkv_score_select over an 8-bit cache: the same scores, kept_seg and kv_len,
+ * bit for bit, that fkv_score_select gives for a bf16 cache of the values that
+ * K8 stands for.  K_cur is bf16 (shape->dtype FKV_BF16: FKV_ERR_SHAPE
+ * otherwise).  V8 and v_scale are not read.  Workspace as in fkv_score_select. */
+fkv_status fkv_score_select_q8(const fkv_shape *shape, const fkv_head *heads,
+                               const fkv_cache8 *cache, const int32_t *frame_slot,
+                               const void *K_cur, float *scores, int32_t *kept_seg, int32_t *kv_len,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
+/* Attention of n_q query tokens over every head's kept history in an 8-bit
+ * cache and n_cur current tokens: for head h and query row r,
+ *   O[h][r] = softmax(scale * Q[h][r] . keys^T) . values
+ * with keys [kept tokens of head h; K_cur[h]] and likewise the values, no mask.
+ *   Q, O         bf16 [n_heads][n_q][d], n_q >= 1
+ *   K_cur, V_cur bf16 [n_heads][n_cur][d], n_cur >= 0 (may be NULL for 0)
+ *   lse          float [n_heads][n_q] (nullable): log sum_j exp(z_j)
+ * The kept tokens are those of fkv_chunk_attention_paged: the frames of a
+ * FKV_STATIC head's budget, the segments kept_seg[h] covering kv_len[h] tokens
+ * of a FKV_DYNAMIC head (kv_len read on the device, clamped to [0, H*F];
+ * kept_seg and kv_len are needed when a head is dynamic and H > 0).  Any F and
+ * L that fkv_shape allows; n_q and n_cur need not be the chunk's C*F.  A head
+ * without any key (nothing kept, n_cur = 0) gets O = 0 and lse = -infinity.
+ * bf16 only (FKV_ERR_SHAPE for FKV_F32; also n_q or n_cur rows of 2^31 bytes
+ * or more).  Products are bf16 with fp32 accumulation: codes times scales are
+ * exact, probabilities are rounded to bf16 for the value product.
+ *
+ * With a workspace of at least fkv_chunk_attention_q8_workspace_size bytes
+ * (its arguments as this call's; zero-filled before its first use, every call
+ * leaves it ready for the next; calls that share one are ordered by the
+ * caller) the work is split over the whole device: few query tokens along the
+ * keys, whose parts are joined by the last of them; with NULL one workgroup
+ * computes a query tile of a head from its first key to its last.
+ * FKV_ERR_CAPACITY if the workspace is smaller. */
+fkv_status fkv_chunk_attention_q8_workspace_size(const fkv_shape *shape, const fkv_head *heads,
+                                                 int32_t n_q, int32_t n_cur, size_t *bytes);
+fkv_status fkv_chunk_attention_q8(const fkv_shape *shape, const fkv_head *heads,
+                                  const fkv_cache8 *cache, const int32_t *frame_slot,
+                                  const int32_t *kept_seg, const int32_t *kv_len, const void *Q,
+                                  int32_t n_q, const void *K_cur, const void *V_cur, int32_t n_cur,
+                                  float scale, void *O, float *lse, void *workspace,
+                                  size_t workspace_bytes, void *stream);
+
 /* Message describing the calling thread's last non-OK status ("" if none). */
 const char *fkv_last_error(void);
 

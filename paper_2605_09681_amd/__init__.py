@@ -21,6 +21,12 @@ Entry points (see ``include/fkv.h`` for the full contract):
   -- the FP8 variant of the chunk attention (App. F)
 * :func:`fkv_attention_mass`, :func:`fkv_classify_heads` -- offline head
   profiling (Sec. 4.1, Eq. 1)
+* :func:`fkv_rotate_chunk`, :func:`fkv_append_frames_rotated` -- position
+  rotation of a chunk's queries and keys, and the cache write with it
+* :func:`fkv_append_frames_q8`, :func:`fkv_score_select_q8`,
+  :func:`fkv_chunk_attention_q8` -- a rolling cache held in 8 bits
+  (:class:`Cache8`): its write, its scoring and selection, and attention of any
+  number of query tokens over it
 * :func:`fkv_score_pooled`, :func:`fkv_select_compact_pooled` -- the
   first-block proxy of Sec. 4.3: one similarity row pooled over all heads,
   shared by the dynamic heads of every layer
@@ -40,7 +46,9 @@ FKV_OK, FKV_ERR_ARG, FKV_ERR_SHAPE, FKV_ERR_CAPACITY, FKV_ERR_DEVICE = range(5)
 FKV_BF16, FKV_F32 = 0, 1
 FKV_STATIC, FKV_DYNAMIC = 0, 1
 FKV_SCOPE_FRAME, FKV_SCOPE_GLOBAL = 0, 1
+FKV_PAIR_ADJACENT, FKV_PAIR_HALVES = 0, 1
 FKV_MAX_HEADS, FKV_MAX_FRAMES, FKV_MAX_SEGMENTS = 64, 256, 4096
+FKV_MAX_POSITION = 1 << 24
 
 EXPORTED = ("fkv_num_segments", "fkv_kept_tokens_max", "fkv_compress_static",
             "fkv_score_workspace_size", "fkv_score_segments", "fkv_select_compact",
@@ -52,7 +60,9 @@ EXPORTED = ("fkv_num_segments", "fkv_kept_tokens_max", "fkv_compress_static",
             "fkv_chunk_attention_static", "fkv_chunk_attention_paged",
             "fkv_fp8_sizes", "fkv_fp8_pack", "fkv_fp8_pack_paged",
             "fkv_chunk_attention_fp8", "fkv_attention_mass_workspace_size", "fkv_attention_mass",
-            "fkv_classify_heads", "fkv_last_error")
+            "fkv_classify_heads", "fkv_rotate_chunk", "fkv_append_frames_rotated", "fkv_append_frames_q8",
+            "fkv_score_select_q8", "fkv_chunk_attention_q8_workspace_size", "fkv_chunk_attention_q8",
+            "fkv_last_error")
 
 
 class FkvLibraryMissing(RuntimeError):
@@ -77,6 +87,21 @@ class fkv_head(ctypes.Structure):
     _fields_ = [("type", ctypes.c_int32), ("sink_frames", ctypes.c_int32),
                 ("recent_frames", ctypes.c_int32), ("keep_k", ctypes.c_int32),
                 ("scope", ctypes.c_int32)]
+
+
+class fkv_rope(ctypes.Structure):
+    _fields_ = [("frame_pairs", ctypes.c_int32), ("row_pairs", ctypes.c_int32), ("col_pairs", ctypes.c_int32),
+                ("row_tokens", ctypes.c_int32), ("token_step", ctypes.c_int32), ("pairing", ctypes.c_int32),
+                ("theta", ctypes.c_double)]
+
+
+class fkv_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("head_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64)]
+
+
+class fkv_cache8(ctypes.Structure):
+    _fields_ = [("K8", ctypes.c_void_p), ("V8", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("block_tokens", ctypes.c_int32)]
 
 
 _lib = None
@@ -149,6 +174,19 @@ def lib():
         L.fkv_attention_mass.restype = ctypes.c_int
         L.fkv_classify_heads.argtypes = [P, I32, I32, I32, I32, I32, F, P]
         L.fkv_classify_heads.restype = ctypes.c_int
+        Rp, Rw, C8 = ctypes.POINTER(fkv_rope), ctypes.POINTER(fkv_rows), ctypes.POINTER(fkv_cache8)
+        L.fkv_rotate_chunk.argtypes = [S, Rp, P, Rw, Rw, Rw, P, P, P, P]
+        L.fkv_rotate_chunk.restype = ctypes.c_int
+        L.fkv_append_frames_rotated.argtypes = [S, Rp, P, Rw, Rw, I32, P, P, P, P]
+        L.fkv_append_frames_rotated.restype = ctypes.c_int
+        L.fkv_append_frames_q8.argtypes = [S, Rp, P, Rw, Rw, I32, P, C8, P]
+        L.fkv_append_frames_q8.restype = ctypes.c_int
+        L.fkv_score_select_q8.argtypes = [S, Hd, C8, P, P, P, P, P, P, SZ, P]
+        L.fkv_score_select_q8.restype = ctypes.c_int
+        L.fkv_chunk_attention_q8_workspace_size.argtypes = [S, Hd, I32, I32, ctypes.POINTER(SZ)]
+        L.fkv_chunk_attention_q8_workspace_size.restype = ctypes.c_int
+        L.fkv_chunk_attention_q8.argtypes = [S, Hd, C8, P, P, P, P, I32, P, P, I32, F, P, P, P, SZ, P]
+        L.fkv_chunk_attention_q8.restype = ctypes.c_int
         L.fkv_last_error.argtypes = []
         L.fkv_last_error.restype = ctypes.c_char_p
         _lib = L
@@ -665,6 +703,201 @@ def fkv_classify_heads(mass, hist_frames: int, sink_frames: int = 1, transition_
     _raise(lib().fkv_classify_heads(m.ctypes.data_as(ctypes.c_void_p), n_heads, n_bins, int(hist_frames),
                                     int(sink_frames), int(transition_frames), ctypes.c_float(alpha), out))
     return list(out)
+
+
+# ---------------------------------------------------------------------------
+# position rotation and the 8-bit rolling cache
+# ---------------------------------------------------------------------------
+def make_rope(frame_pairs: int, row_pairs: int = 0, col_pairs: int = 0, row_tokens: int = 1, token_step: int = 0,
+              theta: float = 10000.0, pairing: int = FKV_PAIR_ADJACENT) -> fkv_rope:
+    """How channel pairs turn with position: the first ``frame_pairs`` by the
+    frame position, then ``row_pairs`` by the token's row and ``col_pairs`` by its
+    column in rows of ``row_tokens`` tokens (see fkv.h)."""
+    return fkv_rope(int(frame_pairs), int(row_pairs), int(col_pairs), int(row_tokens), int(token_step), int(pairing),
+                    float(theta))
+
+
+class Cache8:
+    """A rolling cache held in 8 bits: ``K``, ``V`` float8_e4m3fn
+    [n_heads][cap_frames][F][d] and ``k_scale``, ``v_scale`` float32
+    [n_heads][cap_frames][ceil(F / block_tokens)], powers of two."""
+
+    def __init__(self, K, V, k_scale, v_scale, block_tokens: int):
+        self.K, self.V, self.k_scale, self.v_scale, self.block_tokens = K, V, k_scale, v_scale, int(block_tokens)
+
+    @classmethod
+    def zeros(cls, shape: fkv_shape, block_tokens: int = 64, device="cuda"):
+        """An empty cache of the shape's slots (codes 0, scales 1)."""
+        size = (shape.n_heads, shape.cap_frames, shape.frame_tokens, shape.head_dim)
+        nb = -(-shape.frame_tokens // int(block_tokens))
+        code = lambda: torch.zeros(size, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)  # noqa: E731
+        scale = lambda: torch.ones(size[:2] + (nb,), dtype=torch.float32, device=device)  # noqa: E731
+        return cls(code(), code(), scale(), scale(), block_tokens)
+
+
+def _cache8(shape: fkv_shape, c: Cache8):
+    if not isinstance(c, Cache8):
+        raise TypeError("cache must be a Cache8")
+    if c.block_tokens not in (16, 32, 64, 128):
+        raise ValueError(f"block_tokens {c.block_tokens} is not 16, 32, 64 or 128")
+    size = (shape.n_heads, shape.cap_frames, shape.frame_tokens, shape.head_dim)
+    nb = size[:2] + (-(-shape.frame_tokens // c.block_tokens),)
+    f8 = torch.float8_e4m3fn
+    return fkv_cache8(_check(c.K, "cache.K", f8, size), _check(c.V, "cache.V", f8, size),
+                      _check(c.k_scale, "cache.k_scale", torch.float32, nb),
+                      _check(c.v_scale, "cache.v_scale", torch.float32, nb), c.block_tokens)
+
+
+def _rows(t: torch.Tensor, name: str, shape: fkv_shape, n: int):
+    """Rows [n_heads][n][d] of any head and token stride, the channels adjacent."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must be a GPU tensor (got {t.device})")
+    if t.dtype != _torch_dtype(shape):
+        raise TypeError(f"{name} must be {_torch_dtype(shape)} (got {t.dtype})")
+    if tuple(t.shape) != (shape.n_heads, n, shape.head_dim):
+        raise ValueError(f"{name} must have shape {(shape.n_heads, n, shape.head_dim)} (got {tuple(t.shape)})")
+    if t.stride(2) != 1:
+        raise ValueError(f"{name}: the channels of a row must be adjacent")
+    # (a dimension of one element may report any stride)
+    return fkv_rows(t.data_ptr(), t.stride(0) if shape.n_heads > 1 else 0, t.stride(1) if n > 1 else 0)
+
+
+def _positions(frame_pos, n: int):
+    vals = [int(v) for v in (frame_pos.tolist() if hasattr(frame_pos, "tolist") else frame_pos)]
+    if len(vals) != n:
+        raise ValueError(f"frame_pos needs {n} entries (got {len(vals)})")
+    if any(not -FKV_MAX_POSITION <= v <= FKV_MAX_POSITION for v in vals):
+        raise ValueError(f"frame_pos outside +-{FKV_MAX_POSITION}")
+    return (ctypes.c_int32 * max(n, 1))(*vals)
+
+
+def _device_of(*tensors):
+    """The one device of a call's tensors: the call runs on it, whichever device is current."""
+    devs = {t.device for t in tensors if t is not None}
+    if len(devs) != 1:
+        raise ValueError(f"tensors on more than one device: {sorted(map(str, devs))}")
+    return devs.pop()
+
+
+def _on(device, fn, args, stream):
+    """Calls fn(*args, stream) with ``device`` current and, by default, its current stream."""
+    with torch.cuda.device(device):
+        s = torch.cuda.current_stream(device) if stream is None else stream
+        _raise(fn(*args, ctypes.c_void_p(s.cuda_stream)))
+
+
+def fkv_rotate_chunk(shape: fkv_shape, rope: fkv_rope, frame_pos, Q, K, V, Qr, Kr, Vr, stream=None):
+    """Q and K of the chunk rotated into Qr and Kr, V copied into Vr
+    ([n_heads][C*F][d] contiguous).  Q, K, V may be any strided views of that
+    shape with adjacent channels (a projection's [tokens][3][n_heads][d], say).
+    A pair of Nones is left out."""
+    dt, n = _torch_dtype(shape), _lq(shape)
+    size = (shape.n_heads, n, shape.head_dim)
+    pos = _positions(frame_pos, shape.chunk_frames)
+    src, dst = [], []
+    for t, o, name in ((Q, Qr, "Q"), (K, Kr, "K"), (V, Vr, "V")):
+        if (t is None) != (o is None):
+            raise ValueError(f"{name} and its output must both be given or both be None")
+        src.append(None if t is None else ctypes.byref(_rows(t, name, shape, n)))
+        dst.append(None if o is None else _check(o, name + "r", dt, size))
+    if all(t is None for t in (Q, K, V)):
+        raise ValueError("nothing to rotate")
+    dev = _device_of(Q, K, V, Qr, Kr, Vr)
+    _on(dev, lib().fkv_rotate_chunk, (ctypes.byref(shape), ctypes.byref(rope), pos, *src, *dst), stream)
+
+
+def fkv_append_frames_rotated(shape: fkv_shape, rope: fkv_rope, frame_pos, K_new, V_new, dst_slot, K_hist, V_hist,
+                              stream=None):
+    """fkv_append_frames with the keys of frame f rotated at frame_pos[f] on the
+    way.  K_new, V_new: strided views [n_heads][n*F][d] with adjacent channels."""
+    dt = _torch_dtype(shape)
+    hist = (shape.n_heads, shape.cap_frames, shape.frame_tokens, shape.head_dim)
+    slots = [int(v) for v in dst_slot]
+    n = len(slots)
+    kn, vn = (_rows(t, name, shape, n * shape.frame_tokens) for t, name in ((K_new, "K_new"), (V_new, "V_new")))
+    kh, vh = _check(K_hist, "K_hist", dt, hist), _check(V_hist, "V_hist", dt, hist)
+    arr = (ctypes.c_int32 * max(n, 1))(*slots)
+    _on(_device_of(K_new, V_new, K_hist, V_hist), lib().fkv_append_frames_rotated,
+        (ctypes.byref(shape), ctypes.byref(rope), _positions(frame_pos, n), ctypes.byref(kn), ctypes.byref(vn), n, arr,
+         kh, vh), stream)
+
+
+def fkv_append_frames_q8(shape: fkv_shape, rope: Optional[fkv_rope], frame_pos, K_new, V_new, dst_slot, cache: Cache8,
+                         stream=None):
+    """fkv_append_frames into an 8-bit cache, the keys rotated on the way (rope
+    and frame_pos None: as they are).  K_new, V_new as in
+    fkv_append_frames_rotated; the shape's dtype is theirs."""
+    slots = [int(v) for v in dst_slot]
+    n = len(slots)
+    kn, vn = (_rows(t, name, shape, n * shape.frame_tokens) for t, name in ((K_new, "K_new"), (V_new, "V_new")))
+    c = _cache8(shape, cache)
+    arr = (ctypes.c_int32 * max(n, 1))(*slots)
+    _on(_device_of(K_new, V_new, cache.K, cache.V, cache.k_scale, cache.v_scale), lib().fkv_append_frames_q8,
+        (ctypes.byref(shape), None if rope is None else ctypes.byref(rope),
+         None if rope is None else _positions(frame_pos, n), ctypes.byref(kn), ctypes.byref(vn), n, arr,
+         ctypes.byref(c)), stream)
+
+
+def fkv_score_select_q8(shape: fkv_shape, heads, cache: Cache8, frame_slot, K_cur, scores, kept_seg, kv_len,
+                        workspace: Optional[torch.Tensor] = None, stream=None):
+    """fkv_score_select over the keys of an 8-bit cache.  If ``workspace`` is
+    None a zero-filled one is allocated (through torch's caching allocator)."""
+    n_seg = fkv_num_segments(shape)
+    c = _cache8(shape, cache)
+    sl = _slots(frame_slot, shape.hist_frames)
+    kc = _check(K_cur, "K_cur", _torch_dtype(shape), (shape.n_heads, _lq(shape), shape.head_dim))
+    sc = _check(scores, "scores", torch.float32, (shape.n_heads, n_seg))
+    ks = _check(kept_seg, "kept_seg", torch.int32, (shape.n_heads, n_seg))
+    kl = _check(kv_len, "kv_len", torch.int32, (shape.n_heads,))
+    if workspace is None:
+        need = fkv_score_workspace_size(shape, heads)
+        workspace = torch.zeros(max(need, 1), dtype=torch.uint8, device=K_cur.device)
+    ws = _check(workspace, "workspace", torch.uint8)
+    _on(_device_of(cache.K, cache.V, cache.k_scale, cache.v_scale, K_cur, scores, kept_seg, kv_len, workspace),
+        lib().fkv_score_select_q8, (ctypes.byref(shape), _heads(shape, heads), ctypes.byref(c), sl, kc, sc, ks, kl, ws,
+                                    workspace.numel()), stream)
+    return workspace
+
+
+def fkv_chunk_attention_q8_workspace_size(shape: fkv_shape, heads, n_q: int, n_cur: int) -> int:
+    """Bytes of the workspace of fkv_chunk_attention_q8 on the current device."""
+    out = ctypes.c_size_t(0)
+    _raise(lib().fkv_chunk_attention_q8_workspace_size(ctypes.byref(shape), _heads(shape, heads), int(n_q), int(n_cur),
+                                                       ctypes.byref(out)))
+    return int(out.value)
+
+
+def fkv_chunk_attention_q8(shape: fkv_shape, heads, cache: Cache8, frame_slot, kept_seg, kv_len, Q, K_cur, V_cur,
+                           scale: float, O, lse: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None, stream=None):
+    """Attention of the query tokens Q [n_heads][n_q][d] over every head's kept
+    history in the 8-bit cache and the current tokens K_cur, V_cur
+    [n_heads][n_cur][d] (None, or n_cur = 0: none).  ``workspace``: uint8 device
+    tensor of fkv_chunk_attention_q8_workspace_size bytes, zero-filled before its
+    first use; None runs one workgroup per query tile."""
+    bf = torch.bfloat16
+    n_q = Q.shape[1] if Q.dim() == 3 else -1
+    n_cur = 0 if K_cur is None else K_cur.shape[1] if K_cur.dim() == 3 else -1
+    n_seg = fkv_num_segments(shape)
+    qs, cs = (shape.n_heads, n_q, shape.head_dim), (shape.n_heads, n_cur, shape.head_dim)
+    c = _cache8(shape, cache)
+    sl = _slots(frame_slot, shape.hist_frames)
+    ks = None if kept_seg is None else _check(kept_seg, "kept_seg", torch.int32, (shape.n_heads, n_seg))
+    kl = None if kv_len is None else _check(kv_len, "kv_len", torch.int32, (shape.n_heads,))
+    if (K_cur is None) != (V_cur is None):
+        raise ValueError("K_cur and V_cur must both be given or both be None")
+    kq = None if K_cur is None else _check(K_cur, "K_cur", bf, cs)
+    vq = None if V_cur is None else _check(V_cur, "V_cur", bf, cs)
+    q, o = _check(Q, "Q", bf, qs), _check(O, "O", bf, qs)
+    ls = None if lse is None else _check(lse, "lse", torch.float32, (shape.n_heads, n_q))
+    ws, nws = None, 0
+    if workspace is not None:
+        ws, nws = _check(workspace, "workspace", torch.uint8), workspace.numel()
+    _on(_device_of(cache.K, cache.V, cache.k_scale, cache.v_scale, kept_seg, kv_len, Q, K_cur, V_cur, O, lse, workspace),
+        lib().fkv_chunk_attention_q8, (ctypes.byref(shape), _heads(shape, heads), ctypes.byref(c), sl, ks, kl, q, n_q, kq,
+                                       vq, n_cur, ctypes.c_float(scale), o, ls, ws, nws), stream)
 
 
 def fkv_last_error() -> str:

@@ -103,6 +103,26 @@ fkv_status check_slots(const fkv_shape *s, const int32_t *slots) {
     return FKV_OK;
 }
 
+fkv_status check_n_frames(const fkv_shape *s, int32_t n_frames) {
+    if (n_frames < 0 || n_frames > s->cap_frames)
+        return fail(FKV_ERR_ARG, "n_frames %d outside [0, cap_frames=%d]", n_frames, s->cap_frames);
+    return FKV_OK;
+}
+
+// Slots of new frames: distinct, inside the cache.
+fkv_status check_dst_slots(const fkv_shape *s, int32_t n_frames, const int32_t *dst_slot) {
+    if (n_frames > 0 && !dst_slot) return fail(FKV_ERR_ARG, "dst_slot is NULL");
+    bool used[FKV_MAX_FRAMES] = {};
+    for (int f = 0; f < n_frames; ++f) {
+        const int sl = dst_slot[f];
+        if (sl < 0 || sl >= s->cap_frames)
+            return fail(FKV_ERR_ARG, "dst_slot[%d] = %d outside [0, %d)", f, sl, s->cap_frames);
+        if (used[sl]) return fail(FKV_ERR_ARG, "dst_slot[%d] = %d is given twice", f, sl);
+        used[sl] = true;
+    }
+    return FKV_OK;
+}
+
 // --------------------------------------------------------------- budgets
 struct StaticPlan {
     int n_first, gap, n_kept;
@@ -320,7 +340,8 @@ struct SelectOut {
 fkv_status score_impl(const fkv_shape *shape, const fkv::HeadList &list, bool pooled, const void *K_hist,
                       const int32_t *frame_slot, const void *K_cur, float *scores, void *workspace,
                       void *stream, const char *what, fkv::ScoreMode mode = fkv::kScoreModeFull,
-                      double *stats = nullptr, const SelectOut *select = nullptr) {
+                      double *stats = nullptr, const SelectOut *select = nullptr,
+                      const fkv_cache8 *q8 = nullptr) {
     fkv::ScoreArgs a;
     memset(&a, 0, sizeof a);
     a.heads = list;
@@ -358,6 +379,14 @@ fkv_status score_impl(const fkv_shape *shape, const fkv::HeadList &list, bool po
         }
     }
     (void)hipGetLastError();
+    if (q8) {  // K_hist holds codes; one scale for each block of tokens
+        a.k_scale = q8->k_scale;
+        a.q8_blocks = (shape->frame_tokens + q8->block_tokens - 1) / q8->block_tokens;
+        a.q8_shift = __builtin_ctz((unsigned)q8->block_tokens);
+        a.q8_row_shift = shape->head_dim == 128 ? 4 : 3;
+        a.q8_unit_tokens = shape->frame_tokens / a.units;
+        return device_status(fkv::launch_score_q8(a, (hipStream_t)stream), what);
+    }
     return device_status(fkv::launch_score(a, shape->dtype == FKV_F32, (hipStream_t)stream), what);
 }
 
@@ -739,19 +768,10 @@ fkv_status fkv_append_frames(const fkv_shape *shape, const void *K_new, const vo
                              const int32_t *dst_slot, void *K_hist, void *V_hist, void *stream) {
     fkv_status st;
     if ((st = check_shape(shape)) != FKV_OK) return st;
-    if (n_frames < 0 || n_frames > shape->cap_frames)
-        return fail(FKV_ERR_ARG, "n_frames %d outside [0, cap_frames=%d]", n_frames, shape->cap_frames);
+    if ((st = check_n_frames(shape, n_frames)) != FKV_OK) return st;
     if (n_frames == 0) return ok();
     if (!K_new || !V_new || !K_hist || !V_hist) return fail(FKV_ERR_ARG, "NULL tensor pointer");
-    if (!dst_slot) return fail(FKV_ERR_ARG, "dst_slot is NULL");
-    bool used[FKV_MAX_FRAMES] = {};
-    for (int f = 0; f < n_frames; ++f) {
-        const int sl = dst_slot[f];
-        if (sl < 0 || sl >= shape->cap_frames)
-            return fail(FKV_ERR_ARG, "dst_slot[%d] = %d outside [0, %d)", f, sl, shape->cap_frames);
-        if (used[sl]) return fail(FKV_ERR_ARG, "dst_slot[%d] = %d is given twice", f, sl);
-        used[sl] = true;
-    }
+    if ((st = check_dst_slots(shape, n_frames, dst_slot)) != FKV_OK) return st;
     fkv::AppendArgs a;
     memset(&a, 0, sizeof a);
     a.K_new = (const uint8_t *)K_new;
@@ -1270,6 +1290,353 @@ fkv_status fkv_classify_heads(const float *mass, int32_t n_heads, int32_t n_bins
         head_type[h] = is_static ? FKV_STATIC : FKV_DYNAMIC;
     }
     return ok();
+}
+
+}  // extern "C"
+
+// ------------------------------- position rotation, appending, 8-bit caches
+namespace {
+
+bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+fkv_status check_rope(const fkv_shape *s, const fkv_rope *r, const int32_t *frame_pos, int n_frames) {
+    if (!r) return fail(FKV_ERR_ARG, "rope is NULL");
+    if (r->frame_pairs < 0 || r->row_pairs < 0 || r->col_pairs < 0 ||
+        (int64_t)r->frame_pairs + r->row_pairs + r->col_pairs > s->head_dim / 2)
+        return fail(FKV_ERR_ARG, "%d + %d + %d channel pairs do not fit %d", r->frame_pairs, r->row_pairs,
+                    r->col_pairs, s->head_dim / 2);
+    if (r->row_tokens < 1 || r->row_tokens > s->frame_tokens)
+        return fail(FKV_ERR_ARG, "row_tokens %d outside [1, frame_tokens=%d]", r->row_tokens, s->frame_tokens);
+    if (r->token_step != 0 && r->token_step != 1)
+        return fail(FKV_ERR_ARG, "token_step %d is neither 0 nor 1", r->token_step);
+    if (r->pairing != FKV_PAIR_ADJACENT && r->pairing != FKV_PAIR_HALVES)
+        return fail(FKV_ERR_ARG, "pairing %d is not FKV_PAIR_ADJACENT or FKV_PAIR_HALVES", r->pairing);
+    if (!(r->theta >= 1.0) || !isfinite(r->theta)) return fail(FKV_ERR_ARG, "theta %g is below 1 or not finite", r->theta);
+    if (n_frames > 0 && !frame_pos) return fail(FKV_ERR_ARG, "frame_pos is NULL");
+    for (int f = 0; f < n_frames; ++f)
+        if (frame_pos[f] < -FKV_MAX_POSITION || frame_pos[f] > FKV_MAX_POSITION)
+            return fail(FKV_ERR_ARG, "frame_pos[%d] = %d outside +-%d", f, frame_pos[f], FKV_MAX_POSITION);
+    return FKV_OK;
+}
+
+fkv::RopeTable rope_table(const fkv_rope *r) {
+    fkv::RopeTable t;
+    memset(&t, 0, sizeof t);
+    t.row_tokens = 1;
+    if (!r) return t;
+    t.on = 1;
+    t.row_tokens = r->row_tokens;
+    t.token_step = r->token_step;
+    t.halves = r->pairing == FKV_PAIR_HALVES;
+    const int n[3] = {r->frame_pairs, r->row_pairs, r->col_pairs};
+    int j = 0;
+    for (int x = 0; x < 3; ++x)
+        for (int i = 0; i < n[x]; ++i) t.turns[j++] = pow(r->theta, -(double)i / n[x]) / 6.283185307179586476925286766559;
+    t.end_frame = n[0];
+    t.end_row = n[0] + n[1];
+    t.end_col = n[0] + n[1] + n[2];
+    return t;
+}
+
+fkv_status check_rows(const fkv_shape *s, const fkv_rows *r, const char *name) {
+    if (!r->data) return fail(FKV_ERR_ARG, "%s: NULL tensor pointer", name);
+    if (!aligned16(r->data)) return fail(FKV_ERR_ARG, "%s is not 16-byte aligned", name);
+    const int64_t per = 16 / (int64_t)elem_size(s);   // elements in 16 bytes
+    if (r->head_stride < 0 || r->token_stride < 0 || r->head_stride % per || r->token_stride % per)
+        return fail(FKV_ERR_ARG, "%s: strides %lld and %lld must be non-negative multiples of %lld elements", name,
+                    (long long)r->head_stride, (long long)r->token_stride, (long long)per);
+    return FKV_OK;
+}
+
+fkv_status check_cache8(const fkv_cache8 *c, bool values) {
+    if (!c) return fail(FKV_ERR_ARG, "cache is NULL");
+    const int32_t b = c->block_tokens;
+    if (b != 16 && b != 32 && b != 64 && b != 128)
+        return fail(FKV_ERR_ARG, "block_tokens %d is not 16, 32, 64 or 128", b);
+    if (!c->K8 || !c->k_scale || (values && (!c->V8 || !c->v_scale))) return fail(FKV_ERR_ARG, "NULL cache pointer");
+    if (!aligned16(c->K8) || (values && !aligned16(c->V8))) return fail(FKV_ERR_ARG, "K8 or V8 is not 16-byte aligned");
+    return FKV_OK;
+}
+
+int scale_blocks(const fkv_shape *s, const fkv_cache8 *c) { return (s->frame_tokens + c->block_tokens - 1) / c->block_tokens; }
+
+void rotate_source(fkv::RotateArgs *a, int t, const fkv_shape *s, const fkv_rows *r, void *dst) {
+    const int64_t es = (int64_t)elem_size(s);
+    a->src[t] = (const uint8_t *)r->data;
+    a->dst[t] = (uint8_t *)dst;
+    a->src_head[t] = r->head_stride * es;
+    a->src_tok[t] = r->token_stride * es;
+}
+
+// floor(2^64 / P) + 1 as two words (0, 0 for P = 1), for j / P by multiplication
+void magic_of(int32_t P, uint32_t *hi, uint32_t *lo) {
+    *hi = *lo = 0;
+    if (P <= 1) return;
+    const unsigned __int128 m = (((unsigned __int128)1) << 64) / (uint64_t)P + 1;
+    *hi = (uint32_t)(uint64_t)(m >> 32);
+    *lo = (uint32_t)(uint64_t)m;
+}
+
+fkv_status check_q8_call(const fkv_shape *s, const fkv_head *heads, int32_t n_q, int32_t n_cur) {
+    fkv_status st;
+    if ((st = check_shape(s)) != FKV_OK) return st;
+    if ((st = check_heads(s, heads)) != FKV_OK) return st;
+    if (s->dtype != FKV_BF16) return fail(FKV_ERR_SHAPE, "attention over an 8-bit cache needs bf16");
+    if (n_q < 1 || n_cur < 0) return fail(FKV_ERR_ARG, "n_q %d < 1 or n_cur %d < 0", n_q, n_cur);
+    const int64_t most = std::max(n_q, n_cur);
+    if (most * s->head_dim * 2 >= (int64_t)1 << 31) return fail(FKV_ERR_SHAPE, "%lld rows span 2^31 bytes or more", (long long)most);
+    return FKV_OK;
+}
+
+// How an 8-bit attention call (checked) is divided: parts per (head, query
+// tile), so that about one workgroup runs per compute unit and a part keeps a
+// tile for each of its waves.
+struct Q8Plan {
+    int n_split;
+    size_t counter_bytes, bytes;
+};
+
+int q8_query_tiles(int32_t n_q) { return (n_q + fkv::kAttnQ8Rows - 1) / fkv::kAttnQ8Rows; }
+
+fkv_status q8_plan(const fkv_shape *s, const fkv_head *heads, int32_t n_q, int32_t n_cur, Q8Plan *p) {
+    fkv_status st;
+    int blocks = 0;
+    if ((st = balanced_blocks(&blocks)) != FKV_OK) return st;
+    int64_t kept = 0;
+    for (int h = 0; h < s->n_heads; ++h) {
+        int64_t n = 0;
+        if ((st = fkv_kept_tokens_max(s, heads, h, &n)) != FKV_OK) return st;
+        kept = std::max(kept, n);
+    }
+    const int64_t tiles = (kept + 63) / 64 + ((int64_t)n_cur + 63) / 64;
+    const int64_t items = (int64_t)s->n_heads * q8_query_tiles(n_q);
+    p->n_split = (int)std::max<int64_t>(1, std::min<int64_t>(blocks / items, (tiles + 7) / 8));
+    p->counter_bytes = p->n_split > 1 ? fkv::attention_counter_bytes(items) : 0;
+    p->bytes = p->counter_bytes +
+               (p->n_split > 1 ? (size_t)items * p->n_split * fkv::attn_q8_part_floats(s->head_dim) * sizeof(float) : 0);
+    return FKV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+fkv_status fkv_rotate_chunk(const fkv_shape *shape, const fkv_rope *rope, const int32_t *frame_pos,
+                            const fkv_rows *Q, const fkv_rows *K, const fkv_rows *V, void *Qr, void *Kr,
+                            void *Vr, void *stream) {
+    fkv_status st;
+    if ((st = check_shape(shape)) != FKV_OK) return st;
+    const int C = shape->chunk_frames;
+    if (C > FKV_MAX_FRAMES) return fail(FKV_ERR_SHAPE, "chunk_frames %d exceeds %d", C, FKV_MAX_FRAMES);
+    if ((st = check_rope(shape, rope, frame_pos, C)) != FKV_OK) return st;
+    const fkv_rows *in[3] = {Q, K, V};
+    void *out[3] = {Qr, Kr, Vr};
+    const char *name[3] = {"Q", "K", "V"};
+    fkv::RotateArgs a;
+    memset(&a, 0, sizeof a);
+    bool any = false;
+    for (int t = 0; t < 3; ++t) {
+        if (!in[t] && !out[t]) continue;
+        if (!in[t] || !out[t]) return fail(FKV_ERR_ARG, "%s and its output must both be given or both be NULL", name[t]);
+        if ((st = check_rows(shape, in[t], name[t])) != FKV_OK) return st;
+        if (!aligned16(out[t])) return fail(FKV_ERR_ARG, "%sr is not 16-byte aligned", name[t]);
+        rotate_source(&a, t, shape, in[t], out[t]);
+        any = true;
+    }
+    if (!any) return fail(FKV_ERR_ARG, "nothing to rotate");
+    a.F = shape->frame_tokens;
+    a.n_frames = C;
+    a.n_heads = shape->n_heads;
+    a.dst_head = (int64_t)C * a.F * shape->head_dim * (int64_t)elem_size(shape);
+    a.rope = rope_table(rope);
+    for (int f = 0; f < C; ++f) {
+        a.pos.slot[f] = frame_pos[f];
+        a.slots.slot[f] = f;
+    }
+    (void)hipGetLastError();
+    return device_status(fkv::launch_rotate(a, shape->head_dim, shape->dtype == FKV_F32, (hipStream_t)stream),
+                         "fkv_rotate_chunk launch");
+}
+
+fkv_status fkv_append_frames_rotated(const fkv_shape *shape, const fkv_rope *rope, const int32_t *frame_pos,
+                                     const fkv_rows *K_new, const fkv_rows *V_new, int32_t n_frames,
+                                     const int32_t *dst_slot, void *K_hist, void *V_hist, void *stream) {
+    fkv_status st;
+    if ((st = check_shape(shape)) != FKV_OK) return st;
+    if ((st = check_n_frames(shape, n_frames)) != FKV_OK) return st;
+    if ((st = check_dst_slots(shape, n_frames, dst_slot)) != FKV_OK) return st;
+    if ((st = check_rope(shape, rope, frame_pos, n_frames)) != FKV_OK) return st;
+    if (n_frames == 0) return ok();
+    if (!K_new || !V_new || !K_hist || !V_hist) return fail(FKV_ERR_ARG, "NULL tensor pointer");
+    if ((st = check_rows(shape, K_new, "K_new")) != FKV_OK) return st;
+    if ((st = check_rows(shape, V_new, "V_new")) != FKV_OK) return st;
+    if (!aligned16(K_hist) || !aligned16(V_hist)) return fail(FKV_ERR_ARG, "K_hist or V_hist is not 16-byte aligned");
+    fkv::RotateArgs a;
+    memset(&a, 0, sizeof a);
+    rotate_source(&a, 1, shape, K_new, K_hist);
+    rotate_source(&a, 2, shape, V_new, V_hist);
+    a.F = shape->frame_tokens;
+    a.n_frames = n_frames;
+    a.n_heads = shape->n_heads;
+    a.dst_head = (int64_t)shape->cap_frames * a.F * shape->head_dim * (int64_t)elem_size(shape);
+    a.rope = rope_table(rope);
+    for (int f = 0; f < n_frames; ++f) {
+        a.pos.slot[f] = frame_pos[f];
+        a.slots.slot[f] = dst_slot[f];
+    }
+    (void)hipGetLastError();
+    return device_status(fkv::launch_rotate(a, shape->head_dim, shape->dtype == FKV_F32, (hipStream_t)stream),
+                         "fkv_append_frames_rotated launch");
+}
+
+fkv_status fkv_append_frames_q8(const fkv_shape *shape, const fkv_rope *rope, const int32_t *frame_pos,
+                                const fkv_rows *K_new, const fkv_rows *V_new, int32_t n_frames,
+                                const int32_t *dst_slot, const fkv_cache8 *cache, void *stream) {
+    fkv_status st;
+    if ((st = check_shape(shape)) != FKV_OK) return st;
+    if ((st = check_cache8(cache, true)) != FKV_OK) return st;
+    if ((st = check_n_frames(shape, n_frames)) != FKV_OK) return st;
+    if ((st = check_dst_slots(shape, n_frames, dst_slot)) != FKV_OK) return st;
+    if (rope && (st = check_rope(shape, rope, frame_pos, n_frames)) != FKV_OK) return st;
+    if (n_frames == 0) return ok();
+    if (!K_new || !V_new) return fail(FKV_ERR_ARG, "NULL tensor pointer");
+    if ((st = check_rows(shape, K_new, "K_new")) != FKV_OK) return st;
+    if ((st = check_rows(shape, V_new, "V_new")) != FKV_OK) return st;
+    const int64_t es = (int64_t)elem_size(shape);
+    fkv::AppendQ8Args a;
+    memset(&a, 0, sizeof a);
+    a.K = (const uint8_t *)K_new->data;
+    a.V = (const uint8_t *)V_new->data;
+    a.k_head = K_new->head_stride * es;
+    a.k_tok = K_new->token_stride * es;
+    a.v_head = V_new->head_stride * es;
+    a.v_tok = V_new->token_stride * es;
+    a.K8 = (uint8_t *)cache->K8;
+    a.V8 = (uint8_t *)cache->V8;
+    a.k_scale = cache->k_scale;
+    a.v_scale = cache->v_scale;
+    a.F = shape->frame_tokens;
+    a.cap = shape->cap_frames;
+    a.n_frames = n_frames;
+    a.n_heads = shape->n_heads;
+    a.block_tokens = cache->block_tokens;
+    a.n_blocks = scale_blocks(shape, cache);
+    a.rope = rope_table(rope);
+    for (int f = 0; f < n_frames; ++f) {
+        a.pos.slot[f] = rope ? frame_pos[f] : 0;
+        a.slots.slot[f] = dst_slot[f];
+    }
+    (void)hipGetLastError();
+    return device_status(fkv::launch_append_q8(a, shape->head_dim, shape->dtype == FKV_F32, (hipStream_t)stream),
+                         "fkv_append_frames_q8 launch");
+}
+
+fkv_status fkv_score_select_q8(const fkv_shape *shape, const fkv_head *heads, const fkv_cache8 *cache,
+                               const int32_t *frame_slot, const void *K_cur, float *scores, int32_t *kept_seg,
+                               int32_t *kv_len, void *workspace, size_t workspace_bytes, void *stream) {
+    fkv_status st;
+    if ((st = check_shape(shape)) != FKV_OK) return st;
+    if ((st = check_heads(shape, heads)) != FKV_OK) return st;
+    if (shape->dtype != FKV_BF16) return fail(FKV_ERR_SHAPE, "scoring over an 8-bit cache needs bf16");
+    if ((st = check_slots(shape, frame_slot)) != FKV_OK) return st;
+    if (!kv_len) return fail(FKV_ERR_ARG, "kv_len is NULL");
+    size_t need = 0;
+    if ((st = fkv_score_workspace_size(shape, heads, &need)) != FKV_OK) return st;
+    if (need == 0)  // no dynamic head, or nothing cached: every dynamic head keeps nothing
+        return select_impl(shape, heads, nullptr, false, kept_seg, kv_len, stream, "fkv_score_select_q8 launch");
+    if ((st = check_cache8(cache, false)) != FKV_OK) return st;
+    if (!K_cur || !scores || !kept_seg) return fail(FKV_ERR_ARG, "NULL tensor pointer");
+    if (!workspace) return fail(FKV_ERR_ARG, "workspace is NULL");
+    if (workspace_bytes < need)
+        return fail(FKV_ERR_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+    fkv::HeadList list;
+    memset(&list, 0, sizeof list);
+    for (int h = 0; h < shape->n_heads; ++h)
+        if (heads[h].type == FKV_DYNAMIC) list.head[list.n++] = h;
+    const SelectOut out{heads, kept_seg, kv_len};
+    return score_impl(shape, list, false, cache->K8, frame_slot, K_cur, scores, workspace, stream,
+                      "fkv_score_select_q8 launch", fkv::kScoreModeFull, nullptr, &out, cache);
+}
+
+fkv_status fkv_chunk_attention_q8_workspace_size(const fkv_shape *shape, const fkv_head *heads, int32_t n_q,
+                                                 int32_t n_cur, size_t *bytes) {
+    fkv_status st;
+    Q8Plan p;
+    if ((st = check_q8_call(shape, heads, n_q, n_cur)) != FKV_OK) return st;
+    if (!bytes) return fail(FKV_ERR_ARG, "bytes is NULL");
+    if ((st = q8_plan(shape, heads, n_q, n_cur, &p)) != FKV_OK) return st;
+    *bytes = p.bytes;
+    return ok();
+}
+
+fkv_status fkv_chunk_attention_q8(const fkv_shape *shape, const fkv_head *heads, const fkv_cache8 *cache,
+                                  const int32_t *frame_slot, const int32_t *kept_seg, const int32_t *kv_len,
+                                  const void *Q, int32_t n_q, const void *K_cur, const void *V_cur,
+                                  int32_t n_cur, float scale, void *O, float *lse, void *workspace,
+                                  size_t workspace_bytes, void *stream) {
+    fkv_status st;
+    if ((st = check_q8_call(shape, heads, n_q, n_cur)) != FKV_OK) return st;
+    if ((st = check_slots(shape, frame_slot)) != FKV_OK) return st;
+    const int H = shape->hist_frames;
+    if (H > 0) {
+        if ((st = check_cache8(cache, true)) != FKV_OK) return st;
+        for (int h = 0; h < shape->n_heads; ++h)
+            if (heads[h].type == FKV_DYNAMIC && (!kept_seg || !kv_len))
+                return fail(FKV_ERR_ARG, "kept_seg or kv_len is NULL with a dynamic head");
+    }
+    if (!Q || !O || (n_cur > 0 && (!K_cur || !V_cur))) return fail(FKV_ERR_ARG, "NULL tensor pointer");
+    if (!(scale > 0.f) || !isfinite(scale)) return fail(FKV_ERR_ARG, "scale %g must be positive and finite", (double)scale);
+    Q8Plan p = {1, 0, 0};
+    if (workspace && (st = q8_plan(shape, heads, n_q, n_cur, &p)) != FKV_OK) return st;
+    if (workspace && workspace_bytes < p.bytes)
+        return fail(FKV_ERR_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, p.bytes);
+
+    fkv::AttnQ8Args a;
+    memset(&a, 0, sizeof a);
+    if (H > 0) {
+        a.K8 = (const uint8_t *)cache->K8;
+        a.V8 = (const uint8_t *)cache->V8;
+        a.k_scale = cache->k_scale;
+        a.v_scale = cache->v_scale;
+        a.n_blocks = scale_blocks(shape, cache);
+        a.block_shift = __builtin_ctz((unsigned)cache->block_tokens);
+    }
+    a.Q = (const uint16_t *)Q;
+    a.K_cur = (const uint16_t *)K_cur;
+    a.V_cur = (const uint16_t *)V_cur;
+    a.O = (uint16_t *)O;
+    a.lse = lse;
+    a.kept_seg = kept_seg;
+    a.kv_len = kv_len;
+    a.n_heads = shape->n_heads;
+    a.n_q = n_q;
+    a.n_cur = n_cur;
+    a.F = shape->frame_tokens;
+    a.L = shape->seg_tokens;
+    a.H = H;
+    a.cap = shape->cap_frames;
+    a.n_seg = fkv_num_segments(shape);
+    magic_of(a.F, &a.mf_hi, &a.mf_lo);
+    magic_of(a.L, &a.ml_hi, &a.ml_lo);
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.n_qtiles = q8_query_tiles(n_q);
+    a.n_split = p.n_split;
+    a.counters = (uint32_t *)workspace;
+    if (workspace) a.part = (float *)((char *)workspace + p.counter_bytes);
+    for (int h = 0; h < shape->n_heads; ++h) {
+        if (heads[h].type == FKV_DYNAMIC) {
+            a.st_kept[h] = H > 0 ? -1 : 0;
+            continue;
+        }
+        const StaticPlan sp = static_plan(H, heads[h]);
+        a.st_first[h] = sp.n_first;
+        a.st_gap[h] = sp.gap;
+        a.st_kept[h] = sp.n_kept;
+    }
+    for (int t = 0; t < H; ++t) a.slots.slot[t] = frame_slot[t];
+    (void)hipGetLastError();
+    return device_status(fkv::launch_attention_q8(a, shape->head_dim, (hipStream_t)stream),
+                         "fkv_chunk_attention_q8 launch");
 }
 
 const char *fkv_last_error(void) { return g_err; }

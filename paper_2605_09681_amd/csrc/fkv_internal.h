@@ -63,6 +63,43 @@ struct AppendArgs {
     SlotTable slots;                // destination slot of new frame f
 };
 
+// ------------------------------------------- position rotation and appending
+// Rotation as the kernels use it: pair j of the d/2 pairs turns by
+// position * turns[j], in turns (1 = a full circle); pairs [0, end_frame) by the
+// frame position, [end_frame, end_row) by the row, [end_row, end_col) by the
+// column, the others not at all.
+struct RopeTable {
+    int32_t end_frame, end_row, end_col;
+    int32_t row_tokens, token_step, halves;  // halves: FKV_PAIR_HALVES
+    int32_t on;                              // 0: no rotation
+    double turns[64];                        // theta^(-i/n) / (2 pi)
+};
+
+// Rows of up to three tensors (0 and 1 rotated, 2 not; a NULL source is left
+// out) into frames of the destination: row p of new frame f of head h goes to
+// row slot[f] * F + p of that head.
+struct RotateArgs {
+    const uint8_t *src[3];
+    uint8_t *dst[3];
+    int64_t src_head[3], src_tok[3];   // bytes
+    int64_t dst_head;                  // bytes per head of a destination
+    int32_t F, n_frames, n_heads, heads_per_wg;
+    RopeTable rope;
+    SlotTable pos;                     // frame position of new frame f
+    SlotTable slots;
+};
+
+struct AppendQ8Args {
+    const uint8_t *K, *V;
+    int64_t k_head, k_tok, v_head, v_tok;  // bytes
+    uint8_t *K8, *V8;
+    float *k_scale, *v_scale;
+    int32_t F, cap, n_frames, n_heads, heads_per_wg;
+    int32_t block_tokens, n_blocks;        // tokens per scale, scales per frame
+    RopeTable rope;
+    SlotTable pos, slots;
+};
+
 // ---------------------------------------------------------------- selection
 struct SelectArgs {
     const float *scores;            // head h's row at scores + h * score_stride
@@ -111,6 +148,12 @@ struct ScoreArgs {
     int32_t t_begin, n_frames;      // streamed frames (frame H is the first frame of K_cur)
     int32_t select;                 // 1: also the BottomK selection (the fields at the end)
     int32_t lds_rows;               // doubles of dynamic LDS for the finishing workgroup's row sums
+    // 8-bit history (launch_score_q8): K_hist holds E4M3 codes, frame_vecs and
+    // unit_vecs count 16-byte vectors of the bf16 values they stand for
+    const float *k_scale;           // [n_heads][cap][q8_blocks]
+    int32_t q8_blocks, q8_shift;    // scales per frame, log2 of the tokens per scale
+    int32_t q8_row_shift;           // log2 of the vectors per token row
+    int32_t q8_unit_tokens;         // tokens per unit
     HeadList heads;
     SlotTable slots;
     // BottomK parameters per listed head (fused selection)
@@ -190,6 +233,31 @@ struct Fp8PackArgs {
     SlotTable slots;
 };
 
+// ------------------------------------------------- attention over 8-bit caches
+struct AttnQ8Args {
+    const uint8_t *K8, *V8;
+    const float *k_scale, *v_scale;
+    const uint16_t *Q, *K_cur, *V_cur;
+    uint16_t *O;
+    float *lse;
+    const int32_t *kept_seg, *kv_len;   // dynamic heads
+    int32_t n_heads, n_q, n_cur;
+    int32_t F, L, H, cap, n_seg;
+    int32_t n_blocks, block_shift;      // scales per frame, log2 of the tokens per scale
+    uint32_t mf_hi, mf_lo, ml_hi, ml_lo;  // floor(2^64 / F) + 1 and floor(2^64 / L) + 1 (0 for 1)
+    float scale_log2;                   // scale * log2(e)
+    int32_t n_qtiles;                   // query tiles per head
+    int32_t n_split;                    // parts per (head, query tile); 1: no workspace
+    float *part;                        // [head][query tile][part] slots of attn_q8_part_floats
+    uint32_t *counters;                 // arrivals per (head, query tile), kItemCounterStride apart
+    // the expanded copy (attn_q8 over large chunks): bf16 [n_heads][slab][d], and its lengths
+    uint16_t *Kc, *Vc;
+    int32_t *kv_out;
+    int64_t slab;
+    int32_t st_first[FKV_MAX_HEADS], st_gap[FKV_MAX_HEADS], st_kept[FKV_MAX_HEADS];  // st_kept < 0: dynamic
+    SlotTable slots;
+};
+
 constexpr int kScoreThreads = 256;
 constexpr int kAttnRowsBf16 = 256;  // query rows per attention workgroup (bf16 MFMA kernel)
 constexpr int kAttnKeysPerTile = 64; // keys per tile of the bf16 MFMA kernel
@@ -207,6 +275,7 @@ hipError_t launch_select(const SelectArgs &a, hipStream_t s);
 hipError_t launch_select_copy(const SelectCopyArgs &a, int max_pieces, hipStream_t s);
 // one scoring launch in a.mode (full pass, history statistics, or cached scores)
 hipError_t launch_score(const ScoreArgs &a, bool f32, hipStream_t s);
+hipError_t launch_score_q8(const ScoreArgs &a, hipStream_t s);  // full pass over an 8-bit history
 void score_workspace_layout(ScoreArgs &a, void *ws, int n_list, int H, int units, int n_cg);
 hipError_t launch_attention_bf16(const AttnArgs &a, int head_dim, hipStream_t s);
 size_t attention_part_bytes(int head_dim);  // bytes of one partial-result slot (bf16 kernel)
@@ -226,5 +295,14 @@ inline size_t fp8_stats_doubles(int n_heads, int n_chunks, int d) { return (size
 hipError_t launch_fp8_pack(const Fp8PackArgs &a, hipStream_t s);
 hipError_t launch_attention_fp8(const AttnArgs &a, int head_dim, hipStream_t s);
 hipError_t launch_attention_f32(const AttnArgs &a, int head_dim, hipStream_t s);
+
+// rotation, appending with rotation, appending to 8-bit caches (k_rope.hip)
+hipError_t launch_rotate(const RotateArgs &a, int head_dim, bool f32, hipStream_t s);
+hipError_t launch_append_q8(const AppendQ8Args &a, int head_dim, bool f32, hipStream_t s);
+
+// attention over 8-bit caches (k_attn_q8.hip)
+constexpr int kAttnQ8Rows = 16;             // query rows of a tile
+hipError_t launch_attention_q8(const AttnQ8Args &a, int head_dim, hipStream_t s);
+inline size_t attn_q8_part_floats(int head_dim) { return (size_t)kAttnQ8Rows * (head_dim + 2); }
 
 }  // namespace fkv

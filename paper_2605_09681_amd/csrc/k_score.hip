@@ -114,6 +114,14 @@ struct Vec<true> {  // 4 fp32
     __device__ static __forceinline__ double at(const u32x4 &v, int e) { return (double)__uint_as_float(v[e]); }
 };
 
+// 8 E4M3 codes and their scale (a power of two) as 8 bf16, exactly.
+__device__ __forceinline__ u32x4 widen8(uint32_t c0, uint32_t c1, float scale) {
+    return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c0, scale, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c0, scale, true)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c1, scale, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c1, scale, true))};
+}
+
 // A lane's columns of one frame widened to fp64 (exact), vector 0 then vector
 // 1, elements in order: each element is converted once, and the frame serves
 // as the current frame (its squares, its product with the previous frame) and
@@ -326,7 +334,12 @@ __device__ void finish_pooled(const ScoreArgs &a) {
     }
 }
 
-template <bool F32, bool DIRECT>
+// Q8: an 8-bit history (E4M3 codes with a power-of-two scale per block of tokens).
+// A lane loads 8 codes where it would load a 16-byte vector of bf16 and widens
+// them (exactly) to that vector: from there on every lane, sum and order is
+// the bf16 kernel's, so the scores are those of the bf16 cache that the codes
+// stand for, bit for bit.
+template <bool F32, bool DIRECT, bool Q8 = false>
 __global__ __launch_bounds__(kThreads, 5) void score_kernel(ScoreArgs a) {
     extern __shared__ double dyn[];            // finisher rows (lds_rows), this workgroup's sums (2 n_frames),
                                                // then (selecting) n_seg keys, n_seg floats, 2 n_seg bytes
@@ -352,6 +365,23 @@ __global__ __launch_bounds__(kThreads, 5) void score_kernel(ScoreArgs a) {
     const u32x4 *cur = (const u32x4 *)a.K_cur + (int64_t)h * a.cur_head_vecs + (int64_t)u * a.unit_vecs;
     auto load = [&](int f, u32x4 (&x)[kV]) {
         const int t = a.t_begin + f;
+        if constexpr (Q8) {
+            if (t < a.H) {
+                const int64_t slot = (int64_t)h * a.cap + a.slots.slot[t];
+                const uint2 *base = (const uint2 *)a.K_hist + slot * a.frame_vecs + (int64_t)u * a.unit_vecs;
+                const float *scale = a.k_scale + slot * a.q8_blocks;
+#pragma unroll
+                for (int j = 0; j < kV; ++j) {
+                    x[j] = u32x4{0, 0, 0, 0};
+                    if (ok[j]) {
+                        const uint2 c = base[col[j]];
+                        const float sc = scale[(u * a.q8_unit_tokens + (col[j] >> a.q8_row_shift)) >> a.q8_shift];
+                        x[j] = widen8(c.x, c.y, sc);
+                    }
+                }
+                return;
+            }
+        }
         const u32x4 *base = t < a.H ? hist + (int64_t)a.slots.slot[t] * a.frame_vecs : cur;
 #pragma unroll
         for (int j = 0; j < kV; ++j) x[j] = ok[j] ? __builtin_nontemporal_load(base + col[j]) : u32x4{0, 0, 0, 0};
@@ -442,13 +472,22 @@ void score_workspace_layout(ScoreArgs &a, void *ws, int n_list, int H, int units
     a.group = a.totals + (size_t)n_list * rows;
 }
 
-hipError_t launch_score(const ScoreArgs &a0, bool f32, hipStream_t s) {
-    ScoreArgs a = a0;
-    if (a.heads.n == 0 || a.n_frames <= 0) return hipSuccess;
+namespace {
+
+// Dynamic LDS of a launch; sets a.lds_rows.
+size_t score_lds(ScoreArgs &a) {
     a.lds_rows = a.units * a.n_frames * 2;
     size_t lds = (size_t)(a.lds_rows + a.n_frames * 2) * sizeof(double);   // + this workgroup's sums
     if (a.select) lds += (size_t)a.n_seg * (sizeof(uint64_t) + sizeof(float) + 2);
-    lds = (lds + 15) & ~(size_t)15;
+    return (lds + 15) & ~(size_t)15;
+}
+
+}  // namespace
+
+hipError_t launch_score(const ScoreArgs &a0, bool f32, hipStream_t s) {
+    ScoreArgs a = a0;
+    if (a.heads.n == 0 || a.n_frames <= 0) return hipSuccess;
+    const size_t lds = score_lds(a);
     const dim3 grid((unsigned)a.n_cg, (unsigned)a.units, (unsigned)a.heads.n);
     const bool direct = one_member(a);
     if (f32 && direct)
@@ -459,6 +498,16 @@ hipError_t launch_score(const ScoreArgs &a0, bool f32, hipStream_t s) {
         hipLaunchKernelGGL((score_kernel<false, true>), grid, dim3(kThreads), lds, s, a);
     else
         hipLaunchKernelGGL((score_kernel<false, false>), grid, dim3(kThreads), lds, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_score_q8(const ScoreArgs &a0, hipStream_t s) {
+    ScoreArgs a = a0;
+    if (a.heads.n == 0 || a.n_frames <= 0) return hipSuccess;
+    const size_t lds = score_lds(a);
+    const dim3 grid((unsigned)a.n_cg, (unsigned)a.units, (unsigned)a.heads.n);
+    if (one_member(a)) hipLaunchKernelGGL((score_kernel<false, true, true>), grid, dim3(kThreads), lds, s, a);
+    else hipLaunchKernelGGL((score_kernel<false, false, true>), grid, dim3(kThreads), lds, s, a);
     return hipGetLastError();
 }
 
