@@ -735,57 +735,82 @@ class Cache8:
         return cls(code(), code(), scale(), scale(), block_tokens)
 
 
-def _cache8(shape: fkv_shape, c: Cache8):
+def _ptr(t: torch.Tensor, name: str, dtype, size, device: int) -> int:
+    """_check with the size given and the device already known (its index)."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device and t.shape == size and t.is_contiguous():
+        return t.data_ptr()
+    _check(t, name, dtype, size)
+    raise ValueError(f"{name} is on {t.device}, other tensors of the call on cuda:{device}")
+
+
+def _device_of(t: torch.Tensor, name: str) -> int:
+    """Index of the GPU that a call runs on, whichever is current: that of its tensor t."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor (got {t.device})")
+    return t.get_device()
+
+
+def _cache8(shape: fkv_shape, c: Cache8, device: int):
     if not isinstance(c, Cache8):
         raise TypeError("cache must be a Cache8")
     if c.block_tokens not in (16, 32, 64, 128):
         raise ValueError(f"block_tokens {c.block_tokens} is not 16, 32, 64 or 128")
     size = (shape.n_heads, shape.cap_frames, shape.frame_tokens, shape.head_dim)
-    nb = size[:2] + (-(-shape.frame_tokens // c.block_tokens),)
-    f8 = torch.float8_e4m3fn
-    return fkv_cache8(_check(c.K, "cache.K", f8, size), _check(c.V, "cache.V", f8, size),
-                      _check(c.k_scale, "cache.k_scale", torch.float32, nb),
-                      _check(c.v_scale, "cache.v_scale", torch.float32, nb), c.block_tokens)
+    nb = size[:2] + (-(-size[2] // c.block_tokens),)
+    f8, f32 = torch.float8_e4m3fn, torch.float32
+    return fkv_cache8(_ptr(c.K, "cache.K", f8, size, device), _ptr(c.V, "cache.V", f8, size, device),
+                      _ptr(c.k_scale, "cache.k_scale", f32, nb, device), _ptr(c.v_scale, "cache.v_scale", f32, nb, device),
+                      c.block_tokens)
 
 
-def _rows(t: torch.Tensor, name: str, shape: fkv_shape, n: int):
+def _rows(t: torch.Tensor, name: str, dtype, size, device: int):
     """Rows [n_heads][n][d] of any head and token stride, the channels adjacent."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if t.device.type != "cuda":
-        raise ValueError(f"{name} must be a GPU tensor (got {t.device})")
-    if t.dtype != _torch_dtype(shape):
-        raise TypeError(f"{name} must be {_torch_dtype(shape)} (got {t.dtype})")
-    if tuple(t.shape) != (shape.n_heads, n, shape.head_dim):
-        raise ValueError(f"{name} must have shape {(shape.n_heads, n, shape.head_dim)} (got {tuple(t.shape)})")
-    if t.stride(2) != 1:
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on cuda:{device} (got {t.device})")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
+    if t.shape != size:
+        raise ValueError(f"{name} must have shape {size} (got {tuple(t.shape)})")
+    head, token, channel = t.stride()
+    if channel != 1:
         raise ValueError(f"{name}: the channels of a row must be adjacent")
     # (a dimension of one element may report any stride)
-    return fkv_rows(t.data_ptr(), t.stride(0) if shape.n_heads > 1 else 0, t.stride(1) if n > 1 else 0)
+    return fkv_rows(t.data_ptr(), head if size[0] > 1 else 0, token if size[1] > 1 else 0)
+
+
+def _ints(values, n: int, name: str):
+    """A host int32 array of n entries from a sequence, numpy array or tensor."""
+    vals = values.tolist() if hasattr(values, "tolist") else values
+    if len(vals) != n:
+        raise ValueError(f"{name} needs {n} entries (got {len(vals)})")
+    return (ctypes.c_int32 * max(n, 1))(*map(int, vals))
+
+
+def _frames(shape: fkv_shape, frame_slot):
+    H = shape.hist_frames
+    return _ints(range(H) if frame_slot is None else frame_slot, H, "frame_slot")
 
 
 def _positions(frame_pos, n: int):
-    vals = [int(v) for v in (frame_pos.tolist() if hasattr(frame_pos, "tolist") else frame_pos)]
-    if len(vals) != n:
-        raise ValueError(f"frame_pos needs {n} entries (got {len(vals)})")
+    arr = _ints(frame_pos, n, "frame_pos")
+    vals = frame_pos.tolist() if hasattr(frame_pos, "tolist") else frame_pos
     if any(not -FKV_MAX_POSITION <= v <= FKV_MAX_POSITION for v in vals):
         raise ValueError(f"frame_pos outside +-{FKV_MAX_POSITION}")
-    return (ctypes.c_int32 * max(n, 1))(*vals)
+    return arr
 
 
-def _device_of(*tensors):
-    """The one device of a call's tensors: the call runs on it, whichever device is current."""
-    devs = {t.device for t in tensors if t is not None}
-    if len(devs) != 1:
-        raise ValueError(f"tensors on more than one device: {sorted(map(str, devs))}")
-    return devs.pop()
-
-
-def _on(device, fn, args, stream):
-    """Calls fn(*args, stream) with ``device`` current and, by default, its current stream."""
+def _run(device: int, fn, args, stream):
+    """fn(*args, stream) on ``device``, by default on its current stream."""
+    if device == torch.cuda.current_device():
+        s = (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+        return _raise(fn(*args, s))
     with torch.cuda.device(device):
-        s = torch.cuda.current_stream(device) if stream is None else stream
-        _raise(fn(*args, ctypes.c_void_p(s.cuda_stream)))
+        s = (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+        _raise(fn(*args, s))
 
 
 def fkv_rotate_chunk(shape: fkv_shape, rope: fkv_rope, frame_pos, Q, K, V, Qr, Kr, Vr, stream=None):
@@ -793,19 +818,30 @@ def fkv_rotate_chunk(shape: fkv_shape, rope: fkv_rope, frame_pos, Q, K, V, Qr, K
     ([n_heads][C*F][d] contiguous).  Q, K, V may be any strided views of that
     shape with adjacent channels (a projection's [tokens][3][n_heads][d], say).
     A pair of Nones is left out."""
-    dt, n = _torch_dtype(shape), _lq(shape)
-    size = (shape.n_heads, n, shape.head_dim)
-    pos = _positions(frame_pos, shape.chunk_frames)
-    src, dst = [], []
+    dt = _torch_dtype(shape)
+    size = (shape.n_heads, _lq(shape), shape.head_dim)
+    dev, src, dst = None, [], []
     for t, o, name in ((Q, Qr, "Q"), (K, Kr, "K"), (V, Vr, "V")):
         if (t is None) != (o is None):
             raise ValueError(f"{name} and its output must both be given or both be None")
-        src.append(None if t is None else ctypes.byref(_rows(t, name, shape, n)))
-        dst.append(None if o is None else _check(o, name + "r", dt, size))
-    if all(t is None for t in (Q, K, V)):
+        if t is None:
+            src.append(None)
+            dst.append(None)
+            continue
+        if dev is None:
+            dev = _device_of(t, name)
+        src.append(ctypes.byref(_rows(t, name, dt, size, dev)))
+        dst.append(_ptr(o, name + "r", dt, size, dev))
+    if dev is None:
         raise ValueError("nothing to rotate")
-    dev = _device_of(Q, K, V, Qr, Kr, Vr)
-    _on(dev, lib().fkv_rotate_chunk, (ctypes.byref(shape), ctypes.byref(rope), pos, *src, *dst), stream)
+    pos = _positions(frame_pos, shape.chunk_frames)
+    _run(dev, lib().fkv_rotate_chunk, (ctypes.byref(shape), ctypes.byref(rope), pos, *src, *dst), stream)
+
+
+def _new_rows(shape, K_new, V_new, n, dev):
+    size = (shape.n_heads, n * shape.frame_tokens, shape.head_dim)
+    dt = _torch_dtype(shape)
+    return ctypes.byref(_rows(K_new, "K_new", dt, size, dev)), ctypes.byref(_rows(V_new, "V_new", dt, size, dev))
 
 
 def fkv_append_frames_rotated(shape: fkv_shape, rope: fkv_rope, frame_pos, K_new, V_new, dst_slot, K_hist, V_hist,
@@ -814,14 +850,13 @@ def fkv_append_frames_rotated(shape: fkv_shape, rope: fkv_rope, frame_pos, K_new
     way.  K_new, V_new: strided views [n_heads][n*F][d] with adjacent channels."""
     dt = _torch_dtype(shape)
     hist = (shape.n_heads, shape.cap_frames, shape.frame_tokens, shape.head_dim)
-    slots = [int(v) for v in dst_slot]
-    n = len(slots)
-    kn, vn = (_rows(t, name, shape, n * shape.frame_tokens) for t, name in ((K_new, "K_new"), (V_new, "V_new")))
-    kh, vh = _check(K_hist, "K_hist", dt, hist), _check(V_hist, "V_hist", dt, hist)
-    arr = (ctypes.c_int32 * max(n, 1))(*slots)
-    _on(_device_of(K_new, V_new, K_hist, V_hist), lib().fkv_append_frames_rotated,
-        (ctypes.byref(shape), ctypes.byref(rope), _positions(frame_pos, n), ctypes.byref(kn), ctypes.byref(vn), n, arr,
-         kh, vh), stream)
+    n = len(dst_slot)
+    dev = _device_of(K_new, "K_new")
+    kn, vn = _new_rows(shape, K_new, V_new, n, dev)
+    kh, vh = _ptr(K_hist, "K_hist", dt, hist, dev), _ptr(V_hist, "V_hist", dt, hist, dev)
+    _run(dev, lib().fkv_append_frames_rotated,
+         (ctypes.byref(shape), ctypes.byref(rope), _positions(frame_pos, n), kn, vn, n, _ints(dst_slot, n, "dst_slot"), kh,
+          vh), stream)
 
 
 def fkv_append_frames_q8(shape: fkv_shape, rope: Optional[fkv_rope], frame_pos, K_new, V_new, dst_slot, cache: Cache8,
@@ -829,35 +864,32 @@ def fkv_append_frames_q8(shape: fkv_shape, rope: Optional[fkv_rope], frame_pos, 
     """fkv_append_frames into an 8-bit cache, the keys rotated on the way (rope
     and frame_pos None: as they are).  K_new, V_new as in
     fkv_append_frames_rotated; the shape's dtype is theirs."""
-    slots = [int(v) for v in dst_slot]
-    n = len(slots)
-    kn, vn = (_rows(t, name, shape, n * shape.frame_tokens) for t, name in ((K_new, "K_new"), (V_new, "V_new")))
-    c = _cache8(shape, cache)
-    arr = (ctypes.c_int32 * max(n, 1))(*slots)
-    _on(_device_of(K_new, V_new, cache.K, cache.V, cache.k_scale, cache.v_scale), lib().fkv_append_frames_q8,
-        (ctypes.byref(shape), None if rope is None else ctypes.byref(rope),
-         None if rope is None else _positions(frame_pos, n), ctypes.byref(kn), ctypes.byref(vn), n, arr,
-         ctypes.byref(c)), stream)
+    n = len(dst_slot)
+    dev = _device_of(K_new, "K_new")
+    kn, vn = _new_rows(shape, K_new, V_new, n, dev)
+    c = _cache8(shape, cache, dev)
+    rp, pos = (None, None) if rope is None else (ctypes.byref(rope), _positions(frame_pos, n))
+    _run(dev, lib().fkv_append_frames_q8,
+         (ctypes.byref(shape), rp, pos, kn, vn, n, _ints(dst_slot, n, "dst_slot"), ctypes.byref(c)), stream)
 
 
 def fkv_score_select_q8(shape: fkv_shape, heads, cache: Cache8, frame_slot, K_cur, scores, kept_seg, kv_len,
                         workspace: Optional[torch.Tensor] = None, stream=None):
     """fkv_score_select over the keys of an 8-bit cache.  If ``workspace`` is
     None a zero-filled one is allocated (through torch's caching allocator)."""
-    n_seg = fkv_num_segments(shape)
-    c = _cache8(shape, cache)
-    sl = _slots(frame_slot, shape.hist_frames)
-    kc = _check(K_cur, "K_cur", _torch_dtype(shape), (shape.n_heads, _lq(shape), shape.head_dim))
-    sc = _check(scores, "scores", torch.float32, (shape.n_heads, n_seg))
-    ks = _check(kept_seg, "kept_seg", torch.int32, (shape.n_heads, n_seg))
-    kl = _check(kv_len, "kv_len", torch.int32, (shape.n_heads,))
+    n, n_seg, i32 = shape.n_heads, fkv_num_segments(shape), torch.int32
+    dev = _device_of(K_cur, "K_cur")
+    c = _cache8(shape, cache, dev)
+    kc = _ptr(K_cur, "K_cur", _torch_dtype(shape), (n, _lq(shape), shape.head_dim), dev)
+    sc = _ptr(scores, "scores", torch.float32, (n, n_seg), dev)
+    ks, kl = _ptr(kept_seg, "kept_seg", i32, (n, n_seg), dev), _ptr(kv_len, "kv_len", i32, (n,), dev)
     if workspace is None:
         need = fkv_score_workspace_size(shape, heads)
         workspace = torch.zeros(max(need, 1), dtype=torch.uint8, device=K_cur.device)
-    ws = _check(workspace, "workspace", torch.uint8)
-    _on(_device_of(cache.K, cache.V, cache.k_scale, cache.v_scale, K_cur, scores, kept_seg, kv_len, workspace),
-        lib().fkv_score_select_q8, (ctypes.byref(shape), _heads(shape, heads), ctypes.byref(c), sl, kc, sc, ks, kl, ws,
-                                    workspace.numel()), stream)
+    ws = _ptr(workspace, "workspace", torch.uint8, getattr(workspace, "shape", None), dev)
+    _run(dev, lib().fkv_score_select_q8,
+         (ctypes.byref(shape), _heads(shape, heads), ctypes.byref(c), _frames(shape, frame_slot),
+          kc, sc, ks, kl, ws, workspace.numel()), stream)
     return workspace
 
 
@@ -877,27 +909,31 @@ def fkv_chunk_attention_q8(shape: fkv_shape, heads, cache: Cache8, frame_slot, k
     [n_heads][n_cur][d] (None, or n_cur = 0: none).  ``workspace``: uint8 device
     tensor of fkv_chunk_attention_q8_workspace_size bytes, zero-filled before its
     first use; None runs one workgroup per query tile."""
-    bf = torch.bfloat16
+    bf, i32 = torch.bfloat16, torch.int32
+    n, d = shape.n_heads, shape.head_dim
+    dev = _device_of(Q, "Q")
     n_q = Q.shape[1] if Q.dim() == 3 else -1
-    n_cur = 0 if K_cur is None else K_cur.shape[1] if K_cur.dim() == 3 else -1
-    n_seg = fkv_num_segments(shape)
-    qs, cs = (shape.n_heads, n_q, shape.head_dim), (shape.n_heads, n_cur, shape.head_dim)
-    c = _cache8(shape, cache)
-    sl = _slots(frame_slot, shape.hist_frames)
-    ks = None if kept_seg is None else _check(kept_seg, "kept_seg", torch.int32, (shape.n_heads, n_seg))
-    kl = None if kv_len is None else _check(kv_len, "kv_len", torch.int32, (shape.n_heads,))
+    qs = (n, n_q, d)
+    q, o = _ptr(Q, "Q", bf, qs, dev), _ptr(O, "O", bf, qs, dev)
+    c = _cache8(shape, cache, dev)
+    ks = kl = kq = vq = ls = ws = None
+    n_cur = nws = 0
+    if kept_seg is not None:
+        ks = _ptr(kept_seg, "kept_seg", i32, (n, fkv_num_segments(shape)), dev)
+    if kv_len is not None:
+        kl = _ptr(kv_len, "kv_len", i32, (n,), dev)
     if (K_cur is None) != (V_cur is None):
         raise ValueError("K_cur and V_cur must both be given or both be None")
-    kq = None if K_cur is None else _check(K_cur, "K_cur", bf, cs)
-    vq = None if V_cur is None else _check(V_cur, "V_cur", bf, cs)
-    q, o = _check(Q, "Q", bf, qs), _check(O, "O", bf, qs)
-    ls = None if lse is None else _check(lse, "lse", torch.float32, (shape.n_heads, n_q))
-    ws, nws = None, 0
+    if K_cur is not None:
+        n_cur = K_cur.shape[1] if K_cur.dim() == 3 else -1
+        kq, vq = _ptr(K_cur, "K_cur", bf, (n, n_cur, d), dev), _ptr(V_cur, "V_cur", bf, (n, n_cur, d), dev)
+    if lse is not None:
+        ls = _ptr(lse, "lse", torch.float32, (n, n_q), dev)
     if workspace is not None:
-        ws, nws = _check(workspace, "workspace", torch.uint8), workspace.numel()
-    _on(_device_of(cache.K, cache.V, cache.k_scale, cache.v_scale, kept_seg, kv_len, Q, K_cur, V_cur, O, lse, workspace),
-        lib().fkv_chunk_attention_q8, (ctypes.byref(shape), _heads(shape, heads), ctypes.byref(c), sl, ks, kl, q, n_q, kq,
-                                       vq, n_cur, ctypes.c_float(scale), o, ls, ws, nws), stream)
+        ws, nws = _ptr(workspace, "workspace", torch.uint8, getattr(workspace, "shape", None), dev), workspace.numel()
+    _run(dev, lib().fkv_chunk_attention_q8,
+         (ctypes.byref(shape), _heads(shape, heads), ctypes.byref(c), _frames(shape, frame_slot),
+          ks, kl, q, n_q, kq, vq, n_cur, scale, o, ls, ws, nws), stream)
 
 
 def fkv_last_error() -> str:

@@ -155,9 +155,10 @@ __device__ __forceinline__ int whole_parts(const AttnArgs &a, const WorkList &wl
 // the part's own normalised output o/l rounded to bf16, in the accumulator
 // layout of the waves (4 values per lane and uint2 index
 // ((wave*MB + mb)*4 + g)*64 + lane), then the running max m (log2 units) of
-// the BM rows, then their probability sums l.
-template <int D>
-__device__ __forceinline__ size_t slot_floats() { return (size_t)BM * (D / 2 + 2); }
+// the BM rows, then their probability sums l.  WIDE: slots of BM*(D + 2) floats,
+// the output in fp32 (two uint2 per index above, one after the other).
+template <int D, bool WIDE = false>
+__device__ __forceinline__ size_t slot_floats() { return (size_t)BM * (D / (WIDE ? 1 : 2) + 2); }
 
 __device__ __forceinline__ uint2 pack_bf16x4(float x0, float x1, float x2, float x3) {
     const uint32_t b0 = __builtin_bit_cast(uint16_t, (__bf16)x0), b1 = __builtin_bit_cast(uint16_t, (__bf16)x1);

@@ -23,10 +23,10 @@ namespace attn {
 // thread does it.  The parts were written in this launch by other
 // workgroups, so they are read with device-scope loads; every other part is
 // complete when its workgroup arrives, so nothing waits.
-template <int D, int NT>
+template <int D, int NT, bool WIDE = false>
 __device__ __forceinline__ void merge_rows(const AttnArgs &a, int b0, int b1, int s0, int li, int qt, int w, int t) {
     constexpr int MB = D / 32;             // 32-row blocks of O^T
-    constexpr int kML = BM * D / 2;        // float offset of m within a slot
+    constexpr int kML = BM * D / (WIDE ? 1 : 2);  // float offset of m within a slot
     constexpr int kVecs = MB * 4 * 64;     // uint2s (4 values) of one wave block's accumulators
     constexpr int kPer = kVecs / NT;
     const int h = a.heads.head[li];
@@ -35,17 +35,28 @@ __device__ __forceinline__ void merge_rows(const AttnArgs &a, int b0, int b1, in
     float M = -__builtin_inff(), L = 0.f;
     float x[kPer][4] = {};
     for (int b = b0; b <= b1; ++b) {
-        const float *p = a.part + (size_t)(b == b0 ? s0 : 2 * b) * slot_floats<D>();
+        const float *p = a.part + (size_t)(b == b0 ? s0 : 2 * b) * slot_floats<D, WIDE>();
         const float m = get_shared(p + kML + row), l = get_shared(p + kML + BM + row);
-        uint2 v[kPer];
+        uint2 v[kPer], u[WIDE ? kPer : 1];
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) v[i] = get_shared((const uint2 *)p + (size_t)w * kVecs + i * NT + t);
+        for (int i = 0; i < kPer; ++i) {
+            const size_t at = (size_t)w * kVecs + i * NT + t;
+            v[i] = get_shared((const uint2 *)p + (WIDE ? 2 * at : at));
+            if constexpr (WIDE) u[i] = get_shared((const uint2 *)p + 2 * at + 1);
+        }
         const float Mn = fmaxf(M, m);
         const float s = __builtin_amdgcn_exp2f(M - Mn), wg = __builtin_amdgcn_exp2f(m - Mn) * l;
         M = Mn;
         L = L * s + wg;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
+            if constexpr (WIDE) {
+                x[i][0] = x[i][0] * s + wg * __uint_as_float(v[i].x);
+                x[i][1] = x[i][1] * s + wg * __uint_as_float(v[i].y);
+                x[i][2] = x[i][2] * s + wg * __uint_as_float(u[i].x);
+                x[i][3] = x[i][3] * s + wg * __uint_as_float(u[i].y);
+                continue;
+            }
             x[i][0] = x[i][0] * s + wg * bf16_lo(v[i].x);
             x[i][1] = x[i][1] * s + wg * bf16_hi(v[i].x);
             x[i][2] = x[i][2] * s + wg * bf16_lo(v[i].y);

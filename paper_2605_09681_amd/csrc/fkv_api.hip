@@ -1388,32 +1388,64 @@ fkv_status check_q8_call(const fkv_shape *s, const fkv_head *heads, int32_t n_q,
     return FKV_OK;
 }
 
-// How an 8-bit attention call (checked) is divided: parts per (head, query
-// tile), so that about one workgroup runs per compute unit and a part keeps a
-// tile for each of its waves.
-struct Q8Plan {
-    int n_split;
-    size_t counter_bytes, bytes;
-};
+// Largest kept history of a head (the heads that share a budget share the answer).
+int64_t q8_most_kept(const fkv_shape *s, const fkv_head *heads) {
+    int64_t most = 0;
+    for (int h = 0; h < s->n_heads; ++h) {
+        if (h > 0 && memcmp(&heads[h], &heads[h - 1], sizeof heads[h]) == 0) continue;
+        most = std::max(most, heads[h].type == FKV_STATIC
+                                  ? (int64_t)static_plan(s->hist_frames, heads[h]).n_kept * s->frame_tokens
+                              : s->hist_frames == 0 ? 0
+                                                    : dyn_plan(s, heads[h]).max_tokens);
+    }
+    return most;
+}
 
 int q8_query_tiles(int32_t n_q) { return (n_q + fkv::kAttnQ8Rows - 1) / fkv::kAttnQ8Rows; }
 
+// Query rows from which a chunk (n_q = n_cur) is attended over an expanded copy
+// of the kept history.
+constexpr int kExpandFrom = 256;
+
+// How an 8-bit attention call (checked) is divided.  In place: parts per (head,
+// query tile), so that about one workgroup runs per compute unit and a part
+// keeps a tile for each of its waves.  The workspace starts with the arrival
+// counters of the split items -- at most one for every two workgroups, so a
+// region of one size for all calls, which nothing else is written to -- and then
+// holds the parts.  Expanded: behind that region it holds the counters of the
+// balanced schedule (cleared by the call itself), its parts, the heads' lengths
+// and the copy.
+struct Q8Plan {
+    bool expand;
+    int n_split, blocks;
+    int64_t slab;
+    int64_t n_counters;                                       // expanded: counters to clear
+    size_t counter_at, part_at, len_at, k_at, v_at, bytes;    // byte offsets in the workspace
+};
+
 fkv_status q8_plan(const fkv_shape *s, const fkv_head *heads, int32_t n_q, int32_t n_cur, Q8Plan *p) {
     fkv_status st;
-    int blocks = 0;
-    if ((st = balanced_blocks(&blocks)) != FKV_OK) return st;
-    int64_t kept = 0;
-    for (int h = 0; h < s->n_heads; ++h) {
-        int64_t n = 0;
-        if ((st = fkv_kept_tokens_max(s, heads, h, &n)) != FKV_OK) return st;
-        kept = std::max(kept, n);
+    memset(p, 0, sizeof *p);
+    if ((st = balanced_blocks(&p->blocks)) != FKV_OK) return st;
+    p->slab = q8_most_kept(s, heads);
+    p->expand = n_q == n_cur && n_q >= kExpandFrom;
+    if (p->expand) {
+        const int64_t items = (int64_t)s->n_heads * ((n_q + fkv::kAttnRowsBf16 - 1) / fkv::kAttnRowsBf16);
+        const size_t copy = (size_t)s->n_heads * p->slab * s->head_dim * 2;
+        p->n_counters = items;
+        p->counter_at = fkv::attention_counter_bytes(p->blocks);
+        p->part_at = p->counter_at + fkv::attention_counter_bytes(items);
+        p->len_at = p->part_at + 2 * (size_t)p->blocks * fkv::attention_part_bytes(s->head_dim, true);
+        p->k_at = p->len_at + 256;
+        p->v_at = p->k_at + copy;
+        p->bytes = p->v_at + copy;
+        return FKV_OK;
     }
-    const int64_t tiles = (kept + 63) / 64 + ((int64_t)n_cur + 63) / 64;
+    const int64_t tiles = (p->slab + 63) / 64 + ((int64_t)n_cur + 63) / 64;
     const int64_t items = (int64_t)s->n_heads * q8_query_tiles(n_q);
-    p->n_split = (int)std::max<int64_t>(1, std::min<int64_t>(blocks / items, (tiles + 7) / 8));
-    p->counter_bytes = p->n_split > 1 ? fkv::attention_counter_bytes(items) : 0;
-    p->bytes = p->counter_bytes +
-               (p->n_split > 1 ? (size_t)items * p->n_split * fkv::attn_q8_part_floats(s->head_dim) * sizeof(float) : 0);
+    p->n_split = (int)std::max<int64_t>(1, std::min<int64_t>(p->blocks / items, (tiles + 7) / 8));
+    p->part_at = fkv::attention_counter_bytes(p->blocks);
+    p->bytes = p->n_split > 1 ? p->part_at + (size_t)items * p->n_split * fkv::attn_q8_part_floats(s->head_dim) * sizeof(float) : 0;
     return FKV_OK;
 }
 
@@ -1586,7 +1618,9 @@ fkv_status fkv_chunk_attention_q8(const fkv_shape *shape, const fkv_head *heads,
     }
     if (!Q || !O || (n_cur > 0 && (!K_cur || !V_cur))) return fail(FKV_ERR_ARG, "NULL tensor pointer");
     if (!(scale > 0.f) || !isfinite(scale)) return fail(FKV_ERR_ARG, "scale %g must be positive and finite", (double)scale);
-    Q8Plan p = {1, 0, 0};
+    Q8Plan p;
+    memset(&p, 0, sizeof p);
+    p.n_split = 1;
     if (workspace && (st = q8_plan(shape, heads, n_q, n_cur, &p)) != FKV_OK) return st;
     if (workspace && workspace_bytes < p.bytes)
         return fail(FKV_ERR_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, p.bytes);
@@ -1621,8 +1655,9 @@ fkv_status fkv_chunk_attention_q8(const fkv_shape *shape, const fkv_head *heads,
     a.scale_log2 = scale * 1.4426950408889634f;
     a.n_qtiles = q8_query_tiles(n_q);
     a.n_split = p.n_split;
-    a.counters = (uint32_t *)workspace;
-    if (workspace) a.part = (float *)((char *)workspace + p.counter_bytes);
+    a.counters = (uint32_t *)((char *)workspace + p.counter_at);
+    a.n_counters = p.n_counters;
+    if (workspace) a.part = (float *)((char *)workspace + p.part_at);
     for (int h = 0; h < shape->n_heads; ++h) {
         if (heads[h].type == FKV_DYNAMIC) {
             a.st_kept[h] = H > 0 ? -1 : 0;
@@ -1635,6 +1670,39 @@ fkv_status fkv_chunk_attention_q8(const fkv_shape *shape, const fkv_head *heads,
     }
     for (int t = 0; t < H; ++t) a.slots.slot[t] = frame_slot[t];
     (void)hipGetLastError();
+    if (p.expand) {
+        a.Kc = (uint16_t *)((char *)workspace + p.k_at);
+        a.Vc = (uint16_t *)((char *)workspace + p.v_at);
+        a.kv_out = (int32_t *)((char *)workspace + p.len_at);
+        a.slab = p.slab;
+        if ((st = device_status(fkv::launch_expand_q8(a, shape->head_dim, (hipStream_t)stream),
+                                "fkv_chunk_attention_q8 launch")) != FKV_OK)
+            return st;
+        fkv::AttnArgs b;
+        memset(&b, 0, sizeof b);
+        b.Q = Q;
+        b.Kc = a.Kc;
+        b.Vc = a.Vc;
+        b.K_cur = K_cur;
+        b.V_cur = V_cur;
+        b.O = O;
+        b.lse = lse;
+        b.kv_len = a.kv_out;
+        b.slab = p.slab;
+        b.n_heads = shape->n_heads;
+        b.heads = all_heads(shape->n_heads);
+        b.Lq = n_q;
+        b.scale = scale;
+        b.scale_log2 = a.scale_log2;
+        b.n_qtiles = (n_q + fkv::kAttnRowsBf16 - 1) / fkv::kAttnRowsBf16;
+        b.n_items = b.n_heads * b.n_qtiles;
+        b.items_per_xcd = (b.n_items + 7) / 8;
+        b.n_blocks = p.blocks;
+        b.part = a.part;
+        b.item_counters = a.counters;
+        return device_status(fkv::launch_attention_bf16_wide(b, shape->head_dim, (hipStream_t)stream),
+                             "fkv_chunk_attention_q8 launch");
+    }
     return device_status(fkv::launch_attention_q8(a, shape->head_dim, (hipStream_t)stream),
                          "fkv_chunk_attention_q8 launch");
 }

@@ -250,6 +250,7 @@ struct AttnQ8Args {
     int32_t n_split;                    // parts per (head, query tile); 1: no workspace
     float *part;                        // [head][query tile][part] slots of attn_q8_part_floats
     uint32_t *counters;                 // arrivals per (head, query tile), kItemCounterStride apart
+    int64_t n_counters;                 // expanding: counters to clear
     // the expanded copy (attn_q8 over large chunks): bf16 [n_heads][slab][d], and its lengths
     uint16_t *Kc, *Vc;
     int32_t *kv_out;
@@ -278,7 +279,9 @@ hipError_t launch_score(const ScoreArgs &a, bool f32, hipStream_t s);
 hipError_t launch_score_q8(const ScoreArgs &a, hipStream_t s);  // full pass over an 8-bit history
 void score_workspace_layout(ScoreArgs &a, void *ws, int n_list, int H, int units, int n_cg);
 hipError_t launch_attention_bf16(const AttnArgs &a, int head_dim, hipStream_t s);
-size_t attention_part_bytes(int head_dim);  // bytes of one partial-result slot (bf16 kernel)
+// over a compact copy, balanced schedule, the parts of cut items in fp32
+hipError_t launch_attention_bf16_wide(const AttnArgs &a, int head_dim, hipStream_t s);
+size_t attention_part_bytes(int head_dim, bool wide = false);  // bytes of one partial-result slot (bf16 kernel)
 // Arrival counters of the bf16 balanced schedule: one 256-byte line per item,
 // after the 2 * n_blocks partial-result slots of the workspace.
 constexpr int kItemCounterStride = 64;   // uint32 per counter
@@ -303,6 +306,7 @@ hipError_t launch_append_q8(const AppendQ8Args &a, int head_dim, bool f32, hipSt
 // attention over 8-bit caches (k_attn_q8.hip)
 constexpr int kAttnQ8Rows = 16;             // query rows of a tile
 hipError_t launch_attention_q8(const AttnQ8Args &a, int head_dim, hipStream_t s);
+hipError_t launch_expand_q8(const AttnQ8Args &a, int head_dim, hipStream_t s);  // kept history to Kc, Vc, kv_out
 inline size_t attn_q8_part_floats(int head_dim) { return (size_t)kAttnQ8Rows * (head_dim + 2); }
 
 }  // namespace fkv

@@ -320,7 +320,7 @@ __device__ __forceinline__ void score_block(const uint16_t *ks, int kbase, const
 // whole item and the normalised output (and lse) is written; otherwise the
 // partial result goes to the slot.  Uses every thread of the workgroup and
 // leaves no LDS read pending.
-template <int D, bool PAGED>
+template <int D, bool PAGED, bool WIDE>
 __device__ __forceinline__ void attn_segment(const AttnArgs &a, uint16_t *Ks, uint16_t *Vs, uint32_t *redo, int li,
                                              int qt, int t0, int t1, int rot, float *slot) {
     using C = Cfg<D>;
@@ -599,9 +599,15 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, uint16_t *Ks, ui
             pb[t][j + 1] = (__bf16)e1;
         };
         // The row sum adds the bf16-rounded probabilities -- exactly the P the
-        // value product consumes -- two at a time, in two chains.
+        // value product consumes -- two at a time, in two chains.  WIDE: the
+        // probabilities themselves (e0 and e1 are still the pair's).
         float l2 = 0.f;
         auto sum_pair = [&](int p) {
+            if constexpr (WIDE) {
+                l_run += e0;
+                l2 += e1;
+                return;
+            }
             const int t = p >> 2, j = 2 * (p & 3);
             const bf16x2_t pr = {pb[t][j], pb[t][j + 1]};
             if (t & 1) l2 = __builtin_amdgcn_fdot2_f32_bf16(pr, kOnes2, l2, false);
@@ -795,6 +801,12 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, uint16_t *Ks, ui
         for (int mb = 0; mb < C::MB; ++mb)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
+                if constexpr (WIDE) {
+                    unsigned long long *at = op + 2 * (((wave * C::MB + mb) * 4 + g) * 64 + lane);
+                    put_shared(at, make_uint2(__float_as_uint(o[mb][4 * g] * inv), __float_as_uint(o[mb][4 * g + 1] * inv)));
+                    put_shared(at + 1, make_uint2(__float_as_uint(o[mb][4 * g + 2] * inv), __float_as_uint(o[mb][4 * g + 3] * inv)));
+                    continue;
+                }
                 const uint2 v = pack_bf16x4(o[mb][4 * g] * inv, o[mb][4 * g + 1] * inv, o[mb][4 * g + 2] * inv,
                                             o[mb][4 * g + 3] * inv);
                 put_shared(op + ((wave * C::MB + mb) * 4 + g) * 64 + lane, v);
@@ -803,8 +815,9 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, uint16_t *Ks, ui
             // a sum far above one hands its exponent to the maximum: the weights by
             // which the merge multiplies outputs stay small
             const int e = l_tot > 0x1p24f ? __builtin_amdgcn_frexp_expf(l_tot) : 0;
-            put_shared(slot + BM * D / 2 + wave * 32 + l32, m_run + (float)e);
-            put_shared(slot + BM * D / 2 + BM + wave * 32 + l32, __builtin_amdgcn_ldexpf(l_tot, -e));
+            constexpr int kML = BM * D / (WIDE ? 1 : 2);
+            put_shared(slot + kML + wave * 32 + l32, m_run + (float)e);
+            put_shared(slot + kML + BM + wave * 32 + l32, __builtin_amdgcn_ldexpf(l_tot, -e));
         }
         return;
     }
@@ -826,8 +839,11 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, uint16_t *Ks, ui
 // each XCD (blocks go to the 8 XCDs round-robin) receives a contiguous range
 // of items: the query tiles of a head then share that XCD's L2.
 // BAL = true: the balanced schedule above, with the same XCD-contiguous
-// assignment of ranges (n_blocks is a multiple of 8).
-template <int D, bool BAL, bool PAGED>
+// assignment of ranges (n_blocks is a multiple of 8).  WIDE (the attention over an
+// 8-bit cache): the parts of a cut item stay in fp32 until they are joined, and
+// the row sum, so lse too, adds the probabilities before their rounding; otherwise
+// the parts are rounded to bf16, half the bytes of a slot.
+template <int D, bool BAL, bool PAGED, bool WIDE = false>
 __global__ __launch_bounds__(kThreads, 2) void attn_bf16_kernel(AttnArgs a) {
     using C = Cfg<D>;
     __shared__ __attribute__((aligned(16))) uint16_t Ks[kBufs * C::TILE];
@@ -839,7 +855,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_kernel(AttnArgs a) {
         const int item = (blockIdx.x & 7) * a.items_per_xcd + (blockIdx.x >> 3);
         if (item >= a.n_items) return;
         const int li = item / a.n_qtiles;
-        attn_segment<D, PAGED>(a, Ks, Vs, &redo, li, item - li * a.n_qtiles, 0, entry_tiles<PAGED>(a, li), 0, nullptr);
+        attn_segment<D, PAGED, WIDE>(a, Ks, Vs, &redo, li, item - li * a.n_qtiles, 0, entry_tiles<PAGED>(a, li), 0, nullptr);
         return;
     }
     const WorkList wl = work_list<PAGED>(a);
@@ -887,14 +903,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_bf16_kernel(AttnArgs a) {
             rot = (int)((ibase - sc.start(b0)) % ip.T);
             cur = ibase + t1;
         }
-        float *slot = n_parts == 1 ? nullptr : a.part + (size_t)(2 * r + (first ? 0 : 1)) * slot_floats<D>();
-        attn_segment<D, PAGED>(a, Ks, Vs, &redo, li, qt, t0, t1, rot, slot);
+        float *slot = n_parts == 1 ? nullptr : a.part + (size_t)(2 * r + (first ? 0 : 1)) * slot_floats<D, WIDE>();
+        attn_segment<D, PAGED, WIDE>(a, Ks, Vs, &redo, li, qt, t0, t1, rot, slot);
         if (slot) {
             // the last of the item's parts to arrive combines them (no wait:
             // every other part is complete when its workgroup arrives)
             uint32_t *cnt = a.item_counters + (size_t)(li * a.n_qtiles + qt) * kItemCounterStride;
             if (arrive_last(cnt, (uint32_t)n_parts, &flag))
-                merge_rows<D, 64>(a, b0, b0 + n_parts - 1, s0, li, qt, threadIdx.x >> 6, threadIdx.x & 63);
+                merge_rows<D, 64, WIDE>(a, b0, b0 + n_parts - 1, s0, li, qt, threadIdx.x >> 6, threadIdx.x & 63);
         }
         first = false;
     }
@@ -1134,6 +1150,14 @@ hipError_t launch_attention_bf16(const AttnArgs &a, int head_dim, hipStream_t s)
     return a.paged ? launch_bf16<true>(a, head_dim, s) : launch_bf16<false>(a, head_dim, s);
 }
 
+hipError_t launch_attention_bf16_wide(const AttnArgs &a, int head_dim, hipStream_t s) {
+    if (head_dim == 128)
+        hipLaunchKernelGGL((attn_bf16_kernel<128, true, false, true>), dim3(a.n_blocks), dim3(kThreads), 0, s, a);
+    else
+        hipLaunchKernelGGL((attn_bf16_kernel<64, true, false, true>), dim3(a.n_blocks), dim3(kThreads), 0, s, a);
+    return hipGetLastError();
+}
+
 hipError_t launch_attention_mass(const AttnArgs &a, int head_dim, hipStream_t s) {
     const bool bins_short = a.mass_F <= kShortBin;
     if (head_dim == 128 && bins_short)
@@ -1149,6 +1173,8 @@ hipError_t launch_attention_mass(const AttnArgs &a, int head_dim, hipStream_t s)
     return hipGetLastError();
 }
 
-size_t attention_part_bytes(int head_dim) { return (size_t)kAttnRowsBf16 * (head_dim / 2 + 2) * 4; }
+size_t attention_part_bytes(int head_dim, bool wide) {
+    return (size_t)kAttnRowsBf16 * (head_dim / (wide ? 1 : 2) + 2) * 4;
+}
 
 }  // namespace fkv

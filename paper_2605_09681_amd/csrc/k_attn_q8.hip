@@ -361,7 +361,63 @@ __global__ __launch_bounds__(kThreads) void attn_q8_kernel(AttnQ8Args a) {
     if (a.lse && d == 0) a.lse[out_row] = fmaf(M, kLn2, logf(L));
 }
 
+// Large chunks: the kept history as a bf16 copy [n_heads][slab][d] for the chunk
+// attention's kernel.  A workgroup widens kExpandRows rows of K and V; 16 bytes
+// of codes per thread and row.  grid: x = row group, y = head.
+constexpr int kExpandThreads = 256, kExpandRows = 128;
+template <int D>
+__global__ __launch_bounds__(kExpandThreads) void expand_q8_kernel(AttnQ8Args a) {
+    constexpr int TPR = D / 16, RPP = kExpandThreads / TPR, N = kExpandRows / RPP;   // threads per row, rows per pass
+    __shared__ int slots[FKV_MAX_FRAMES];
+    const int tid = threadIdx.x, h = blockIdx.y;
+    if (tid < a.H) slots[tid] = a.slots.slot[tid];
+    __syncthreads();
+    const History x = history_of(a, h);
+    if (blockIdx.x == 0 && tid == 0) a.kv_out[h] = x.kvl;
+    // the arrival counters of the attention launch that follows
+    const int64_t n_threads = (int64_t)gridDim.x * gridDim.y * kExpandThreads;
+    for (int64_t i = ((int64_t)h * gridDim.x + blockIdx.x) * kExpandThreads + tid; i < a.n_counters; i += n_threads)
+        a.counters[i * kItemCounterStride] = 0;
+    const int j0 = blockIdx.x * kExpandRows + tid / TPR, c = tid % TPR * 16;
+    const uint8_t *K8 = a.K8 + (int64_t)h * a.cap * a.F * D, *V8 = a.V8 + (int64_t)h * a.cap * a.F * D;
+    const float *ks = a.k_scale + (int64_t)h * a.cap * a.n_blocks, *vs = a.v_scale + (int64_t)h * a.cap * a.n_blocks;
+    u32x4 k[N], v[N];
+    float sk[N], sv[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int j = j0 + i * RPP;
+        if (j < x.kvl) {
+            const Place at = place_of(a, x, slots, j);
+            const uint32_t off = (uint32_t)(at.slot * a.F + at.p) * D + c, blk = at.slot * a.n_blocks + (at.p >> a.block_shift);
+            k[i] = __builtin_nontemporal_load((const u32x4 *)(K8 + off));
+            v[i] = __builtin_nontemporal_load((const u32x4 *)(V8 + off));
+            sk[i] = ks[blk];
+            sv[i] = vs[blk];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int j = j0 + i * RPP;
+        if (j < x.kvl) {
+            const int64_t off = ((int64_t)h * a.slab + j) * D + c;
+            u32x4 *dk = (u32x4 *)(a.Kc + off), *dv = (u32x4 *)(a.Vc + off);
+            dk[0] = widen8(k[i][0], k[i][1], sk[i]);
+            dk[1] = widen8(k[i][2], k[i][3], sk[i]);
+            dv[0] = widen8(v[i][0], v[i][1], sv[i]);
+            dv[1] = widen8(v[i][2], v[i][3], sv[i]);
+        }
+    }
+}
+
 }  // namespace
+
+hipError_t launch_expand_q8(const AttnQ8Args &a, int head_dim, hipStream_t s) {
+    const int64_t groups = (a.slab + kExpandRows - 1) / kExpandRows;
+    const dim3 grid((unsigned)(groups > 0 ? groups : 1), (unsigned)a.n_heads);
+    if (head_dim == 64) hipLaunchKernelGGL(expand_q8_kernel<64>, grid, dim3(kExpandThreads), 0, s, a);
+    else hipLaunchKernelGGL(expand_q8_kernel<128>, grid, dim3(kExpandThreads), 0, s, a);
+    return hipGetLastError();
+}
 
 hipError_t launch_attention_q8(const AttnQ8Args &a, int head_dim, hipStream_t s) {
     const dim3 grid((unsigned)((int64_t)a.n_heads * a.n_qtiles * a.n_split));

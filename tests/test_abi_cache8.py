@@ -184,18 +184,18 @@ def test_binding_refusals(fkv):
     with pytest.raises(ValueError):
         fkv.fkv_rotate_chunk(shape, rope, [0, 1], x, None, None, x, None, None)          # CPU tensors
     with pytest.raises(ValueError):
-        fkv.fkv_rotate_chunk(shape, rope, [0], x, None, None, x, None, None)              # one position for two frames
+        fkv._positions([0], 2)                                                            # one position for two frames
     with pytest.raises(ValueError):
-        fkv.fkv_rotate_chunk(shape, rope, [0, 1 << 25], x, None, None, x, None, None)
+        fkv._positions([0, 1 << 25], 2)
     with pytest.raises(ValueError):
         fkv.fkv_rotate_chunk(shape, rope, [0, 1], None, None, None, None, None, None)
     with pytest.raises(ValueError):
         fkv.fkv_rotate_chunk(shape, rope, [0, 1], x, None, None, None, None, None)
     with pytest.raises(TypeError):
-        fkv._cache8(shape, object())
+        fkv._cache8(shape, object(), 0)
     with pytest.raises(ValueError):
-        fkv._cache8(shape, fkv.Cache8.zeros(shape, 64, device="cpu"))                     # CPU tensors
+        fkv._cache8(shape, fkv.Cache8.zeros(shape, 64, device="cpu"), 0)                  # CPU tensors
     bad = fkv.Cache8.zeros(shape, 64, device="cpu")
     bad.block_tokens = 20
     with pytest.raises(ValueError):
-        fkv._cache8(shape, bad)
+        fkv._cache8(shape, bad, 0)
