@@ -596,9 +596,11 @@ fkv_status fkv_append_frames_q8(const fkv_shape *shape, const fkv_rope *rope,
                                 const fkv_rows *V_new, int32_t n_frames, const int32_t *dst_slot,
                                 const fkv_cache8 *cache, void *stream);
 
-/* fkv_score_select over an 8-bit cache: the same scores, kept_seg and kv_len,
- * bit for bit, that fkv_score_select gives for a bf16 cache of the values that
- * K8 stands for.  K_cur is bf16 (shape->dtype FKV_BF16: FKV_ERR_SHAPE
+/* fkv_score_select over an 8-bit cache: the scores, kept_seg and kv_len of the
+ * values that K8 stands for.  Products of codes are exact and summed four at a
+ * time in fp32, the rest in fp64: a score is within 6 * 2^-24 of the cosine, then
+ * rounded once; the selection is exactly fkv_select's on those scores.  The same
+ * bits on every run.  K_cur is bf16 (shape->dtype FKV_BF16: FKV_ERR_SHAPE
  * otherwise).  V8 and v_scale are not read.  Workspace as in fkv_score_select. */
 fkv_status fkv_score_select_q8(const fkv_shape *shape, const fkv_head *heads,
                                const fkv_cache8 *cache, const int32_t *frame_slot,

@@ -805,12 +805,11 @@ def _positions(frame_pos, n: int):
 
 def _run(device: int, fn, args, stream):
     """fn(*args, stream) on ``device``, by default on its current stream."""
-    if device == torch.cuda.current_device():
-        s = (torch.cuda.current_stream() if stream is None else stream).cuda_stream
-        return _raise(fn(*args, s))
+    if device == torch._C._cuda_getDevice():
+        # (the stream's handle alone: a Stream object costs more than a small call's launch)
+        return _raise(fn(*args, torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream))
     with torch.cuda.device(device):
-        s = (torch.cuda.current_stream() if stream is None else stream).cuda_stream
-        _raise(fn(*args, s))
+        _raise(fn(*args, torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream))
 
 
 def fkv_rotate_chunk(shape: fkv_shape, rope: fkv_rope, frame_pos, Q, K, V, Qr, Kr, Vr, stream=None):

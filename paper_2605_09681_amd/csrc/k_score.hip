@@ -114,14 +114,6 @@ struct Vec<true> {  // 4 fp32
     __device__ static __forceinline__ double at(const u32x4 &v, int e) { return (double)__uint_as_float(v[e]); }
 };
 
-// 8 E4M3 codes and their scale (a power of two) as 8 bf16, exactly.
-__device__ __forceinline__ u32x4 widen8(uint32_t c0, uint32_t c1, float scale) {
-    return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c0, scale, false)),
-                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c0, scale, true)),
-                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c1, scale, false)),
-                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c1, scale, true))};
-}
-
 // A lane's columns of one frame widened to fp64 (exact), vector 0 then vector
 // 1, elements in order: each element is converted once, and the frame serves
 // as the current frame (its squares, its product with the previous frame) and
@@ -334,12 +326,41 @@ __device__ void finish_pooled(const ScoreArgs &a) {
     }
 }
 
-// Q8: an 8-bit history (E4M3 codes with a power-of-two scale per block of tokens).
-// A lane loads 8 codes where it would load a 16-byte vector of bf16 and widens
-// them (exactly) to that vector: from there on every lane, sum and order is
-// the bf16 kernel's, so the scores are those of the bf16 cache that the codes
-// stand for, bit for bit.
-template <bool F32, bool DIRECT, bool Q8 = false>
+// The end of a workgroup whose per-frame sums lie in wg_part (LDS, after the
+// finisher's rows): it stores them as one block and arrives; the head's last
+// workgroup finishes the head, the last head's the pooled scores.  FLAT: few
+// workgroups per head arrive on its one counter.
+template <bool DIRECT, bool FLAT = false>
+__device__ __forceinline__ void store_and_finish(const ScoreArgs &a, double *dyn, const double *wg_part, uint32_t *flag) {
+    const int cg = blockIdx.x, u = blockIdx.y, li = blockIdx.z, tid = threadIdx.x, nf = a.n_frames;
+    __syncthreads();
+    {
+        double *blk = a.part + (((int64_t)li * a.units + u) * a.n_cg + cg) * (nf * 2);
+        for (int r = tid; r < nf * 2; r += kThreads) put_shared(blk + r, wg_part[r]);
+    }
+    // two-level arrival of the head's workgroups
+    const int n_wg = a.units * a.n_cg, wi = u * a.n_cg + cg, g1 = wi % kGroups;
+    uint32_t *cnt = a.counters + (int64_t)li * kCountersPerHead * kCounterStride;
+    if (FLAT) {
+        if (!arrive_last(cnt + kGroups * kCounterStride, (uint32_t)n_wg, flag)) return;
+    } else {
+        if (!arrive_last(cnt + g1 * kCounterStride, (uint32_t)((n_wg - g1 + kGroups - 1) / kGroups), flag)) return;
+        if constexpr (!DIRECT) group_sum(a, li, g1);
+        if (!arrive_last(cnt + kGroups * kCounterStride, (uint32_t)min(n_wg, kGroups), flag)) return;
+    }
+    double *T = dyn;
+    uint64_t *s_keys = (uint64_t *)(dyn + a.lds_rows + nf * 2);
+    float *s_scores = (float *)(s_keys + a.n_seg);
+    unsigned char *s_forced = (unsigned char *)(s_scores + a.n_seg);
+    finish_head<DIRECT>(a, li, T, s_keys, s_scores, s_forced, s_forced + a.n_seg);
+    if (a.pooled && a.mode != kScoreModeHistory) {
+        uint32_t *pc = a.counters + (int64_t)a.heads.n * kCountersPerHead * kCounterStride;
+        if (!arrive_last(pc, (uint32_t)a.heads.n, flag)) return;
+        finish_pooled(a);
+    }
+}
+
+template <bool F32, bool DIRECT>
 __global__ __launch_bounds__(kThreads, 5) void score_kernel(ScoreArgs a) {
     extern __shared__ double dyn[];            // finisher rows (lds_rows), this workgroup's sums (2 n_frames),
                                                // then (selecting) n_seg keys, n_seg floats, 2 n_seg bytes
@@ -365,23 +386,6 @@ __global__ __launch_bounds__(kThreads, 5) void score_kernel(ScoreArgs a) {
     const u32x4 *cur = (const u32x4 *)a.K_cur + (int64_t)h * a.cur_head_vecs + (int64_t)u * a.unit_vecs;
     auto load = [&](int f, u32x4 (&x)[kV]) {
         const int t = a.t_begin + f;
-        if constexpr (Q8) {
-            if (t < a.H) {
-                const int64_t slot = (int64_t)h * a.cap + a.slots.slot[t];
-                const uint2 *base = (const uint2 *)a.K_hist + slot * a.frame_vecs + (int64_t)u * a.unit_vecs;
-                const float *scale = a.k_scale + slot * a.q8_blocks;
-#pragma unroll
-                for (int j = 0; j < kV; ++j) {
-                    x[j] = u32x4{0, 0, 0, 0};
-                    if (ok[j]) {
-                        const uint2 c = base[col[j]];
-                        const float sc = scale[(u * a.q8_unit_tokens + (col[j] >> a.q8_row_shift)) >> a.q8_shift];
-                        x[j] = widen8(c.x, c.y, sc);
-                    }
-                }
-                return;
-            }
-        }
         const u32x4 *base = t < a.H ? hist + (int64_t)a.slots.slot[t] * a.frame_vecs : cur;
 #pragma unroll
         for (int j = 0; j < kV; ++j) x[j] = ok[j] ? __builtin_nontemporal_load(base + col[j]) : u32x4{0, 0, 0, 0};
@@ -427,27 +431,150 @@ __global__ __launch_bounds__(kThreads, 5) void score_kernel(ScoreArgs a) {
         put(fb - 1, 1, wave_sum(prev.dot(next)));
     }
 
+    store_and_finish<DIRECT>(a, dyn, wg_part, &flag);
+}
+
+// ------------------------------------------------------------ 8-bit histories
+// The full pass over an 8-bit history (E4M3 codes c with a power-of-two scale s
+// per block of tokens).  A lane owns 16 adjacent channels of a token -- one
+// 16-byte load and one scale per frame, kMaxF8 frames at once -- where the bf16
+// kernel's lane owns two vectors of 8.  Its sums of 16 products are formed in
+// fp32 from the codes themselves, in four chains of four: every product of two
+// codes is exact there (8 significant bits, 2^-18 .. 2^18), whatever the scales,
+// and a chain rounds three times, at most 2^-24 of the chain's magnitudes each;
+// the sum of the chains, its scale (exact: a power of two) and everything beyond
+// the lane is fp64.  A chain is off by 3 * 2^-24 of its products' magnitudes at most,
+// so a score is within 6 * 2^-24 of the cosine before its own rounding whatever the
+// data (the product's sum 3, the two norms 1.5 each), about 2^-31 where signs are
+// mixed; equal frames still score equal, as the same products take the same path.
+// (fp64 products of widened elements, as above, took 25.0 us at 480P: the fp64
+// conversion of every element, with half the bytes to hide it behind.)
+// Frame H is bf16: the lane's 16 elements and their products with frame H - 1
+// are fp64.
+constexpr int kMaxF8 = 6;      // a 480P layer's run of frames per wave
+constexpr int kFlat8 = 32;     // workgroups of a head that arrive on one counter
+
+struct Codes16 {
+    float v[16];
+    __device__ __forceinline__ void set(const u32x4 &c) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[i], true);
+            v[4 * i] = lo[0];
+            v[4 * i + 1] = lo[1];
+            v[4 * i + 2] = hi[0];
+            v[4 * i + 3] = hi[1];
+        }
+    }
+    // sum over 16 channels of this times b, in four chains
+    __device__ __forceinline__ double dot(const Codes16 &b) const {
+        float s[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] = v[i] * b.v[i];
+#pragma unroll
+        for (int i = 4; i < 16; ++i) s[i & 3] = fmaf(v[i], b.v[i], s[i & 3]);
+        return ((double)s[0] + (double)s[1]) + ((double)s[2] + (double)s[3]);
+    }
+};
+
+template <bool DIRECT, bool FLAT>
+__global__ __launch_bounds__(kThreads, 5) void score_q8_kernel(ScoreArgs a) {
+    extern __shared__ double dyn[];            // as in score_kernel
+    __shared__ u32x4 edge[kWaves][64];         // codes and scales of each wave's first frame
+    __shared__ float edge_scale[kWaves][64];
+    __shared__ uint32_t flag;
+
+    const int cg = blockIdx.x, u = blockIdx.y, li = blockIdx.z;
+    const int h = a.heads.head[li];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int nf = a.n_frames, H = a.H;        // nf = H + 1
+    const int nw = min(kWaves, nf);
+    const int fa = w < nw ? (w * nf) / nw : nf;
+    const int fb = w < nw ? ((w + 1) * nf) / nw : nf;
+    const int col = cg * (kCols / 2) + lane;   // 16-channel column of the unit
+    const bool ok = 2 * col < a.unit_vecs;
+    const int64_t frame_cols = a.frame_vecs / 2;
+    const u32x4 *codes = (const u32x4 *)a.K_hist + (int64_t)h * a.cap * frame_cols + (int64_t)u * (a.unit_vecs / 2) + (ok ? col : 0);
+    const float *scales = a.k_scale + (int64_t)h * a.cap * a.q8_blocks +
+                          ((u * a.q8_unit_tokens + (ok ? (2 * col) >> a.q8_row_shift : 0)) >> a.q8_shift);
+    double *wg_part = dyn + a.lds_rows;
+    auto put = [&](int f, int q, double v) {
+        if (lane == 63) wg_part[f * 2 + q] = v;
+    };
+
+    Codes16 prev;
+    float sp = 0.f;                            // the previous frame's scale
+    u32x4 cur[2];                              // frame H
+    const bool has_cur = fa < fb && fb == nf;
+    if (has_cur) {
+        const u32x4 *K = (const u32x4 *)a.K_cur + (int64_t)h * a.cur_head_vecs + (int64_t)u * a.unit_vecs + (ok ? 2 * col : 0);
+        cur[0] = K[0];
+        cur[1] = K[1];
+    }
+    const int fh = min(fb, H);                 // the run's cached frames are [fa, fh)
+    for (int f0 = fa; f0 < fh; f0 += kMaxF8) {
+        u32x4 raw[kMaxF8];
+        float sc[kMaxF8];
+#pragma unroll
+        for (int i = 0; i < kMaxF8; ++i) {
+            const int64_t slot = a.slots.slot[min(f0 + i, H - 1)];   // (past the run: loaded, not used)
+            raw[i] = codes[slot * frame_cols];
+            sc[i] = scales[slot * a.q8_blocks];
+        }
+#pragma unroll
+        for (int i = 0; i < kMaxF8; ++i) {
+            const int f = f0 + i;
+            if (f < fh) {
+                if (f == fa) {
+                    edge[w][lane] = raw[i];
+                    edge_scale[w][lane] = sc[i];
+                }
+                Codes16 now;
+                now.set(raw[i]);
+                const double s = (double)sc[i];
+                const double q = ok ? now.dot(now) * s * s : 0.0;
+                put(f, 0, wave_sum(q));
+                if (f > fa) put(f - 1, 1, wave_sum(ok ? prev.dot(now) * s * (double)sp : 0.0));
+                prev = now;
+                sp = sc[i];
+            }
+        }
+    }
     __syncthreads();
-    {
-        double *blk = a.part + (((int64_t)li * a.units + u) * a.n_cg + cg) * (nf * 2);
-        for (int r = tid; r < nf * 2; r += kThreads) put_shared(blk + r, wg_part[r]);
+    if (has_cur) {
+        double sq = 0.0, dot = 0.0;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const double c = Vec<false>::at(cur[j], e);
+                sq = fma(c, c, sq);
+                dot = fma(c, (double)prev.v[8 * j + e], dot);
+            }
+        put(H, 0, wave_sum(ok ? sq : 0.0));
+        if (fh > fa) put(H - 1, 1, wave_sum(ok ? dot * (double)sp : 0.0));
     }
-    // two-level arrival of the head's workgroups
-    const int n_wg = a.units * a.n_cg, wi = u * a.n_cg + cg, g1 = wi % kGroups;
-    uint32_t *cnt = a.counters + (int64_t)li * kCountersPerHead * kCounterStride;
-    if (!arrive_last(cnt + g1 * kCounterStride, (uint32_t)((n_wg - g1 + kGroups - 1) / kGroups), &flag)) return;
-    if constexpr (!DIRECT) group_sum(a, li, g1);
-    if (!arrive_last(cnt + kGroups * kCounterStride, (uint32_t)min(n_wg, kGroups), &flag)) return;
-    double *T = dyn;
-    uint64_t *s_keys = (uint64_t *)(dyn + a.lds_rows + nf * 2);
-    float *s_scores = (float *)(s_keys + a.n_seg);
-    unsigned char *s_forced = (unsigned char *)(s_scores + a.n_seg);
-    finish_head<DIRECT>(a, li, T, s_keys, s_scores, s_forced, s_forced + a.n_seg);
-    if (a.pooled && a.mode != kScoreModeHistory) {
-        uint32_t *pc = a.counters + (int64_t)a.heads.n * kCountersPerHead * kCounterStride;
-        if (!arrive_last(pc, (uint32_t)a.heads.n, &flag)) return;
-        finish_pooled(a);
+    // the product across the run boundary: this run's last frame with the next run's first
+    if (w + 1 < nw) {
+        Codes16 next;
+        double d;
+        if (fb < H) {
+            next.set(edge[w + 1][lane]);
+            d = prev.dot(next) * (double)sp * (double)edge_scale[w + 1][lane];
+        } else {                               // the next run is frame H alone
+            const u32x4 *K = (const u32x4 *)a.K_cur + (int64_t)h * a.cur_head_vecs + (int64_t)u * a.unit_vecs + (ok ? 2 * col : 0);
+            d = 0.0;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const u32x4 x = K[j];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) d = fma(Vec<false>::at(x, e), (double)prev.v[8 * j + e], d);
+            }
+            d *= (double)sp;
+        }
+        put(fb - 1, 1, wave_sum(ok ? d : 0.0));
     }
+    store_and_finish<DIRECT, FLAT>(a, dyn, wg_part, &flag);
 }
 
 }  // namespace
@@ -506,8 +633,9 @@ hipError_t launch_score_q8(const ScoreArgs &a0, hipStream_t s) {
     if (a.heads.n == 0 || a.n_frames <= 0) return hipSuccess;
     const size_t lds = score_lds(a);
     const dim3 grid((unsigned)a.n_cg, (unsigned)a.units, (unsigned)a.heads.n);
-    if (one_member(a)) hipLaunchKernelGGL((score_kernel<false, true, true>), grid, dim3(kThreads), lds, s, a);
-    else hipLaunchKernelGGL((score_kernel<false, false, true>), grid, dim3(kThreads), lds, s, a);
+    if (!one_member(a)) hipLaunchKernelGGL((score_q8_kernel<false, false>), grid, dim3(kThreads), lds, s, a);
+    else if (a.units * a.n_cg > kFlat8) hipLaunchKernelGGL((score_q8_kernel<true, false>), grid, dim3(kThreads), lds, s, a);
+    else hipLaunchKernelGGL((score_q8_kernel<true, true>), grid, dim3(kThreads), lds, s, a);
     return hipGetLastError();
 }
 

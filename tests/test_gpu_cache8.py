@@ -250,7 +250,8 @@ def _cache(fkv, shape, block, seed, spread=1.0):
     (2, 64, 1, 9, 1, 16, 4, W.SCOPE_GLOBAL), (2, 128, 1560, 3, 1560, 64, 1, W.SCOPE_GLOBAL),
     (2, 128, 520, 2, 2, 16, 100, W.SCOPE_FRAME)])
 def test_score_select_q8(fkv, heads, d, F, H, L, block, k, scope):
-    """Bit for bit what the bf16 cache of the same values gives, and the cosine in 64 bits."""
+    """The cosine in 64 bits, within three roundings of a chain of four products for the product's sum, half as many
+    for each norm, and the score's own; the selection of those scores, and that of the bf16 cache of the same values."""
     budgets = _budgets(1, heads - 1, 1, k, scope)
     shape = _shape(fkv, heads, d, F, H, H + 1, 2, L)
     hs = fkv.make_heads(budgets)
@@ -269,15 +270,43 @@ def test_score_select_q8(fkv, heads, d, F, H, L, block, k, scope):
     plain = val.to(torch.bfloat16)
     assert torch.equal(plain.double(), val)                                      # exact in bf16, as documented
     fkv.fkv_score_select(shape, hs, plain.cuda(), slots, K_cur, *b)
-    for x, y in zip(a, b):
-        assert torch.equal(x, y)
+    assert torch.equal(a[1], b[1]) and torch.equal(a[2], b[2])
+    c = outputs()
+    fkv.fkv_select(shape, hs, a[0], c[1], c[2])
+    assert torch.equal(a[1], c[1]) and torch.equal(a[2], c[2])
     assert bool((a[0][0] == 9).all()) and bool((a[1][0] == 77).all()) and int(a[2][0]) == 55     # the static head's rows
     seq = torch.cat([val[:, slots].reshape(heads, H * F, d), K_cur.cpu().double()], 1)
     for g in range(n_seg):
         lo, hi = g * L, min(g * L + L, H * F)
         u, w = seq[1:, lo:hi].flatten(1), seq[1:, lo + F:hi + F].flatten(1)
         c = (u * w).sum(1) / ((u * u).sum(1) * (w * w).sum(1)).sqrt()
-        assert bool(((a[0].cpu().double()[1:, g] - c).abs() <= F32_STEP * c.abs() + 1e-14).all())
+        assert bool(((a[0].cpu().double()[1:, g] - c).abs() <= F32_STEP * c.abs() + (3 + 3 * c.abs()) * F32_STEP).all())
+
+
+def test_score_select_q8_ties_and_ends(fkv):
+    """Equal frames score exactly one and go to the lower index; blocks at both ends of the scale's range keep their
+    cosine; an all-zero frame scores zero; a NaN code spoils its own segments."""
+    heads, d, F, H = 2, 64, 48, 6
+    shape = _shape(fkv, heads, d, F, H, H, 1)
+    hs = fkv.make_heads(_budgets(0, 2, 0, 3, W.SCOPE_GLOBAL, sink=0))
+    g = _gen(13)
+    one = torch.randn((heads, 1, F, d), generator=g)
+    x = one.expand(-1, H, -1, -1).clone()
+    x[1, :, :16] *= 2.0 ** -118
+    x[1, :, 16:32] *= 2.0 ** 110
+    x[1, 3] = 0
+    cache = fkv.Cache8.zeros(shape, 16)
+    rows = x.reshape(heads, H * F, d).to(torch.bfloat16).cuda()
+    fkv.fkv_append_frames_q8(shape, None, None, rows, rows, list(range(H)), cache)
+    cur = torch.randn((heads, F, d), generator=g).to(torch.bfloat16).cuda()
+    scores = torch.zeros((heads, H), device="cuda")
+    kept, kv = torch.zeros((heads, H), dtype=torch.int32, device="cuda"), torch.zeros(heads, dtype=torch.int32, device="cuda")
+    fkv.fkv_score_select_q8(shape, hs, cache, list(range(H)), cur, scores, kept, kv)
+    assert scores[0, :5].tolist() == [1.0] * 5 and kept[0].tolist() == [0, 1, 5, -1, -1, -1]
+    assert scores[1, :5].tolist() == [1.0, 1.0, 0.0, 0.0, 1.0] and kept[1].tolist()[:3] == [2, 3, 5]
+    cache.K.view(torch.uint8)[0, 4, 7, 7] = 0x7f
+    fkv.fkv_score_select_q8(shape, hs, cache, list(range(H)), cur, scores, kept, kv)
+    assert scores[0].isnan().tolist() == [False, False, False, True, True, False] and kept[0].tolist()[:3] == [0, 1, 5]
 
 
 def test_score_select_q8_without_history(fkv):
