@@ -521,8 +521,8 @@ fkv_status fkv_chunk_attention_fp8(const fkv_shape *shape, const void *Q8,
  * one-dimensional order of a token sequence; 0 gives a whole frame one
  * position).  frame_pos is a HOST array, |frame_pos[f]| <= FKV_MAX_POSITION.
  * Pair j is channels (2j, 2j + 1) (FKV_PAIR_ADJACENT) or (j, j + d/2)
- * (FKV_PAIR_HALVES).  Angles are reduced in fp64; the products are fp32, and
- * each result is rounded once to the output's type. */
+ * (FKV_PAIR_HALVES).  Angles are reduced in 64-bit integers; products are fp32,
+ * and each result is rounded once to the output's type. */
 #define FKV_MAX_POSITION (1 << 24)
 typedef enum { FKV_PAIR_ADJACENT = 0, FKV_PAIR_HALVES = 1 } fkv_pairing;
 typedef struct {

@@ -65,14 +65,14 @@ struct AppendArgs {
 
 // ------------------------------------------- position rotation and appending
 // Rotation as the kernels use it: pair j of the d/2 pairs turns by
-// position * turns[j], in turns (1 = a full circle); pairs [0, end_frame) by the
+// position * turns[j] / 2^64 full circles; pairs [0, end_frame) by the
 // frame position, [end_frame, end_row) by the row, [end_row, end_col) by the
 // column, the others not at all.
 struct RopeTable {
     int32_t end_frame, end_row, end_col;
     int32_t row_tokens, token_step, halves;  // halves: FKV_PAIR_HALVES
     int32_t on;                              // 0: no rotation
-    double turns[64];                        // theta^(-i/n) / (2 pi)
+    struct { uint32_t lo, hi; } turns[64];   // theta^(-i/n) / (2 pi) * 2^64
 };
 
 // Rows of up to three tensors (0 and 1 rotated, 2 not; a NULL source is left

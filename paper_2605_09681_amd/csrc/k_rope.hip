@@ -3,24 +3,27 @@
 // into a cache held in 8 bits with a scale for each head and block of tokens.
 //
 // Channel pair j of a rotated row, (x, y), becomes (x cos a - y sin a, x sin a +
-// y cos a) with a = position * theta^(-i/n).  The host passes theta^(-i/n) /
-// (2 pi) in fp64 (turns per position); position * turns is formed in fp64 and
-// reduced to [-1/2, 1/2] turns there -- positions reach 2^24, where fp32 would
-// keep no digit of the angle -- and only the remainder is rounded to fp32 for
-// the sine and cosine.
+// y cos a) with a = position * theta^(-i/n).  Positions reach 2^24, where fp32
+// would keep no digit of the angle.  The host passes theta^(-i/n) / (2 pi), turns
+// per position, as a 64-bit fixed-point fraction; position * turns modulo one turn
+// is then an integer product that wraps by itself, of which the kernel keeps the
+// top 32 bits.  Its two top bits give the quadrant, the rest an angle within +-pi/4
+// whose sine and cosine are polynomials in fp32 (Chebyshev fits, off by at most
+// 2^-23 with their roundings).
 //
 // An item is one token and 8 + 8 channels: [8v, 8v + 8) and the 8 channels d/2
 // further on, which are each other's partners under FKV_PAIR_HALVES and two
 // runs of four adjacent pairs otherwise: 8 pairs either way, 8 items per row of
 // 128.  A thread computes the sines and cosines of its item once and walks the
 // heads of its workgroup with them: they depend on the token alone, and they are
-// the costly part (fp64 reduction and about 40 instructions per pair).
+// the costly part.
 #include "fkv_internal.h"
 
 namespace fkv {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kAppendThreads = 512;      // largest workgroup of the 8-bit append: a block of 64 x 128
 constexpr float kE4M3Max = 448.f;
 
 __device__ __forceinline__ uint32_t pack_bf16(float x, float y) {
@@ -66,10 +69,24 @@ struct Turn {
     float c[8], s[8];
 };
 
+// Sine and cosine of `turns` / 2^32 turns.
+__device__ __forceinline__ void sin_cos(int32_t turns, float *sn, float *cs) {
+    const int32_t q = (int32_t)((uint32_t)turns + 0x20000000u) >> 30;     // quadrant, -2..1
+    const int32_t r = (int32_t)((uint32_t)turns - ((uint32_t)q << 30));   // within 1/8 turn of it
+    const float x = (float)r * 0x1.921fb6p-30f;                           // 2 pi / 2^32
+    const float y = x * x;
+    const float s = fmaf(y * x, fmaf(y, fmaf(y, -0x1.9acap-13f, 0x1.110c2ap-7f), -0x1.555552p-3f), x);
+    const float c = fmaf(y * y, fmaf(y, fmaf(y, 0x1.9bd8eep-16f, -0x1.6c12d4p-10f), 0x1.555554p-5f), fmaf(y, -0.5f, 1.f));
+    const bool odd = q & 1;
+    const float a = odd ? c : s, b = odd ? s : c;
+    *sn = q & 2 ? -a : a;                                                 // s, c, -s, -c by quadrant
+    *cs = (q + 1) & 2 ? -b : b;                                           // c, -s, -c, s
+}
+
 // turns: the table in LDS (a per-lane index into the launch arguments would copy
 // them to scratch).  v: the item within its row of D channels.
 template <int D>
-__device__ __forceinline__ Turn turn_of(const RopeTable &r, const double *turns, int frame_pos, int p, int v) {
+__device__ __forceinline__ Turn turn_of(const RopeTable &r, const uint2 *turns, int frame_pos, int p, int v) {
     const int row = p / r.row_tokens, col = p - row * r.row_tokens;
     const int t = frame_pos + (r.token_step ? p : 0);
     const int e0 = r.end_frame, e1 = r.end_row, e2 = r.end_col, halves = r.halves;
@@ -78,9 +95,10 @@ __device__ __forceinline__ Turn turn_of(const RopeTable &r, const double *turns,
     for (int e = 0; e < 8; ++e) {
         const int j = halves ? 8 * v + e : 4 * v + (e & 3) + (e >> 2) * (D / 4);
         const int pos = j < e0 ? t : j < e1 ? row : j < e2 ? col : 0;
-        const double a = (double)pos * turns[j];
-        const float f = (float)(a - rint(a));
-        sincospif(2.f * f, &w.s[e], &w.c[e]);
+        // the high word of pos * (hi 2^32 + lo) mod 2^64, pos signed
+        const uint2 f = turns[j];
+        const uint32_t hi = (uint32_t)pos * f.y + __umulhi((uint32_t)pos, f.x) - (pos < 0 ? f.x : 0u);
+        sin_cos((int32_t)hi, &w.s[e], &w.c[e]);
     }
     return w;
 }
@@ -105,8 +123,8 @@ __device__ __forceinline__ void turn(const Turn &w, bool halves, float (&x)[8], 
     }
 }
 
-__device__ __forceinline__ void load_turns(const RopeTable &r, double *turns) {
-    if (threadIdx.x < 64) turns[threadIdx.x] = r.turns[threadIdx.x];
+__device__ __forceinline__ void load_turns(const RopeTable &r, uint2 *turns) {
+    if (threadIdx.x < 64) turns[threadIdx.x] = make_uint2(r.turns[threadIdx.x].lo, r.turns[threadIdx.x].hi);
     __syncthreads();
 }
 
@@ -114,7 +132,7 @@ __device__ __forceinline__ void load_turns(const RopeTable &r, double *turns) {
 template <int D, bool F32>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a) {
     constexpr int ES = F32 ? 4 : 2, IPR = D / 16;         // items per row
-    __shared__ double turns[64];
+    __shared__ uint2 turns[64];
     load_turns(a.rope, turns);
     const int f = blockIdx.y, v = threadIdx.x % IPR;
     const int p = blockIdx.x * (kThreads / IPR) + threadIdx.x / IPR;
@@ -151,8 +169,39 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a) {
     }
 }
 
+typedef short i16x2_t __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+
+// Magnitudes are compared as integers: the bits of |x| grow with |x|, infinities
+// and NaN above all numbers.  Beyond kPlainBits -- 448 * 2^119, the largest that
+// the scales reach -- a block takes the careful way: its scale from the finite
+// elements alone, its codes clamped, NaN for what is not finite.
+constexpr uint32_t kPlainBits = 0x7f600000u;
+
+__device__ __forceinline__ uint32_t max_bits8(const float (&x)[8], uint32_t m) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(x[e]) & 0x7fffffffu);
+    return m;
+}
+// The same of 8 elements as they lie in memory (bf16: two at a time).
+template <bool F32>
+__device__ __forceinline__ uint32_t max_bits8(const Raw8<F32> &r, uint32_t m) {
+    if constexpr (F32) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = max(m, r.v[e >> 2][e & 3] & 0x7fffffffu);
+    } else {
+        u16x2_t t = __builtin_bit_cast(u16x2_t, (uint32_t)(r.v[0][0] & 0x7fff7fffu));
+#pragma unroll
+        for (int e = 1; e < 4; ++e)
+            t = __builtin_elementwise_max(t, __builtin_bit_cast(u16x2_t, (uint32_t)(r.v[0][e] & 0x7fff7fffu)));
+        m = max(m, (uint32_t)max(t[0], t[1]) << 16);
+    }
+    return m;
+}
+
 // Largest finite magnitude of 8 elements and m.
-__device__ __forceinline__ float amax8(const float (&x)[8], float m) {
+__device__ __forceinline__ float finite_max8(const float (&x)[8], float m) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const float b = fabsf(x[e]);
@@ -161,135 +210,182 @@ __device__ __forceinline__ float amax8(const float (&x)[8], float m) {
     return m;
 }
 
-// Exponent k of a block's scale: the smallest with amax <= 448 * 2^k, in [-100, 119]; 0 for an all-zero block.
-__device__ __forceinline__ int scale_exponent(float amax) {
-    const uint32_t b = __float_as_uint(amax);
-    if (b == 0) return 0;
-    const int e = (int)(b >> 23) - 127;                       // (a subnormal amax is far below the clamp)
-    const int k = (b & 0x7fffffu) <= 0x600000u ? e - 8 : e - 7;  // 448 = 1.75 * 2^8
+// Exponent k of the scale of a block with largest magnitude `bits`: the smallest
+// with amax <= 448 * 2^k, in [-100, 119]; 0 for an all-zero block.
+__device__ __forceinline__ int scale_exponent(uint32_t bits) {
+    if (bits == 0) return 0;
+    const int e = (int)(bits >> 23) - 127;                       // (a subnormal amax is far below the clamp)
+    const int k = (bits & 0x7fffffu) <= 0x600000u ? e - 8 : e - 7;  // 448 = 1.75 * 2^8
     return min(max(k, -100), 119);
 }
 
-// 8 codes of x * 2^-k.
-__device__ __forceinline__ uint2 codes8(const float (&x)[8], float inv) {
-    float y[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float z = __builtin_amdgcn_fmed3f(x[e] * inv, -kE4M3Max, kE4M3Max);
-        y[e] = fabsf(x[e]) < __builtin_inff() ? z : __builtin_nanf("");
-    }
+// 8 codes of x / scale (v_cvt_scalef32_pk_fp8: one rounding, to nearest even).
+__device__ __forceinline__ uint2 codes8(const float (&x)[8], float scale) {
     uint2 c;
-    c.x = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false), true);
-    c.y = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], 0, false), true);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        i16x2_t w = {0, 0};
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, x[4 * i], x[4 * i + 1], scale, false);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, x[4 * i + 2], x[4 * i + 3], scale, true);
+        (i ? c.y : c.x) = __builtin_bit_cast(uint32_t, w);
+    }
     return c;
 }
+template <bool F32>
+__device__ __forceinline__ uint2 codes8(const Raw8<F32> &r, float scale) {
+    if constexpr (F32) {
+        float x[8];
+        r.get(x);
+        return codes8(x, scale);
+    } else {
+        uint2 c;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            i16x2_t w = {0, 0};
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2_t, (uint32_t)r.v[0][2 * i]), scale, false);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(w, __builtin_bit_cast(bf16x2_t, (uint32_t)r.v[0][2 * i + 1]), scale, true);
+            (i ? c.y : c.x) = __builtin_bit_cast(uint32_t, w);
+        }
+        return c;
+    }
+}
+// The careful way: at most 448 in magnitude, NaN for what is not finite.
+__device__ __forceinline__ uint2 careful_codes8(const float (&x)[8], float scale) {
+    const float most = kE4M3Max * scale;
+    float y[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        y[e] = fabsf(x[e]) < __builtin_inff() ? __builtin_amdgcn_fmed3f(x[e], -most, most) : __builtin_nanf("");
+    return codes8(y, scale);
+}
 
-// One workgroup: one block of tokens of one frame, for heads_per_wg heads; IPT
-// items per thread.  grid: x = block of the frame, y = new frame, z = group of heads.
-template <int D, bool F32, int IPT>
-__global__ __launch_bounds__(kThreads) void append_q8_kernel(AppendQ8Args a) {
+// Largest m of the workgroup; r: its waves' words of LDS, used again two calls later.
+__device__ __forceinline__ uint32_t block_max(uint32_t m, uint32_t *r) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o));
+    const int n = blockDim.x >> 6;
+    if (n > 1) {
+        if ((threadIdx.x & 63) == 0) r[threadIdx.x >> 6] = m;
+        __syncthreads();
+        for (int i = 0; i < n; ++i) m = max(m, r[i]);
+    }
+    return m;
+}
+
+// One workgroup: one block of tokens of one frame, its keys or its values
+// (ROTATE: keys that turn; otherwise rows as they are), for heads_per_wg heads;
+// IPT items per thread.
+template <int D, bool F32, int IPT, bool ROTATE>
+__device__ __forceinline__ void append_block(const AppendQ8Args &a, bool values, int h0, int h1, const uint2 *turns,
+                                             uint32_t (*red)[2][kAppendThreads / 64]) {
     constexpr int ES = F32 ? 4 : 2, IPR = D / 16;
-    __shared__ double turns[64];
-    __shared__ float red[2][2][kThreads / 64];           // [parity][K, V][wave]
-    const bool rope = a.rope.on;
-    if (rope) load_turns(a.rope, turns);
     const int f = blockIdx.y, b = blockIdx.x, v = threadIdx.x % IPR;
     const int step = blockDim.x / IPR, p0 = b * a.block_tokens + threadIdx.x / IPR;
     const bool halves = a.rope.halves;
-    const int n_waves = blockDim.x >> 6, wave = threadIdx.x >> 6;
     const int slot = a.slots.slot[f];
+    const uint8_t *src = values ? a.V : a.K;
+    const int64_t src_head = values ? a.v_head : a.k_head, src_tok = values ? a.v_tok : a.k_tok;
+    uint8_t *dst = values ? a.V8 : a.K8;
+    float *scales = values ? a.v_scale : a.k_scale;
     Turn w[IPT];
-    if (rope) {
-#pragma unroll
-        for (int i = 0; i < IPT; ++i) w[i] = turn_of<D>(a.rope, turns, a.pos.slot[f], p0 + i * step, v);
-    }
-    const int h0 = blockIdx.z * a.heads_per_wg, h1 = min(h0 + a.heads_per_wg, a.n_heads);
     for (int h = h0; h < h1; ++h) {
-        const uint8_t *K = a.K + h * a.k_head + v * 8 * ES, *V = a.V + h * a.v_head + v * 8 * ES;
-        Raw8<F32> kr[IPT][2], vr[IPT][2];
+        const uint8_t *X = src + h * src_head + v * 8 * ES;
+        Raw8<F32> r[IPT][2];
 #pragma unroll
         for (int i = 0; i < IPT; ++i) {
             const int p = p0 + i * step;
-            kr[i][0] = kr[i][1] = vr[i][0] = vr[i][1] = Raw8<F32>{};
+            r[i][0] = r[i][1] = Raw8<F32>{};
             if (p < a.F) {
                 const int64_t tok = (int64_t)f * a.F + p;
-                kr[i][0].load(K + tok * a.k_tok);
-                kr[i][1].load(K + tok * a.k_tok + D / 2 * ES);
-                vr[i][0].load(V + tok * a.v_tok);
-                vr[i][1].load(V + tok * a.v_tok + D / 2 * ES);
+                r[i][0].load(X + tok * src_tok);
+                r[i][1].load(X + tok * src_tok + D / 2 * ES);
             }
         }
-        float kx[IPT][2][8], mk = 0.f, mv = 0.f;
+        if (ROTATE && h == h0) {                         // (while the first rows are on their way)
+#pragma unroll
+            for (int i = 0; i < IPT; ++i) w[i] = turn_of<D>(a.rope, turns, a.pos.slot[f], p0 + i * step, v);
+        }
+        float x[IPT][2][8];
+        uint32_t m = 0;
 #pragma unroll
         for (int i = 0; i < IPT; ++i) {
-            kr[i][0].get(kx[i][0]);
-            kr[i][1].get(kx[i][1]);
-            if (rope) turn(w[i], halves, kx[i][0], kx[i][1]);
-            mk = amax8(kx[i][1], amax8(kx[i][0], mk));
-            float x[8];
-            vr[i][0].get(x);
-            mv = amax8(x, mv);
-            vr[i][1].get(x);
-            mv = amax8(x, mv);
+            if constexpr (ROTATE) {
+                r[i][0].get(x[i][0]);
+                r[i][1].get(x[i][1]);
+                turn(w[i], halves, x[i][0], x[i][1]);
+                m = max_bits8(x[i][1], max_bits8(x[i][0], m));
+            } else {
+                m = max_bits8(r[i][1], max_bits8(r[i][0], m));
+            }
         }
+        m = block_max(m, red[0][h & 1]);
+        const bool careful = m > kPlainBits;             // (the same in every thread)
+        if (careful) {
+            float top = 0.f;
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
-            mk = fmaxf(mk, __shfl_xor(mk, o));
-            mv = fmaxf(mv, __shfl_xor(mv, o));
+            for (int i = 0; i < IPT; ++i)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    if constexpr (!ROTATE) r[i][k].get(x[i][k]);
+                    top = finite_max8(x[i][k], top);
+                }
+            m = block_max(__float_as_uint(top), red[1][h & 1]);
         }
-        if (n_waves > 1) {
-            float(&r)[2][kThreads / 64] = red[h & 1];    // the other half is read by slower waves of the head before
-            if ((threadIdx.x & 63) == 0) {
-                r[0][wave] = mk;
-                r[1][wave] = mv;
-            }
-            __syncthreads();
-            for (int i = 0; i < n_waves; ++i) {
-                mk = fmaxf(mk, r[0][i]);
-                mv = fmaxf(mv, r[1][i]);
-            }
-        }
-        const int ek = scale_exponent(mk), ev = scale_exponent(mv);
-        const float ik = __uint_as_float((uint32_t)(127 - ek) << 23), iv = __uint_as_float((uint32_t)(127 - ev) << 23);
-        const int64_t at = ((int64_t)h * a.cap + slot) * a.n_blocks + b;
-        if (threadIdx.x == 0) {
-            a.k_scale[at] = __uint_as_float((uint32_t)(127 + ek) << 23);
-            a.v_scale[at] = __uint_as_float((uint32_t)(127 + ev) << 23);
-        }
+        const float scale = __uint_as_float((uint32_t)(127 + scale_exponent(m)) << 23);
+        if (threadIdx.x == 0) scales[((int64_t)h * a.cap + slot) * a.n_blocks + b] = scale;
 #pragma unroll
         for (int i = 0; i < IPT; ++i) {
             const int p = p0 + i * step;
             if (p < a.F) {
-                const int64_t row = (((int64_t)h * a.cap + slot) * a.F + p) * D + v * 8;
-                *(uint2 *)(a.K8 + row) = codes8(kx[i][0], ik);
-                *(uint2 *)(a.K8 + row + D / 2) = codes8(kx[i][1], ik);
-                float x[8];
-                vr[i][0].get(x);
-                *(uint2 *)(a.V8 + row) = codes8(x, iv);
-                vr[i][1].get(x);
-                *(uint2 *)(a.V8 + row + D / 2) = codes8(x, iv);
+                uint8_t *row = dst + (((int64_t)h * a.cap + slot) * a.F + p) * D + v * 8;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    uint2 c;
+                    if (careful) c = careful_codes8(x[i][k], scale);
+                    else if constexpr (ROTATE) c = codes8(x[i][k], scale);
+                    else c = codes8(r[i][k], scale);
+                    *(uint2 *)(row + k * (D / 2)) = c;
+                }
             }
         }
+    }
+}
+
+// Keys and values in workgroups of their own: half the registers, twice the
+// workgroups to hide the loads, the barrier and the stores of one behind the
+// others.  grid: x = block of the frame, y = new frame, z = 2 * (group of heads) +
+// (1: values).
+template <int D, bool F32, int IPT>
+__global__ __launch_bounds__(kAppendThreads) void append_q8_kernel(AppendQ8Args a) {
+    __shared__ uint2 turns[64];
+    __shared__ uint32_t red[2][2][kAppendThreads / 64];  // [plain, careful][parity of the head][wave]
+    const bool values = blockIdx.z & 1;
+    const int h0 = (blockIdx.z >> 1) * a.heads_per_wg, h1 = min(h0 + a.heads_per_wg, a.n_heads);
+    if (a.rope.on && !values) {
+        load_turns(a.rope, turns);
+        append_block<D, F32, IPT, true>(a, values, h0, h1, turns, red);
+    } else {
+        append_block<D, F32, IPT, false>(a, values, h0, h1, turns, red);
     }
 }
 
 // Heads that one workgroup walks: the sines and cosines of its tokens serve all
-// of them, so as many as leave about four workgroups per compute unit.
-int heads_per_workgroup(int64_t token_groups, int n_heads) {
-    const int64_t groups = (1024 + token_groups - 1) / token_groups;   // groups of heads wanted
+// of them, so as many as leave the device `wanted` workgroups.  Rotating, 480P:
+// 1024 18.9 us, 512 19.4, 256 23.3.  Appending to 8 bits (and as many for the values),
+// 480P: 768 12.2 us, 256 12.4, one head each 13.5; blocks of 16 tokens 12.4, 20.5, 11.8.
+constexpr int kRotateGroups = 1024, kAppendGroups = 768;
+int heads_per_workgroup(int64_t token_groups, int n_heads, int wanted) {
+    const int64_t groups = (wanted + token_groups - 1) / token_groups;   // groups of heads wanted
     return groups >= n_heads ? 1 : (int)((n_heads + groups - 1) / groups);
 }
 
 template <int D, bool F32>
 hipError_t append_q8(AppendQ8Args &a, hipStream_t s) {
-    const int items = a.block_tokens * (D / 16), threads = items < kThreads ? items : kThreads;
-    a.heads_per_wg = heads_per_workgroup((int64_t)a.n_blocks * a.n_frames, a.n_heads);
-    const dim3 grid((unsigned)a.n_blocks, (unsigned)a.n_frames, (unsigned)((a.n_heads + a.heads_per_wg - 1) / a.heads_per_wg));
-    switch (items / threads) {
-    case 1: hipLaunchKernelGGL((append_q8_kernel<D, F32, 1>), grid, dim3(threads), 0, s, a); break;
-    case 2: hipLaunchKernelGGL((append_q8_kernel<D, F32, 2>), grid, dim3(threads), 0, s, a); break;
-    default: hipLaunchKernelGGL((append_q8_kernel<D, F32, 4>), grid, dim3(threads), 0, s, a); break;
-    }
+    const int items = a.block_tokens * (D / 16), threads = items < kAppendThreads ? items : kAppendThreads;
+    a.heads_per_wg = heads_per_workgroup((int64_t)a.n_blocks * a.n_frames, a.n_heads, kAppendGroups);
+    const dim3 grid((unsigned)a.n_blocks, (unsigned)a.n_frames, 2 * (unsigned)((a.n_heads + a.heads_per_wg - 1) / a.heads_per_wg));
+    if (items == threads) hipLaunchKernelGGL((append_q8_kernel<D, F32, 1>), grid, dim3(threads), 0, s, a);
+    else hipLaunchKernelGGL((append_q8_kernel<D, F32, 2>), grid, dim3(threads), 0, s, a);
     return hipGetLastError();
 }
 
@@ -299,7 +395,7 @@ hipError_t launch_rotate(const RotateArgs &a0, int head_dim, bool f32, hipStream
     RotateArgs a = a0;
     if (a.n_frames == 0) return hipSuccess;
     const int per = kThreads / (head_dim / 16), groups = (a.F + per - 1) / per;
-    a.heads_per_wg = heads_per_workgroup((int64_t)groups * a.n_frames, a.n_heads);
+    a.heads_per_wg = heads_per_workgroup((int64_t)groups * a.n_frames, a.n_heads, kRotateGroups);
     const dim3 grid((unsigned)groups, (unsigned)a.n_frames, (unsigned)((a.n_heads + a.heads_per_wg - 1) / a.heads_per_wg));
     if (head_dim == 64 && f32) hipLaunchKernelGGL((rotate_kernel<64, true>), grid, dim3(kThreads), 0, s, a);
     else if (head_dim == 64) hipLaunchKernelGGL((rotate_kernel<64, false>), grid, dim3(kThreads), 0, s, a);

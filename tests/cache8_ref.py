@@ -55,9 +55,9 @@ def rotate64(x: torch.Tensor, rope: Rope, frame_pos, F: int) -> torch.Tensor:
 
 def rotation_slack(x: torch.Tensor, rope: Rope) -> torch.Tensor:
     """Bound on what fp32 arithmetic moves a rotated element by, beside its last
-    rounding: sine and cosine are off by at most 2^-24 of a turn's remainder (2 pi
-    2^-25) and one step of their own (2^-23), the two products and their sum by
-    three half steps: below 2^-21 of |x| + |y|."""
+    rounding: sine and cosine are off by at most 2^-23 (the angle's remainder kept to
+    2^-24 of its size and below 1, and a step of their own), the two products and
+    their sum by three half steps: below 2^-21 of |x| + |y|."""
     a, b = pairs(x.double().abs(), rope.halves)
     s = (a + b) * 2.0 ** -21
     return torch.cat([s, s], -1) if rope.halves else torch.stack([s, s], -1).flatten(-2)
