@@ -17,7 +17,7 @@ __device__ __forceinline__ int head_kvl(const AttnArgs &a, int h) {
     return kvl < 0 ? 0 : (kvl > a.slab ? (int)a.slab : kvl);
 }
 __device__ __forceinline__ int head_tiles(const AttnArgs &a, int h) {
-    return (head_kvl(a, h) + a.Lq + BN - 1) / BN;
+    return (head_kvl(a, h) + a.Lc + BN - 1) / BN;
 }
 // The same for entry li of the launch's head list.  PAGED (a compile-time
 // switch): heads read in place; a static entry's history length follows from
@@ -32,7 +32,7 @@ __device__ __forceinline__ int entry_kvl(const AttnArgs &a, int li) {
 }
 template <bool PAGED = false>
 __device__ __forceinline__ int entry_tiles(const AttnArgs &a, int li) {
-    return (entry_kvl<PAGED>(a, li) + a.Lq + BN - 1) / BN;
+    return (entry_kvl<PAGED>(a, li) + a.Lc + BN - 1) / BN;
 }
 
 // Work items are (entry li of the launch's head list, query tile qt),
@@ -93,7 +93,7 @@ __device__ __forceinline__ WorkList work_list(const AttnArgs &a) {
     int T = 0;
     if (lane < a.heads.n) {
         const int kvl = kept >= 0 ? kept * a.F : head_kvl(a, e);
-        T = (kvl + a.Lq + BN - 1) / BN;
+        T = (kvl + a.Lc + BN - 1) / BN;
     }
     long long v = (long long)a.n_qtiles * T;
 #pragma unroll

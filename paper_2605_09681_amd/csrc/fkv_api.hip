@@ -870,6 +870,7 @@ fkv_status chunk_attention_impl(const fkv_shape *shape, const fkv::HeadList &lis
     a.n_heads = shape->n_heads;
     a.heads = list;
     a.Lq = shape->chunk_frames * shape->frame_tokens;
+    a.Lc = a.Lq;
     a.scale = scale;
     a.scale_log2 = scale * 1.4426950408889634f;
     const int rows = bf16 ? fkv::kAttnRowsBf16 : fkv::kAttnRowsF32;
@@ -1194,6 +1195,7 @@ fkv_status fkv_chunk_attention_fp8(const fkv_shape *shape, const void *Q8, const
     a.n_heads = shape->n_heads;
     a.heads = all_heads(shape->n_heads);
     a.Lq = shape->chunk_frames * shape->frame_tokens;
+    a.Lc = a.Lq;
     a.scale = scale;
     a.scale_log2 = scale * 1.4426950408889634f;
     a.n_qtiles = (a.Lq + fkv::kAttnRowsBf16 - 1) / fkv::kAttnRowsBf16;
@@ -1253,6 +1255,7 @@ fkv_status fkv_attention_mass(const fkv_shape *shape, const void *Q, const void 
     a.n_heads = shape->n_heads;
     a.heads = all_heads(shape->n_heads);
     a.Lq = (int32_t)lq;
+    a.Lc = a.Lq;
     a.scale = scale;
     a.scale_log2 = scale * 1.4426950408889634f;
     a.n_qtiles = (a.Lq + fkv::kAttnRowsBf16 - 1) / fkv::kAttnRowsBf16;
@@ -1407,7 +1410,8 @@ int64_t q8_most_kept(const fkv_shape *s, const fkv_head *heads) {
     return most;
 }
 
-int q8_query_tiles(int32_t n_q) { return (n_q + fkv::kAttnQ8Rows - 1) / fkv::kAttnQ8Rows; }
+int q8_tile(int32_t n_q) { return n_q <= 16 ? 16 : 32; }
+int q8_query_tiles(int32_t n_q) { return (n_q + q8_tile(n_q) - 1) / q8_tile(n_q); }
 
 // Query rows from which a chunk (n_q = n_cur) is attended over an expanded copy
 // of the kept history.
@@ -1451,7 +1455,7 @@ fkv_status q8_plan(const fkv_shape *s, const fkv_head *heads, int32_t n_q, int32
     const int64_t items = (int64_t)s->n_heads * q8_query_tiles(n_q);
     p->n_split = (int)std::max<int64_t>(1, std::min<int64_t>(p->blocks / items, (tiles + 7) / 8));
     p->part_at = fkv::attention_counter_bytes(p->blocks);
-    p->bytes = p->n_split > 1 ? p->part_at + (size_t)items * p->n_split * fkv::attn_q8_part_floats(s->head_dim) * sizeof(float) : 0;
+    p->bytes = p->n_split > 1 ? p->part_at + (size_t)items * p->n_split * fkv::attn_q8_part_floats(s->head_dim, q8_tile(n_q)) * sizeof(float) : 0;
     return FKV_OK;
 }
 
@@ -1659,6 +1663,7 @@ fkv_status fkv_chunk_attention_q8(const fkv_shape *shape, const fkv_head *heads,
     magic_of(a.F, &a.mf_hi, &a.mf_lo);
     magic_of(a.L, &a.ml_hi, &a.ml_lo);
     a.scale_log2 = scale * 1.4426950408889634f;
+    a.q_tile = q8_tile(n_q);
     a.n_qtiles = q8_query_tiles(n_q);
     a.n_split = p.n_split;
     a.counters = (uint32_t *)((char *)workspace + p.counter_at);
@@ -1698,6 +1703,7 @@ fkv_status fkv_chunk_attention_q8(const fkv_shape *shape, const fkv_head *heads,
         b.n_heads = shape->n_heads;
         b.heads = all_heads(shape->n_heads);
         b.Lq = n_q;
+        b.Lc = n_cur;
         b.scale = scale;
         b.scale_log2 = a.scale_log2;
         b.n_qtiles = (n_q + fkv::kAttnRowsBf16 - 1) / fkv::kAttnRowsBf16;

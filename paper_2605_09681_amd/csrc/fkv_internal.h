@@ -170,6 +170,7 @@ struct AttnArgs {
     const int32_t *kv_len;
     int64_t slab;
     int32_t n_heads, Lq;
+    int32_t Lc;                     // current tokens (rows per head of K_cur); Lq but for 8-bit caches
     int32_t n_qtiles;               // ceil(Lq / BM)
     int32_t n_items;                // heads.n * n_qtiles (work item = (list entry, query tile))
     HeadList heads;                 // the heads this launch computes, in schedule order
@@ -246,7 +247,7 @@ struct AttnQ8Args {
     int32_t n_blocks, block_shift;      // scales per frame, log2 of the tokens per scale
     uint32_t mf_hi, mf_lo, ml_hi, ml_lo;  // floor(2^64 / F) + 1 and floor(2^64 / L) + 1 (0 for 1)
     float scale_log2;                   // scale * log2(e)
-    int32_t n_qtiles;                   // query tiles per head
+    int32_t q_tile, n_qtiles;           // query rows per tile (16 or 32), tiles per head
     int32_t n_split;                    // parts per (head, query tile); 1: no workspace
     float *part;                        // [head][query tile][part] slots of attn_q8_part_floats
     uint32_t *counters;                 // arrivals per (head, query tile), kItemCounterStride apart
@@ -304,9 +305,8 @@ hipError_t launch_rotate(const RotateArgs &a, int head_dim, bool f32, hipStream_
 hipError_t launch_append_q8(const AppendQ8Args &a, int head_dim, bool f32, hipStream_t s);
 
 // attention over 8-bit caches (k_attn_q8.hip)
-constexpr int kAttnQ8Rows = 16;             // query rows of a tile
 hipError_t launch_attention_q8(const AttnQ8Args &a, int head_dim, hipStream_t s);
 hipError_t launch_expand_q8(const AttnQ8Args &a, int head_dim, hipStream_t s);  // kept history to Kc, Vc, kv_out
-inline size_t attn_q8_part_floats(int head_dim) { return (size_t)kAttnQ8Rows * (head_dim + 2); }
+inline size_t attn_q8_part_floats(int head_dim, int q_tile) { return (size_t)q_tile * (head_dim + 2); }
 
 }  // namespace fkv

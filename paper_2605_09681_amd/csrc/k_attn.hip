@@ -327,7 +327,7 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, uint16_t *Ks, ui
     const int h = a.heads.head[li];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int l32 = lane & 31, hl = lane >> 5;
-    const int Lq = a.Lq;
+    const int Lq = a.Lq, Lc = WIDE ? a.Lc : Lq;
     const int n = t1 - t0;       // >= 1
 
     // The wave's 32 query rows, in the B-operand layout: lane holds row l32,
@@ -343,13 +343,13 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, uint16_t *Ks, ui
     }
 
     const int kvl = entry_kvl<PAGED>(a, li);
-    const int Lk = kvl + Lq;
+    const int Lk = kvl + Lc;
     const uint16_t *Kc = PAGED ? (const uint16_t *)a.K_hist + (size_t)h * a.cap * a.F * D
                                : (const uint16_t *)a.Kc + (size_t)h * a.slab * D;
     const uint16_t *Vc = PAGED ? (const uint16_t *)a.V_hist + (size_t)h * a.cap * a.F * D
                                : (const uint16_t *)a.Vc + (size_t)h * a.slab * D;
-    const uint16_t *Kq = (const uint16_t *)a.K_cur + (size_t)h * Lq * D;
-    const uint16_t *Vq = (const uint16_t *)a.V_cur + (size_t)h * Lq * D;
+    const uint16_t *Kq = (const uint16_t *)a.K_cur + (size_t)h * Lc * D;
+    const uint16_t *Vq = (const uint16_t *)a.V_cur + (size_t)h * Lc * D;
     const uint32_t ktab = PAGED ? kept_piece_table(a, li, kvl, lane) : 0u;
 
     // Loop-invariant per-thread staging geometry.  K: rows r0 + RPP*i, 16-byte
@@ -409,10 +409,10 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, uint16_t *Ks, ui
     int left = 0;
     bool two = false;
     auto one_tile = [&](const PageCursor &cu) {
-        const TileSrc k = PAGED ? paged_tile<D>(Kc, ktab, P, cu, Kq, kvl, Lk, Lq)
-                                : compact_tile<D>(Kc, Kq, cu.j0, kvl, Lk, Lq);
-        const TileSrc v = PAGED ? paged_tile<D>(Vc, ktab, P, cu, Vq, kvl, Lk, Lq)
-                                : compact_tile<D>(Vc, Vq, cu.j0, kvl, Lk, Lq);
+        const TileSrc k = PAGED ? paged_tile<D>(Kc, ktab, P, cu, Kq, kvl, Lk, Lc)
+                                : compact_tile<D>(Kc, Kq, cu.j0, kvl, Lk, Lc);
+        const TileSrc v = PAGED ? paged_tile<D>(Vc, ktab, P, cu, Vq, kvl, Lk, Lc)
+                                : compact_tile<D>(Vc, Vq, cu.j0, kvl, Lk, Lc);
         krun = k.a;
         vrun = v.a;
         k2 = k.b;

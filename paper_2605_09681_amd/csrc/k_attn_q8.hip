@@ -9,9 +9,9 @@
 // their block's scale into two bf16 values exactly, so after the conversion the
 // arithmetic is that of a bf16 cache.
 //
-// One wave works on its own: it takes every 8th tile of 64 keys of its
-// workgroup's part, keeps its own running maximum, sum and output, and meets the
-// other waves once, at the end.  With v_mfma_f32_16x16x32_bf16, for 16 query rows:
+// One wave works on its own: the keys are split in units of 16 over the waves of all
+// parts of an item; a wave takes 64 keys a step, keeps its own running maximum, sum
+// and output, and meets the other waves once, at the end.  With v_mfma_f32_16x16x32_bf16, for 16 query rows:
 //   S^T = K Q^T   (A = 16 key rows straight from global memory: lane l holds
 //                 channels 64u + 16(l/16) .. + 16 of key l%16, u = 0.., in the
 //                 order in which the products consume them; the queries'
@@ -22,8 +22,7 @@
 //                 time, B = P straight from the S^T accumulators).
 // The sum adds the probabilities before they are rounded to bf16 for the value
 // product.  Parts of an item (head, query tile) meet in fp32 slots of the
-// workspace; the workgroup that arrives last joins them in order.
-#include "handover.h"
+// workspace, which a second launch joins in order.
 #include "fkv_internal.h"
 
 namespace fkv {
@@ -35,8 +34,9 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 512, kWaves = 8;
-constexpr int kTile = 64;                 // keys per tile
-constexpr int kRows = kAttnQ8Rows;        // query rows per tile
+constexpr int kTile = 64;                 // keys per step of a wave
+constexpr int kUnit = 16;                 // keys: the grain of the split over waves
+constexpr int kJoinThreads = 256, kJoin = 4;  // joining: threads of a workgroup, parts loaded at a time
 constexpr float kLn2 = 0.69314718055994530942f;
 
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
@@ -106,8 +106,10 @@ __device__ __forceinline__ u32x4 widen8(uint32_t c0, uint32_t c1, float scale) {
 }
 __device__ __forceinline__ bf16x8_t frag(const u32x4 &v) { return __builtin_bit_cast(bf16x8_t, v); }
 
-template <int D>
+// MT: query tiles of 16 rows that a wave holds.
+template <int D, int MT>
 struct Cfg {
+    static constexpr int ROWS = 16 * MT;          // query rows of an item
     static constexpr int U = D / 64;              // 64-channel halves of a row
     static constexpr int KS = D / 32;             // steps of the score product
     static constexpr int MB = D / 16;             // 16-channel blocks of the output
@@ -116,35 +118,60 @@ struct Cfg {
     static constexpr int VS = D + 16;
     static constexpr int REGION = kTile * VS;     // elements per wave
     static constexpr int OS = D + 4;              // a wave's output rows in LDS (floats)
-    static_assert(kRows * OS * 4 + 2 * kRows * 4 <= REGION * 2, "a wave's result fits its value rows");
+    static_assert(ROWS * OS * 4 + 2 * ROWS * 4 <= REGION * 2, "a wave's result fits its value rows");
 };
 
 typedef __attribute__((address_space(3))) bf16x4_t lds_bf16x4_t;
 
-template <int D>
+template <int D, int MT>
 struct Wave {
-    using C = Cfg<D>;
-    bf16x8_t q[C::KS];
-    f32x4_t o[C::MB];
-    float m, l;             // running maximum (log2 units) and this lane's share of the sum
+    using C = Cfg<D, MT>;
+    bf16x8_t q[MT][C::KS];
+    f32x4_t o[MT][C::MB];
+    float m[MT], l[MT];     // running maximum (log2 units) and this lane's share of the sum
 
-    // The tile's scores s[i] (keys 16i + 4(lane/16) + r of column lane%16) become
+    __device__ __forceinline__ void init(const uint16_t *Q, int q0, int n_q, int lane) {
+        const int g = lane >> 4, c = lane & 15;
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            m[t] = neg_inf();
+            l[t] = 0.f;
+            const int row = q0 + 16 * t + c;
+#pragma unroll
+            for (int mb = 0; mb < C::MB; ++mb) o[t][mb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < C::KS; ++k)
+                q[t][k] = frag(row < n_q ? *(const u32x4 *)(Q + (int64_t)row * D + (k >> 1) * 64 + g * 16 + (k & 1) * 8)
+                                         : u32x4{0, 0, 0, 0});
+        }
+    }
+
+    // Tile t's scores s[i] (keys 16i + 4(lane/16) + r of column lane%16) become
     // probabilities; keys from `valid` on do not exist.
-    __device__ __forceinline__ void softmax(f32x4_t (&s)[4], float scale_log2, int valid, int g) {
+    __device__ __forceinline__ void softmax(int t, f32x4_t (&s)[4], float scale_log2, int valid, int g) {
         float top = neg_inf();
+        if (valid >= kTile) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const float z = s[i][r] * scale_log2;
-                s[i][r] = 16 * i + 4 * g + r < valid ? z : neg_inf();
-                top = fmaxf(top, s[i][r]);
-            }
+                for (int r = 0; r < 4; ++r) {
+                    s[i][r] *= scale_log2;
+                    top = fmaxf(top, s[i][r]);
+                }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    s[i][r] = 16 * i + 4 * g + r < valid ? s[i][r] * scale_log2 : neg_inf();
+                    top = fmaxf(top, s[i][r]);
+                }
+        }
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
-        const float mn = fmaxf(m, top), base = mn == neg_inf() ? 0.f : mn;
-        const float alpha = __builtin_amdgcn_exp2f(m - base);
-        m = mn;
+        const float mn = fmaxf(m[t], top), base = mn == neg_inf() ? 0.f : mn;
+        const float alpha = __builtin_amdgcn_exp2f(m[t] - base);
+        m[t] = mn;
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -153,78 +180,89 @@ struct Wave {
                 s[i][r] = __builtin_amdgcn_exp2f(s[i][r] - base);
                 sum += s[i][r];
             }
-        l = l * alpha + sum;
+        l[t] = l[t] * alpha + sum;
         if (__ballot(alpha != 1.f)) {
 #pragma unroll
-            for (int mb = 0; mb < C::MB; ++mb) o[mb] *= alpha;
+            for (int mb = 0; mb < C::MB; ++mb) o[t][mb] *= alpha;
         }
     }
 
-    // O^T += V^T P^T with the tile's value rows in LDS.
-    __device__ __forceinline__ void values(const f32x4_t (&p)[4], uint16_t *v, int lane) {
+    // O^T += V^T P^T with the step's value rows in LDS.
+    __device__ __forceinline__ void values(const f32x4_t (&p)[MT][4], uint16_t *v, int lane) {
         const int g = lane >> 4, c = lane & 15;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            bf16x8_t b;
+        for (int k = 0; k < 2; ++k) {
+            bf16x8_t b[MT];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                b[r] = (__bf16)p[2 * t][r];
-                b[4 + r] = (__bf16)p[2 * t + 1][r];
-            }
-            uint16_t *row = v + (32 * t + 4 * g + (c >> 2)) * C::VS + 4 * (c & 3);
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    b[t][r] = (__bf16)p[t][2 * k][r];
+                    b[t][4 + r] = (__bf16)p[t][2 * k + 1][r];
+                }
+            uint16_t *row = v + (32 * k + 4 * g + (c >> 2)) * C::VS + 4 * (c & 3);
 #pragma unroll
             for (int mb = 0; mb < C::MB; ++mb) {
                 const bf16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t *)(row + 16 * mb));
                 const bf16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t *)(row + 16 * C::VS + 16 * mb));
                 const bf16x8_t f = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-                o[mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, b, o[mb], 0, 0, 0);
+#pragma unroll
+                for (int t = 0; t < MT; ++t) o[t][mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, b[t], o[t][mb], 0, 0, 0);
             }
         }
     }
 };
 
-// grid: (head, query tile, part), part innermost.
+// Channels d .. d + 3 of an output row from its sums; empty: the row's head has no key.
 template <int D>
+__device__ __forceinline__ void put_row(const AttnQ8Args &a, int64_t row, int d, const f32x4_t &acc, float M, float L, bool empty) {
+    const float inv = empty ? 0.f : 1.f / L;
+    uint32_t b[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) b[k] = __builtin_bit_cast(uint16_t, (__bf16)(acc[k] * inv));
+    *(uint2 *)(a.O + row * D + d) = make_uint2(b[0] | (b[1] << 16), b[2] | (b[3] << 16));
+    if (a.lse && d == 0) a.lse[row] = empty ? neg_inf() : fmaf(M, kLn2, logf(L));
+}
+
+// Workgroups go to the 8 XCDs in turn: the query tiles of one (head, part), which
+// read the same keys, take consecutive places of one XCD and share its L2.
+template <int D, int MT>
 __global__ __launch_bounds__(kThreads) void attn_q8_kernel(AttnQ8Args a) {
-    using C = Cfg<D>;
+    using C = Cfg<D, MT>;
+    constexpr int kRows = C::ROWS;
     __shared__ __attribute__((aligned(16))) uint16_t lds[kWaves * C::REGION];
     __shared__ int slots[FKV_MAX_FRAMES];
-    __shared__ uint32_t flag;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, c = lane & 15;
-    const int part = blockIdx.x % a.n_split, item = blockIdx.x / a.n_split;
-    const int h = item / a.n_qtiles, q0 = (item - h * a.n_qtiles) * kRows;
+    const int place = blockIdx.x >> 3, group = (blockIdx.x & 7) + 8 * (place / a.n_qtiles), qt = place % a.n_qtiles;
+    const int h = group / a.n_split, part = group - h * a.n_split;
+    if (h >= a.n_heads) return;
+    const int item = h * a.n_qtiles + qt, q0 = qt * kRows;
     if (tid < a.H) slots[tid] = a.slots.slot[tid];
     __syncthreads();
 
+    // The keys in units of 16: uh of the history, then those of the current tokens,
+    // split evenly over the waves of all parts.
     const History x = history_of(a, h);
-    const int th = (x.kvl + kTile - 1) / kTile, T = th + (a.n_cur + kTile - 1) / kTile;
-    const int t0 = (int)((int64_t)T * part / a.n_split), t1 = (int)((int64_t)T * (part + 1) / a.n_split);
+    const int uh = (x.kvl + kUnit - 1) / kUnit, units = uh + (a.n_cur + kUnit - 1) / kUnit;
+    const int n_waves = a.n_split * kWaves, wi = part * kWaves + w;
+    const int u0 = (int)((int64_t)units * wi / n_waves), u1 = (int)((int64_t)units * (wi + 1) / n_waves);
 
-    Wave<D> s;
-    s.m = neg_inf();
-    s.l = 0.f;
-#pragma unroll
-    for (int mb = 0; mb < C::MB; ++mb) s.o[mb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    const bool row_ok = q0 + c < a.n_q;
-#pragma unroll
-    for (int k = 0; k < C::KS; ++k) {
-        const int d = (k >> 1) * 64 + g * 16 + (k & 1) * 8;
-        s.q[k] = frag(row_ok ? *(const u32x4 *)(a.Q + ((int64_t)h * a.n_q + q0 + c) * D + d) : u32x4{0, 0, 0, 0});
-    }
+    Wave<D, MT> s;
+    s.init(a.Q + (int64_t)h * a.n_q * D, q0, a.n_q, lane);
     uint16_t *vt = lds + w * C::REGION;
-    const uint8_t *K8 = a.K8 + (int64_t)h * a.cap * a.F * D, *V8 = a.V8 + (int64_t)h * a.cap * a.F * D;
-    const float *ks = a.k_scale + (int64_t)h * a.cap * a.n_blocks, *vs = a.v_scale + (int64_t)h * a.cap * a.n_blocks;
-    const uint16_t *Kn = a.K_cur + (int64_t)h * a.n_cur * D, *Vn = a.V_cur + (int64_t)h * a.n_cur * D;
 
-    for (int t = t0 + w; t < t1; t += kWaves) {
-        f32x4_t z[4];
-        const bool hist = t < th;
-        const int j0 = (hist ? t : t - th) * kTile, valid = (hist ? x.kvl : a.n_cur) - j0;
-        if (hist) {
-            const Place at = place_of(a, x, slots, min(j0 + lane, x.kvl - 1));
-            const int row = at.slot * a.F + at.p, blk = at.slot * a.n_blocks + (at.p >> a.block_shift);
-            const float sk = ks[blk], sv = vs[blk];
-            u32x4 kr[4][C::U], vr[4][C::U];
+    // History: a step's rows are in flight while the step before weights its values.
+    const int jend = min(u1 * kUnit, x.kvl);
+    if (u0 * kUnit < jend) {
+        const uint8_t *K8 = a.K8 + (int64_t)h * a.cap * a.F * D, *V8 = a.V8 + (int64_t)h * a.cap * a.F * D;
+        const float *ks = a.k_scale + (int64_t)h * a.cap * a.n_blocks, *vs = a.v_scale + (int64_t)h * a.cap * a.n_blocks;
+        u32x4 kr[4][C::U], vr[4][C::U];
+        float sk, sv;
+        // Rows of 64 keys whose places the lanes hold, one each (past the wave's last key
+        // the last one again: its line is there already).
+        auto load = [&](int row, int blk) {
+            sk = ks[blk];
+            sv = vs[blk];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint32_t off = (uint32_t)__shfl(row, 16 * i + c) * D + g * 16;
@@ -234,15 +272,30 @@ __global__ __launch_bounds__(kThreads) void attn_q8_kernel(AttnQ8Args a) {
                     vr[i][u] = *(const u32x4 *)(V8 + off + 64 * u);
                 }
             }
+        };
+        auto row_of = [&](int j) {
+            const Place at = place_of(a, x, slots, min(j + lane, jend - 1));
+            return make_int2(at.slot * a.F + at.p, at.slot * a.n_blocks + (at.p >> a.block_shift));
+        };
+        int j0 = u0 * kUnit;
+        int2 at = row_of(j0);
+        load(at.x, at.y);
+        for (; j0 < jend; j0 += kTile) {
+            const int next = j0 + kTile, valid = jend - j0;
+            // (the next step's places first: a look-up in kept_seg returns with this step's rows)
+            at = row_of(next);
+            f32x4_t z[MT][4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float sc = __shfl(sk, 16 * i + c);
-                z[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int k = 0; k < C::KS; ++k) {
                     const u32x4 r = kr[i][k >> 1];
-                    z[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(widen8(r[2 * (k & 1)], r[2 * (k & 1) + 1], sc)),
-                                                                   s.q[k], z[i], 0, 0, 0);
+                    const bf16x8_t f = frag(widen8(r[2 * (k & 1)], r[2 * (k & 1) + 1], sc));
+#pragma unroll
+                    for (int t = 0; t < MT; ++t)
+                        z[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, s.q[t][k], k ? z[t][i] : f32x4_t{0.f, 0.f, 0.f, 0.f},
+                                                                          0, 0, 0);
                 }
             }
             wave_sync();
@@ -258,107 +311,160 @@ __global__ __launch_bounds__(kThreads) void attn_q8_kernel(AttnQ8Args a) {
                     dst[1] = widen8(r[2], r[3], sc);
                 }
             }
-        } else {
+            if (next < jend) load(at.x, at.y);
+#pragma unroll
+            for (int t = 0; t < MT; ++t) s.softmax(t, z[t], a.scale_log2, valid, g);
             wave_sync();
+            s.values(z, vt, lane);
+        }
+    }
+    // Current tokens, bf16.
+    const int cend = min((u1 - uh) * kUnit, a.n_cur);
+    for (int j0 = max(u0 - uh, 0) * kUnit; j0 < cend; j0 += kTile) {
+        const uint16_t *Kn = a.K_cur + (int64_t)h * a.n_cur * D, *Vn = a.V_cur + (int64_t)h * a.n_cur * D;
+        const int valid = cend - j0;
+        f32x4_t z[MT][4];
+        wave_sync();
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int key = 16 * i + c;
-                const bool ok = key < valid;
-                const int64_t off = (int64_t)(j0 + (ok ? key : 0)) * D + g * 16;
-                z[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < 4; ++i) {
+            const int key = 16 * i + c;
+            const bool ok = key < valid;
+            const int64_t off = (int64_t)(j0 + (ok ? key : 0)) * D + g * 16;
 #pragma unroll
-                for (int k = 0; k < C::KS; ++k) {
-                    const u32x4 r = *(const u32x4 *)(Kn + off + 64 * (k >> 1) + 8 * (k & 1));
-                    z[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(r), s.q[k], z[i], 0, 0, 0);
-                }
+            for (int k = 0; k < C::KS; ++k) {
+                const bf16x8_t f = frag(*(const u32x4 *)(Kn + off + 64 * (k >> 1) + 8 * (k & 1)));
 #pragma unroll
-                for (int u = 0; u < C::U; ++u) {
-                    u32x4 *dst = (u32x4 *)(vt + key * C::VS + 64 * u + 16 * g);
+                for (int t = 0; t < MT; ++t)
+                    z[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, s.q[t][k], k ? z[t][i] : f32x4_t{0.f, 0.f, 0.f, 0.f}, 0,
+                                                                      0, 0);
+            }
 #pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        dst[e] = ok ? *(const u32x4 *)(Vn + off + 64 * u + 8 * e) : u32x4{0, 0, 0, 0};
-                }
+            for (int u = 0; u < C::U; ++u) {
+                u32x4 *dst = (u32x4 *)(vt + key * C::VS + 64 * u + 16 * g);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) dst[e] = ok ? *(const u32x4 *)(Vn + off + 64 * u + 8 * e) : u32x4{0, 0, 0, 0};
             }
         }
-        s.softmax(z, a.scale_log2, valid, g);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) s.softmax(t, z[t], a.scale_log2, valid, g);
         wave_sync();
         s.values(z, vt, lane);
     }
 
     // the wave's result into its region of LDS: output rows, maxima, sums
-    s.l += __shfl_xor(s.l, 16);
-    s.l += __shfl_xor(s.l, 32);
     wave_sync();
     float *mine = (float *)vt;
 #pragma unroll
-    for (int mb = 0; mb < C::MB; ++mb) *(f32x4_t *)(mine + c * C::OS + 16 * mb + 4 * g) = s.o[mb];
-    if (lane < kRows) {
-        mine[kRows * C::OS + lane] = s.m;
-        mine[kRows * C::OS + kRows + lane] = s.l;
+    for (int t = 0; t < MT; ++t) {
+        s.l[t] += __shfl_xor(s.l[t], 16);
+        s.l[t] += __shfl_xor(s.l[t], 32);
+#pragma unroll
+        for (int mb = 0; mb < C::MB; ++mb) *(f32x4_t *)(mine + (16 * t + c) * C::OS + 16 * mb + 4 * g) = s.o[t][mb];
+        if (lane < 16) {
+            mine[kRows * C::OS + 16 * t + lane] = s.m[t];
+            mine[kRows * C::OS + kRows + 16 * t + lane] = s.l[t];
+        }
     }
     __syncthreads();
 
-    // thread -> row r, channels d .. d + 3
-    const int r = tid / (D / 4), d = tid % (D / 4) * 4;
-    const bool active = r < kRows && q0 + r < a.n_q;
-    float M = neg_inf(), L = 0.f;
-    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-    if (active) {
+    // Element groups of this thread: row r, channels d .. d + 3.
+    constexpr int kGroups = kRows * D / 4, kPer = (kGroups + kThreads - 1) / kThreads;
+    const int rows = min(kRows, a.n_q - q0);
+    float M[kPer], L[kPer];
+    f32x4_t acc[kPer];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        const int r = (e * kThreads + tid) / (D / 4), d = (e * kThreads + tid) % (D / 4) * 4;
+        M[e] = neg_inf();
+        L[e] = 0.f;
+        acc[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if (r >= rows) continue;
         const float *base = (const float *)lds;
         constexpr int RF = C::REGION / 2;                 // floats per region
-        for (int i = 0; i < kWaves; ++i) M = fmaxf(M, base[i * RF + kRows * C::OS + r]);
-        const float ref = M == neg_inf() ? 0.f : M;
+        for (int i = 0; i < kWaves; ++i) M[e] = fmaxf(M[e], base[i * RF + kRows * C::OS + r]);
+        const float ref = M[e] == neg_inf() ? 0.f : M[e];
         for (int i = 0; i < kWaves; ++i) {
             const float wt = __builtin_amdgcn_exp2f(base[i * RF + kRows * C::OS + r] - ref);
-            L += wt * base[i * RF + kRows * C::OS + kRows + r];
-            acc += wt * *(const f32x4_t *)(base + i * RF + r * C::OS + d);
+            L[e] += wt * base[i * RF + kRows * C::OS + kRows + r];
+            acc[e] += wt * *(const f32x4_t *)(base + i * RF + r * C::OS + d);
         }
     }
-    const int64_t out_row = (int64_t)h * a.n_q + q0 + r;
-    if (a.n_split > 1) {
-        float *slots_of = a.part + (size_t)item * a.n_split * (kRows * (D + 2));
-        float *slot = slots_of + (size_t)part * (kRows * (D + 2));
-        if (active) {
-            uint64_t *dst = (uint64_t *)(slot + r * D + d);
-            put_shared((unsigned long long *)dst, make_uint2(__float_as_uint(acc[0]), __float_as_uint(acc[1])));
-            put_shared((unsigned long long *)dst + 1, make_uint2(__float_as_uint(acc[2]), __float_as_uint(acc[3])));
+    if (a.n_split > 1) {                                  // joined by join_q8_kernel
+        float *slot = a.part + ((size_t)item * a.n_split + part) * (kRows * (D + 2));
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            const int r = (e * kThreads + tid) / (D / 4), d = (e * kThreads + tid) % (D / 4) * 4;
+            if (r >= rows) continue;
+            *(f32x4_t *)(slot + r * D + d) = acc[e];
             if (d == 0) {
-                put_shared(slot + kRows * D + r, M);
-                put_shared(slot + kRows * D + kRows + r, L);
+                slot[kRows * D + r] = M[e];
+                slot[kRows * D + kRows + r] = L[e];
             }
         }
-        if (!arrive_last(a.counters + (size_t)item * kItemCounterStride, (uint32_t)a.n_split, &flag)) return;
-        M = neg_inf();
-        L = 0.f;
-        acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        if (active) {
-            for (int j = 0; j < a.n_split; ++j) {
-                const float *p = slots_of + (size_t)j * (kRows * (D + 2));
-                const float mj = get_shared(p + kRows * D + r), lj = get_shared(p + kRows * D + kRows + r);
-                const uint2 u = get_shared((const uint2 *)(p + r * D + d)), v = get_shared((const uint2 *)(p + r * D + d) + 1);
-                const float Mn = fmaxf(M, mj), ref = Mn == neg_inf() ? 0.f : Mn;
-                const float so = __builtin_amdgcn_exp2f(M - ref), sn = __builtin_amdgcn_exp2f(mj - ref);
-                M = Mn;
-                L = L * so + lj * sn;
-                acc[0] = acc[0] * so + __uint_as_float(u.x) * sn;
-                acc[1] = acc[1] * so + __uint_as_float(u.y) * sn;
-                acc[2] = acc[2] * so + __uint_as_float(v.x) * sn;
-                acc[3] = acc[3] * so + __uint_as_float(v.y) * sn;
-            }
-        }
-    }
-    if (!active) return;
-    if (T == 0) {                                          // no key at all
-        *(uint2 *)(a.O + out_row * D + d) = make_uint2(0, 0);
-        if (a.lse && d == 0) a.lse[out_row] = neg_inf();
         return;
     }
-    const float inv = 1.f / L;
-    uint32_t b[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) b[e] = __builtin_bit_cast(uint16_t, (__bf16)(acc[e] * inv));
-    *(uint2 *)(a.O + out_row * D + d) = make_uint2(b[0] | (b[1] << 16), b[2] | (b[3] << 16));
-    if (a.lse && d == 0) a.lse[out_row] = fmaf(M, kLn2, logf(L));
+    for (int e = 0; e < kPer; ++e) {
+        const int r = (e * kThreads + tid) / (D / 4), d = (e * kThreads + tid) % (D / 4) * 4;
+        if (r < rows) put_row<D>(a, (int64_t)h * a.n_q + q0 + r, d, acc[e], M[e], L[e], units == 0);
+    }
+}
+
+// Joins the parts of the items: M = max_j m_j, L = sum_j 2^(m_j - M) l_j and likewise
+// the outputs.  A launch of its own: the parts then cross as ordinary cached stores
+// and loads, every row has a workgroup, and the workspace holds no counters.  (Joined
+// by the part that arrives last, 480P: one query token 29.2 us, 16 tokens 24.0, 32
+// tokens 32.7; so ONE_US, Q16_US, Q32_US.)  One workgroup per row and head: D/4 threads
+// take 4 channels each, kLanes of them every kLanes'th part, then the lanes' sums meet
+// in LDS, always in the same order.  grid: x = row, y = head.
+template <int D>
+__global__ __launch_bounds__(kJoinThreads) void join_q8_kernel(AttnQ8Args a) {
+    constexpr int kLanes = kJoinThreads / (D / 4);
+    __shared__ f32x4_t sum[kLanes][D / 4];
+    __shared__ float top[kLanes], total[kLanes];
+    const int h = blockIdx.y, row = blockIdx.x, t = threadIdx.x % (D / 4), lane = threadIdx.x / (D / 4);
+    const int qt = row / a.q_tile, r = row - qt * a.q_tile;
+    const size_t slot = (size_t)a.q_tile * (D + 2);
+    const float *p = a.part + ((size_t)h * a.n_qtiles + qt) * a.n_split * slot;
+    const float *pm = p + (size_t)a.q_tile * D + r, *pl = pm + a.q_tile, *po = p + (size_t)r * D + 4 * t;
+    float M = neg_inf(), L = 0.f;
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+    auto add = [&](float m, float l, const f32x4_t &o) {
+        const float Mn = fmaxf(M, m), ref = Mn == neg_inf() ? 0.f : Mn;
+        const float so = __builtin_amdgcn_exp2f(M - ref), sn = __builtin_amdgcn_exp2f(m - ref);
+        M = Mn;
+        L = L * so + l * sn;
+        acc = acc * so + o * sn;
+    };
+    for (int j0 = lane; j0 < a.n_split; j0 += kJoin * kLanes) {
+        float mj[kJoin], lj[kJoin];
+        f32x4_t o[kJoin];
+#pragma unroll
+        for (int j = 0; j < kJoin; ++j) {
+            const size_t at = (size_t)min(j0 + j * kLanes, a.n_split - 1) * slot;
+            mj[j] = pm[at];
+            lj[j] = pl[at];
+            o[j] = *(const f32x4_t *)(po + at);
+        }
+        // (all loads before the first use, and no branch that they could sink behind: one
+        // memory latency, not one each)
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < kJoin; ++j) {
+            const bool ok = j0 + j * kLanes < a.n_split;
+            add(ok ? mj[j] : neg_inf(), ok ? lj[j] : 0.f, ok ? o[j] : f32x4_t{0.f, 0.f, 0.f, 0.f});
+        }
+    }
+    sum[lane][t] = acc;
+    if (t == 0) {
+        top[lane] = M;
+        total[lane] = L;
+    }
+    __syncthreads();
+    if (lane > 0) return;
+    for (int i = 1; i < kLanes; ++i) add(top[i], total[i], sum[i][t]);
+    const History hist = history_of(a, h);
+    put_row<D>(a, (int64_t)h * a.n_q + row, 4 * t, acc, M, L, hist.kvl + a.n_cur == 0);
 }
 
 // Large chunks: the kept history as a bf16 copy [n_heads][slab][d] for the chunk
@@ -420,9 +526,17 @@ hipError_t launch_expand_q8(const AttnQ8Args &a, int head_dim, hipStream_t s) {
 }
 
 hipError_t launch_attention_q8(const AttnQ8Args &a, int head_dim, hipStream_t s) {
-    const dim3 grid((unsigned)((int64_t)a.n_heads * a.n_qtiles * a.n_split));
-    if (head_dim == 64) hipLaunchKernelGGL(attn_q8_kernel<64>, grid, dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL(attn_q8_kernel<128>, grid, dim3(kThreads), 0, s, a);
+    const int64_t groups = ((int64_t)a.n_heads * a.n_split + 7) / 8 * 8;
+    const dim3 grid((unsigned)(groups * a.n_qtiles));
+    if (head_dim == 64 && a.q_tile == 16) hipLaunchKernelGGL((attn_q8_kernel<64, 1>), grid, dim3(kThreads), 0, s, a);
+    else if (head_dim == 64) hipLaunchKernelGGL((attn_q8_kernel<64, 2>), grid, dim3(kThreads), 0, s, a);
+    else if (a.q_tile == 16) hipLaunchKernelGGL((attn_q8_kernel<128, 1>), grid, dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((attn_q8_kernel<128, 2>), grid, dim3(kThreads), 0, s, a);
+    if (a.n_split > 1) {
+        const dim3 join((unsigned)a.n_q, (unsigned)a.n_heads);
+        if (head_dim == 64) hipLaunchKernelGGL(join_q8_kernel<64>, join, dim3(kJoinThreads), 0, s, a);
+        else hipLaunchKernelGGL(join_q8_kernel<128>, join, dim3(kJoinThreads), 0, s, a);
+    }
     return hipGetLastError();
 }
 
