@@ -625,13 +625,13 @@ fkv_status fkv_score_select_q8(const fkv_shape *shape, const fkv_head *heads,
  * exact, probabilities are rounded to bf16 for the value product.
  *
  * With a workspace of at least fkv_chunk_attention_q8_workspace_size bytes
- * (its arguments as this call's; zero-filled before its first use, every call
- * leaves it ready for the next, of the same sizes or others; calls that share
- * one are ordered by the caller) the work is split over the whole device: few
- * query tokens along the keys, whose parts are joined by the last of them; a
- * large chunk with n_q = n_cur over a bf16 copy of the kept tokens in the
- * workspace.  With NULL one workgroup computes a query tile of a head from its first key to
- * its last.  FKV_ERR_CAPACITY if the workspace is smaller. */
+ * (its arguments as this call's; it needs no initialisation, and calls of any
+ * sizes may share one in turn, ordered by the caller) the work is spread over the
+ * whole device: few query tokens are split along the keys, whose parts are joined
+ * in fp32; a large chunk is attended over a bf16 copy of the kept tokens in the
+ * workspace.  With NULL one workgroup computes a query tile of a head from its
+ * first key to its last.  FKV_ERR_CAPACITY if the workspace is smaller.  The same
+ * bits on every run of the same call. */
 fkv_status fkv_chunk_attention_q8_workspace_size(const fkv_shape *shape, const fkv_head *heads,
                                                  int32_t n_q, int32_t n_cur, size_t *bytes);
 fkv_status fkv_chunk_attention_q8(const fkv_shape *shape, const fkv_head *heads,

@@ -906,8 +906,8 @@ def fkv_chunk_attention_q8(shape: fkv_shape, heads, cache: Cache8, frame_slot, k
     """Attention of the query tokens Q [n_heads][n_q][d] over every head's kept
     history in the 8-bit cache and the current tokens K_cur, V_cur
     [n_heads][n_cur][d] (None, or n_cur = 0: none).  ``workspace``: uint8 device
-    tensor of fkv_chunk_attention_q8_workspace_size bytes, zero-filled before its
-    first use; None runs one workgroup per query tile."""
+    tensor of fkv_chunk_attention_q8_workspace_size bytes (no initialisation);
+    None runs one workgroup per query tile."""
     bf, i32 = torch.bfloat16, torch.int32
     n, d = shape.n_heads, shape.head_dim
     dev = _device_of(Q, "Q")

@@ -1410,53 +1410,69 @@ int64_t q8_most_kept(const fkv_shape *s, const fkv_head *heads) {
     return most;
 }
 
-int q8_tile(int32_t n_q) { return n_q <= 16 ? 16 : 32; }
-int q8_query_tiles(int32_t n_q) { return (n_q + q8_tile(n_q) - 1) / q8_tile(n_q); }
-
-// Query rows from which a chunk (n_q = n_cur) is attended over an expanded copy
-// of the kept history.
-constexpr int kExpandFrom = 256;
-
-// How an 8-bit attention call (checked) is divided.  In place: parts per (head,
-// query tile), so that about one workgroup runs per compute unit and a part
-// keeps a tile for each of its waves.  The workspace starts with the arrival
-// counters of the split items -- at most one for every two workgroups, so a
-// region of one size for all calls, which nothing else is written to -- and then
-// holds the parts.  Expanded: behind that region it holds the counters of the
-// balanced schedule (cleared by the call itself), its parts, the heads' lengths
-// and the copy.
+// How an 8-bit attention call (checked) is divided; the unit of the rules is a
+// wave's step, 64 keys by one query tile.
+//
+// Query tile: 32 rows where the work fills the device (a step of 32 rows takes a
+// wave about 1.5 steps of 16), 16 rows while it does not: up to kNarrowSteps
+// steps for each of the device's 8 waves per CU, and always for up to 16 rows.
+// 16 heads of 64, 27 key tiles, 256 query rows: 16-row tiles 11.6 us, 32-row 13.7;
+// 512 rows 22.4 and 16.6; 12 heads of 128 at 480P, 64 rows 37.1 and 30.8.
+//
+// Parts: where a wave would walk more than kWholeSteps steps and the device has
+// workgroups to spare, an item (head, query tile) is cut into parts of at least two
+// steps a wave, one workgroup each; the parts are joined by a second launch of 3 to 4
+// us.  480P, 16 rows: one workgroup per head 128 us, 21 parts 20.1; 128 rows of the
+// small layer above (5 steps) 11.2 whole, 14.6 cut.
+//
+// Expanded: chunks of kExpandRows rows and kExpandSteps steps or more are attended
+// over a bf16 copy of the kept history, by the 256-row kernel of
+// fkv_chunk_attention, which runs four times as many products a second but pays for
+// the copy and, with few items, for joining large parts.  480P, 12 heads: 512 rows
+// (53 thousand steps) in place 139 us, expanded 141; 1024 rows (110) 246 and 169;
+// 4096 rows 1300 and 462; 24 heads, 600 rows, 3 frames (38) 101 and 113; one head,
+// 600 rows 48 and 232.
+//
+// The workspace holds the parts, or, expanded, the counters of the balanced
+// schedule (cleared by the call itself), its parts, the heads' lengths and the copy.
+constexpr int kNarrowSteps = 4, kWholeSteps = 5, kExpandRows = 512;
+constexpr int64_t kExpandSteps = 60000;
 struct Q8Plan {
     bool expand;
-    int n_split, blocks;
+    int q_tile, n_qtiles, n_split, blocks;
     int64_t slab;
-    int64_t n_counters;                                       // expanded: counters to clear
-    size_t counter_at, part_at, len_at, k_at, v_at, bytes;    // byte offsets in the workspace
+    int64_t n_counters;                           // expanded: counters to clear
+    size_t part_at, len_at, k_at, v_at, bytes;    // byte offsets in the workspace
 };
 
-fkv_status q8_plan(const fkv_shape *s, const fkv_head *heads, int32_t n_q, int32_t n_cur, Q8Plan *p) {
-    fkv_status st;
-    memset(p, 0, sizeof *p);
-    if ((st = balanced_blocks(&p->blocks)) != FKV_OK) return st;
-    p->slab = q8_most_kept(s, heads);
-    p->expand = n_q == n_cur && n_q >= kExpandFrom;
-    if (p->expand) {
+// blocks: the device's workgroups of the schedules (one per CU), 0 without a workspace.
+Q8Plan q8_plan(const fkv_shape *s, const fkv_head *heads, int32_t n_q, int32_t n_cur, int blocks) {
+    Q8Plan p;
+    memset(&p, 0, sizeof p);
+    p.blocks = blocks;
+    p.slab = q8_most_kept(s, heads);
+    const int64_t tiles = (p.slab + 63) / 64 + ((int64_t)n_cur + 63) / 64;
+    auto steps = [&](int tile) { return (int64_t)s->n_heads * ((n_q + tile - 1) / tile) * tiles; };
+    p.expand = blocks > 0 && n_cur > 0 && n_q >= kExpandRows && steps(32) >= kExpandSteps;
+    if (p.expand) {
         const int64_t items = (int64_t)s->n_heads * ((n_q + fkv::kAttnRowsBf16 - 1) / fkv::kAttnRowsBf16);
-        const size_t copy = (size_t)s->n_heads * p->slab * s->head_dim * 2;
-        p->n_counters = items;
-        p->counter_at = fkv::attention_counter_bytes(p->blocks);
-        p->part_at = p->counter_at + fkv::attention_counter_bytes(items);
-        p->len_at = p->part_at + 2 * (size_t)p->blocks * fkv::attention_part_bytes(s->head_dim, true);
-        p->k_at = p->len_at + 256;
-        p->v_at = p->k_at + copy;
-        p->bytes = p->v_at + copy;
-        return FKV_OK;
+        const size_t copy = (size_t)s->n_heads * p.slab * s->head_dim * 2;
+        p.n_counters = items;
+        p.part_at = fkv::attention_counter_bytes(items);
+        p.len_at = p.part_at + 2 * (size_t)blocks * fkv::attention_part_bytes(s->head_dim, true);
+        p.k_at = p.len_at + 256;
+        p.v_at = p.k_at + copy;
+        p.bytes = p.v_at + copy;
+        return p;
     }
-    const int64_t tiles = (p->slab + 63) / 64 + ((int64_t)n_cur + 63) / 64;
-    const int64_t items = (int64_t)s->n_heads * q8_query_tiles(n_q);
-    p->n_split = (int)std::max<int64_t>(1, std::min<int64_t>(p->blocks / items, (tiles + 7) / 8));
-    p->part_at = fkv::attention_counter_bytes(p->blocks);
-    p->bytes = p->n_split > 1 ? p->part_at + (size_t)items * p->n_split * fkv::attn_q8_part_floats(s->head_dim, q8_tile(n_q)) * sizeof(float) : 0;
-    return FKV_OK;
+    p.q_tile = n_q <= 16 || steps(16) <= (int64_t)kNarrowSteps * 8 * (blocks > 0 ? blocks : 256) ? 16 : 32;
+    p.n_qtiles = (n_q + p.q_tile - 1) / p.q_tile;
+    const int64_t items = (int64_t)s->n_heads * p.n_qtiles, wave_steps = (tiles + 7) / 8;
+    p.n_split = 1;
+    if (wave_steps > kWholeSteps) p.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(blocks / items, (wave_steps + 1) / 2));
+    if (p.n_split > 1)
+        p.bytes = (size_t)items * p.n_split * fkv::attn_q8_part_floats(s->head_dim, p.q_tile) * sizeof(float);
+    return p;
 }
 
 }  // namespace
@@ -1603,11 +1619,11 @@ fkv_status fkv_score_select_q8(const fkv_shape *shape, const fkv_head *heads, co
 fkv_status fkv_chunk_attention_q8_workspace_size(const fkv_shape *shape, const fkv_head *heads, int32_t n_q,
                                                  int32_t n_cur, size_t *bytes) {
     fkv_status st;
-    Q8Plan p;
     if ((st = check_q8_call(shape, heads, n_q, n_cur)) != FKV_OK) return st;
     if (!bytes) return fail(FKV_ERR_ARG, "bytes is NULL");
-    if ((st = q8_plan(shape, heads, n_q, n_cur, &p)) != FKV_OK) return st;
-    *bytes = p.bytes;
+    int blocks = 0;
+    if ((st = balanced_blocks(&blocks)) != FKV_OK) return st;
+    *bytes = q8_plan(shape, heads, n_q, n_cur, blocks).bytes;
     return ok();
 }
 
@@ -1628,10 +1644,9 @@ fkv_status fkv_chunk_attention_q8(const fkv_shape *shape, const fkv_head *heads,
     }
     if (!Q || !O || (n_cur > 0 && (!K_cur || !V_cur))) return fail(FKV_ERR_ARG, "NULL tensor pointer");
     if (!(scale > 0.f) || !isfinite(scale)) return fail(FKV_ERR_ARG, "scale %g must be positive and finite", (double)scale);
-    Q8Plan p;
-    memset(&p, 0, sizeof p);
-    p.n_split = 1;
-    if (workspace && (st = q8_plan(shape, heads, n_q, n_cur, &p)) != FKV_OK) return st;
+    int blocks = 0;
+    if (workspace && (st = balanced_blocks(&blocks)) != FKV_OK) return st;
+    const Q8Plan p = q8_plan(shape, heads, n_q, n_cur, blocks);
     if (workspace && workspace_bytes < p.bytes)
         return fail(FKV_ERR_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, p.bytes);
 
@@ -1663,10 +1678,10 @@ fkv_status fkv_chunk_attention_q8(const fkv_shape *shape, const fkv_head *heads,
     magic_of(a.F, &a.mf_hi, &a.mf_lo);
     magic_of(a.L, &a.ml_hi, &a.ml_lo);
     a.scale_log2 = scale * 1.4426950408889634f;
-    a.q_tile = q8_tile(n_q);
-    a.n_qtiles = q8_query_tiles(n_q);
+    a.q_tile = p.q_tile;
+    a.n_qtiles = p.n_qtiles;
     a.n_split = p.n_split;
-    a.counters = (uint32_t *)((char *)workspace + p.counter_at);
+    a.counters = (uint32_t *)workspace;
     a.n_counters = p.n_counters;
     if (workspace) a.part = (float *)((char *)workspace + p.part_at);
     for (int h = 0; h < shape->n_heads; ++h) {

@@ -250,8 +250,8 @@ struct AttnQ8Args {
     int32_t q_tile, n_qtiles;           // query rows per tile (16 or 32), tiles per head
     int32_t n_split;                    // parts per (head, query tile); 1: no workspace
     float *part;                        // [head][query tile][part] slots of attn_q8_part_floats
-    uint32_t *counters;                 // arrivals per (head, query tile), kItemCounterStride apart
-    int64_t n_counters;                 // expanding: counters to clear
+    uint32_t *counters;                 // expanding: the attention launch's arrival counters to clear,
+    int64_t n_counters;                 // kItemCounterStride apart, and how many
     // the expanded copy (attn_q8 over large chunks): bf16 [n_heads][slab][d], and its lengths
     uint16_t *Kc, *Vc;
     int32_t *kv_out;

@@ -37,6 +37,7 @@ constexpr int kThreads = 512, kWaves = 8;
 constexpr int kTile = 64;                 // keys per step of a wave
 constexpr int kUnit = 16;                 // keys: the grain of the split over waves
 constexpr int kJoinThreads = 256, kJoin = 4;  // joining: threads of a workgroup, parts loaded at a time
+constexpr float kSlack = 8.f;             // log2 units that the softmax's reference may lag behind
 constexpr float kLn2 = 0.69314718055994530942f;
 
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
@@ -147,44 +148,43 @@ struct Wave {
     }
 
     // Tile t's scores s[i] (keys 16i + 4(lane/16) + r of column lane%16) become
-    // probabilities; keys from `valid` on do not exist.
+    // probabilities; keys from `valid` on do not exist.  The reference m moves only
+    // where a score passes it by more than kSlack: probabilities then reach 2^kSlack,
+    // which costs no digit in fp32 or bf16, and a step without such a score needs
+    // neither the other lanes' maxima nor a new scale for the outputs.
     __device__ __forceinline__ void softmax(int t, f32x4_t (&s)[4], float scale_log2, int valid, int g) {
-        float top = neg_inf();
-        if (valid >= kTile) {
+        if (valid < kTile) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    s[i][r] *= scale_log2;
-                    top = fmaxf(top, s[i][r]);
-                }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    s[i][r] = 16 * i + 4 * g + r < valid ? s[i][r] * scale_log2 : neg_inf();
-                    top = fmaxf(top, s[i][r]);
-                }
+                for (int r = 0; r < 4; ++r) s[i][r] = 16 * i + 4 * g + r < valid ? s[i][r] : neg_inf();
         }
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float mn = fmaxf(m[t], top), base = mn == neg_inf() ? 0.f : mn;
-        const float alpha = __builtin_amdgcn_exp2f(m[t] - base);
-        m[t] = mn;
+        float top = neg_inf();
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) top = fmaxf(top, s[i][r]);
+        top *= scale_log2;
+        if (__ballot(top > m[t] + kSlack)) {
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float mn = top > m[t] + kSlack ? top : m[t];
+            const float alpha = mn == m[t] ? 1.f : __builtin_amdgcn_exp2f(m[t] - mn);
+            m[t] = mn;
+            l[t] *= alpha;
+#pragma unroll
+            for (int mb = 0; mb < C::MB; ++mb) o[t][mb] *= alpha;
+        }
+        const float base = m[t] == neg_inf() ? 0.f : m[t];
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                s[i][r] = __builtin_amdgcn_exp2f(s[i][r] - base);
+                s[i][r] = __builtin_amdgcn_exp2f(fmaf(s[i][r], scale_log2, -base));
                 sum += s[i][r];
             }
-        l[t] = l[t] * alpha + sum;
-        if (__ballot(alpha != 1.f)) {
-#pragma unroll
-            for (int mb = 0; mb < C::MB; ++mb) o[t][mb] *= alpha;
-        }
+        l[t] += sum;
     }
 
     // O^T += V^T P^T with the step's value rows in LDS.
@@ -224,8 +224,9 @@ __device__ __forceinline__ void put_row(const AttnQ8Args &a, int64_t row, int d,
     if (a.lse && d == 0) a.lse[row] = empty ? neg_inf() : fmaf(M, kLn2, logf(L));
 }
 
-// Workgroups go to the 8 XCDs in turn: the query tiles of one (head, part), which
-// read the same keys, take consecutive places of one XCD and share its L2.
+// Workgroups go to the 8 XCDs in turn: each XCD takes a contiguous run of the list
+// (head, part, query tile), tiles innermost, so the tiles that read the same keys
+// mostly share an L2.
 template <int D, int MT>
 __global__ __launch_bounds__(kThreads) void attn_q8_kernel(AttnQ8Args a) {
     using C = Cfg<D, MT>;
@@ -233,7 +234,8 @@ __global__ __launch_bounds__(kThreads) void attn_q8_kernel(AttnQ8Args a) {
     __shared__ __attribute__((aligned(16))) uint16_t lds[kWaves * C::REGION];
     __shared__ int slots[FKV_MAX_FRAMES];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, c = lane & 15;
-    const int place = blockIdx.x >> 3, group = (blockIdx.x & 7) + 8 * (place / a.n_qtiles), qt = place % a.n_qtiles;
+    const int place = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+    const int group = place / a.n_qtiles, qt = place - group * a.n_qtiles;
     const int h = group / a.n_split, part = group - h * a.n_split;
     if (h >= a.n_heads) return;
     const int item = h * a.n_qtiles + qt, q0 = qt * kRows;
@@ -260,17 +262,13 @@ __global__ __launch_bounds__(kThreads) void attn_q8_kernel(AttnQ8Args a) {
         float sk, sv;
         // Rows of 64 keys whose places the lanes hold, one each (past the wave's last key
         // the last one again: its line is there already).
-        auto load = [&](int row, int blk) {
-            sk = ks[blk];
-            sv = vs[blk];
+        auto load = [&](const uint8_t *base, const float *scale, int2 at, u32x4 (&r)[4][C::U], float &sc) {
+            sc = scale[at.y];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t off = (uint32_t)__shfl(row, 16 * i + c) * D + g * 16;
+                const uint32_t off = (uint32_t)__shfl(at.x, 16 * i + c) * D + g * 16;
 #pragma unroll
-                for (int u = 0; u < C::U; ++u) {
-                    kr[i][u] = *(const u32x4 *)(K8 + off + 64 * u);
-                    vr[i][u] = *(const u32x4 *)(V8 + off + 64 * u);
-                }
+                for (int u = 0; u < C::U; ++u) r[i][u] = *(const u32x4 *)(base + off + 64 * u);
             }
         };
         auto row_of = [&](int j) {
@@ -279,25 +277,29 @@ __global__ __launch_bounds__(kThreads) void attn_q8_kernel(AttnQ8Args a) {
         };
         int j0 = u0 * kUnit;
         int2 at = row_of(j0);
-        load(at.x, at.y);
+        load(K8, ks, at, kr, sk);
+        load(V8, vs, at, vr, sv);
         for (; j0 < jend; j0 += kTile) {
             const int next = j0 + kTile, valid = jend - j0;
             // (the next step's places first: a look-up in kept_seg returns with this step's rows)
             at = row_of(next);
             f32x4_t z[MT][4];
+            float sc[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float sc = __shfl(sk, 16 * i + c);
+            for (int i = 0; i < 4; ++i) sc[i] = __shfl(sk, 16 * i + c);
 #pragma unroll
-                for (int k = 0; k < C::KS; ++k) {
+            for (int k = 0; k < C::KS; ++k) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
                     const u32x4 r = kr[i][k >> 1];
-                    const bf16x8_t f = frag(widen8(r[2 * (k & 1)], r[2 * (k & 1) + 1], sc));
+                    const bf16x8_t f = frag(widen8(r[2 * (k & 1)], r[2 * (k & 1) + 1], sc[i]));
 #pragma unroll
                     for (int t = 0; t < MT; ++t)
                         z[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, s.q[t][k], k ? z[t][i] : f32x4_t{0.f, 0.f, 0.f, 0.f},
                                                                           0, 0, 0);
                 }
             }
+            if (next < jend) load(K8, ks, at, kr, sk);
             wave_sync();
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -311,7 +313,7 @@ __global__ __launch_bounds__(kThreads) void attn_q8_kernel(AttnQ8Args a) {
                     dst[1] = widen8(r[2], r[3], sc);
                 }
             }
-            if (next < jend) load(at.x, at.y);
+            if (next < jend) load(V8, vs, at, vr, sv);
 #pragma unroll
             for (int t = 0; t < MT; ++t) s.softmax(t, z[t], a.scale_log2, valid, g);
             wave_sync();
@@ -323,28 +325,45 @@ __global__ __launch_bounds__(kThreads) void attn_q8_kernel(AttnQ8Args a) {
     for (int j0 = max(u0 - uh, 0) * kUnit; j0 < cend; j0 += kTile) {
         const uint16_t *Kn = a.K_cur + (int64_t)h * a.n_cur * D, *Vn = a.V_cur + (int64_t)h * a.n_cur * D;
         const int valid = cend - j0;
-        f32x4_t z[MT][4];
-        wave_sync();
+        // all the step's key rows and half of its value rows in flight at once, the other
+        // half as the key rows' registers come free
+        u32x4 kq[4][C::KS], vq[2][2][2 * C::U];
+        uint32_t off[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int key = 16 * i + c;
-            const bool ok = key < valid;
-            const int64_t off = (int64_t)(j0 + (ok ? key : 0)) * D + g * 16;
+            off[i] = (uint32_t)(j0 + min(16 * i + c, valid - 1)) * D + g * 16;
 #pragma unroll
-            for (int k = 0; k < C::KS; ++k) {
-                const bf16x8_t f = frag(*(const u32x4 *)(Kn + off + 64 * (k >> 1) + 8 * (k & 1)));
+            for (int k = 0; k < C::KS; ++k) kq[i][k] = *(const u32x4 *)(Kn + off[i] + 64 * (k >> 1) + 8 * (k & 1));
+        }
+        auto load_values = [&](int half) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int u = 0; u < 2 * C::U; ++u)
+                    vq[half][i][u] = *(const u32x4 *)(Vn + off[2 * half + i] + 64 * (u >> 1) + 8 * (u & 1));
+        };
+        load_values(0);
+        f32x4_t z[MT][4];
+#pragma unroll
+        for (int k = 0; k < C::KS; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int t = 0; t < MT; ++t)
-                    z[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, s.q[t][k], k ? z[t][i] : f32x4_t{0.f, 0.f, 0.f, 0.f}, 0,
-                                                                      0, 0);
-            }
+                    z[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(kq[i][k]), s.q[t][k],
+                                                                      k ? z[t][i] : f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+        load_values(1);
+        wave_sync();
 #pragma unroll
-            for (int u = 0; u < C::U; ++u) {
-                u32x4 *dst = (u32x4 *)(vt + key * C::VS + 64 * u + 16 * g);
+        for (int half = 0; half < 2; ++half)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) dst[e] = ok ? *(const u32x4 *)(Vn + off + 64 * u + 8 * e) : u32x4{0, 0, 0, 0};
+            for (int i = 0; i < 2; ++i) {
+                const int key = 16 * (2 * half + i) + c;
+#pragma unroll
+                for (int u = 0; u < 2 * C::U; ++u)
+                    *(u32x4 *)(vt + key * C::VS + 64 * (u >> 1) + 16 * g + 8 * (u & 1)) =
+                        key < valid ? vq[half][i][u] : u32x4{0, 0, 0, 0};
             }
-        }
 #pragma unroll
         for (int t = 0; t < MT; ++t) s.softmax(t, z[t], a.scale_log2, valid, g);
         wave_sync();
@@ -526,8 +545,7 @@ hipError_t launch_expand_q8(const AttnQ8Args &a, int head_dim, hipStream_t s) {
 }
 
 hipError_t launch_attention_q8(const AttnQ8Args &a, int head_dim, hipStream_t s) {
-    const int64_t groups = ((int64_t)a.n_heads * a.n_split + 7) / 8 * 8;
-    const dim3 grid((unsigned)(groups * a.n_qtiles));
+    const dim3 grid((unsigned)(((int64_t)a.n_heads * a.n_split * a.n_qtiles + 7) / 8 * 8));
     if (head_dim == 64 && a.q_tile == 16) hipLaunchKernelGGL((attn_q8_kernel<64, 1>), grid, dim3(kThreads), 0, s, a);
     else if (head_dim == 64) hipLaunchKernelGGL((attn_q8_kernel<64, 2>), grid, dim3(kThreads), 0, s, a);
     else if (a.q_tile == 16) hipLaunchKernelGGL((attn_q8_kernel<128, 1>), grid, dim3(kThreads), 0, s, a);
