@@ -34,7 +34,9 @@ from typing import Optional, Sequence, Union
 
 import torch
 
-from . import (FKV_DYNAMIC, FKV_STATIC, fkv_append_frames, fkv_attention_mass,
+from . import (Cache8, FKV_DYNAMIC, FKV_STATIC, fkv_append_frames, fkv_append_frames_q8,
+               fkv_append_frames_rotated, fkv_attention_mass, fkv_chunk_attention_q8,
+               fkv_chunk_attention_q8_workspace_size, fkv_rope, fkv_rotate_chunk, fkv_score_select_q8,
                fkv_attention_workspace_size, fkv_chunk_attention, fkv_chunk_attention_heads,
                fkv_chunk_attention_paged, fkv_chunk_attention_static, fkv_classify_heads, fkv_score_select,
                fkv_select,
@@ -385,25 +387,38 @@ class RolloutStack:
     similarity statistics once per chunk (the history is fixed during the
     chunk's AR steps); ``incremental=True`` in :meth:`run_layer` /
     :meth:`score_pooled` then reads only the last history frame and the chunk's
-    first frame per head."""
+    first frame per head.
+
+    ``rope`` (see make_rope): positions.  :meth:`rotate` turns the chunk's queries
+    and keys as the projection leaves them into the buffers that
+    :meth:`run_layer` takes, and :meth:`append` with ``frame_pos`` turns the keys
+    on their way into the cache.
+
+    ``cache="e4m3"`` holds every layer's cache in 8 bits (``cache8``, one
+    :class:`Cache8` per layer, a scale per head and ``block_tokens`` tokens; half
+    the memory of bf16): :meth:`append` quantises, :meth:`run_layer` scores and
+    selects from the 8-bit keys and attends any number of query tokens over the
+    kept 8-bit history and the current bf16 tokens.  The shared compressed
+    buffers, incremental rescoring and :meth:`score_pooled` do not exist then (a
+    row computed elsewhere may still be passed as ``pooled``)."""
 
     def __init__(self, n_layers: int, n_heads: int, head_dim: int, frame_tokens: int, window: int,
                  chunk_frames: int, seg_tokens: int, dtype: str = "bf16", device="cuda",
-                 overlap: Union[bool, str] = True, step_mode: Optional[str] = None):
+                 overlap: Union[bool, str] = True, step_mode: Optional[str] = None,
+                 rope: Optional[fkv_rope] = None, cache: Optional[str] = None, block_tokens: int = 64):
+        if cache not in (None, "e4m3"):
+            raise ValueError(f"cache {cache!r} is neither None nor 'e4m3'")
+        if cache == "e4m3" and (dtype not in ("bf16", 0) or step_mode is not None):
+            raise ValueError("an 8-bit cache needs dtype bf16 and takes no step_mode")
         self.n_layers, self.n_heads, self.d = n_layers, n_heads, head_dim
         self.F, self.window, self.C, self.L = frame_tokens, window, chunk_frames, seg_tokens
         self.dtype_name = dtype
         self.dtype = torch.bfloat16 if dtype in ("bf16", 0) else torch.float32
         self.device = torch.device(device)
         dev, dt = self.device, self.dtype
-        hist = (n_heads, window, frame_tokens, head_dim)
-        self.K_hist = [torch.zeros(hist, dtype=dt, device=dev) for _ in range(n_layers)]
-        self.V_hist = [torch.zeros(hist, dtype=dt, device=dev) for _ in range(n_layers)]
         full = self._shape(window)
         self.n_seg_max = fkv_num_segments(full)
-        self.slab = window * frame_tokens
-        self.Kc = torch.zeros((n_heads, self.slab, head_dim), dtype=dt, device=dev)
-        self.Vc = torch.zeros_like(self.Kc)
+        self.rope, self.cache = rope, cache
         self.kv_len = torch.zeros((n_heads,), dtype=torch.int32, device=dev)
         self._scores = torch.zeros((n_heads * max(self.n_seg_max, 1),), dtype=torch.float32, device=dev)
         self._kept = torch.full((n_heads * max(self.n_seg_max, 1),), -1, dtype=torch.int32, device=dev)
@@ -412,12 +427,24 @@ class RolloutStack:
         all_dyn = make_heads([_Budget(FKV_DYNAMIC, 0, 0, 0, 1)] * n_heads)
         # (scoring workspaces are zero-filled once: the one-launch reduction's arrival counters)
         self.score_ws = torch.zeros(max(fkv_score_workspace_size(full, all_dyn), 1), dtype=torch.uint8, device=dev)
+        self.scale = 1.0 / math.sqrt(head_dim)
+        self._shapes, self._heads = {}, {}
+        if cache == "e4m3":
+            self.step_mode = "q8"
+            self.cache8 = [Cache8.zeros(full, block_tokens, dev) for _ in range(n_layers)]
+            self._q8_bytes, self._q8_ws = {}, []
+            return
+        hist = (n_heads, window, frame_tokens, head_dim)
+        self.K_hist = [torch.zeros(hist, dtype=dt, device=dev) for _ in range(n_layers)]
+        self.V_hist = [torch.zeros(hist, dtype=dt, device=dev) for _ in range(n_layers)]
+        self.slab = window * frame_tokens
+        self.Kc = torch.zeros((n_heads, self.slab, head_dim), dtype=dt, device=dev)
+        self.Vc = torch.zeros_like(self.Kc)
         self.pooled_ws = torch.zeros(max(fkv_score_pooled_workspace_size(full), 1), dtype=torch.uint8, device=dev)
         with torch.cuda.device(dev):
             n = fkv_attention_workspace_size(full)
         self.attn_ws = torch.zeros(max(n, 1), dtype=torch.uint8, device=dev) if n > 0 else None
         self.attn_ws2 = torch.zeros_like(self.attn_ws) if (n > 0 and overlap) else None
-        self.scale = 1.0 / math.sqrt(head_dim)
         self.side = torch.cuda.Stream(device=dev) if overlap else None
         self.always = overlap == "always"
         self.static_in_place = static_in_place_supported(dtype, frame_tokens)
@@ -427,7 +454,6 @@ class RolloutStack:
         if step_mode not in ("paged", "compact") or (step_mode == "paged" and not can_paged):
             raise ValueError(f"step_mode {step_mode!r} is not available for this shape")
         self.step_mode = step_mode
-        self._shapes, self._heads = {}, {}
         # per-layer statistics of incremental rescoring (listed heads x window x units x 2)
         units = frame_tokens // min(seg_tokens, frame_tokens)
         self._stats_len = n_heads * window * units * 2
@@ -464,6 +490,7 @@ class RolloutStack:
     def history(self, layer: int, budgets, frame_slot, pooled: bool = False):
         """Per-frame statistics of the layer's history (its dynamic heads, or
         every head for the pooled proxy); valid until the history changes."""
+        self._needs_bf16_cache("history")
         H = len(frame_slot)
         if H == 0:
             return
@@ -476,6 +503,7 @@ class RolloutStack:
     def score_pooled(self, layer: int, frame_slot, K_cur, incremental: bool = False):
         """The first-block proxy: one score row pooled over all heads of ``layer``
         (from the statistics of :meth:`history` when ``incremental``)."""
+        self._needs_bf16_cache("score_pooled")
         H = len(frame_slot)
         if H == 0:
             return self.pooled_row[:0]
@@ -497,9 +525,21 @@ class RolloutStack:
         shape = self.shape(H)
         heads, key = self._budget_array(budgets)
         types = [b[0] for b in key]
-        Kh, Vh = self.K_hist[layer], self.V_hist[layer]
         scores, kept = self.views(H)
         has_static, has_dynamic = FKV_STATIC in types, FKV_DYNAMIC in types
+        if self.step_mode == "q8":
+            if incremental:
+                raise ValueError("an 8-bit cache has no incremental rescoring")
+            c8 = self.cache8[layer]
+            if has_dynamic:
+                if pooled is not None:
+                    fkv_select(shape, heads, pooled, kept, self.kv_len, shared_row=True)
+                else:
+                    fkv_score_select_q8(shape, heads, c8, frame_slot, K_cur, scores, kept, self.kv_len, self.score_ws)
+            fkv_chunk_attention_q8(shape, heads, c8, frame_slot, kept, self.kv_len, Q, K_cur, V_cur, self.scale, O, lse,
+                                   self._q8_workspace(shape, heads, (key, H, Q.shape[1], K_cur.shape[1])))
+            return
+        Kh, Vh = self.K_hist[layer], self.V_hist[layer]
         if self.step_mode == "paged":
             # one stream: scores + kept segments, then one attention launch over
             # every head with its kept history read in place (no copy)
@@ -553,9 +593,41 @@ class RolloutStack:
         else:
             fkv_chunk_attention(shape, Q, *att, lse, self.attn_ws)
 
-    def append(self, layer: int, K_new, V_new, dst_slots):
-        """Write a finished chunk's frames ([n_heads][n*F][d]) into the layer's cache slots."""
-        fkv_append_frames(self.shape(0), K_new, V_new, dst_slots, self.K_hist[layer], self.V_hist[layer])
+    def _needs_bf16_cache(self, what: str):
+        if self.cache == "e4m3":
+            raise ValueError(f"{what}: not available for an 8-bit cache")
+
+    def _q8_workspace(self, shape, heads, key):
+        """The 8-bit attention's workspace: the largest so far.  Smaller ones stay
+        allocated, as a graph captured with one of them still writes to it."""
+        if key not in self._q8_bytes:
+            with torch.cuda.device(self.device):
+                self._q8_bytes[key] = fkv_chunk_attention_q8_workspace_size(shape, heads, key[2], key[3])
+        if not self._q8_ws or self._q8_bytes[key] > self._q8_ws[-1].numel():
+            self._q8_ws.append(torch.empty(max(self._q8_bytes[key], 1), dtype=torch.uint8, device=self.device))
+        return self._q8_ws[-1]
+
+    def rotate(self, frame_pos, Q, K, V, Qr, Kr, Vr):
+        """The chunk's Q and K turned by ``rope`` and its V as it is, from any strided
+        views [n_heads][C*F][d] into contiguous Qr, Kr, Vr; frame f at frame_pos[f]."""
+        if self.rope is None:
+            raise ValueError("the stack has no rope")
+        fkv_rotate_chunk(self.shape(0), self.rope, frame_pos, Q, K, V, Qr, Kr, Vr)
+
+    def append(self, layer: int, K_new, V_new, dst_slots, frame_pos=None):
+        """Write a finished chunk's frames ([n_heads][n*F][d]) into the layer's cache
+        slots; with ``frame_pos`` (one position per frame) K_new is turned by ``rope``
+        on the way.  Strided views are taken with frame_pos or an 8-bit cache."""
+        if frame_pos is not None and self.rope is None:
+            raise ValueError("frame_pos needs the stack's rope")
+        rope = None if frame_pos is None else self.rope
+        if self.cache == "e4m3":
+            fkv_append_frames_q8(self.shape(0), rope, frame_pos, K_new, V_new, dst_slots, self.cache8[layer])
+        elif rope is not None:
+            fkv_append_frames_rotated(self.shape(0), rope, frame_pos, K_new, V_new, dst_slots, self.K_hist[layer],
+                                      self.V_hist[layer])
+        else:
+            fkv_append_frames(self.shape(0), K_new, V_new, dst_slots, self.K_hist[layer], self.V_hist[layer])
 
 
 class _Budget:
