@@ -767,19 +767,19 @@ def _cache8(shape: fkv_shape, c: Cache8, device: int):
 
 def _rows(t: torch.Tensor, name: str, dtype, size, device: int):
     """Rows [n_heads][n][d] of any head and token stride, the channels adjacent."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device and t.shape == size:
+        head, token, channel = t.stride()
+        if channel != 1:
+            raise ValueError(f"{name}: the channels of a row must be adjacent")
+        # (a dimension of one element may report any stride)
+        return fkv_rows(t.data_ptr(), head if size[0] > 1 else 0, token if size[1] > 1 else 0)
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if t.get_device() != device:
-        raise ValueError(f"{name} must be on cuda:{device} (got {t.device})")
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype} (got {t.dtype})")
-    if t.shape != size:
-        raise ValueError(f"{name} must have shape {size} (got {tuple(t.shape)})")
-    head, token, channel = t.stride()
-    if channel != 1:
-        raise ValueError(f"{name}: the channels of a row must be adjacent")
-    # (a dimension of one element may report any stride)
-    return fkv_rows(t.data_ptr(), head if size[0] > 1 else 0, token if size[1] > 1 else 0)
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on cuda:{device} (got {t.device})")
+    raise ValueError(f"{name} must have shape {size} (got {tuple(t.shape)})")
 
 
 def _ints(values, n: int, name: str):
@@ -787,7 +787,7 @@ def _ints(values, n: int, name: str):
     vals = values.tolist() if hasattr(values, "tolist") else values
     if len(vals) != n:
         raise ValueError(f"{name} needs {n} entries (got {len(vals)})")
-    return (ctypes.c_int32 * max(n, 1))(*map(int, vals))
+    return (ctypes.c_int32 * (n or 1))(*map(int, vals))
 
 
 def _frames(shape: fkv_shape, frame_slot):
@@ -796,11 +796,16 @@ def _frames(shape: fkv_shape, frame_slot):
 
 
 def _positions(frame_pos, n: int):
-    arr = _ints(frame_pos, n, "frame_pos")
     vals = frame_pos.tolist() if hasattr(frame_pos, "tolist") else frame_pos
-    if any(not -FKV_MAX_POSITION <= v <= FKV_MAX_POSITION for v in vals):
+    if len(vals) and not (-FKV_MAX_POSITION <= min(vals) and max(vals) <= FKV_MAX_POSITION):
         raise ValueError(f"frame_pos outside +-{FKV_MAX_POSITION}")
-    return arr
+    return _ints(vals, n, "frame_pos")
+
+
+def _n_seg(shape: fkv_shape) -> int:
+    """fkv_num_segments of a shape that the call itself checks."""
+    L = shape.seg_tokens
+    return -(-shape.hist_frames * shape.frame_tokens // L) if L > 0 else 0
 
 
 def _run(device: int, fn, args, stream):
@@ -876,7 +881,7 @@ def fkv_score_select_q8(shape: fkv_shape, heads, cache: Cache8, frame_slot, K_cu
                         workspace: Optional[torch.Tensor] = None, stream=None):
     """fkv_score_select over the keys of an 8-bit cache.  If ``workspace`` is
     None a zero-filled one is allocated (through torch's caching allocator)."""
-    n, n_seg, i32 = shape.n_heads, fkv_num_segments(shape), torch.int32
+    n, n_seg, i32 = shape.n_heads, _n_seg(shape), torch.int32
     dev = _device_of(K_cur, "K_cur")
     c = _cache8(shape, cache, dev)
     kc = _ptr(K_cur, "K_cur", _torch_dtype(shape), (n, _lq(shape), shape.head_dim), dev)
@@ -918,7 +923,7 @@ def fkv_chunk_attention_q8(shape: fkv_shape, heads, cache: Cache8, frame_slot, k
     ks = kl = kq = vq = ls = ws = None
     n_cur = nws = 0
     if kept_seg is not None:
-        ks = _ptr(kept_seg, "kept_seg", i32, (n, fkv_num_segments(shape)), dev)
+        ks = _ptr(kept_seg, "kept_seg", i32, (n, _n_seg(shape)), dev)
     if kv_len is not None:
         kl = _ptr(kv_len, "kv_len", i32, (n,), dev)
     if (K_cur is None) != (V_cur is None):
