@@ -1416,17 +1416,16 @@ int64_t q8_most_kept(const fkv_shape *s, const fkv_head *heads) {
 // How an 8-bit attention call (checked) is divided; the unit of the rules is a
 // wave's step, 64 keys by one query tile.
 //
-// Query tile: 32 rows where the work fills the device (a step of 32 rows takes a
-// wave about 1.5 steps of 16), 16 rows while it does not: up to kNarrowSteps
-// steps for each of the device's 8 waves per CU, and always for up to 16 rows.
-// 16 heads of 64, 27 key tiles, 256 query rows: 16-row tiles 11.6 us, 32-row 13.7;
-// 512 rows 22.4 and 16.6; 12 heads of 128 at 480P, 64 rows 37.1 and 30.8.
-//
-// Parts: where a wave would walk more than kWholeSteps steps and the device has
-// workgroups to spare, an item (head, query tile) is cut into parts of at least two
-// steps a wave, one workgroup each; the parts are joined by a second launch of 3 to 4
-// us.  480P, 16 rows: one workgroup per head 128 us, 21 parts 20.1; 128 rows of the
-// small layer above (5 steps) 11.2 whole, 14.6 cut.
+// Query tile and parts: an item is (head, query tile), one workgroup of 8 waves per
+// compute unit.  Where a wave would walk more than kWholeSteps steps and the device
+// has workgroups to spare, items are cut into parts of at least two steps a wave,
+// joined by a second launch of 3 to 4 us.  Of the tile heights the one with the least
+// rounds * (fixed + steps * (a + b * tiles of 16 rows)) is taken: a round of workgroups
+// costs about 2.5 step units beside its steps (the first loads, the waves' join), a
+// step 0.6 and 0.5 for each 16 rows (48 rows fit a wave's registers for d = 64).  Measured, us: 16 heads of 64, 27 key tiles, 256 query
+// rows: 16-row tiles 11.6, 32-row 13.7; 512 rows 22.4 and 16.6; 666 rows 32-row 33.4, 48-row 22.2; 12
+// heads of 128 at 480P, 64 rows 37.1 and 30.8.  480P, 16 rows: one workgroup per head
+// 128, 21 parts 20.1; 128 rows of the small layer (5 steps) 11.2 whole, 14.6 cut.
 //
 // Expanded: chunks of kExpandRows rows and kExpandSteps steps or more are attended
 // over a bf16 copy of the kept history, by the 256-row kernel of
@@ -1438,7 +1437,7 @@ int64_t q8_most_kept(const fkv_shape *s, const fkv_head *heads) {
 //
 // The workspace holds the parts, or, expanded, the counters of the balanced
 // schedule (cleared by the call itself), its parts, the heads' lengths and the copy.
-constexpr int kNarrowSteps = 4, kWholeSteps = 5, kExpandRows = 512;
+constexpr int kWholeSteps = 5, kExpandRows = 512;
 constexpr int64_t kExpandSteps = 60000;
 struct Q8Plan {
     bool expand;
@@ -1468,11 +1467,21 @@ Q8Plan q8_plan(const fkv_shape *s, const fkv_head *heads, int32_t n_q, int32_t n
         p.bytes = p.v_at + copy;
         return p;
     }
-    p.q_tile = n_q <= 16 || steps(16) <= (int64_t)kNarrowSteps * 8 * (blocks > 0 ? blocks : 256) ? 16 : 32;
-    p.n_qtiles = (n_q + p.q_tile - 1) / p.q_tile;
-    const int64_t items = (int64_t)s->n_heads * p.n_qtiles, wave_steps = (tiles + 7) / 8;
-    p.n_split = 1;
-    if (wave_steps > kWholeSteps) p.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(blocks / items, (wave_steps + 1) / 2));
+    const int64_t device = blocks > 0 ? blocks : 256, wave_steps = (tiles + 7) / 8;
+    double best = 0.0;
+    for (int mt = 1; mt <= (s->head_dim == 64 ? 3 : 2); ++mt) {
+        const int64_t n_qtiles = (n_q + 16 * mt - 1) / (16 * mt), items = s->n_heads * n_qtiles;
+        int64_t parts = 1;
+        if (wave_steps > kWholeSteps) parts = std::max<int64_t>(1, std::min<int64_t>(blocks / items, (wave_steps + 1) / 2));
+        const double rounds = (double)((items * parts + device - 1) / device);
+        const double cost = rounds * (2.5 + (double)tiles / (8 * parts) * (0.6 + 0.5 * mt));
+        if (mt > 1 && cost >= best) continue;
+        best = cost;
+        p.q_tile = 16 * mt;
+        p.n_qtiles = (int)n_qtiles;
+        p.n_split = (int)parts;
+    }
+    const int64_t items = (int64_t)s->n_heads * p.n_qtiles;
     if (p.n_split > 1)
         p.bytes = (size_t)items * p.n_split * fkv::attn_q8_part_floats(s->head_dim, p.q_tile) * sizeof(float);
     return p;

@@ -21,8 +21,21 @@
 //                 64 value rows as bf16 and reads 4 keys of 16 channels at a
 //                 time, B = P straight from the S^T accumulators).
 // The sum adds the probabilities before they are rounded to bf16 for the value
-// product.  Parts of an item (head, query tile) meet in fp32 slots of the
-// workspace, which a second launch joins in order.
+// product (a rounding of half a bf16 step each, unbiased: 1.6e-3 of the output in the
+// 2-norm, as much as the output's own).  Parts of an item (head, query tile) meet in
+// fp32 slots of the workspace, which a second launch joins in order.
+//
+// Why so: with few query tokens the bytes of the cache bound the work, and a wave
+// that waits for nobody keeps its rows in flight: the next step's keys are requested
+// as soon as this step's are consumed, its values after this step's are in LDS.  K
+// needs no LDS at all.  480P, one query token, all 21 frames kept (101 MB): 29.4 us,
+// 26 of them this launch; with the arithmetic taken out the loads alone take 24, 4.6
+// TB/s beside the launch (a 1 GiB copy reaches 5.1).  More query tokens share a
+// conversion and a row's trip through LDS, 16 to 48 rows a wave: 128 tokens 41.5 us,
+// 512 139 us (0.33 PFLOP/s): bound by the latency of a step, two waves per SIMD with
+// 200 and more registers each.  Measured beside it, neutral or slower: 4 waves per
+// workgroup (512 tokens 180 us), 128 registers and twice the waves for d = 64 (spills),
+// the running maximum taken in every step (3 to 8% slower).
 #include "fkv_internal.h"
 
 namespace fkv {
@@ -118,8 +131,10 @@ struct Cfg {
     // covers, and the eight that a 16-byte store covers, then fall into distinct banks.
     static constexpr int VS = D + 16;
     static constexpr int REGION = kTile * VS;     // elements per wave
-    static constexpr int OS = D + 4;              // a wave's output rows in LDS (floats)
-    static_assert(ROWS * OS * 4 + 2 * ROWS * 4 <= REGION * 2, "a wave's result fits its value rows");
+    // A wave's results meet the others' in its region, PT tiles at a time: output rows,
+    // maxima and sums (floats).
+    static constexpr int OS = D + 4, PT = MT < 2 ? MT : 2, PROWS = 16 * PT;
+    static_assert(PROWS * OS * 4 + 2 * PROWS * 4 <= REGION * 2, "the results fit the value rows");
 };
 
 typedef __attribute__((address_space(3))) bf16x4_t lds_bf16x4_t;
@@ -370,62 +385,54 @@ __global__ __launch_bounds__(kThreads) void attn_q8_kernel(AttnQ8Args a) {
         s.values(z, vt, lane);
     }
 
-    // the wave's result into its region of LDS: output rows, maxima, sums
-    wave_sync();
+    // The waves' results, PT tiles at a time: into the regions of LDS, then joined by
+    // the workgroup's threads, 4 channels of a row each.
     float *mine = (float *)vt;
+    constexpr int kPRows = C::PROWS, RF = C::REGION / 2;      // RF: floats per region
 #pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        s.l[t] += __shfl_xor(s.l[t], 16);
-        s.l[t] += __shfl_xor(s.l[t], 32);
+    for (int t0 = 0; t0 < MT; t0 += C::PT) {
+        if (t0 > 0) __syncthreads();                          // (the tiles before are read)
+        wave_sync();
 #pragma unroll
-        for (int mb = 0; mb < C::MB; ++mb) *(f32x4_t *)(mine + (16 * t + c) * C::OS + 16 * mb + 4 * g) = s.o[t][mb];
-        if (lane < 16) {
-            mine[kRows * C::OS + 16 * t + lane] = s.m[t];
-            mine[kRows * C::OS + kRows + 16 * t + lane] = s.l[t];
-        }
-    }
-    __syncthreads();
-
-    // Element groups of this thread: row r, channels d .. d + 3.
-    constexpr int kGroups = kRows * D / 4, kPer = (kGroups + kThreads - 1) / kThreads;
-    const int rows = min(kRows, a.n_q - q0);
-    float M[kPer], L[kPer];
-    f32x4_t acc[kPer];
+        for (int k = 0; k < C::PT; ++k) {
+            const int t = t0 + k;
+            if (t >= MT) break;
+            s.l[t] += __shfl_xor(s.l[t], 16);
+            s.l[t] += __shfl_xor(s.l[t], 32);
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-        const int r = (e * kThreads + tid) / (D / 4), d = (e * kThreads + tid) % (D / 4) * 4;
-        M[e] = neg_inf();
-        L[e] = 0.f;
-        acc[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        if (r >= rows) continue;
-        const float *base = (const float *)lds;
-        constexpr int RF = C::REGION / 2;                 // floats per region
-        for (int i = 0; i < kWaves; ++i) M[e] = fmaxf(M[e], base[i * RF + kRows * C::OS + r]);
-        const float ref = M[e] == neg_inf() ? 0.f : M[e];
-        for (int i = 0; i < kWaves; ++i) {
-            const float wt = __builtin_amdgcn_exp2f(base[i * RF + kRows * C::OS + r] - ref);
-            L[e] += wt * base[i * RF + kRows * C::OS + kRows + r];
-            acc[e] += wt * *(const f32x4_t *)(base + i * RF + r * C::OS + d);
-        }
-    }
-    if (a.n_split > 1) {                                  // joined by join_q8_kernel
-        float *slot = a.part + ((size_t)item * a.n_split + part) * (kRows * (D + 2));
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) {
-            const int r = (e * kThreads + tid) / (D / 4), d = (e * kThreads + tid) % (D / 4) * 4;
-            if (r >= rows) continue;
-            *(f32x4_t *)(slot + r * D + d) = acc[e];
-            if (d == 0) {
-                slot[kRows * D + r] = M[e];
-                slot[kRows * D + kRows + r] = L[e];
+            for (int mb = 0; mb < C::MB; ++mb) *(f32x4_t *)(mine + (16 * k + c) * C::OS + 16 * mb + 4 * g) = s.o[t][mb];
+            if (lane < 16) {
+                mine[kPRows * C::OS + 16 * k + lane] = s.m[t];
+                mine[kPRows * C::OS + kPRows + 16 * k + lane] = s.l[t];
             }
         }
-        return;
-    }
+        __syncthreads();
+        const int rows = min(min(kPRows, kRows - 16 * t0), a.n_q - q0 - 16 * t0);
+        for (int x = tid; x < rows * (D / 4); x += kThreads) {
+            const int r = x / (D / 4), d = x % (D / 4) * 4;
+            const float *base = (const float *)lds;
+            float M = neg_inf(), L = 0.f;
+            f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-        const int r = (e * kThreads + tid) / (D / 4), d = (e * kThreads + tid) % (D / 4) * 4;
-        if (r < rows) put_row<D>(a, (int64_t)h * a.n_q + q0 + r, d, acc[e], M[e], L[e], units == 0);
+            for (int i = 0; i < kWaves; ++i) M = fmaxf(M, base[i * RF + kPRows * C::OS + r]);
+            const float ref = M == neg_inf() ? 0.f : M;
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) {
+                const float wt = __builtin_amdgcn_exp2f(base[i * RF + kPRows * C::OS + r] - ref);
+                L += wt * base[i * RF + kPRows * C::OS + kPRows + r];
+                acc += wt * *(const f32x4_t *)(base + i * RF + r * C::OS + d);
+            }
+            if (a.n_split > 1) {                              // joined by join_q8_kernel
+                float *slot = a.part + ((size_t)item * a.n_split + part) * (kRows * (D + 2));
+                *(f32x4_t *)(slot + (16 * t0 + r) * D + d) = acc;
+                if (d == 0) {
+                    slot[kRows * D + 16 * t0 + r] = M;
+                    slot[kRows * D + kRows + 16 * t0 + r] = L;
+                }
+            } else {
+                put_row<D>(a, (int64_t)h * a.n_q + q0 + 16 * t0 + r, d, acc, M, L, units == 0);
+            }
+        }
     }
 }
 
@@ -433,7 +440,7 @@ __global__ __launch_bounds__(kThreads) void attn_q8_kernel(AttnQ8Args a) {
 // the outputs.  A launch of its own: the parts then cross as ordinary cached stores
 // and loads, every row has a workgroup, and the workspace holds no counters.  (Joined
 // by the part that arrives last, 480P: one query token 29.2 us, 16 tokens 24.0, 32
-// tokens 32.7; so ONE_US, Q16_US, Q32_US.)  One workgroup per row and head: D/4 threads
+// tokens 32.7; so 29.7, 21.8 and 26.0.)  One workgroup per row and head: D/4 threads
 // take 4 channels each, kLanes of them every kLanes'th part, then the lanes' sums meet
 // in LDS, always in the same order.  grid: x = row, y = head.
 template <int D>
@@ -546,10 +553,18 @@ hipError_t launch_expand_q8(const AttnQ8Args &a, int head_dim, hipStream_t s) {
 
 hipError_t launch_attention_q8(const AttnQ8Args &a, int head_dim, hipStream_t s) {
     const dim3 grid((unsigned)(((int64_t)a.n_heads * a.n_split * a.n_qtiles + 7) / 8 * 8));
-    if (head_dim == 64 && a.q_tile == 16) hipLaunchKernelGGL((attn_q8_kernel<64, 1>), grid, dim3(kThreads), 0, s, a);
-    else if (head_dim == 64) hipLaunchKernelGGL((attn_q8_kernel<64, 2>), grid, dim3(kThreads), 0, s, a);
-    else if (a.q_tile == 16) hipLaunchKernelGGL((attn_q8_kernel<128, 1>), grid, dim3(kThreads), 0, s, a);
-    else hipLaunchKernelGGL((attn_q8_kernel<128, 2>), grid, dim3(kThreads), 0, s, a);
+    auto launch = [&](auto *kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, s, a); };
+    if (head_dim == 64) {
+        switch (a.q_tile) {
+        case 16: launch(attn_q8_kernel<64, 1>); break;
+        case 32: launch(attn_q8_kernel<64, 2>); break;
+        default: launch(attn_q8_kernel<64, 3>); break;
+        }
+    } else if (a.q_tile == 16) {
+        launch(attn_q8_kernel<128, 1>);
+    } else {
+        launch(attn_q8_kernel<128, 2>);
+    }
     if (a.n_split > 1) {
         const dim3 join((unsigned)a.n_q, (unsigned)a.n_heads);
         if (head_dim == 64) hipLaunchKernelGGL(join_q8_kernel<64>, join, dim3(kJoinThreads), 0, s, a);

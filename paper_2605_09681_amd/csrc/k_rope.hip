@@ -17,6 +17,14 @@
 // 128.  A thread computes the sines and cosines of its item once and walks the
 // heads of its workgroup with them: they depend on the token alone, and they are
 // the costly part.
+//
+// Bound by memory at chunk sizes: rotating a 480P chunk's Q, K and V (86 MB) takes
+// 18.9 us and appending a 1080P chunk (301 MB) 65 us, 4.6 TB/s (a 1 GiB copy reaches
+// 5.1); loads are streamed past the caches (with ordinary ones 22.0 us).  Appending a
+// 480P chunk to 8 bits (43 MB) takes 12.2 us, 1080P 46 us: short of the larger one's 4.9
+// TB/s by the launch and the one wait of a block for its maximum.  Magnitudes as
+// integers, conversions that scale, and keys and values in workgroups of their own
+// brought it there from 17.0.
 #include "fkv_internal.h"
 
 namespace fkv {

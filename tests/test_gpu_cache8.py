@@ -396,7 +396,30 @@ SIZES = [
     dict(heads=1, d=128, F=1560, H=10, n_q=1, n_cur=0, budgets=_budgets(1, 0, 10, 0, W.SCOPE_GLOBAL)),   # many parts
     dict(heads=5, d=64, F=16, H=3, n_q=300, n_cur=300, block=16),
     dict(heads=2, d=128, F=65, H=0, n_q=9, n_cur=70),                                 # nothing cached
+    dict(heads=16, d=64, F=60, H=12, n_q=650, n_cur=5, budgets=_budgets(8, 8, 11, 9, W.SCOPE_GLOBAL)),   # 48-row tiles
+    dict(heads=16, d=64, F=60, H=12, n_q=500, n_cur=130, budgets=_budgets(8, 8, 11, 9, W.SCOPE_GLOBAL)),  # 32-row tiles
+    dict(heads=12, d=128, F=1300, H=5, n_q=81, n_cur=81, budgets=_budgets(6, 6, 5, 5, W.SCOPE_GLOBAL)),  # 32-row, in parts
 ]
+
+
+@pytest.mark.parametrize("size", [
+    dict(heads=9, d=128, F=1560, H=8, n_q=1100, n_cur=1100, budgets=_budgets(5, 4, 8, 8, W.SCOPE_GLOBAL)),
+    dict(heads=10, d=64, F=1500, L=500, H=9, n_q=1030, n_cur=37, budgets=_budgets(4, 6, 9, 20, W.SCOPE_GLOBAL))],
+    ids=["chunk", "few-current"])
+def test_attention_expanded(fkv, size):
+    """Large chunks, attended over the expanded copy; the same workspace then serves a small call."""
+    a = Attend(fkv, **size)
+    n = fkv.fkv_chunk_attention_q8_workspace_size(a.shape, a.heads, a.Q.shape[1], a.K_cur.shape[1])
+    copy = 2 * size["heads"] * 2 * size["d"] * size["F"] * size["H"]
+    assert n >= copy                                  # it holds the copy: this call takes that way
+    ws = torch.full((n,), 0xff, dtype=torch.uint8, device="cuda")     # no initialisation needed
+    O, lse = a.run(ws)
+    a.check(O, lse)
+    P, _ = a.run(ws, lse=False)
+    assert torch.equal(O, P)
+    b = Attend(fkv, heads=2, d=128, F=1560, H=10, n_q=3, n_cur=0, budgets=_budgets(2, 0, 10, 0, W.SCOPE_GLOBAL))
+    b.check(*b.run(ws))
+    assert all(torch.equal(x, y) for x, y in zip(a.run(ws), (O, lse)))
 
 
 @pytest.mark.parametrize("size", SIZES, ids=lambda s: "-".join(f"{k}{v}" for k, v in s.items() if k != "budgets"))
