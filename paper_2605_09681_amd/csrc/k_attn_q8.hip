@@ -496,7 +496,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_q8_kernel(AttnQ8Args a) {
 // Large chunks: the kept history as a bf16 copy [n_heads][slab][d] for the chunk
 // attention's kernel.  A workgroup widens kExpandRows rows of K and V; 16 bytes
 // of codes per thread and row.  grid: x = row group, y = head.
-constexpr int kExpandThreads = 256, kExpandRows = 128;
+constexpr int kExpandThreads = 256, kExpandRows = 64;
 template <int D>
 __global__ __launch_bounds__(kExpandThreads) void expand_q8_kernel(AttnQ8Args a) {
     constexpr int TPR = D / 16, RPP = kExpandThreads / TPR, N = kExpandRows / RPP;   // threads per row, rows per pass
