@@ -1442,7 +1442,7 @@ constexpr int64_t kExpandSteps = 60000;
 struct Q8Plan {
     bool expand;
     int q_tile, n_qtiles, n_split, blocks;
-    int64_t slab;
+    int64_t slab;                                 // expanded: rows per head of the copy
     int64_t n_counters;                           // expanded: counters to clear
     size_t part_at, len_at, k_at, v_at, bytes;    // byte offsets in the workspace
 };
@@ -1452,8 +1452,12 @@ Q8Plan q8_plan(const fkv_shape *s, const fkv_head *heads, int32_t n_q, int32_t n
     Q8Plan p;
     memset(&p, 0, sizeof p);
     p.blocks = blocks;
-    p.slab = q8_most_kept(s, heads);
-    const int64_t tiles = (p.slab + 63) / 64 + ((int64_t)n_cur + 63) / 64;
+    const int64_t kept = q8_most_kept(s, heads);
+    // a dynamic head attends whatever kv_len says, up to its whole history, whatever its budget
+    p.slab = kept;
+    for (int h = 0; h < s->n_heads; ++h)
+        if (heads[h].type == FKV_DYNAMIC) p.slab = (int64_t)s->hist_frames * s->frame_tokens;
+    const int64_t tiles = (kept + 63) / 64 + ((int64_t)n_cur + 63) / 64;
     auto steps = [&](int tile) { return (int64_t)s->n_heads * ((n_q + tile - 1) / tile) * tiles; };
     p.expand = blocks > 0 && n_cur > 0 && n_q >= kExpandRows && steps(32) >= kExpandSteps;
     if (p.expand) {

@@ -502,6 +502,23 @@ def test_attention_bad_lists_stay_inside(fkv):
     a.check(O, lse)
 
 
+def test_attention_expanded_bad_lists_stay_inside(fkv):
+    """The same of a large chunk: the expanded copy has room for every token that kv_len may claim (the whole history,
+    beyond the budgets), and the heads beside the lying one are right."""
+    a = Attend(fkv, heads=10, d=64, F=700, H=12, n_q=1600, n_cur=1600, budgets=_budgets(9, 1, 11, 1, W.SCOPE_GLOBAL))
+    n = fkv.fkv_chunk_attention_q8_workspace_size(a.shape, a.heads, 1600, 1600)
+    assert n >= 2 * 2 * 64 * 10 * 12 * 700
+    ws = torch.zeros(n + (1 << 16), dtype=torch.uint8, device="cuda")
+    a.kept[9], a.kv_len[9] = np.arange(12), 12 * 700                  # more than its budget keeps: attended as it says
+    O, lse = a.run(ws[:n])
+    a.check(O, lse)
+    a.kept[9], a.kv_len[9] = 2 ** 31 - 1, 2 ** 31 - 1
+    O, lse = a.run(ws[:n])
+    a.kept[9], a.kv_len[9] = 11, 12 * 700                             # clamped: the last segment over and over
+    a.check(O, lse)     # (to the bounds: the parts are cut by every head's length, so other heads' last bits move too)
+    assert not bool(ws[n:].any())
+
+
 def test_attention_repeats_and_shares_a_workspace(fkv):
     """The same bits on every run; one workspace serves calls of other sizes in turn."""
     a = Attend(fkv, heads=2, d=128, F=300, H=6, n_q=3, n_cur=3, budgets=_budgets(1, 1, 5, 5, W.SCOPE_GLOBAL))
