@@ -621,7 +621,7 @@ fkv_status fkv_score_select_q8(const fkv_shape *shape, const fkv_head *heads,
  * L that fkv_shape allows; n_q and n_cur need not be the chunk's C*F.  A head
  * without any key (nothing kept, n_cur = 0) gets O = 0 and lse = -infinity.
  * bf16 only (FKV_ERR_SHAPE for FKV_F32; also n_q or n_cur rows of 2^31 bytes
- * or more).  Products are bf16 with fp32 accumulation: codes times scales are
+ * or more, and 2^22 or more query tiles of all heads).  Products are bf16 with fp32 accumulation: codes times scales are
  * exact, probabilities are rounded to bf16 for the value product.
  *
  * With a workspace of at least fkv_chunk_attention_q8_workspace_size bytes

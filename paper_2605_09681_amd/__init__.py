@@ -889,7 +889,8 @@ def fkv_score_select_q8(shape: fkv_shape, heads, cache: Cache8, frame_slot, K_cu
     ks, kl = _ptr(kept_seg, "kept_seg", i32, (n, n_seg), dev), _ptr(kv_len, "kv_len", i32, (n,), dev)
     if workspace is None:
         need = fkv_score_workspace_size(shape, heads)
-        workspace = torch.zeros(max(need, 1), dtype=torch.uint8, device=K_cur.device)
+        with torch.cuda.stream(stream):               # (filled on the stream that uses it)
+            workspace = torch.zeros(max(need, 1), dtype=torch.uint8, device=K_cur.device)
     ws = _ptr(workspace, "workspace", torch.uint8, getattr(workspace, "shape", None), dev)
     _run(dev, lib().fkv_score_select_q8,
          (ctypes.byref(shape), _heads(shape, heads), ctypes.byref(c), _frames(shape, frame_slot),

@@ -1620,6 +1620,7 @@ fkv_status fkv_score_select_q8(const fkv_shape *shape, const fkv_head *heads, co
         return select_impl(shape, heads, nullptr, false, kept_seg, kv_len, stream, "fkv_score_select_q8 launch");
     if ((st = check_cache8(cache, false)) != FKV_OK) return st;
     if (!K_cur || !scores || !kept_seg) return fail(FKV_ERR_ARG, "NULL tensor pointer");
+    if (!aligned16(K_cur)) return fail(FKV_ERR_ARG, "K_cur is not 16-byte aligned");
     if (!workspace) return fail(FKV_ERR_ARG, "workspace is NULL");
     if (workspace_bytes < need)
         return fail(FKV_ERR_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
@@ -1659,12 +1660,17 @@ fkv_status fkv_chunk_attention_q8(const fkv_shape *shape, const fkv_head *heads,
                 return fail(FKV_ERR_ARG, "kept_seg or kv_len is NULL with a dynamic head");
     }
     if (!Q || !O || (n_cur > 0 && (!K_cur || !V_cur))) return fail(FKV_ERR_ARG, "NULL tensor pointer");
+    if (!aligned16(Q) || !aligned16(O) || !aligned16(K_cur) || !aligned16(V_cur) || !aligned16(workspace))
+        return fail(FKV_ERR_ARG, "Q, O, K_cur, V_cur or the workspace is not 16-byte aligned");
     if (!(scale > 0.f) || !isfinite(scale)) return fail(FKV_ERR_ARG, "scale %g must be positive and finite", (double)scale);
     int blocks = 0;
     if (workspace && (st = balanced_blocks(&blocks)) != FKV_OK) return st;
     const Q8Plan p = q8_plan(shape, heads, n_q, n_cur, blocks);
     if (workspace && workspace_bytes < p.bytes)
         return fail(FKV_ERR_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, p.bytes);
+    // (a launch holds fewer than 2^32 threads, 512 in a workgroup)
+    if (!p.expand && (int64_t)shape->n_heads * p.n_qtiles * p.n_split >= (int64_t)1 << 22)
+        return fail(FKV_ERR_SHAPE, "%d heads of %d query tokens are too many for one call", shape->n_heads, n_q);
 
     fkv::AttnQ8Args a;
     memset(&a, 0, sizeof a);

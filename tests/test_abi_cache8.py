@@ -144,6 +144,7 @@ def test_score_arguments(fkv):
     assert _score(fkv, slots=(0, 1, 2, 4)) == 1
     for name in ("K", "scores", "kept", "kv", "ws"):
         assert _score(fkv, **{name: None}) == 1, name
+    assert _score(fkv, K=FAKE + 8) == 1
     assert _score(fkv, short=1) == 3
 
 
@@ -165,8 +166,13 @@ def test_attention_arguments(fkv):
     assert _attend(fkv, slots=None) == 1 and _attend(fkv, slots=(0, 1, 2, 7)) == 1
     for name in ("kept", "kv", "Q", "K", "O"):
         assert _attend(fkv, **{name: None}) == 1, name
+    for name in ("Q", "K", "O"):
+        assert _attend(fkv, **{name: FAKE + 8}) == 1, name
     for scale in (0.0, -1.0, math.inf, math.nan):
         assert _attend(fkv, scale=scale) == 1, scale
+    many = fkv.make_shape(64, 64, 64, 4, 4, 1, 64, "bf16")     # more query tiles than one launch holds
+    heads = fkv.make_heads([W.HeadBudget(W.STATIC, 1, 1)] * 64)
+    assert _attend(fkv, shape=many, heads=heads, n_q=1 << 22, K=None, n_cur=0) == 2
     bad = fkv.make_heads((W.HeadBudget(W.STATIC, -1, 1), W.HeadBudget(W.DYNAMIC, 0, 0, 2)))
     assert _attend(fkv, heads=bad) == 1
     size = ctypes.c_size_t(0)

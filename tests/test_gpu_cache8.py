@@ -194,6 +194,32 @@ def test_append_q8_not_finite(fkv):
         assert torch.equal(c.view(torch.uint8)[~bad], want.reshape(x.shape).view(torch.uint8)[~bad])
 
 
+@pytest.mark.parametrize("halves", [False, True])
+def test_append_q8_rotated_not_finite(fkv, halves):
+    """A rotated pair with an infinity or a NaN becomes NaN, both channels; everything else as without it."""
+    rope = Rope(32, 16, 16, row_tokens=8, halves=halves)
+    shape = _shape(fkv, 1, 128, 40, 0, 2, 1)
+    x = torch.randn((1, 40, 128), generator=_gen(8)).to(torch.bfloat16)
+    y = x.clone()
+    hit = torch.zeros(x.shape, dtype=torch.bool)
+    for tok, ch, v in ((2, 6, math.inf), (20, 40, math.nan), (39, 63, -math.inf)):
+        y[0, tok, ch] = v
+        pair = [ch, ch + 64] if halves else [ch & ~1, ch | 1]
+        for c in pair:
+            x[0, tok, c] = 0                     # (a pair of zeros: no part in the block's scale)
+            hit[0, tok, c] = True
+            if c != ch:
+                y[0, tok, c] = 1
+    caches = []
+    for t in (x, y):
+        caches.append(fkv.Cache8.zeros(shape, 16))
+        fkv.fkv_append_frames_q8(shape, rope.make(fkv), [5], t.cuda(), t.cuda(), [1], caches[-1])
+    a, b = (c.K.cpu()[:, 1] for c in caches)
+    assert torch.equal(caches[0].k_scale, caches[1].k_scale)
+    assert torch.equal(a.view(torch.uint8)[~hit], b.view(torch.uint8)[~hit])
+    assert bool(torch.isnan(b.float()[hit]).all())
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("name", ["video", "sequence", "partial"])
 @pytest.mark.parametrize("d,F,block", [(128, 70, 32), (64, 129, 128), (128, 1, 16)])
