@@ -218,10 +218,13 @@ __device__ void group_sum(const ScoreArgs &a, int li, int g) {
         double acc = 0.0;
         for (int k0 = j; k0 < nm; k0 += 4 * 8) {
             double v[8];
+            // a place beyond the last member reads the last one again: a load that
+            // every lane makes needs no branch, so the eight are in flight together
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int k = k0 + 4 * i;
-                v[i] = k < nm ? get_shared(p + (int64_t)(c0 + k * kGroups) * blk) : 0.0;
+                const double x = get_shared(p + (int64_t)(c0 + min(k, nm - 1) * kGroups) * blk);
+                v[i] = k < nm ? x : 0.0;
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) acc += v[i];
@@ -249,6 +252,8 @@ __device__ void finish_head(const ScoreArgs &a, int li, double *T, uint64_t *s_k
     // groups 0 .. min(n_wg, kGroups) - 1 have members and wrote every row; the
     // others were not written by this call
     const int n_groups = DIRECT ? kGroups : min(a.units * a.n_cg, kGroups);
+    // (clamped, as above: with a branch per load the wait for this memory is paid
+    // in turn; scoring of 480p 17.1 -> 16.7 us, of the small grid 9.8 -> 9.2 us)
     for (int r = tid; r < n_rows; r += kThreads) {
         double v[kGroups];
         if constexpr (DIRECT) {
@@ -257,11 +262,15 @@ __device__ void finish_head(const ScoreArgs &a, int li, double *T, uint64_t *s_k
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
                 const int c = (g - c0 + kGroups) % kGroups;   // the unit's member of group g
-                v[g] = c < a.n_cg ? get_shared(p + (int64_t)c * blk) : 0.0;
+                const double x = get_shared(p + (int64_t)min(c, a.n_cg - 1) * blk);
+                v[g] = c < a.n_cg ? x : 0.0;
             }
         } else {
 #pragma unroll
-            for (int g = 0; g < kGroups; ++g) v[g] = g < n_groups ? get_shared(G + (int64_t)g * n_rows + r) : 0.0;
+            for (int g = 0; g < kGroups; ++g) {
+                const double x = get_shared(G + (int64_t)min(g, n_groups - 1) * n_rows + r);
+                v[g] = g < n_groups ? x : 0.0;
+            }
         }
         double acc = 0.0;
 #pragma unroll
