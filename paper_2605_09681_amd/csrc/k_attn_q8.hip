@@ -35,7 +35,8 @@
 // 512 139 us (0.33 PFLOP/s): bound by the latency of a step, two waves per SIMD with
 // 200 and more registers each.  Measured beside it, neutral or slower: 4 waves per
 // workgroup (512 tokens 180 us), 128 registers and twice the waves for d = 64 (spills),
-// the running maximum taken in every step (3 to 8% slower).
+// the running maximum taken in every step (3 to 8% slower), 12 waves per workgroup for
+// d = 64 (168 registers spill: 666 tokens of 16 heads 21 to 55 us; one token 11.1 to 10.8).
 #include "fkv_internal.h"
 
 namespace fkv {
