@@ -36,9 +36,12 @@
 // nothing in a wave waits for a row maximum: the exponentials' reference is the
 // row maximum of the segment's first tile.  Probabilities may then exceed one,
 // in bf16 and fp32 by 2^100 and more without loss (their relative rounding is
-// the same); a segment in which a sum passes 2^100 or an output is not finite is
+// the same); a segment in which a sum passes 2^100, or falls below 2^-100 though
+// its row has scores, or an output is not finite is
 // computed again with a running maximum (it moves where a tile's exceeds it by
-// more than 8 in log2 units).  That costs the segment twice and more, and a NaN
+// more than 8 in log2 units; far_shift: rows whose every score lies beyond 2^31 of
+// them -- keys of -1e30 throughout, say -- for which the 480P launch went from 485.0
+// to 486.0 us, both kernels in turn).  That costs the segment twice and more, and a NaN
 // or an infinity in Q or V always brings it about: 480P step 509 us, 967 with one
 // NaN in one static head's V, 1086 with one in every head's.
 // Bound: at 1080P the clock, which the power of the products holds at 1.73-1.85
@@ -515,8 +518,12 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, uint16_t *Ks, ui
     };
 
     f32x16_t o[C::MB];
-    float m_run, l_run;   // reference of the exponentials (log2 units); this lane's share of the running sum
-    const float c2 = a.scale_log2;
+    float m_run, l_run;   // reference of the exponentials; this lane's share of the running sum
+    // A score in the units of m_run is score * c2: log2 units, or 2^-k of them in a
+    // row of far scores (far_shift below).
+    float c2;
+    const int c2_exp = __builtin_amdgcn_frexp_expf(a.scale_log2);
+    auto shift_of = [&]() { return c2_exp - __builtin_amdgcn_frexp_expf(c2); };   // k
 
     bool every = false;   // take every tile's row maximum
     for (;;) {
@@ -524,6 +531,7 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, uint16_t *Ks, ui
         for (int mb = 0; mb < C::MB; ++mb) o[mb] = f32x16_t{};
         m_run = -__builtin_inff();
         l_run = 0.f;
+        c2 = a.scale_log2;
         f32x16_t s[2];
         bf16x8_t pb[4];
         bf16x8_t fr[kPrefetch];
@@ -614,21 +622,28 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, uint16_t *Ks, ui
             else l_run = __builtin_amdgcn_fdot2_f32_bf16(pr, kOnes2, l_run, false);
         };
         int it = 0;
-        // Row maximum of the tile whose scores s holds, in log2 units.
+        // Row maximum of the tile whose scores s holds.
         auto row_max = [&](const f32x16_t &s0, const f32x16_t &s1) {
             float mx = fmaxf(s0[0], s0[1]);
 #pragma unroll
             for (int i = 2; i < 16; ++i) mx = fmaxf(mx, s0[i]);
 #pragma unroll
             for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s1[i]);
-            return fmaxf(mx, __shfl_xor(mx, 32)) * c2;
+            return fmaxf(mx, __shfl_xor(mx, 32));
         };
-        // A finite reference above every score of a row maximum mx: the rounding of a
-        // score times c2 passes the exponent by half a step, which overflows it where
-        // a step of mx is large (scores of -1e30).
-        auto above = [](float mx) {
-            mx = fmaxf(mx, -kLowest);
-            return mx <= kLowest ? fminf(fmaf(fabsf(mx), 0x1p-23f, mx), kLowest) : mx;
+        // Far scores.  m_run rounds the maximum times c2, and the exponent keeps the
+        // difference, up to half a step of m_run: within 2^6 below 2^31 log2 units, but
+        // beyond them past what an exponent holds.  There both are taken 2^k times
+        // smaller: the step stays within 2^6, and scores that differ at all, by 2^-24 of
+        // their size, still differ by 2^5 units, so that a lower one weighs nothing, as
+        // it should.  k for a row maximum mx:
+        auto far_shift = [&](float mx) { return max(0, __builtin_amdgcn_frexp_expf(mx) + c2_exp - 31); };
+        // The finite reference for a row maximum mx in the units of c: a step above it
+        // (where a step is less than a unit), so that none of its tile's probabilities
+        // passes one.
+        auto above = [](float mx, float c) {
+            const float x = fmaxf(mx * c, -kLowest);
+            return fabsf(x) < 0x1p24f ? fmaf(fabsf(x), 0x1p-23f, x) : x;
         };
         // Pair of probabilities formed in step x: those of key block 0 from its
         // second step after run A on, those of key block 1 from the second after run
@@ -693,8 +708,14 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, uint16_t *Ks, ui
         }
         // A row whose scores here are all -inf takes the lowest finite reference: its
         // keys weigh nothing, and the first other ones overflow its sum.
-        m_run = row_max(s[0], s[1]);
-        m_run = every ? above(m_run) : fmaxf(m_run, -kLowest);
+        const float first = row_max(s[0], s[1]);
+        const uint64_t scored = __ballot(first > -__builtin_inff());
+        if (every) {
+            c2 = __builtin_amdgcn_ldexpf(c2, -far_shift(first));
+            m_run = above(first, c2);
+        } else {
+            m_run = fmaxf(first * c2, -kLowest);
+        }
         set_m();
 #pragma unroll
         for (int p = 0; p < kLate; ++p) {
@@ -723,11 +744,16 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, uint16_t *Ks, ui
                 for (int kk = 0; kk < C::KS; ++kk)
                     s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read_a(xC + kk, it), qf[kk],
                                                                    kk == 0 ? f32x16_t{} : s[0], 0, 0, 0);
-                mx = above(fmaxf(mx, row_max(s[0], s[0])));
-                if (__ballot(mx > m_run + kRescaleSlack)) {
-                    const bool move = mx > m_run + kRescaleSlack, far = move && mx - m_run > kFarMove;
-                    const float up = far ? mx - m_run : move ? ceilf(mx - m_run) : 0.f;
-                    const float alpha = __builtin_amdgcn_exp2f(-up);
+                mx = fmaxf(mx, row_max(s[0], s[0]));
+                const bool move = above(mx, c2) > m_run + kRescaleSlack;
+                if (__ballot(move)) {
+                    // (a row of far scores takes the units of its new maximum with it)
+                    const int k0 = shift_of(), k = move ? far_shift(mx) : k0;
+                    const float c = __builtin_amdgcn_ldexpf(a.scale_log2, -k), m = above(mx, c);
+                    const float rise = m - __builtin_amdgcn_ldexpf(m_run, k0 - k);
+                    const bool far = move && (rise > kFarMove || (k0 | k) != 0);
+                    const float up = far ? rise : move ? ceilf(rise) : 0.f;
+                    const float alpha = __builtin_amdgcn_exp2f(-__builtin_amdgcn_ldexpf(up, k));
                     l_run *= alpha;
                     l2 *= alpha;
 #pragma unroll
@@ -739,7 +765,8 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, uint16_t *Ks, ui
                         e1 *= alpha;
                         round_pair(p);
                     }
-                    m_run = far ? mx : m_run + up;
+                    m_run = far ? m : m_run + up;
+                    c2 = c;
                 }
             }
             set_m();
@@ -776,13 +803,16 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, uint16_t *Ks, ui
             __syncthreads();
             break;
         }
-        // redo?
+        // redo?  (Also a row whose sum is next to nothing though it has scores: far
+        // ones, whose reference is not theirs by half a step of it.)
         float z = 0.f;
 #pragma unroll
         for (int mb = 0; mb < C::MB; ++mb)
 #pragma unroll
             for (int i = 0; i < 16; ++i) z = fmaf(o[mb][i], 0.f, z);
-        if (__ballot(qok && !(l_run <= kSumLimit && z == 0.f)) && lane == 0) *redo = 1;
+        const float sum = l_run + __shfl_xor(l_run, 32);
+        const bool lost = (scored >> lane & 1) && sum < 1.f / kSumLimit;
+        if (__ballot(qok && (lost || !(l_run <= kSumLimit && z == 0.f))) && lane == 0) *redo = 1;
         __syncthreads();
         if (__builtin_amdgcn_readfirstlane((int)*(volatile uint32_t *)redo) == 0) break;
         __syncthreads();
@@ -792,6 +822,7 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, uint16_t *Ks, ui
 
     const float l_tot = l_run + __shfl_xor(l_run, 32);
     float inv = 1.f / l_tot;
+    m_run = __builtin_amdgcn_fmed3f(__builtin_amdgcn_ldexpf(m_run, shift_of()), -kLowest, kLowest);   // log2 units
     if (slot) {
         if (l_tot == 0.f) inv = 0.f;   // a part whose keys all score -inf: weight 0, not 0 * inf
         // device-scope stores: the workgroup that merges the item may run on
@@ -812,9 +843,9 @@ __device__ __forceinline__ void attn_segment(const AttnArgs &a, uint16_t *Ks, ui
                 put_shared(op + ((wave * C::MB + mb) * 4 + g) * 64 + lane, v);
             }
         if (hl == 0) {
-            // a sum far above one hands its exponent to the maximum: the weights by
-            // which the merge multiplies outputs stay small
-            const int e = l_tot > 0x1p24f ? __builtin_amdgcn_frexp_expf(l_tot) : 0;
+            // a sum far above one hands its exponent to the maximum, where that can hold
+            // it: the weights by which the merge multiplies outputs stay small
+            const int e = l_tot > 0x1p24f && fabsf(m_run) < 0x1p14f ? __builtin_amdgcn_frexp_expf(l_tot) : 0;
             constexpr int kML = BM * D / (WIDE ? 1 : 2);
             put_shared(slot + kML + wave * 32 + l32, m_run + (float)e);
             put_shared(slot + kML + BM + wave * 32 + l32, __builtin_amdgcn_ldexpf(l_tot, -e));
