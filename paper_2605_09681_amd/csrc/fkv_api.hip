@@ -9,6 +9,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <limits>
 #include <mutex>
 #include <vector>
 
@@ -1699,7 +1700,7 @@ fkv_status fkv_chunk_attention_q8(const fkv_shape *shape, const fkv_head *heads,
     a.n_seg = fkv_num_segments(shape);
     magic_of(a.F, &a.mf_hi, &a.mf_lo);
     magic_of(a.L, &a.ml_hi, &a.ml_lo);
-    a.scale_log2 = scale * 1.4426950408889634f;
+    a.scale_log2 = std::min(scale * 1.4426950408889634f, std::numeric_limits<float>::max());
     a.q_tile = p.q_tile;
     a.n_qtiles = p.n_qtiles;
     a.n_split = p.n_split;

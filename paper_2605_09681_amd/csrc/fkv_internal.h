@@ -246,7 +246,7 @@ struct AttnQ8Args {
     int32_t F, L, H, cap, n_seg;
     int32_t n_blocks, block_shift;      // scales per frame, log2 of the tokens per scale
     uint32_t mf_hi, mf_lo, ml_hi, ml_lo;  // floor(2^64 / F) + 1 and floor(2^64 / L) + 1 (0 for 1)
-    float scale_log2;                   // scale * log2(e)
+    float scale_log2;                   // scale * log2(e), finite
     int32_t q_tile, n_qtiles;           // query rows per tile (16, 32; d 64: 48), tiles per head
     int32_t n_split;                    // parts per (head, query tile); 1: no workspace
     float *part;                        // [head][query tile][part] slots of attn_q8_part_floats

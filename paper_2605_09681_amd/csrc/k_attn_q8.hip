@@ -52,6 +52,7 @@ constexpr int kTile = 64;                 // keys per step of a wave
 constexpr int kUnit = 16;                 // keys: the grain of the split over waves
 constexpr int kJoinThreads = 256, kJoin = 4;  // joining: threads of a workgroup, parts loaded at a time
 constexpr float kSlack = 8.f;             // log2 units that the softmax's reference may lag behind
+constexpr float kFar = 0x1p24f;           // log2 units from which a reference is kept as a score
 constexpr float kLn2 = 0.69314718055994530942f;
 
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
@@ -145,14 +146,20 @@ struct Wave {
     using C = Cfg<D, MT>;
     bf16x8_t q[MT][C::KS];
     f32x4_t o[MT][C::MB];
-    float m[MT], l[MT];     // running maximum (log2 units) and this lane's share of the sum
+    // The softmax's reference is the score *shift plus m log2 units (shift in LDS, read
+    // once a row of the wave is far); l: this lane's share of the sum.
+    float m[MT], l[MT], *shift;
+    bool far;
 
-    __device__ __forceinline__ void init(const uint16_t *Q, int q0, int n_q, int lane) {
+    __device__ __forceinline__ void init(const uint16_t *Q, int q0, int n_q, int lane, float *lds) {
         const int g = lane >> 4, c = lane & 15;
+        shift = lds + lane;
+        far = false;
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
             m[t] = neg_inf();
             l[t] = 0.f;
+            shift[64 * t] = 0.f;
             const int row = q0 + 16 * t + c;
 #pragma unroll
             for (int mb = 0; mb < C::MB; ++mb) o[t][mb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -164,10 +171,15 @@ struct Wave {
     }
 
     // Tile t's scores s[i] (keys 16i + 4(lane/16) + r of column lane%16) become
-    // probabilities; keys from `valid` on do not exist.  The reference m moves only
+    // probabilities; keys from `valid` on do not exist.  The reference moves only
     // where a score passes it by more than kSlack: probabilities then reach 2^kSlack,
     // which costs no digit in fp32 or bf16, and a step without such a score needs
     // neither the other lanes' maxima nor a new scale for the outputs.
+    // Far rows: m rounds its score times scale_log2, and the exponent keeps the
+    // difference, half a step of m at most; of scores of 1e13 or -1e30 that is more than
+    // an exponent holds.  From kFar on the reference is the score itself, subtracted
+    // from the others before they are scaled: of nearby scores the difference is exact.
+    // (Every score so: 480P, 512 rows 161 us instead of 140.)
     __device__ __forceinline__ void softmax(int t, f32x4_t (&s)[4], float scale_log2, int valid, int g) {
         if (valid < kTile) {
 #pragma unroll
@@ -180,16 +192,29 @@ struct Wave {
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) top = fmaxf(top, s[i][r]);
-        top *= scale_log2;
-        if (__ballot(top > m[t] + kSlack)) {
+        float sh = far ? shift[64 * t] : 0.f;
+        if (__ballot((top - sh) * scale_log2 > m[t] + kSlack)) {
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
-            const float mn = top > m[t] + kSlack ? top : m[t];
-            const float alpha = mn == m[t] ? 1.f : __builtin_amdgcn_exp2f(m[t] - mn);
+            const float z = top * scale_log2;
+            const bool move = (top - sh) * scale_log2 > m[t] + kSlack, to_far = move && !(fabsf(z) < kFar);
+            float mn = move ? z : m[t], alpha = mn == m[t] ? 1.f : __builtin_amdgcn_exp2f(m[t] - mn);
+            if (far || __ballot(to_far)) {
+                const float next = to_far ? top : move ? 0.f : sh;
+                mn = to_far ? 0.f : mn;
+                const float rise = (next - sh) * scale_log2 + (mn - m[t]);
+                alpha = !move ? 1.f : m[t] == neg_inf() ? 0.f : __builtin_amdgcn_exp2f(-rise);
+                far = true;
+                shift[64 * t] = sh = next;
+            }
             m[t] = mn;
             l[t] *= alpha;
 #pragma unroll
             for (int mb = 0; mb < C::MB; ++mb) o[t][mb] *= alpha;
+        }
+        if (far) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] -= sh;
         }
         const float base = m[t] == neg_inf() ? 0.f : m[t];
         float sum = 0.f;
@@ -201,6 +226,11 @@ struct Wave {
                 sum += s[i][r];
             }
         l[t] += sum;
+    }
+
+    // Tile t's reference as a score (a far row's m is 0).
+    __device__ __forceinline__ float reference(int t, float scale_log2) const {
+        return (far ? shift[64 * t] : 0.f) + m[t] / scale_log2;
     }
 
     // O^T += V^T P^T with the step's value rows in LDS.
@@ -237,7 +267,7 @@ __device__ __forceinline__ void put_row(const AttnQ8Args &a, int64_t row, int d,
 #pragma unroll
     for (int k = 0; k < 4; ++k) b[k] = __builtin_bit_cast(uint16_t, (__bf16)(acc[k] * inv));
     *(uint2 *)(a.O + row * D + d) = make_uint2(b[0] | (b[1] << 16), b[2] | (b[3] << 16));
-    if (a.lse && d == 0) a.lse[row] = empty ? neg_inf() : fmaf(M, kLn2, logf(L));
+    if (a.lse && d == 0) a.lse[row] = empty ? neg_inf() : fmaf(M * kLn2, a.scale_log2, logf(L));
 }
 
 // Workgroups go to the 8 XCDs in turn: each XCD takes a contiguous run of the list
@@ -249,6 +279,7 @@ __global__ __launch_bounds__(kThreads) void attn_q8_kernel(AttnQ8Args a) {
     constexpr int kRows = C::ROWS;
     __shared__ __attribute__((aligned(16))) uint16_t lds[kWaves * C::REGION];
     __shared__ int slots[FKV_MAX_FRAMES];
+    __shared__ float shifts[kWaves][MT * 64];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, c = lane & 15;
     const int place = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
     const int group = place / a.n_qtiles, qt = place - group * a.n_qtiles;
@@ -266,7 +297,7 @@ __global__ __launch_bounds__(kThreads) void attn_q8_kernel(AttnQ8Args a) {
     const int u0 = (int)((int64_t)units * wi / n_waves), u1 = (int)((int64_t)units * (wi + 1) / n_waves);
 
     Wave<D, MT> s;
-    s.init(a.Q + (int64_t)h * a.n_q * D, q0, a.n_q, lane);
+    s.init(a.Q + (int64_t)h * a.n_q * D, q0, a.n_q, lane, shifts[w]);
     uint16_t *vt = lds + w * C::REGION;
 
     // History: a step's rows are in flight while the step before weights its values.
@@ -387,7 +418,8 @@ __global__ __launch_bounds__(kThreads) void attn_q8_kernel(AttnQ8Args a) {
     }
 
     // The waves' results, PT tiles at a time: into the regions of LDS, then joined by
-    // the workgroup's threads, 4 channels of a row each.
+    // the workgroup's threads, 4 channels of a row each.  References meet as scores, their
+    // differences scaled: nothing but the rounding of a score, also for far rows.
     float *mine = (float *)vt;
     constexpr int kPRows = C::PROWS, RF = C::REGION / 2;      // RF: floats per region
 #pragma unroll
@@ -402,8 +434,9 @@ __global__ __launch_bounds__(kThreads) void attn_q8_kernel(AttnQ8Args a) {
             s.l[t] += __shfl_xor(s.l[t], 32);
 #pragma unroll
             for (int mb = 0; mb < C::MB; ++mb) *(f32x4_t *)(mine + (16 * k + c) * C::OS + 16 * mb + 4 * g) = s.o[t][mb];
+            const float ref = s.reference(t, a.scale_log2);
             if (lane < 16) {
-                mine[kPRows * C::OS + 16 * k + lane] = s.m[t];
+                mine[kPRows * C::OS + 16 * k + lane] = ref;
                 mine[kPRows * C::OS + kPRows + 16 * k + lane] = s.l[t];
             }
         }
@@ -419,7 +452,7 @@ __global__ __launch_bounds__(kThreads) void attn_q8_kernel(AttnQ8Args a) {
             const float ref = M == neg_inf() ? 0.f : M;
 #pragma unroll
             for (int i = 0; i < kWaves; ++i) {
-                const float wt = __builtin_amdgcn_exp2f(base[i * RF + kPRows * C::OS + r] - ref);
+                const float wt = __builtin_amdgcn_exp2f((base[i * RF + kPRows * C::OS + r] - ref) * a.scale_log2);
                 L += wt * base[i * RF + kPRows * C::OS + kPRows + r];
                 acc += wt * *(const f32x4_t *)(base + i * RF + r * C::OS + d);
             }
@@ -437,8 +470,8 @@ __global__ __launch_bounds__(kThreads) void attn_q8_kernel(AttnQ8Args a) {
     }
 }
 
-// Joins the parts of the items: M = max_j m_j, L = sum_j 2^(m_j - M) l_j and likewise
-// the outputs.  A launch of its own: the parts then cross as ordinary cached stores
+// Joins the parts of the items: M = max_j m_j, L = sum_j 2^((m_j - M) scale_log2) l_j and
+// likewise the outputs.  A launch of its own: the parts then cross as ordinary cached stores
 // and loads, every row has a workgroup, and the workspace holds no counters.  (Joined
 // by the part that arrives last, 480P: one query token 29.2 us, 16 tokens 24.0, 32
 // tokens 32.7; so 29.7, 21.8 and 26.0.)  One workgroup per row and head: D/4 threads
@@ -458,7 +491,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_q8_kernel(AttnQ8Args a) {
     f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
     auto add = [&](float m, float l, const f32x4_t &o) {
         const float Mn = fmaxf(M, m), ref = Mn == neg_inf() ? 0.f : Mn;
-        const float so = __builtin_amdgcn_exp2f(M - ref), sn = __builtin_amdgcn_exp2f(m - ref);
+        const float so = __builtin_amdgcn_exp2f((M - ref) * a.scale_log2), sn = __builtin_amdgcn_exp2f((m - ref) * a.scale_log2);
         M = Mn;
         L = L * so + l * sn;
         acc = acc * so + o * sn;
