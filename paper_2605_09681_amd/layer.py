@@ -396,7 +396,10 @@ class RolloutStack:
 
     ``cache="e4m3"`` holds every layer's cache in 8 bits (``cache8``, one
     :class:`Cache8` per layer, a scale per head and ``block_tokens`` tokens; half
-    the memory of bf16): :meth:`append` quantises, :meth:`run_layer` scores and
+    the memory of bf16, and one workspace for all layers, in which large chunks
+    are attended over a bf16 copy of a layer's kept history: with a dynamic head
+    as much as one layer's cache in bf16, 191 MiB for 12 heads of 128 at 480P):
+    :meth:`append` quantises, :meth:`run_layer` scores and
     selects from the 8-bit keys and attends any number of query tokens over the
     kept 8-bit history and the current bf16 tokens.  The shared compressed
     buffers, incremental rescoring and :meth:`score_pooled` do not exist then (a
@@ -432,7 +435,7 @@ class RolloutStack:
         if cache == "e4m3":
             self.step_mode = "q8"
             self.cache8 = [Cache8.zeros(full, block_tokens, dev) for _ in range(n_layers)]
-            self._q8_bytes, self._q8_ws = {}, []
+            self._q8_bytes, self._q8_ws, self._q8_stream, self._q8_captured = {}, None, None, []
             return
         hist = (n_heads, window, frame_tokens, head_dim)
         self.K_hist = [torch.zeros(hist, dtype=dt, device=dev) for _ in range(n_layers)]
@@ -537,7 +540,7 @@ class RolloutStack:
                 else:
                     fkv_score_select_q8(shape, heads, c8, frame_slot, K_cur, scores, kept, self.kv_len, self.score_ws)
             fkv_chunk_attention_q8(shape, heads, c8, frame_slot, kept, self.kv_len, Q, K_cur, V_cur, self.scale, O, lse,
-                                   self._q8_workspace(shape, heads, (key, H, Q.shape[1], K_cur.shape[1])))
+                                   self._q8_workspace(heads, (key, H, Q.shape[1], K_cur.shape[1])))
             return
         Kh, Vh = self.K_hist[layer], self.V_hist[layer]
         if self.step_mode == "paged":
@@ -597,15 +600,25 @@ class RolloutStack:
         if self.cache == "e4m3":
             raise ValueError(f"{what}: not available for an 8-bit cache")
 
-    def _q8_workspace(self, shape, heads, key):
-        """The 8-bit attention's workspace: the largest so far.  Smaller ones stay
-        allocated, as a graph captured with one of them still writes to it."""
-        if key not in self._q8_bytes:
-            with torch.cuda.device(self.device):
-                self._q8_bytes[key] = fkv_chunk_attention_q8_workspace_size(shape, heads, key[2], key[3])
-        if not self._q8_ws or self._q8_bytes[key] > self._q8_ws[-1].numel():
-            self._q8_ws.append(torch.empty(max(self._q8_bytes[key], 1), dtype=torch.uint8, device=self.device))
-        return self._q8_ws[-1]
+    def _q8_workspace(self, heads, key):
+        """The 8-bit attention's workspace: the largest so far, sized for the full
+        window, so that a window that fills up does not replace it chunk by chunk.  A
+        smaller one stays allocated only if a graph was captured with it, which still
+        writes to it."""
+        with torch.cuda.device(self.device):
+            if key not in self._q8_bytes:
+                self._q8_bytes[key] = max(fkv_chunk_attention_q8_workspace_size(self.shape(H), heads, key[2], key[3])
+                                          for H in {key[1], self.window})
+            stream = torch.cuda.current_stream()
+            if self._q8_ws is None or self._q8_bytes[key] > self._q8_ws.numel():
+                self._q8_ws = torch.empty(max(self._q8_bytes[key], 1), dtype=torch.uint8, device=self.device)
+                self._q8_stream = stream
+            if torch.cuda.is_current_stream_capturing():
+                if not any(w is self._q8_ws for w in self._q8_captured):
+                    self._q8_captured.append(self._q8_ws)
+            elif stream != self._q8_stream:
+                self._q8_ws.record_stream(stream)      # freed only after this stream's use of it
+        return self._q8_ws
 
     def rotate(self, frame_pos, Q, K, V, Qr, Kr, Vr):
         """The chunk's Q and K turned by ``rope`` and its V as it is, from any strided
