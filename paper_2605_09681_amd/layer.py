@@ -403,7 +403,10 @@ class RolloutStack:
     selects from the 8-bit keys and attends any number of query tokens over the
     kept 8-bit history and the current bf16 tokens.  The shared compressed
     buffers, incremental rescoring and :meth:`score_pooled` do not exist then (a
-    row computed elsewhere may still be passed as ``pooled``)."""
+    row computed elsewhere may still be passed as ``pooled``).  ``K_cur`` and
+    ``V_cur`` may then hold any number of current tokens, or be None, unless a
+    dynamic head is scored: that compares the chunk's first frame, so K_cur is the
+    whole chunk's."""
 
     def __init__(self, n_layers: int, n_heads: int, head_dim: int, frame_tokens: int, window: int,
                  chunk_frames: int, seg_tokens: int, dtype: str = "bf16", device="cuda",
@@ -534,13 +537,15 @@ class RolloutStack:
             if incremental:
                 raise ValueError("an 8-bit cache has no incremental rescoring")
             c8 = self.cache8[layer]
+            if K_cur is None and has_dynamic and pooled is None:
+                raise ValueError("scoring the dynamic heads needs the chunk's K_cur")
             if has_dynamic:
                 if pooled is not None:
                     fkv_select(shape, heads, pooled, kept, self.kv_len, shared_row=True)
                 else:
                     fkv_score_select_q8(shape, heads, c8, frame_slot, K_cur, scores, kept, self.kv_len, self.score_ws)
             fkv_chunk_attention_q8(shape, heads, c8, frame_slot, kept, self.kv_len, Q, K_cur, V_cur, self.scale, O, lse,
-                                   self._q8_workspace(heads, (key, H, Q.shape[1], K_cur.shape[1])))
+                                   self._q8_workspace(heads, (key, H, Q.shape[1], 0 if K_cur is None else K_cur.shape[1])))
             return
         Kh, Vh = self.K_hist[layer], self.V_hist[layer]
         if self.step_mode == "paged":
