@@ -196,11 +196,19 @@ def lib():
 # ---------------------------------------------------------------------------
 # argument marshalling
 # ---------------------------------------------------------------------------
+def _i32(v, name: str) -> int:
+    """v as a whole number of 32 bits (ctypes would cut others down to one)."""
+    i = int(v)
+    if i != v or not -1 << 31 <= i < 1 << 31:
+        raise ValueError(f"{name}: {v} is not a whole number of 32 bits")
+    return i
+
+
 def make_shape(n_heads, head_dim, frame_tokens, hist_frames, cap_frames, chunk_frames,
                seg_tokens, dtype) -> fkv_shape:
     dt = {"bf16": FKV_BF16, "f32": FKV_F32, FKV_BF16: FKV_BF16, FKV_F32: FKV_F32}[dtype]
-    return fkv_shape(n_heads, head_dim, frame_tokens, hist_frames, cap_frames, chunk_frames,
-                     seg_tokens, dt)
+    sizes = (n_heads, head_dim, frame_tokens, hist_frames, cap_frames, chunk_frames, seg_tokens)
+    return fkv_shape(*(_i32(v, "shape") for v in sizes), dt)
 
 
 def make_heads(budgets: Sequence) -> ctypes.Array:
@@ -209,7 +217,7 @@ def make_heads(budgets: Sequence) -> ctypes.Array:
     arr = (fkv_head * len(budgets))()
     for i, b in enumerate(budgets):
         vals = (b.type, b.sink_frames, b.recent_frames, b.keep_k, b.scope) if hasattr(b, "type") else tuple(b)
-        arr[i] = fkv_head(*map(int, vals))
+        arr[i] = fkv_head(*(_i32(v, f"budget of head {i}") for v in vals))
     return arr
 
 
@@ -235,13 +243,7 @@ def _slots(frame_slot, H):
     if frame_slot is None:
         import numpy as np
         frame_slot = np.arange(H, dtype="int32")
-    arr = (ctypes.c_int32 * max(H, 1))()
-    vals = [int(v) for v in (frame_slot.tolist() if hasattr(frame_slot, "tolist") else frame_slot)]
-    if len(vals) != H:
-        raise ValueError(f"frame_slot needs {H} entries (got {len(vals)})")
-    for i, v in enumerate(vals):
-        arr[i] = v
-    return arr
+    return _ints(frame_slot, H, "frame_slot")
 
 
 def _heads(shape: fkv_shape, heads, allow_none: bool = False):
@@ -281,7 +283,7 @@ def fkv_num_segments(shape: fkv_shape) -> int:
 
 def fkv_kept_tokens_max(shape: fkv_shape, heads, head: int) -> int:
     out = ctypes.c_int64(0)
-    _raise(lib().fkv_kept_tokens_max(ctypes.byref(shape), _heads(shape, heads), int(head), ctypes.byref(out)))
+    _raise(lib().fkv_kept_tokens_max(ctypes.byref(shape), _heads(shape, heads), _i32(head, "head"), ctypes.byref(out)))
     return int(out.value)
 
 
@@ -373,13 +375,13 @@ def fkv_append_frames(shape: fkv_shape, K_new, V_new, dst_slot, K_hist, V_hist, 
     slots dst_slot (host ints, one per frame)."""
     dt = _torch_dtype(shape)
     hist = (shape.n_heads, shape.cap_frames, shape.frame_tokens, shape.head_dim)
-    slots = [int(v) for v in dst_slot]
-    n = len(slots)
+    dst_slot = list(dst_slot)
+    n = len(dst_slot)
+    slots = _ints(dst_slot, n, "dst_slot")
     new = (shape.n_heads, n * shape.frame_tokens, shape.head_dim)
     kn, vn = _check(K_new, "K_new", dt, new), _check(V_new, "V_new", dt, new)
     kh, vh = _check(K_hist, "K_hist", dt, hist), _check(V_hist, "V_hist", dt, hist)
-    arr = (ctypes.c_int32 * max(n, 1))(*slots)
-    _raise(lib().fkv_append_frames(ctypes.byref(shape), kn, vn, n, arr, kh, vh, _stream(stream)))
+    _raise(lib().fkv_append_frames(ctypes.byref(shape), kn, vn, n, slots, kh, vh, _stream(stream)))
 
 
 def fkv_score_pooled_workspace_size(shape: fkv_shape) -> int:
@@ -532,8 +534,8 @@ def fkv_chunk_attention_heads(shape: fkv_shape, heads: Sequence[int], Q, Kc, Vc,
     heads' rows of O and lse are left untouched."""
     q, kc, vc, slab, kl, kq, vq, o, ls, ws, nws = _attention_args(shape, Q, Kc, Vc, kv_len, K_cur, V_cur, O,
                                                                   lse, workspace)
-    ids = [int(h) for h in heads]
-    arr = (ctypes.c_int32 * max(len(ids), 1))(*ids)
+    ids = list(heads)
+    arr = _ints(ids, len(ids), "heads")
     _raise(lib().fkv_chunk_attention_heads(ctypes.byref(shape), arr, len(ids), q, kc, vc, slab, kl, kq, vq,
                                            ctypes.c_float(scale), o, ls, ws, nws, _stream(stream)))
 
@@ -585,8 +587,8 @@ def fkv_chunk_attention_paged(shape: fkv_shape, heads, K_hist, V_hist, frame_slo
         ws, nws = _check(workspace, "workspace", torch.uint8), workspace.numel()
     arr, n = None, 0
     if head_list is not None:
-        ids = [int(h) for h in head_list]
-        arr, n = (ctypes.c_int32 * max(len(ids), 1))(*ids), len(ids)
+        ids = list(head_list)
+        arr, n = _ints(ids, len(ids), "head_list"), len(ids)
     _raise(lib().fkv_chunk_attention_paged(ctypes.byref(shape), _heads(shape, heads), arr, n, kh, vh, sl, ks, kl,
                                            q, kq, vq, ctypes.c_float(scale), o, ls, ws, nws, _stream(stream)))
 
@@ -667,7 +669,7 @@ def fkv_chunk_attention_fp8(shape: fkv_shape, Q8, K8, V8T, slab: int, kv_len, sc
 
 def fkv_attention_mass_workspace_size(shape: fkv_shape, n_bins: int) -> int:
     out = ctypes.c_size_t(0)
-    _raise(lib().fkv_attention_mass_workspace_size(ctypes.byref(shape), int(n_bins), ctypes.byref(out)))
+    _raise(lib().fkv_attention_mass_workspace_size(ctypes.byref(shape), _i32(n_bins, "n_bins"), ctypes.byref(out)))
     return int(out.value)
 
 
@@ -700,8 +702,8 @@ def fkv_classify_heads(mass, hist_frames: int, sink_frames: int = 1, transition_
     m = np.ascontiguousarray(mass.cpu().numpy() if isinstance(mass, torch.Tensor) else mass, dtype=np.float32)
     n_heads, n_bins = m.shape
     out = (ctypes.c_int32 * n_heads)()
-    _raise(lib().fkv_classify_heads(m.ctypes.data_as(ctypes.c_void_p), n_heads, n_bins, int(hist_frames),
-                                    int(sink_frames), int(transition_frames), ctypes.c_float(alpha), out))
+    _raise(lib().fkv_classify_heads(m.ctypes.data_as(ctypes.c_void_p), n_heads, n_bins,
+                                    *(_i32(v, "frames") for v in (hist_frames, sink_frames, transition_frames)), ctypes.c_float(alpha), out))
     return list(out)
 
 
@@ -713,8 +715,8 @@ def make_rope(frame_pairs: int, row_pairs: int = 0, col_pairs: int = 0, row_toke
     """How channel pairs turn with position: the first ``frame_pairs`` by the
     frame position, then ``row_pairs`` by the token's row and ``col_pairs`` by its
     column in rows of ``row_tokens`` tokens (see fkv.h)."""
-    return fkv_rope(int(frame_pairs), int(row_pairs), int(col_pairs), int(row_tokens), int(token_step), int(pairing),
-                    float(theta))
+    counts = (frame_pairs, row_pairs, col_pairs, row_tokens, token_step, pairing)
+    return fkv_rope(*(_i32(v, "rope") for v in counts), float(theta))
 
 
 class Cache8:
@@ -783,11 +785,15 @@ def _rows(t: torch.Tensor, name: str, dtype, size, device: int):
 
 
 def _ints(values, n: int, name: str):
-    """A host int32 array of n entries from a sequence, numpy array or tensor."""
-    vals = values.tolist() if hasattr(values, "tolist") else values
+    """A host int32 array of n entries from a sequence, numpy array or tensor of
+    whole numbers (ctypes would cut others down to 32 bits)."""
+    vals = values.tolist() if hasattr(values, "tolist") else list(values)
     if len(vals) != n:
         raise ValueError(f"{name} needs {n} entries (got {len(vals)})")
-    return (ctypes.c_int32 * (n or 1))(*map(int, vals))
+    ints = list(map(int, vals))
+    if ints != vals or (n and not (-1 << 31 <= min(ints) and max(ints) < 1 << 31)):
+        raise ValueError(f"{name}: {vals} are not whole numbers of 32 bits")
+    return (ctypes.c_int32 * (n or 1))(*ints)
 
 
 def _frames(shape: fkv_shape, frame_slot):
@@ -901,8 +907,8 @@ def fkv_score_select_q8(shape: fkv_shape, heads, cache: Cache8, frame_slot, K_cu
 def fkv_chunk_attention_q8_workspace_size(shape: fkv_shape, heads, n_q: int, n_cur: int) -> int:
     """Bytes of the workspace of fkv_chunk_attention_q8 on the current device."""
     out = ctypes.c_size_t(0)
-    _raise(lib().fkv_chunk_attention_q8_workspace_size(ctypes.byref(shape), _heads(shape, heads), int(n_q), int(n_cur),
-                                                       ctypes.byref(out)))
+    _raise(lib().fkv_chunk_attention_q8_workspace_size(ctypes.byref(shape), _heads(shape, heads), _i32(n_q, "n_q"),
+                                                       _i32(n_cur, "n_cur"), ctypes.byref(out)))
     return int(out.value)
 
 
