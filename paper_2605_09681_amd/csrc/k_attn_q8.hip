@@ -28,12 +28,13 @@
 // Why so: with few query tokens the bytes of the cache bound the work, and a wave
 // that waits for nobody keeps its rows in flight: the next step's keys are requested
 // as soon as this step's are consumed, its values after this step's are in LDS.  K
-// needs no LDS at all.  480P, one query token, all 21 frames kept (101 MB): 29.4 us,
-// 26 of them this launch; with the arithmetic taken out the loads alone take 24, 4.6
+// needs no LDS at all.  480P, one query token, all 21 frames kept (101 MB): 28.3 us,
+// 25 of them this launch; with the arithmetic taken out the loads alone take 24, 4.6
 // TB/s beside the launch (a 1 GiB copy reaches 5.1).  More query tokens share a
-// conversion and a row's trip through LDS, 16 to 48 rows a wave: 128 tokens 41.5 us,
-// 512 139 us (0.33 PFLOP/s): bound by the latency of a step, two waves per SIMD with
-// 200 and more registers each.  Measured beside it, neutral or slower: 4 waves per
+// conversion and a row's trip through LDS, 16 to 48 rows a wave: 128 tokens 42.0 us,
+// 512 140 us (0.33 PFLOP/s): bound by the latency of a step, two waves per SIMD with
+// 200 and more registers each (256 at d = 128 and 32 rows, where five more are spilled
+// before the history's loop and come back after it, none within a loop).  Measured beside it, neutral or slower: 4 waves per
 // workgroup (512 tokens 180 us), 128 registers and twice the waves for d = 64 (spills),
 // the running maximum taken in every step (3 to 8% slower), 12 waves per workgroup for
 // d = 64 (168 registers spill: 666 tokens of 16 heads 21 to 55 us; one token 11.1 to 10.8).

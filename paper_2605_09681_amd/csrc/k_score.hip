@@ -460,8 +460,18 @@ __global__ __launch_bounds__(kThreads, 5) void score_kernel(ScoreArgs a) {
 // conversion of every element, with half the bytes to hide it behind.)
 // Frame H is bf16: the lane's 16 elements and their products with frame H - 1
 // are fp64.
-constexpr int kMaxF8 = 6;      // a 480P layer's run of frames per wave
-constexpr int kFlat8 = 32;     // workgroups of a head that arrive on one counter
+
+// Frames that a wave has in flight (a wave's run is a quarter of H + 1 frames).  More
+// hide more of the latency and take registers; 4, 6 and 8, frames of 1560 tokens of 128,
+// us: H = 5 10.6, 11.2 and 14.0; 13 14.0, 14.2 and 16.7; 19 17.0, 16.2 and 19.0; 21 17.8,
+// 16.8 and 19.4; 31 20.8, 21.7 and 23.4; 47 27.8, 27.7 and 31.0; 200 frames of 156 41.7,
+// 40.3 and 39.8.
+constexpr int kMaxF8 = 6;
+// Up to kFlat8 workgroups of a head arrive on one counter, others in two levels.  One
+// counter against two levels, us: 13 workgroups 8.2 and 8.8, 20 8.6 and 9.3, 21 9.4 and
+// 10.1, 39 9.5 and 10.2; but 50 units of one workgroup 32.2 and 31.1, 195 108.9 and 106.8,
+// 1000 452 and 440.
+constexpr int kFlat8 = 32;
 
 struct Codes16 {
     float v[16];
