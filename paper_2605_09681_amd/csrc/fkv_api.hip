@@ -1432,7 +1432,7 @@ int64_t q8_most_kept(const fkv_shape *s, const fkv_head *heads) {
 // over a bf16 copy of the kept history, by the 256-row kernel of
 // fkv_chunk_attention, which runs four times as many products a second but pays for
 // the copy and, with few items, for joining large parts.  480P, 12 heads: 512 rows
-// (53 thousand steps) in place 139 us, expanded 141; 1024 rows (110) 246 and 169;
+// (53 thousand steps) in place 140 us, expanded 141; 1024 rows (110) 246 and 169;
 // 4096 rows 1300 and 462; 24 heads, 600 rows, 3 frames (38) 101 and 113; one head,
 // 600 rows 48 and 232.
 //

@@ -131,7 +131,8 @@ struct Cfg {
     static constexpr int KS = D / 32;             // steps of the score product
     static constexpr int MB = D / 16;             // 16-channel blocks of the output
     // Value rows in LDS, padded by 32 bytes: the four rows that a transpose read
-    // covers, and the eight that a 16-byte store covers, then fall into distinct banks.
+    // covers, and the eight that a 16-byte store covers, then fall into distinct banks
+    // by the layout (the conflict counter still reads 0.3 of the LDS cycles).
     static constexpr int VS = D + 16;
     static constexpr int REGION = kTile * VS;     // elements per wave
     // A wave's results meet the others' in its region, PT tiles at a time: output rows,
