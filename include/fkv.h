@@ -641,6 +641,128 @@ fkv_status fkv_chunk_attention_q8(const fkv_shape *shape, const fkv_head *heads,
                                   float scale, void *O, float *lse, void *workspace,
                                   size_t workspace_bytes, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Paged caches of many sequences.
+ *
+ * A pool of pages of page_tokens tokens holds the caches of any number of
+ * sequences (device memory, 16-byte aligned):
+ *   K_pages, V_pages [n_pages][n_kv_heads][page_tokens][d]
+ * Token t of sequence i lies in page page_table[i][t / page_tokens], row t %
+ * page_tokens.  A page may serve several sequences (a shared beginning).  A
+ * call takes a batch of sequences, whose new tokens' rows follow one another in
+ * the batch's tensors: sequence i's are rows q_start[i] .. q_start[i + 1] - 1,
+ * its last tokens, at positions seq_len[i] - n_i .. seq_len[i] - 1.
+ *   page_table  device int32 [n_seqs][max_pages]; entries behind a sequence's
+ *               last page are not read
+ *   seq_len     device int32 [n_seqs]: tokens of the sequence, new ones included
+ *   q_start     device int32 [n_seqs + 1], not falling
+ *   n_tokens    rows of the batch's tensors (0 enqueues nothing); rows before
+ *               q_start[0] and from q_start[n_seqs] on belong to no sequence and
+ *               are left as they are
+ *   max_new     >= every n_i: of a sequence with more new tokens only the first
+ *               max_new are served
+ *   sum_len     >= the sum of seq_len (read by the expanded latent form alone,
+ *               which has room for that many tokens and leaves out those beyond)
+ * Lengths, starts and pages are read on the device when the call runs, so a
+ * captured graph serves other values later; values outside their range are held
+ * to it (a key on a page outside the pool is read from another page, a new
+ * token's row there is not written).  A sequence without new tokens takes no
+ * part.  A new token at a position before 0 (more new tokens than tokens) sees
+ * no key of a causal call and is not appended.
+ *
+ * Limits (FKV_ERR_SHAPE): n_seqs up to FKV_MAX_SEQS, n_tokens up to 2^24,
+ * page_tokens 1 to 2^20, n_pages * n_kv_heads * page_tokens below 2^31; a
+ * sequence's tokens beyond 2^30 are not seen. */
+#define FKV_MAX_SEQS 4096
+typedef struct {
+    int32_t n_seqs, max_pages, page_tokens, n_pages, n_tokens, max_new;
+    int64_t sum_len;
+    const int32_t *page_table, *seq_len, *q_start;   /* device */
+} fkv_batch;
+
+/* Which keys a key head's queries see beside the causal order: recent_tokens <
+ * 0: all; else the sequence's first sink_tokens and, of the others, its own key
+ * and the recent_tokens before it (not causal: the new tokens and the
+ * recent_tokens before the first of them) -- a static head's budget (Eq. 2) in
+ * tokens. */
+typedef struct {
+    int32_t sink_tokens;   /* >= 0 */
+    int32_t recent_tokens; /* >= -1 */
+} fkv_span;
+
+/* The batch's new keys and values into their pages: row r of head h of K_new /
+ * V_new ([n_heads][n_tokens][head_dim], strided as fkv_rows) to its sequence's
+ * place for it.  V_new and V_pages may both be NULL (a latent cache: one head of
+ * latent rows).  dtype: FKV_BF16 or FKV_F32; a row is a multiple of 16 bytes,
+ * at most 16384.  Other rows of the pages keep their bytes.  Sequences that
+ * share a page must not both have new tokens in it. */
+fkv_status fkv_append_paged(const fkv_batch *batch, int32_t n_heads, int32_t head_dim, int32_t dtype,
+                            const fkv_rows *K_new, const fkv_rows *V_new, void *K_pages, void *V_pages,
+                            void *stream);
+
+/* Attention of every sequence's new tokens over its pages (its new tokens'
+ * keys and values must be in them already):
+ *   O[h][r] = softmax(scale * Q[h][r] . keys^T) . values
+ * over the keys that the row sees, of key head h / (n_heads / n_kv_heads).
+ * causal 1: a new token sees keys up to its own position; 0: every key of its
+ * sequence (the new tokens are a chunk whose tokens see one another).  spans:
+ * HOST array [n_kv_heads], or NULL: no head is limited.
+ *   Q, O   bf16 rows [n_heads][n_tokens][d], strided as fkv_rows (O is written;
+ *          it overlaps no input, and its rows do not overlap)
+ *   lse    float [n_heads][n_tokens] (nullable): log sum_j exp(z_j)
+ * A row that sees no key gets O = 0 and lse = -infinity.  What lies in pages
+ * behind a sequence's last token, or at keys that a row does not see, has no
+ * effect on it, infinities and NaNs included.  head_dim 64 or 128, n_heads a
+ * multiple of n_kv_heads, both up to FKV_MAX_HEADS.  Products are bf16 with
+ * fp32 accumulation, softmax and sums fp32; probabilities are rounded to bf16
+ * for the value product.
+ *
+ * With a workspace of fkv_paged_attention_workspace_size bytes (for the same
+ * batch sizes, on the same device; no initialisation; calls may share one in
+ * turn, ordered by the caller) long sequences are split along their keys and the parts joined
+ * in fp32; with NULL one workgroup takes a tile of rows from its first key to
+ * its last.  FKV_ERR_CAPACITY if the workspace is smaller.  The same bits on
+ * every run of the same call. */
+fkv_status fkv_paged_attention_workspace_size(const fkv_batch *batch, int32_t n_heads, int32_t n_kv_heads,
+                                              int32_t head_dim, size_t *bytes);
+fkv_status fkv_paged_attention(const fkv_batch *batch, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                               const fkv_rows *Q, const void *K_pages, const void *V_pages, int32_t causal,
+                               const fkv_span *spans, float scale, const fkv_rows *O, float *lse, void *workspace,
+                               size_t workspace_bytes, void *stream);
+
+/* Attention over a paged latent cache: pages [n_pages][page_tokens][latent_dim +
+ * FKV_LATENT_ROT] bf16 hold one row for each token and all heads, a latent vector c and
+ * a rotated key r (fkv_append_paged writes them as one head of latent_dim + 64
+ * channels).  Head h's key is [W_k[h] c | r], its value W_v[h] c:
+ *   Q      bf16 rows [n_heads][n_tokens][d + 64]: the channels that meet
+ *          W_k c, then those that meet r (rotated by the caller)
+ *   W_k, W_v  bf16 [n_heads][d][latent_dim], contiguous
+ *   O      bf16 rows [n_heads][n_tokens][d]
+ * Masks, empty rows and span (one for all heads; NULL: not limited) as in
+ * fkv_paged_attention.  latent_dim 256 or 512, head_dim d 64 or 128, n_heads up to
+ * FKV_MAX_HEADS.  Two forms of the same sum:
+ *   FKV_LATENT_ABSORBED  queries are taken through W_k, all heads attend the
+ *                        latent rows themselves, outputs are taken through W_v:
+ *                        each cached row is read once for all heads;
+ *   FKV_LATENT_EXPANDED  every head's keys and values of all cached tokens are
+ *                        made first (in the workspace), then attended;
+ *   FKV_LATENT_AUTO      each sequence by its new tokens: absorbed up to
+ *                        FKV_LATENT_FEW - 1 of them, expanded from there on.
+ * What lies between the products (absorbed queries and outputs, expanded keys
+ * and values) is rounded to bf16.  The workspace (fkv_latent_attention_workspace_size bytes
+ * for the same batch sizes and form, no initialisation, shared in turn) is
+ * needed.  FKV_ERR_SHAPE also for a sum_len above 2^30 and an expanded form of more
+ * than 65535 blocks of 128 tokens (one more a sequence than sum_len needs). */
+#define FKV_LATENT_ROT 64
+#define FKV_LATENT_FEW 128
+typedef enum { FKV_LATENT_AUTO = 0, FKV_LATENT_ABSORBED = 1, FKV_LATENT_EXPANDED = 2 } fkv_latent_form;
+fkv_status fkv_latent_attention_workspace_size(const fkv_batch *batch, int32_t n_heads, int32_t head_dim,
+                                               int32_t latent_dim, int32_t form, size_t *bytes);
+fkv_status fkv_latent_attention(const fkv_batch *batch, int32_t n_heads, int32_t head_dim, int32_t latent_dim,
+                                const fkv_rows *Q, const void *pages, const void *W_k, const void *W_v,
+                                int32_t causal, const fkv_span *span, float scale, const fkv_rows *O, int32_t form,
+                                void *workspace, size_t workspace_bytes, void *stream);
+
 /* Message describing the calling thread's last non-OK status ("" if none). */
 const char *fkv_last_error(void);
 

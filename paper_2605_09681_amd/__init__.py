@@ -27,6 +27,10 @@ Entry points (see ``include/fkv.h`` for the full contract):
   :func:`fkv_chunk_attention_q8` -- a rolling cache held in 8 bits
   (:class:`Cache8`): its write, its scoring and selection, and attention of any
   number of query tokens over it
+* :func:`fkv_append_paged`, :func:`fkv_paged_attention` -- the paged cache of many
+  sequences (:class:`PagedBatch`): its write, and attention of every sequence's
+  new tokens over its pages
+* :func:`fkv_latent_attention` -- the same over a paged cache of latent rows
 * :func:`fkv_score_pooled`, :func:`fkv_select_compact_pooled` -- the
   first-block proxy of Sec. 4.3: one similarity row pooled over all heads,
   shared by the dynamic heads of every layer
@@ -49,6 +53,8 @@ FKV_SCOPE_FRAME, FKV_SCOPE_GLOBAL = 0, 1
 FKV_PAIR_ADJACENT, FKV_PAIR_HALVES = 0, 1
 FKV_MAX_HEADS, FKV_MAX_FRAMES, FKV_MAX_SEGMENTS = 64, 256, 4096
 FKV_MAX_POSITION = 1 << 24
+FKV_LATENT_AUTO, FKV_LATENT_ABSORBED, FKV_LATENT_EXPANDED = 0, 1, 2
+FKV_LATENT_ROT, FKV_LATENT_FEW, FKV_MAX_SEQS = 64, 128, 4096
 
 EXPORTED = ("fkv_num_segments", "fkv_kept_tokens_max", "fkv_compress_static",
             "fkv_score_workspace_size", "fkv_score_segments", "fkv_select_compact",
@@ -62,7 +68,8 @@ EXPORTED = ("fkv_num_segments", "fkv_kept_tokens_max", "fkv_compress_static",
             "fkv_chunk_attention_fp8", "fkv_attention_mass_workspace_size", "fkv_attention_mass",
             "fkv_classify_heads", "fkv_rotate_chunk", "fkv_append_frames_rotated", "fkv_append_frames_q8",
             "fkv_score_select_q8", "fkv_chunk_attention_q8_workspace_size", "fkv_chunk_attention_q8",
-            "fkv_last_error")
+            "fkv_append_paged", "fkv_paged_attention_workspace_size", "fkv_paged_attention",
+            "fkv_latent_attention_workspace_size", "fkv_latent_attention", "fkv_last_error")
 
 
 class FkvLibraryMissing(RuntimeError):
@@ -102,6 +109,17 @@ class fkv_rows(ctypes.Structure):
 class fkv_cache8(ctypes.Structure):
     _fields_ = [("K8", ctypes.c_void_p), ("V8", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
                 ("v_scale", ctypes.c_void_p), ("block_tokens", ctypes.c_int32)]
+
+
+class fkv_batch(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("page_tokens", ctypes.c_int32),
+                ("n_pages", ctypes.c_int32), ("n_tokens", ctypes.c_int32), ("max_new", ctypes.c_int32),
+                ("sum_len", ctypes.c_int64), ("page_table", ctypes.c_void_p), ("seq_len", ctypes.c_void_p),
+                ("q_start", ctypes.c_void_p)]
+
+
+class fkv_span(ctypes.Structure):
+    _fields_ = [("sink_tokens", ctypes.c_int32), ("recent_tokens", ctypes.c_int32)]
 
 
 _lib = None
@@ -187,6 +205,17 @@ def lib():
         L.fkv_chunk_attention_q8_workspace_size.restype = ctypes.c_int
         L.fkv_chunk_attention_q8.argtypes = [S, Hd, C8, P, P, P, P, I32, P, P, I32, F, P, P, P, SZ, P]
         L.fkv_chunk_attention_q8.restype = ctypes.c_int
+        B, Sp = ctypes.POINTER(fkv_batch), ctypes.POINTER(fkv_span)
+        L.fkv_append_paged.argtypes = [B, I32, I32, I32, Rw, Rw, P, P, P]
+        L.fkv_append_paged.restype = ctypes.c_int
+        L.fkv_paged_attention_workspace_size.argtypes = [B, I32, I32, I32, ctypes.POINTER(SZ)]
+        L.fkv_paged_attention_workspace_size.restype = ctypes.c_int
+        L.fkv_paged_attention.argtypes = [B, I32, I32, I32, Rw, P, P, I32, Sp, F, Rw, P, P, SZ, P]
+        L.fkv_paged_attention.restype = ctypes.c_int
+        L.fkv_latent_attention_workspace_size.argtypes = [B, I32, I32, I32, I32, ctypes.POINTER(SZ)]
+        L.fkv_latent_attention_workspace_size.restype = ctypes.c_int
+        L.fkv_latent_attention.argtypes = [B, I32, I32, I32, Rw, P, P, P, I32, Sp, F, Rw, I32, P, SZ, P]
+        L.fkv_latent_attention.restype = ctypes.c_int
         L.fkv_last_error.argtypes = []
         L.fkv_last_error.restype = ctypes.c_char_p
         _lib = L
@@ -945,6 +974,173 @@ def fkv_chunk_attention_q8(shape: fkv_shape, heads, cache: Cache8, frame_slot, k
     _run(dev, lib().fkv_chunk_attention_q8,
          (ctypes.byref(shape), _heads(shape, heads), ctypes.byref(c), _frames(shape, frame_slot),
           ks, kl, q, n_q, kq, vq, n_cur, scale, o, ls, ws, nws), stream)
+
+
+class PagedBatch:
+    """The sequences of a call over paged caches (see fkv_batch in include/fkv.h).
+
+    ``page_table`` int32 [n_seqs][max_pages], ``seq_len`` int32 [n_seqs] (new
+    tokens included) and ``q_start`` int32 [n_seqs + 1] (rows of each sequence's
+    new tokens) lie on the GPU and may be written between calls.  ``n_tokens``
+    rows have the batch's tensors; ``max_new`` is at least every sequence's new
+    tokens, ``sum_len`` at least the sum of ``seq_len`` (the expanded latent form
+    needs it)."""
+
+    def __init__(self, page_table, seq_len, q_start, page_tokens: int, n_tokens: int, max_new: int, sum_len: int = 0):
+        self.device = _device_of(page_table, "page_table")
+        n = page_table.shape[0] if page_table.dim() == 2 else -1
+        table = _ptr(page_table, "page_table", torch.int32, (n, page_table.shape[-1]), self.device)
+        lens = _ptr(seq_len, "seq_len", torch.int32, (n,), self.device)
+        starts = _ptr(q_start, "q_start", torch.int32, (n + 1,), self.device)
+        total = int(sum_len)
+        if total != sum_len or not 0 <= total < 1 << 62:
+            raise ValueError(f"sum_len: {sum_len} is not a whole number of tokens")
+        self.page_table, self.seq_len, self.q_start = page_table, seq_len, q_start
+        self.n_seqs, self.page_tokens, self.n_tokens = n, _i32(page_tokens, "page_tokens"), _i32(n_tokens, "n_tokens")
+        self.max_new, self.sum_len = _i32(max_new, "max_new"), total
+        self._c = fkv_batch(n, page_table.shape[1], self.page_tokens, 1, self.n_tokens, self.max_new, total, table, lens, starts)
+
+    def _arg(self, n_pages: int):
+        """The C batch of a call over n_pages pages (one of its own: calls of other threads have theirs)."""
+        c = fkv_batch.from_buffer_copy(self._c)
+        c.n_pages = n_pages
+        return ctypes.byref(c)
+
+
+def _batch(batch) -> "PagedBatch":
+    if not isinstance(batch, PagedBatch):
+        raise TypeError("batch must be a PagedBatch")
+    return batch
+
+
+def _pages(t, name: str, dtype, page_tokens: int, device: int):
+    """Pages [n_pages][n_heads][page_tokens][width], contiguous."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dim() != 4:
+        raise ValueError(f"{name} must have 4 dimensions (got shape {tuple(t.shape)})")
+    return _ptr(t, name, dtype, (t.shape[0], t.shape[1], page_tokens, t.shape[3]), device)
+
+
+def _spans(spans, n: int):
+    """A host fkv_span array from (sink_tokens, recent_tokens) pairs, recent_tokens -1 or None for all."""
+    if spans is None:
+        return None
+    if len(spans) != n:
+        raise ValueError(f"spans has {len(spans)} entries for {n} key heads")
+    arr = (fkv_span * n)()
+    for y, (sink, recent) in enumerate(spans):
+        arr[y] = fkv_span(_i32(sink, "sink_tokens"), -1 if recent is None else _i32(recent, "recent_tokens"))
+    return arr
+
+
+def fkv_append_paged(batch: PagedBatch, K_new, V_new, K_pages, V_pages, stream=None):
+    """The batch's new keys and values into their pages.  K_new, V_new: bf16 or
+    fp32 views [n_heads][n_tokens][d] with adjacent channels; K_pages, V_pages
+    [n_pages][n_heads][page_tokens][d].  V_new and V_pages None: keys (or latent
+    rows, one head) alone."""
+    b = _batch(batch)
+    if not isinstance(K_pages, torch.Tensor) or K_pages.dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError("K_pages must be a bfloat16 or float32 tensor")
+    if (V_new is None) != (V_pages is None):
+        raise ValueError("V_new and V_pages must both be given or both be None")
+    dt = K_pages.dtype
+    kp = _pages(K_pages, "K_pages", dt, b.page_tokens, b.device)
+    n_pages, heads, _, d = K_pages.shape
+    size = (heads, b.n_tokens, d)
+    vp = vn = None
+    if V_pages is not None:
+        vp = _ptr(V_pages, "V_pages", dt, K_pages.shape, b.device)
+        vn = ctypes.byref(_rows(V_new, "V_new", dt, size, b.device))
+    _run(b.device, lib().fkv_append_paged,
+         (b._arg(n_pages), heads, d, FKV_BF16 if dt is torch.bfloat16 else FKV_F32,
+          ctypes.byref(_rows(K_new, "K_new", dt, size, b.device)), vn, kp, vp), stream)
+
+
+def fkv_paged_attention_workspace_size(batch: PagedBatch, n_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    """Bytes of the workspace of fkv_paged_attention on the batch's device."""
+    out = ctypes.c_size_t(0)
+    b = _batch(batch)
+    with torch.cuda.device(b.device):
+        _raise(lib().fkv_paged_attention_workspace_size(b._arg(1), _i32(n_heads, "n_heads"), _i32(n_kv_heads, "n_kv_heads"),
+                                                        _i32(head_dim, "head_dim"), ctypes.byref(out)))
+    return int(out.value)
+
+
+def fkv_paged_attention(batch: PagedBatch, Q, K_pages, V_pages, scale: float, O, causal: bool = True, spans=None,
+                        lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """Attention of every sequence's new tokens over its pages.  Q, O: bf16
+    views [n_heads][n_tokens][d] with adjacent channels; K_pages, V_pages
+    [n_pages][n_kv_heads][page_tokens][d]; spans: per key head (sink_tokens,
+    recent_tokens), recent_tokens -1 for all, or None; lse float32
+    [n_heads][n_tokens].  ``workspace``: uint8 device tensor of
+    fkv_paged_attention_workspace_size bytes (no initialisation); None splits
+    nothing."""
+    b, bf = _batch(batch), torch.bfloat16
+    kp = _pages(K_pages, "K_pages", bf, b.page_tokens, b.device)
+    n_pages, kv, _, d = K_pages.shape
+    vp = _ptr(V_pages, "V_pages", bf, K_pages.shape, b.device)
+    n_heads = Q.shape[0] if isinstance(Q, torch.Tensor) and Q.dim() == 3 else -1
+    size = (n_heads, b.n_tokens, d)
+    q, o = _rows(Q, "Q", bf, size, b.device), _rows(O, "O", bf, size, b.device)
+    ls = ws = None
+    nws = 0
+    if lse is not None:
+        ls = _ptr(lse, "lse", torch.float32, size[:2], b.device)
+    if workspace is not None:
+        ws, nws = _ptr(workspace, "workspace", torch.uint8, getattr(workspace, "shape", None), b.device), workspace.numel()
+    _run(b.device, lib().fkv_paged_attention,
+         (b._arg(n_pages), n_heads, kv, d, ctypes.byref(q), kp, vp, int(bool(causal)), _spans(spans, kv), scale,
+          ctypes.byref(o), ls, ws, nws), stream)
+
+
+_FORMS = {"auto": FKV_LATENT_AUTO, "absorbed": FKV_LATENT_ABSORBED, "expanded": FKV_LATENT_EXPANDED}
+
+
+def _form(form) -> int:
+    if form not in _FORMS:
+        raise ValueError(f"form {form!r} is not one of {sorted(_FORMS)}")
+    return _FORMS[form]
+
+
+def fkv_latent_attention_workspace_size(batch: PagedBatch, n_heads: int, head_dim: int, latent_dim: int,
+                                        form: str = "auto") -> int:
+    """Bytes of the workspace of fkv_latent_attention on the batch's device."""
+    out = ctypes.c_size_t(0)
+    b = _batch(batch)
+    with torch.cuda.device(b.device):
+        _raise(lib().fkv_latent_attention_workspace_size(b._arg(1), _i32(n_heads, "n_heads"), _i32(head_dim, "head_dim"),
+                                                         _i32(latent_dim, "latent_dim"), _form(form), ctypes.byref(out)))
+    return int(out.value)
+
+
+def fkv_latent_attention(batch: PagedBatch, Q, pages, W_k, W_v, scale: float, O, causal: bool = True, span=None,
+                         form: str = "auto", workspace: Optional[torch.Tensor] = None, stream=None):
+    """Attention over a paged latent cache.  Q: bf16 view [n_heads][n_tokens][d +
+    64]; pages [n_pages][1][page_tokens][latent_dim + 64]; W_k, W_v
+    [n_heads][d][latent_dim]; O: bf16 view [n_heads][n_tokens][d]; span:
+    (sink_tokens, recent_tokens) or None.  form: "auto", "absorbed" or "expanded".
+    ``workspace``: uint8 device tensor of fkv_latent_attention_workspace_size
+    bytes (no initialisation); None allocates one (through torch's caching
+    allocator)."""
+    b, bf = _batch(batch), torch.bfloat16
+    pp = _pages(pages, "pages", bf, b.page_tokens, b.device)
+    n_pages, one, _, width = pages.shape
+    if one != 1:
+        raise ValueError(f"pages of a latent cache have one head (got {one})")
+    R = width - FKV_LATENT_ROT
+    n_heads, d = (W_k.shape[0], W_k.shape[1]) if isinstance(W_k, torch.Tensor) and W_k.dim() == 3 else (-1, -1)
+    wk, wv = _ptr(W_k, "W_k", bf, (n_heads, d, R), b.device), _ptr(W_v, "W_v", bf, (n_heads, d, R), b.device)
+    q = _rows(Q, "Q", bf, (n_heads, b.n_tokens, d + FKV_LATENT_ROT), b.device)
+    o = _rows(O, "O", bf, (n_heads, b.n_tokens, d), b.device)
+    if workspace is None:
+        need = fkv_latent_attention_workspace_size(b, n_heads, d, R, form)
+        with torch.cuda.stream(stream):                # (used on that stream)
+            workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=pages.device)
+    ws = _ptr(workspace, "workspace", torch.uint8, getattr(workspace, "shape", None), b.device)
+    _run(b.device, lib().fkv_latent_attention,
+         (b._arg(n_pages), n_heads, d, R, ctypes.byref(q), pp, wk, wv, int(bool(causal)),
+          None if span is None else _spans([span], 1), scale, ctypes.byref(o), _form(form), ws, workspace.numel()), stream)
 
 
 def fkv_last_error() -> str:

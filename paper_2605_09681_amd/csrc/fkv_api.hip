@@ -244,6 +244,12 @@ size_t score_bytes(const fkv_shape *shape, int n_list) {
 
 }  // namespace
 
+namespace fkv {
+fkv_status api_error(fkv_status st, const char *message) { return fail(st, "%s", message); }
+fkv_status api_ok() { return ok(); }
+fkv_status api_compute_units(int *n) { return balanced_blocks(n); }
+}  // namespace fkv
+
 extern "C" {
 
 int32_t fkv_num_segments(const fkv_shape *shape) {

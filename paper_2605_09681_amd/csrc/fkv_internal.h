@@ -260,6 +260,12 @@ struct AttnQ8Args {
     SlotTable slots;
 };
 
+// The thread's error message and status (fkv_api.hip), for entry points of other files; the
+// current device's compute units, held to a multiple of 8.
+fkv_status api_error(fkv_status st, const char *message);
+fkv_status api_ok();
+fkv_status api_compute_units(int *n);
+
 constexpr int kScoreThreads = 256;
 constexpr int kAttnRowsBf16 = 256;  // query rows per attention workgroup (bf16 MFMA kernel)
 constexpr int kAttnKeysPerTile = 64; // keys per tile of the bf16 MFMA kernel

@@ -1,0 +1,273 @@
+// k_latent.hip -- the matrix products around attention over latent rows, gfx950 MFMA.
+//
+// Absorbed form: q'_h = W_k,h^T q_h before the attention, o_h = W_v,h o'_h after it; both
+// are rounded to bf16 for the matrix units, as the queries and outputs themselves are.
+// Expanded form: k_h = W_k,h c and v_h = W_v,h c of every cached token, rounded to bf16
+// as a cache of its own keys and values would hold them.
+#include "paged.h"
+
+namespace fkv {
+namespace {
+
+using namespace paged;
+
+typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(3))) bf16x4_t lds_bf16x4_t;
+
+constexpr int NT = 256;
+
+__device__ __forceinline__ bf16x8_t frag(const u32x4 &v) { return __builtin_bit_cast(bf16x8_t, v); }
+
+__device__ __forceinline__ uint2 pack4(float x0, float x1, float x2, float x3) {
+    const uint32_t b0 = __builtin_bit_cast(uint16_t, (__bf16)x0), b1 = __builtin_bit_cast(uint16_t, (__bf16)x1);
+    const uint32_t b2 = __builtin_bit_cast(uint16_t, (__bf16)x2), b3 = __builtin_bit_cast(uint16_t, (__bf16)x3);
+    return make_uint2(b0 | (b1 << 16), b2 | (b3 << 16));
+}
+
+// q'[t][h][r] = sum_c W_k[h][c][r] q[t][h][c]: 64 latent channels of a head and 16 TM tokens a
+// workgroup, 16 channels a wave; the weights' 64 columns lie in LDS and are read transposed.  The last
+// column block copies the queries' rotated channels.  grid: x = token tile, y = head, z = column block.
+template <int D, int TM>
+__global__ __launch_bounds__(NT) void latent_absorb_kernel(LatentArgs a) {
+    __shared__ __attribute__((aligned(16))) uint16_t wt[D * 64];
+    const PagedArgs &p = a.p;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, c = lane & 15;
+    const int x = blockIdx.z, h = blockIdx.y, t0 = blockIdx.x * (16 * TM), width = a.R + kLatentRot;
+    const uint16_t *Q = p.Q + (int64_t)h * p.q_head;
+    uint16_t *out = a.q_abs + (int64_t)h * width + 64 * x;
+    if (x == 0 && h == 0 && w == 0) {
+        Seq s;
+        const bool mine = owner_of(p, lane < 16 * TM && t0 + lane < p.n_tokens ? t0 + lane : -1, &s) >= 0;
+        if (lane < 16 * TM && t0 + lane < p.n_tokens) a.owned[t0 + lane] = mine;
+    }
+    if (64 * x == a.R) {
+        for (int id = tid; id < 16 * TM * 8; id += NT) {
+            const int t = t0 + id / 8;
+            if (t < p.n_tokens)
+                *(u32x4 *)(out + (int64_t)t * p.n_heads * width + id % 8 * 8) = *(const u32x4 *)(Q + (int64_t)t * p.q_tok + D + id % 8 * 8);
+        }
+        return;
+    }
+    const uint16_t *W = a.W_k + (int64_t)h * D * a.R + 64 * x;
+#pragma unroll
+    for (int i = 0; i < D * 8 / NT; ++i) {
+        const int id = tid + i * NT, k = id / 8;
+        *(u32x4 *)(wt + k * 64 + place<8, false>(k, id % 8) * 8) = *(const u32x4 *)(W + (int64_t)k * a.R + id % 8 * 8);
+    }
+    uint2 q[TM][D / 16];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const uint16_t *row = Q + (int64_t)min(t0 + 16 * i + c, p.n_tokens - 1) * p.q_tok + 4 * g;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) q[i][k] = *(const uint2 *)(row + 16 * k);
+    }
+    __syncthreads();
+    f32x4_t acc[TM];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    const int ch = 2 * w + ((c & 3) >> 1);
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k) {
+        const int ka = 32 * k + 4 * g + (c >> 2), kc = ka + 16;
+        const bf16x4_t u = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t *)(wt + ka * 64 + place<8, false>(ka, ch) * 8 + 4 * (c & 1)));
+        const bf16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t *)(wt + kc * 64 + place<8, false>(kc, ch) * 8 + 4 * (c & 1)));
+        const bf16x8_t f = __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            const u32x4 b = {q[i][2 * k].x, q[i][2 * k].y, q[i][2 * k + 1].x, q[i][2 * k + 1].y};
+            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, frag(b), acc[i], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int t = t0 + 16 * i + c;
+        if (t < p.n_tokens)
+            *(uint2 *)(out + (int64_t)t * p.n_heads * width + 16 * w + 4 * g) = pack4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+    }
+}
+
+// o[t][h][c] = sum_r W_v[h][c][r] o'[t][h][r], for the tokens that a sequence of the launch holds:
+// 16 channels a wave, both operands straight from memory.  grid: x = token tile, y = head, z = 64 channels.
+template <int R, int TM>
+__global__ __launch_bounds__(NT) void latent_unabsorb_kernel(LatentArgs a, int D) {
+    const PagedArgs &p = a.p;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, c = lane & 15;
+    const int h = blockIdx.y, t0 = blockIdx.x * (16 * TM), c0 = 64 * blockIdx.z + 16 * w;
+    const uint16_t *W = a.W_v + ((int64_t)h * D + c0 + c) * R + 8 * g;
+    const uint16_t *row[TM];
+    f32x4_t acc[TM];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        row[i] = a.o_abs + ((int64_t)min(t0 + 16 * i + c, p.n_tokens - 1) * p.n_heads + h) * R + 8 * g;
+        acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+    constexpr int kAhead = TM == 1 ? 16 : 4;
+#pragma unroll kAhead
+    for (int k = 0; k < R / 32; ++k) {
+        const bf16x8_t f = frag(*(const u32x4 *)(W + 32 * k));
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, frag(*(const u32x4 *)(row[i] + 32 * k)), acc[i], 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int t = t0 + 16 * i + c;
+        if (t < p.n_tokens && a.owned[t])
+            *(uint2 *)(p.O + (int64_t)t * p.o_tok + (int64_t)h * p.o_head + c0 + 4 * g) = pack4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+    }
+}
+
+// Keys and values of 128 cached tokens of a sequence: 128 of the heads' 2 D channels a
+// workgroup, 64 x 64 a wave, latent channels 64 at a time through two LDS buffers.  The last column
+// block copies the tokens' rotated keys to every head.  grid: x = column block, y = token block.
+template <int D, int R>
+__global__ __launch_bounds__(NT, 2) void latent_expand_kernel(LatentArgs a) {
+    constexpr int STEP = 64, N = 128 * STEP / 8 / NT;      // chunks per thread and operand
+    __shared__ __attribute__((aligned(16))) uint16_t lat[2][128 * STEP], wts[2][128 * STEP];
+    const PagedArgs &p = a.p;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, hh = lane >> 5, c = lane & 31;
+    Seq s;
+    int i = 0;
+    const int j0 = locate_block(p, blockIdx.y, &s, &i);
+    if (j0 < 0) return;
+    const int64_t base = (int64_t)blockIdx.y * kSeqRows;
+    const int n = (int)min((int64_t)min(s.len - j0, kSeqRows), p.head_rows - base);
+    if (n <= 0) return;
+    // no new token sees these keys
+    if (p.recent[0] >= 0 && j0 >= p.sink[0] && j0 + n <= s.first - p.recent[0]) return;
+    const int32_t *pages = p.table + (int64_t)i * p.max_pages;
+    const int width = R + kLatentRot;
+    constexpr int W = D + kLatentRot;
+    const int cols = p.n_heads * 2 * D / 128;
+    // this lane's two of the block's rows
+    const int row_a = pool_row(p, pages, 0, min(j0 + lane, j0 + n - 1)), row_b = pool_row(p, pages, 0, min(j0 + 64 + lane, j0 + n - 1));
+    if ((int)blockIdx.x == cols) {
+        for (int k0 = 0; k0 < 128; k0 += NT / 8) {
+            const int k = k0 + tid / 8, r = __shfl(k & 64 ? row_b : row_a, k & 63);
+            const u32x4 v = *(const u32x4 *)(p.K + (int64_t)r * width + R + tid % 8 * 8);
+            if (k >= n) continue;
+            for (int h = 0; h < p.n_heads; ++h) *(u32x4 *)(a.K_exp + (h * p.head_rows + base + k) * W + D + tid % 8 * 8) = v;
+        }
+        return;
+    }
+    // Channel rows of the block: K's or V's of one head, or (D = 64) K's and V's.
+    const int h = blockIdx.x * 128 / (2 * D), second = blockIdx.x * 128 % (2 * D);   // second: first channel among the head's 2 D
+    const uint16_t *w0 = second ? a.W_v + (int64_t)h * D * R : a.W_k + (int64_t)h * D * R;
+    const uint16_t *w1 = D == 64 ? a.W_v + (int64_t)h * D * R : w0 + (int64_t)64 * R;
+    const uint16_t *from_l[N], *from_w[N];
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+        const int id = tid + u * NT, k = id / 8;
+        from_l[u] = p.K + (int64_t)__shfl(k & 64 ? row_b : row_a, k & 63) * width + id % 8 * 8;
+        from_w[u] = (k < 64 ? w0 : w1) + (int64_t)(k & 63) * R + id % 8 * 8;
+    }
+    u32x4 lr[N], wr[N];
+    auto load = [&](int k) {
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            lr[u] = *(const u32x4 *)(from_l[u] + k * STEP);
+            wr[u] = *(const u32x4 *)(from_w[u] + k * STEP);
+        }
+    };
+    auto store = [&](int buf) {
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int id = tid + u * NT, k = id / 8, at = k * STEP + place<8, true>(k, id % 8) * 8;
+            *(u32x4 *)(lat[buf] + at) = lr[u];
+            *(u32x4 *)(wts[buf] + at) = wr[u];
+        }
+    };
+    f32x16_t acc[2][2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int v = 0; v < 2; ++v)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[u][v][r] = 0.f;
+    const int wc = w & 1, wk = w >> 1;                     // this wave's 64 channels and 64 tokens
+    load(0);
+    store(0);
+    load(1);
+#pragma unroll 1
+    for (int k = 0; k < R / STEP; ++k) {
+        __syncthreads();
+        const int buf = k & 1;
+        if (k + 1 < R / STEP) store(buf ^ 1);
+        if (k + 2 < R / STEP) load(k + 2);
+#pragma unroll
+        for (int u = 0; u < STEP / 16; ++u) {
+            bf16x8_t fa[2], fb[2];
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+                fa[v] = frag(*(const u32x4 *)(wts[buf] + (64 * wc + 32 * v + c) * STEP + place<8, true>(c, 2 * u + hh) * 8));
+                fb[v] = frag(*(const u32x4 *)(lat[buf] + (64 * wk + 32 * v + c) * STEP + place<8, true>(c, 2 * u + hh) * 8));
+            }
+#pragma unroll
+            for (int v = 0; v < 2; ++v)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) acc[v][x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[v], fb[x], acc[v][x], 0, 0, 0);
+        }
+    }
+    const bool value = D == 64 ? wc == 1 : second != 0;
+    uint16_t *out = value ? a.V_exp : a.K_exp;
+    const int stride = value ? D : W, c0 = D == 64 ? 0 : 64 * wc;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const int k = 64 * wk + 32 * x + c;
+        if (k >= n) continue;
+        uint16_t *to = out + (h * p.head_rows + base + k) * stride + c0 + 4 * hh;
+#pragma unroll
+        for (int v = 0; v < 2; ++v)
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                *(uint2 *)(to + 32 * v + 8 * u) =
+                    pack4(acc[v][x][4 * u], acc[v][x][4 * u + 1], acc[v][x][4 * u + 2], acc[v][x][4 * u + 3]);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_latent_absorb(const LatentArgs &a, int head_dim, hipStream_t s) {
+    const bool few = a.p.n_tokens <= 32;
+    const int tile = few ? 16 : 64;
+    const dim3 grid((a.p.n_tokens + tile - 1) / tile, a.p.n_heads, a.R / 64 + 1);
+    if (head_dim == 64) {
+        if (few) hipLaunchKernelGGL((latent_absorb_kernel<64, 1>), grid, dim3(NT), 0, s, a);
+        else hipLaunchKernelGGL((latent_absorb_kernel<64, 4>), grid, dim3(NT), 0, s, a);
+    } else {
+        if (few) hipLaunchKernelGGL((latent_absorb_kernel<128, 1>), grid, dim3(NT), 0, s, a);
+        else hipLaunchKernelGGL((latent_absorb_kernel<128, 4>), grid, dim3(NT), 0, s, a);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_latent_unabsorb(const LatentArgs &a, int head_dim, hipStream_t s) {
+    const bool few = a.p.n_tokens <= 32;
+    const int tile = few ? 16 : 64;
+    const dim3 grid((a.p.n_tokens + tile - 1) / tile, a.p.n_heads, head_dim / 64);
+    if (a.R == 256) {
+        if (few) hipLaunchKernelGGL((latent_unabsorb_kernel<256, 1>), grid, dim3(NT), 0, s, a, head_dim);
+        else hipLaunchKernelGGL((latent_unabsorb_kernel<256, 4>), grid, dim3(NT), 0, s, a, head_dim);
+    } else {
+        if (few) hipLaunchKernelGGL((latent_unabsorb_kernel<512, 1>), grid, dim3(NT), 0, s, a, head_dim);
+        else hipLaunchKernelGGL((latent_unabsorb_kernel<512, 4>), grid, dim3(NT), 0, s, a, head_dim);
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_latent_expand(const LatentArgs &a, int head_dim, hipStream_t s) {
+    const dim3 grid((unsigned)(a.p.n_heads * 2 * head_dim / 128 + 1), (unsigned)(a.p.head_rows / kSeqRows));
+    if (head_dim == 64) {
+        if (a.R == 256) hipLaunchKernelGGL((latent_expand_kernel<64, 256>), grid, dim3(NT), 0, s, a);
+        else hipLaunchKernelGGL((latent_expand_kernel<64, 512>), grid, dim3(NT), 0, s, a);
+    } else {
+        if (a.R == 256) hipLaunchKernelGGL((latent_expand_kernel<128, 256>), grid, dim3(NT), 0, s, a);
+        else hipLaunchKernelGGL((latent_expand_kernel<128, 512>), grid, dim3(NT), 0, s, a);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace fkv

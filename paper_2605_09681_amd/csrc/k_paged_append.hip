@@ -1,0 +1,69 @@
+// k_paged_append.hip -- new tokens of many sequences into their pages: token t of a
+// sequence's n new ones is its token len - n + t, which lies in page table[i][p / P], row
+// p % P.  A workgroup copies up to 64 tokens of all heads, 16 bytes a lane and step; the
+// places of its tokens are worked out once, by one wave.  Bound by memory.
+#include "paged.h"
+
+namespace fkv {
+namespace {
+
+using namespace paged;
+
+constexpr int kThreads = 256, kBatch = 4;   // rows' chunks in flight per thread
+
+__global__ __launch_bounds__(kThreads) void paged_append_kernel(PagedAppendArgs a) {
+    const PagedArgs &b = a.batch;
+    __shared__ int page_of[64], row_of[64];
+    const int t0 = blockIdx.x * a.block_tokens, n = min(a.block_tokens, b.n_tokens - t0);
+    if (threadIdx.x < 64) {
+        const int lane = threadIdx.x;
+        Seq s = {0, 0, 0, 0};
+        const int i = owner_of(b, lane < n ? t0 + lane : -1, &s);
+        int page = -1, row = 0;
+        if (i >= 0) {
+            const int p = s.first + t0 + lane - s.start;
+            if (p >= 0 && p < b.cap) {
+                const int k = div_magic(p, b.mp_hi, b.mp_lo);
+                page = b.table[(int64_t)i * b.max_pages + k];
+                if (page >= b.n_pages) page = -1;        // (a page outside the pool is not written)
+                row = p - k * b.page_tokens;
+            }
+        }
+        page_of[lane] = page;
+        row_of[lane] = row;
+    }
+    __syncthreads();
+    const int total = n * a.heads * a.chunks;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        if (!a.src[w]) continue;
+        for (int id0 = threadIdx.x; id0 < total; id0 += kThreads * kBatch) {
+            u32x4 v[kBatch];
+            uint8_t *to[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const int id = id0 + k * kThreads, r = div_magic(id, a.chunks_hi, a.chunks_lo), c = id - r * a.chunks;
+                const int t = div_magic(r, a.heads_hi, a.heads_lo), h = r - t * a.heads;
+                to[k] = nullptr;
+                if (id < total && page_of[t] >= 0) {
+                    to[k] = a.dst[w] + ((((int64_t)page_of[t] * a.heads + h) * b.page_tokens + row_of[t]) * a.chunks + c) * 16;
+                    v[k] = __builtin_nontemporal_load(
+                        (const u32x4 *)(a.src[w] + (int64_t)(t0 + t) * a.tok[w] + (int64_t)h * a.head[w] + c * 16));
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k)
+                if (to[k]) *(u32x4 *)to[k] = v[k];
+        }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_paged_append(const PagedAppendArgs &a, hipStream_t s) {
+    const int groups = (a.batch.n_tokens + a.block_tokens - 1) / a.block_tokens;
+    hipLaunchKernelGGL(paged_append_kernel, dim3((unsigned)groups), dim3(kThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace fkv

@@ -1,0 +1,342 @@
+// paged.h -- the paged cache of many sequences as the kernels see it: the batch,
+// which keys a query row sees, and how the work is split over the workgroups.
+//
+// Sequence i has len tokens in the cache; its last n are new, rows start ..
+// start + n - 1 of the batch's tensors.  With `group` query heads to a key head, the
+// query rows of one key head are r = token * group + (head within the group), so heads
+// that share keys share tiles.  Lengths, starts and the page table are device data that
+// a captured graph may change between replays: every value is held to its range here, and
+// the split over workgroups is worked out from them by every wave (two short passes over
+// the sequences, 64 a step), not on the host.
+#pragma once
+
+#include "fkv_internal.h"
+
+namespace fkv {
+
+// Every tensor that the paged kernels take; also the launch's plan.
+struct PagedArgs {
+    const uint16_t *Q, *K, *V;      // rows; page pools [n_pages][kv][page_tokens][d] (or the expanded copies)
+    uint16_t *O;
+    float *lse;                     // [n_heads][n_tokens], may be NULL
+    int64_t q_tok, q_head, o_tok, o_head;   // elements
+    const int32_t *table, *seq_len, *q_start;
+    int32_t n_seqs, max_pages, page_tokens, n_pages, n_tokens, max_new, cap;   // cap: tokens that a table row holds
+    uint32_t mp_hi, mp_lo;          // floor(2^64 / page_tokens) + 1 (0 for 1)
+    int32_t n_heads, kv, group;
+    int32_t causal;
+    float scale_log2;               // scale * log2(e), finite
+    // The launch takes the sequences with lo <= new tokens <= hi.
+    int32_t lo, hi;
+    int32_t target;                 // workgroups to split for; 0: no workspace, no split
+    int32_t min_tiles;              // key tiles that a part is worth
+    int32_t n_work, n_slots;        // workgroups launched, slots in `part`
+    float *part;
+    int32_t join_tokens;            // tokens per workgroup of the join
+    int32_t wide;                   // the most keys outside the new tokens that a head sees; < 0: all
+    int64_t head_rows;              // expanded copies: rows per head
+    int32_t sink[FKV_MAX_HEADS], recent[FKV_MAX_HEADS];   // per key head; recent < 0: every key
+};
+
+constexpr int kLatentRot = FKV_LATENT_ROT;
+
+// Attention of rows-per-tile (16, 32, 64) query rows, its parts joined (k_paged_attn.hip).
+hipError_t launch_paged_attention(const PagedArgs &a, int head_dim, int rows, hipStream_t s);
+hipError_t launch_latent_rows(const PagedArgs &a, int latent_dim, int rows, hipStream_t s);
+// Attention of tiles of kPagedTileRows query rows, its parts joined (k_paged_tile.hip).
+constexpr int kPagedTileRows = 128;
+hipError_t launch_paged_tiles(const PagedArgs &a, int head_dim, hipStream_t s);
+hipError_t launch_expanded_tiles(const PagedArgs &a, int head_dim, hipStream_t s);
+inline int paged_row_tile(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+
+// Rows into the pages (k_paged_append.hip).
+struct PagedAppendArgs {
+    const uint8_t *src[2];          // keys, values (NULL: left out)
+    uint8_t *dst[2];                // pools [n_pages][heads][page_tokens][row]
+    int64_t tok[2], head[2];        // bytes
+    int32_t heads, chunks;          // 16-byte chunks per row
+    uint32_t chunks_hi, chunks_lo, heads_hi, heads_lo;   // magic, as mp_hi, mp_lo
+    int32_t block_tokens;           // tokens per workgroup, at most 64
+    PagedArgs batch;                // its batch fields
+};
+hipError_t launch_paged_append(const PagedAppendArgs &a, hipStream_t s);
+
+// Latent attention's products (k_latent.hip).
+struct LatentArgs {
+    PagedArgs p;                    // Q: the caller's rows, K: the latent pool, O: the caller's output
+    const uint16_t *W_k, *W_v;      // [n_heads][d][R]
+    int32_t R;
+    uint16_t *q_abs;                // absorbed: [n_tokens][n_heads][R + 64]
+    uint16_t *o_abs;                // absorbed: [n_tokens][n_heads][R]
+    int32_t *owned;                 // absorbed: [n_tokens], 1 where a sequence of the launch holds the token
+    uint16_t *K_exp, *V_exp;        // expanded: [n_heads][head_rows][d + 64], [n_heads][head_rows][d]
+};
+hipError_t launch_latent_absorb(const LatentArgs &a, int head_dim, hipStream_t s);
+hipError_t launch_latent_unabsorb(const LatentArgs &a, int head_dim, hipStream_t s);
+hipError_t launch_latent_expand(const LatentArgs &a, int head_dim, hipStream_t s);
+
+namespace paged {
+
+constexpr int kSeqRows = 128;       // rows of the expanded copies are dealt to sequences in these
+
+__device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
+
+// j / P for 0 <= j < 2^31 with floor(2^64 / P) + 1 = hi * 2^32 + lo (0 for P = 1).
+__device__ __forceinline__ int div_magic(int j, uint32_t hi, uint32_t lo) {
+    if (hi == 0 && lo == 0) return j;
+    return (int)(((uint64_t)(uint32_t)j * hi + __umulhi((uint32_t)j, lo)) >> 32);
+}
+
+struct Seq {
+    int len, start, n, first;       // first: position of the first new token (negative: more new tokens than tokens)
+};
+
+__device__ __forceinline__ Seq sequence(const PagedArgs &a, int i) {
+    Seq s = {0, 0, 0, 0};
+    if (i < a.n_seqs) {
+        s.len = min(max(a.seq_len[i], 0), a.cap);
+        s.start = min(max(a.q_start[i], 0), a.n_tokens);
+        const int n = min(max(a.q_start[i + 1], s.start), a.n_tokens) - s.start;
+        s.n = min(n, a.max_new);
+        s.first = s.len - n;
+    }
+    return s;
+}
+
+// Which keys of a sequence the query rows of a token see: j < end and (j < sink or j >= low).
+struct Sight {
+    int end, low;
+};
+__device__ __forceinline__ Sight sight(const PagedArgs &a, const Seq &s, int recent, int token) {
+    const int p = a.causal ? s.first + token : s.first;
+    return Sight{a.causal ? min(p + 1, s.len) : s.len, recent < 0 ? 0 : p - recent};
+}
+__device__ __forceinline__ bool sees(const Sight &v, int sink, int j) { return j < v.end && (j < sink || j >= v.low); }
+
+// The key tiles that tokens t0 .. t1 of a sequence visit: [0, a_tiles) and, from tile
+// b_first on, the others; KT keys each.
+struct Tiles {
+    int a_tiles, b_first, n;
+    Sight least, most;              // what every row of the tile sees at the least, and some row at the most
+    __device__ __forceinline__ int key(int t, int kt) const { return (t < a_tiles ? t : b_first + t - a_tiles) * kt; }
+};
+template <int KT>
+__device__ __forceinline__ Tiles tiles_of(const PagedArgs &a, const Seq &s, int sink, int recent, int t0, int t1) {
+    const Sight f = sight(a, s, recent, t0), l = sight(a, s, recent, t1);
+    Tiles x;
+    x.least = Sight{f.end, l.low};
+    x.most = Sight{l.end, f.low};
+    const int end = (max(l.end, 0) + KT - 1) / KT, low = min(max(f.low, 0) / KT, end);
+    x.b_first = low;
+    x.a_tiles = min((min(sink, max(l.end, 0)) + KT - 1) / KT, low);
+    x.n = x.a_tiles + end - low;
+    return x;
+}
+// Keys j0 .. j0 + KT - 1 are seen by every row.
+template <int KT>
+__device__ __forceinline__ bool all_seen(const Tiles &x, int sink, int j0) {
+    return j0 + KT <= x.least.end && (j0 + KT <= sink || j0 >= x.least.low);
+}
+
+// One workgroup's work: part `part` of `parts` of row tile rt of key head y of a sequence.
+struct Work {
+    Seq s;
+    int i;                          // the sequence
+    int y, rt, part, parts;
+    int slot;                       // of the item's part 0; the next part's is `step` further
+    int step;
+    int64_t base;                   // the sequence's first row in the expanded copies
+    bool ok;
+};
+
+// The launch's split: keys are dealt in parts of at least part_tiles tiles, about `target`
+// parts in all; where there are as many items as that, only items of more than twice the
+// share are cut.  A sequence's items are all cut alike, its parts dealt evenly over each item's tiles.
+struct Split {
+    float part_tiles;
+    template <int ROWS, int KT>
+    static __device__ __forceinline__ void counts(const PagedArgs &a, const Seq &s, int *rts, int *tiles) {
+        const bool mine = s.n > 0 && s.n >= a.lo && s.n <= a.hi;
+        *rts = mine ? (int)(((int64_t)s.n * a.group + ROWS - 1) / ROWS) : 0;
+        const int64_t keys = a.wide < 0 ? s.len : min((int64_t)s.len, (int64_t)a.wide + s.n + 2 * KT);
+        *tiles = max((int)((keys + KT - 1) / KT), 1);
+    }
+    template <int ROWS, int KT>
+    static __device__ __forceinline__ Split make(const PagedArgs &a) {
+        const int lane = threadIdx.x & 63;
+        float sum = 0.f, items = 0.f;
+        for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
+            int rts, tiles;
+            counts<ROWS, KT>(a, sequence(a, i0 + lane), &rts, &tiles);
+            sum += (float)rts * (float)tiles;
+            items += (float)rts;
+        }
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) {
+            sum += __shfl_xor(sum, d);
+            items += __shfl_xor(items, d);
+        }
+        const float share = ceilf(sum * (float)a.kv / (float)a.target);
+        return Split{fmaxf((float)a.min_tiles, items * (float)a.kv >= (float)a.target ? 2.f * share : share)};
+    }
+    __device__ __forceinline__ int parts(const PagedArgs &a, int tiles) const {
+        return a.target > 0 ? max((int)ceilf((float)tiles / part_tiles), 1) : 1;
+    }
+};
+
+// Looks for work item `want` (token < 0), or for the sequence that holds batch row `token`.
+// Every lane of a wave calls it; the result is the same in all.
+template <int ROWS, int KT>
+__device__ __forceinline__ Work locate(const PagedArgs &a, int want, int token) {
+    const int lane = threadIdx.x & 63;
+    const Split split = a.target > 0 ? Split::make<ROWS, KT>(a) : Split{0.f};
+    Work w;
+    w.ok = false;
+    int done = 0, slots = 0;
+    int64_t rows = 0;
+    for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
+        const Seq s = sequence(a, i0 + lane);
+        int rts, tiles;
+        Split::counts<ROWS, KT>(a, s, &rts, &tiles);
+        const int parts = split.parts(a, tiles), c = a.kv * rts * parts, cut = parts > 1 ? c : 0;
+        const int blocks = rts > 0 ? (s.len + kSeqRows - 1) / kSeqRows : 0;
+        int ic = c, is = cut, ib = blocks;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int uc = __shfl_up(ic, d), us = __shfl_up(is, d), ub = __shfl_up(ib, d);
+            if (lane >= d) {
+                ic += uc;
+                is += us;
+                ib += ub;
+            }
+        }
+        const uint64_t found = token < 0 ? __ballot(done + ic > want)
+                                         : __ballot(rts > 0 && token >= s.start && token - s.start < s.n);
+        if (found) {
+            const int l = __builtin_ctzll(found);
+            auto at = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+            w.i = i0 + l;
+            w.s = Seq{at(s.len), at(s.start), at(s.n), at(s.first)};
+            const int rt = at(rts), first = done + at(ic) - at(c);
+            w.parts = at(parts);
+            w.step = a.kv * rt;
+            w.base = (rows + at(ib) - at(blocks)) * kSeqRows;
+            const int slot = slots + at(is) - at(cut);
+            if (token < 0) {
+                const int local = want - first;
+                w.part = local / w.step;
+                const int u = local - w.part * w.step;
+                w.y = u / rt;
+                w.rt = rt - 1 - (u - w.y * rt);          // the longest rows of a causal chunk first
+                w.slot = slot + u;
+            } else {
+                w.part = 0;
+                w.y = w.rt = 0;
+                w.slot = slot;                           // of key head 0's last row tile
+            }
+            w.ok = true;
+            return w;
+        }
+        done += __builtin_amdgcn_readlane(ic, 63);
+        slots += __builtin_amdgcn_readlane(is, 63);
+        rows += __builtin_amdgcn_readlane(ib, 63);
+    }
+    return w;
+}
+
+// The sequence that holds this lane's batch row `token` (-1: none, or not one of the launch's), and the
+// sequence.  Every lane of a wave calls it.
+__device__ __forceinline__ int owner_of(const PagedArgs &a, int token, Seq *held) {
+    const int lane = threadIdx.x & 63;
+    int owner = -1;
+    for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
+        const Seq s = sequence(a, i0 + lane);
+        const int n = s.n >= a.lo && s.n <= a.hi ? s.n : 0, count = min(64, a.n_seqs - i0);
+        for (int l = 0; l < count; ++l) {
+            const int start = __builtin_amdgcn_readlane(s.start, l), m = __builtin_amdgcn_readlane(n, l);
+            if (owner < 0 && token >= start && token - start < m) {
+                owner = i0 + l;
+                *held = Seq{__builtin_amdgcn_readlane(s.len, l), start, m, __builtin_amdgcn_readlane(s.first, l)};
+            }
+        }
+    }
+    return owner;
+}
+
+// Block `want` of kSeqRows rows of the expanded copies: the sequence, its number in *seq, and the
+// block's first key (-1: no such block).
+__device__ __forceinline__ int locate_block(const PagedArgs &a, int want, Seq *held, int *seq) {
+    const int lane = threadIdx.x & 63;
+    int done = 0;
+    for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
+        const Seq s = sequence(a, i0 + lane);
+        const int blocks = s.n > 0 && s.n >= a.lo && s.n <= a.hi ? (s.len + kSeqRows - 1) / kSeqRows : 0;
+        int ib = blocks;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int u = __shfl_up(ib, d);
+            if (lane >= d) ib += u;
+        }
+        const uint64_t found = __ballot(done + ib > want);
+        if (found) {
+            const int l = __builtin_ctzll(found);
+            auto at = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+            *held = Seq{at(s.len), at(s.start), at(s.n), at(s.first)};
+            *seq = i0 + l;
+            return (want - done - at(ib) + at(blocks)) * kSeqRows;
+        }
+        done += __builtin_amdgcn_readlane(ib, 63);
+    }
+    return -1;
+}
+
+// Row of the page pools that holds key j of sequence i (0 <= j < len); a page outside the pool
+// is held to it.
+__device__ __forceinline__ int pool_row(const PagedArgs &a, const int32_t *pages, int y, int j) {
+    const int b = div_magic(j, a.mp_hi, a.mp_lo);
+    const int page = min(max(pages[b], 0), a.n_pages - 1);
+    return (page * a.kv + y) * a.page_tokens + (j - b * a.page_tokens);
+}
+
+// Chunk (16 bytes) c of row k of a tile in LDS lies at chunk place(k, c) of the row: rows that
+// are read together then fall into distinct banks.  CH: chunks per row.  KEYS: rows read one to a
+// lane, the same chunk of each (the score operand, and rows that serve both products);
+// otherwise read four at a time, transposed (the value operand).
+template <int CH, bool KEYS>
+__device__ __forceinline__ int place(int k, int c) {
+    if (CH % 16 == 0) return c ^ (KEYS ? (k & 15) : ((k & 3) << 2 | (k >> 2 & 3)));
+    return c ^ (KEYS ? (k >> 1 & 7) : ((k >> 1 & 1) << 2 | (k >> 2 & 3)));
+}
+
+// Any of the 8 bf16 of v is an infinity or a NaN.
+__device__ __forceinline__ bool special(const u32x4 &v) {
+    bool s = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s |= (v[i] & 0x7f80u) == 0x7f80u || (v[i] & 0x7f800000u) == 0x7f800000u;
+    return s;
+}
+
+// The 8 bf16 of v with 0 for infinities and NaNs; and the reverse, for one value.
+__device__ __forceinline__ u32x4 finite_only(u32x4 v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        v[i] = ((v[i] & 0x7f80u) == 0x7f80u ? 0u : v[i] & 0xffffu) | ((v[i] & 0x7f800000u) == 0x7f800000u ? 0u : v[i] & 0xffff0000u);
+    return v;
+}
+__device__ __forceinline__ float special_only(uint32_t bits) { return (bits & 0x7f80u) == 0x7f80u ? __uint_as_float(bits << 16) : 0.f; }
+
+// Whether any thread of the workgroup says so; every thread calls it.  flag: LDS that is otherwise free
+// (__syncthreads_or takes LDS of its own, with which two workgroups no longer share a CU).
+__device__ __forceinline__ bool any_of(bool mine, int *flag) {
+    __syncthreads();
+    if (threadIdx.x == 0) *flag = 0;
+    __syncthreads();
+    if (mine) *flag = 1;
+    __syncthreads();
+    const bool any = *flag != 0;
+    __syncthreads();
+    return any;
+}
+
+}  // namespace paged
+}  // namespace fkv
