@@ -1,23 +1,28 @@
 // k_paged_attn.hip -- attention of few new tokens of many sequences over paged caches,
 // gfx950 MFMA: single tokens and short chunks (up to 64 query rows of a sequence and key
-// head), with keys and values of their own or, SHARED, with values that are the first DV
-// channels of the key rows (latent rows: all heads read one row).
+// head, or any number over latent rows), with keys and values of their own or, SHARED,
+// with values that are the first DV channels of the key rows (latent rows: all heads
+// read one row).
 //
 //   o = sum_j 2^(c (s_j - m)) v_j / sum_j 2^(c (s_j - m)),  s_j = q . k_j,  c = scale log2 e
 //
 // A workgroup takes one part of an item (sequence, key head, tile of 16 MT query rows)
 // and walks its keys 32 at a time.  The NW waves share each tile of keys, which is read
 // from HBM once and lies in LDS, three tiles deep:
-//   scores   S^T = K Q^T (v_mfma_f32_16x16x32_bf16): the tile's 2 x MT blocks, and
-//            shares of the channels where there are more waves than blocks, are dealt to
-//            the waves; the blocks meet in LDS as fp32;
-//   softmax  every wave forms the probabilities of all rows from there, so that no wave
-//            waits for another's: running maximum and sum in fp32;
+//   scores   S^T = K Q^T (v_mfma_f32_16x16x32_bf16): the tile's 2 x MT blocks of 16 keys
+//            and 16 rows are dealt to the waves, which turn theirs into probabilities
+//            and put those into LDS (bf16; the sum adds them before they are rounded);
 //   values   O^T += V^T P^T: each wave owns DV / NW output channels of all rows (V^T
-//            through the LDS transpose read, P straight from the softmax's registers).
+//            through the LDS transpose read).
 // The scores of tile t + 1 and the values of tile t run in the same stretch between two
 // barriers, one barrier a tile; tile t + 3 is on its way from HBM meanwhile.
-// Probabilities are rounded to bf16 for the value product, the sum adds them before.
+//
+// m is not the maximum but the largest score of the part's first tile: any reference
+// cancels in the quotient, and probabilities above one are as exact in fp32 and bf16 as
+// those below, so nothing waits for other waves' scores.  Where a row's sum leaves
+// [2^-100, 2^100] or an output is not finite, and where an infinity or a NaN lies among
+// values that only some rows see, the part is computed again, tile by tile with a running
+// maximum (`careful`).
 #include <type_traits>
 
 #include "paged_join.h"
@@ -33,7 +38,7 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) bf16x4_t lds_bf16x4_t;
 
 constexpr int KT = 32;              // keys per tile
-constexpr float kSlack = 8.f;       // log2 units that the softmax's reference may lag behind
+constexpr float kFar = 0x1p10f;     // log2 units from which scores are subtracted before they are scaled
 constexpr float kLn2 = 0.69314718055994530942f;
 
 
@@ -51,24 +56,24 @@ struct Cfg {
     static constexpr int ROWS = 16 * MT, NT = 64 * NW;
     static constexpr int CK = DQK / 8, CV = DV / 8;                  // 16-byte chunks per row
     static constexpr int BLOCKS = 2 * MT;                            // 16 x 16 score blocks of a tile
+    static constexpr int PER = (BLOCKS + NW - 1) / NW;               // of a wave: w, w + NW (all of one key block)
     static constexpr int KS = DQK / 32;                              // steps of the score product
-    static constexpr int SHARES = NW > BLOCKS ? NW / BLOCKS : 1;     // of the channels, per block
-    static constexpr int PER = BLOCKS > NW ? BLOCKS / NW : 1;        // blocks per wave
-    static constexpr int STEPS = (KS + SHARES - 1) / SHARES;
     static constexpr int NB = DV / 16 / NW;                          // 16-channel blocks of a wave's output
     static constexpr int NK = (KT * CK + NT - 1) / NT, NV = SHARED ? 0 : (KT * CV + NT - 1) / NT;   // chunks per thread
     static constexpr int TILE = KT * (DQK + (SHARED ? 0 : DV));      // elements
-    static constexpr int SS = KT + 4;                                // floats per row of scores: 16 rows in distinct banks
-    static constexpr int SCORES = SHARES * ROWS * SS;
-    static_assert(DV % (16 * NW) == 0 && KT * CV % NT == 0, "whole blocks and chunks");
+    static constexpr int SS = KT + 4;                                // careful: floats per row of scores (16 rows in distinct banks)
+    static_assert(DV % (16 * NW) == 0 && KT * CV % NT == 0 && NW % 2 == 0, "whole blocks and chunks");
 };
 
 template <int DQK, int DV, bool SHARED, int MT, int NW>
 __global__ __launch_bounds__(64 * NW) void paged_attn_kernel(PagedArgs a) {
     using C = Cfg<DQK, DV, SHARED, MT, NW>;
     __shared__ __attribute__((aligned(16))) uint16_t tiles[3][C::TILE];
-    __shared__ __attribute__((aligned(16))) float scores[2][C::SCORES];
+    // probabilities [2][MT][lane][key block] x 4 bf16; careful: scores [row][SS]
+    __shared__ __attribute__((aligned(16))) float mix[C::ROWS * C::SS];
+    __shared__ float ends[3][MT][2][16];         // per row and key block: first tile's largest scores, sums, whether a key was seen
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
+    static_assert(2 * MT * 64 * 16 <= sizeof mix, "two tiles' probabilities fit");
 
     const Work item = locate<C::ROWS, KT>(a, blockIdx.x, -1);
     if (!item.ok) return;
@@ -79,46 +84,28 @@ __global__ __launch_bounds__(64 * NW) void paged_attn_kernel(PagedArgs a) {
     const Tiles x = tiles_of<KT>(a, s, sink, recent, t_first, t_last);
     const int tb = (int)((int64_t)x.n * item.part / item.parts), te = (int)((int64_t)x.n * (item.part + 1) / item.parts);
     const int32_t *pages = a.table + (int64_t)item.i * a.max_pages;
+    auto row_of = [&](int r) { return min(r, rows - 1) + r0; };
 
-    // This lane's query rows (row 16 t + c).
-    Sight seen[MT];
-    int64_t q_at[MT], o_at[MT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        const int r = min(16 * t + c, rows - 1) + r0, tok = r / a.group, head = y * a.group + r - tok * a.group;
-        seen[t] = sight(a, s, recent, tok);
-        q_at[t] = (int64_t)(s.start + tok) * a.q_tok + (int64_t)head * a.q_head;
-        o_at[t] = (int64_t)(s.start + tok) * a.o_tok + (int64_t)head * a.o_head;
-    }
-
-    // Score blocks of this wave: key block kb of row tiles mt0 + (NW / 2) i, channel steps k0 .. k1 - 1.
-    const int kb = w & 1, mt0 = C::SHARES > 1 ? (w >> 1) % MT : w >> 1, share = C::SHARES > 1 ? (w >> 1) / MT : 0;
-    const int k0 = C::KS * share / C::SHARES, k1 = C::KS * (share + 1) / C::SHARES;
-    bf16x8_t q[C::PER][C::STEPS];
+    // Score blocks of this wave: key block kb of row tiles mt_of(0), mt_of(1).
+    const int kb = w & 1;
+    auto mt_of = [&](int i) { return (w + NW * i) >> 1; };
+    auto mine = [&](int i) { return C::BLOCKS % NW == 0 || w + NW * i < C::BLOCKS; };
+    bf16x8_t q[C::PER][C::KS];
+    Sight seen[C::PER];
 #pragma unroll
     for (int i = 0; i < C::PER; ++i) {
-        const int mt = mt0 + NW / 2 * i;
-        int64_t at = q_at[0];
+        const int r = row_of(16 * mt_of(i) + c), tok = r / a.group, head = y * a.group + r - tok * a.group;
+        const uint16_t *from = a.Q + (int64_t)(s.start + tok) * a.q_tok + (int64_t)head * a.q_head + 8 * g;
+        seen[i] = sight(a, s, recent, tok);
 #pragma unroll
-        for (int t = 1; t < MT; ++t) at = mt == t ? q_at[t] : at;
-#pragma unroll
-        for (int k = 0; k < C::STEPS; ++k)
-            q[i][k] = frag(k0 + k < k1 && 16 * mt + c < rows ? *(const u32x4 *)(a.Q + at + 32 * (k0 + k) + 8 * g) : u32x4{0, 0, 0, 0});
+        for (int k = 0; k < C::KS; ++k)
+            q[i][k] = frag(mine(i) && 16 * mt_of(i) + c < rows ? *(const u32x4 *)(from + 32 * k) : u32x4{0, 0, 0, 0});
     }
-
     f32x4_t o[MT][C::NB];
-    float m[MT], l[MT];
-    auto clear = [&]() {
 #pragma unroll
-        for (int t = 0; t < MT; ++t) {
-            m[t] = neg_inf();
-            l[t] = 0.f;
+    for (int t = 0; t < MT; ++t)
 #pragma unroll
-            for (int b = 0; b < C::NB; ++b) o[t][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        }
-    };
-    clear();
-    bool odd = false;                            // an infinity or a NaN among values that not every row sees
+        for (int b = 0; b < C::NB; ++b) o[t][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
     // Pool rows of a tile's keys, one to a lane (both halves of the wave hold the same 32);
     // keys past the last that a row sees take its place.
@@ -137,124 +124,112 @@ __global__ __launch_bounds__(64 * NW) void paged_attn_kernel(PagedArgs a) {
             vr[i] = *(const u32x4 *)(a.V + (int64_t)__shfl(row_of_lane, k) * DV + (id - k * C::CV) * 8);
         }
     };
+    bool odd = false;                            // an infinity or a NaN among values that not every row sees
     auto store = [&](int t) {
         const int j0 = x.key(t, KT);
-        const bool edge = !all_seen<KT>(x, sink, j0);
         uint16_t *kt = tiles[t % 3], *vt = kt + KT * DQK;
-        // (values of keys that no row sees are cleared, a probability of zero would not silence a NaN)
-        auto clean = [&](u32x4 &v, int k) {
-            if (!sees(x.most, sink, j0 + k)) v = u32x4{0, 0, 0, 0};
-            odd |= special(v);
-        };
+        if (!all_seen<KT>(x, sink, j0)) {
+            // (values of keys that no row sees are cleared: a probability of zero would not silence a NaN)
+            if (SHARED) {
+#pragma unroll
+                for (int i = 0; i < C::NK; ++i) {
+                    if (!sees(x.most, sink, j0 + (tid + i * C::NT) / C::CK)) kr[i] = u32x4{0, 0, 0, 0};
+                    odd |= special(kr[i]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < C::NV; ++i) {
+                if (!sees(x.most, sink, j0 + (tid + i * C::NT) / C::CV)) vr[i] = u32x4{0, 0, 0, 0};
+                odd |= special(vr[i]);
+            }
+        }
 #pragma unroll
         for (int i = 0; i < C::NK; ++i) {
             const int id = tid + i * C::NT, k = id / C::CK;
-            if (SHARED && edge) clean(kr[i], k);
-            if (id < KT * C::CK) *(u32x4 *)(kt + k * DQK + place<C::CK, true>(k, id - k * C::CK) * 8) = kr[i];
+            if (KT * C::CK % C::NT == 0 || id < KT * C::CK) *(u32x4 *)(kt + k * DQK + place<C::CK, true>(k, id - k * C::CK) * 8) = kr[i];
         }
 #pragma unroll
         for (int i = 0; i < C::NV; ++i) {
             const int id = tid + i * C::NT, k = id / C::CV;
-            if (edge) clean(vr[i], k);
             *(u32x4 *)(vt + k * DV + place<C::CV, false>(k, id - k * C::CV) * 8) = vr[i];
         }
     };
+    // This wave's blocks of a tile's scores, two sums each so that half as many products wait for one another.
+    f32x4_t z[C::PER];
+    const bool busy = C::BLOCKS >= NW || w < C::BLOCKS;
     auto score = [&](int t) {
+        if (!busy) return;
         const uint16_t *kt = tiles[t % 3] + (16 * kb + c) * DQK;
-        f32x4_t z[C::PER];
+        f32x4_t u[C::PER];
 #pragma unroll
-        for (int i = 0; i < C::PER; ++i) z[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < C::PER; ++i) z[i] = u[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < C::STEPS; ++k) {
-            if (C::KS % C::SHARES && k0 + k >= k1) break;
-            const bf16x8_t f = frag(*(const u32x4 *)(kt + place<C::CK, true>(16 * kb + c, 4 * (k0 + k) + g) * 8));
+        for (int k = 0; k < C::KS; ++k) {
+            const bf16x8_t f = frag(*(const u32x4 *)(kt + place<C::CK, true>(16 * kb + c, 4 * k + g) * 8));
 #pragma unroll
-            for (int i = 0; i < C::PER; ++i) z[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, q[i][k], z[i], 0, 0, 0);
+            for (int i = 0; i < C::PER; ++i) {
+                f32x4_t &to = k & 1 ? u[i] : z[i];
+                to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, q[i][k], to, 0, 0, 0);
+            }
         }
-        float *to = scores[t & 1] + share * (C::ROWS * C::SS) + c * C::SS + 16 * kb + 4 * g;
 #pragma unroll
-        for (int i = 0; i < C::PER; ++i) *(f32x4_t *)(to + 16 * (mt0 + NW / 2 * i) * C::SS) = z[i];
+        for (int i = 0; i < C::PER; ++i) z[i] += u[i];
     };
-    // CAREFUL: where a value is an infinity or a NaN, only the rows that see it get it (a probability of
-    // zero times it would be a NaN).
-    auto values = [&](int t, auto careful) {
-        constexpr bool CAREFUL = decltype(careful)::value;
-        const int j0 = x.key(t, KT);
-        const bool edge = !all_seen<KT>(x, sink, j0);
-        bf16x8_t p[MT];
+    float ref[C::PER], cm[C::PER], l[C::PER];    // the reference, times scale_log2 (0: taken from the scores before), the sums
+    bool far = false, met[C::PER];               // met: a key of the row's was seen
+    auto probabilities = [&](int t) {
+        if (!busy) return;
+        const int j0 = x.key(t, KT) + 16 * kb + 4 * g;
+        const bool edge = !all_seen<KT>(x, sink, x.key(t, KT));
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            f32x4_t z[2];
+        for (int i = 0; i < C::PER; ++i) {
+            if (far) z[i] -= ref[i];
+            f32x4_t e;
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const float *from = scores[t & 1] + (16 * i + c) * C::SS + 16 * u + 4 * g;
-                z[u] = *(const f32x4_t *)from;
-#pragma unroll
-                for (int h = 1; h < C::SHARES; ++h) z[u] += *(const f32x4_t *)(from + h * (C::ROWS * C::SS));
-                if (edge) {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) z[u][r] = sees(seen[i], sink, j0 + 16 * u + 4 * g + r) ? z[u][r] : neg_inf();
-                }
-            }
-            float top = neg_inf();
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) top = fmaxf(top, z[u][r]);
-            // The reference moves only where a score passes it by more than kSlack (probabilities up
-            // to 2^kSlack lose no digit).  Scores are subtracted before they are scaled: the difference of
-            // nearby scores is exact whatever their size.
-            if (__ballot((top - m[i]) * a.scale_log2 > kSlack)) {
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(top, __shfl_xor(top, 32));
-                const float next = (top - m[i]) * a.scale_log2 > kSlack ? top : m[i];
-                const float alpha = next == m[i] ? 1.f : __builtin_amdgcn_exp2f((m[i] - next) * a.scale_log2);
-                m[i] = next;
-                l[i] *= alpha;
-#pragma unroll
-                for (int b = 0; b < C::NB; ++b) o[i][b] *= alpha;
-            }
-            const float base = m[i] == neg_inf() ? 0.f : m[i];
-            float sum = 0.f;
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int r = 0; r < 4; ++r) e[r] = __builtin_amdgcn_exp2f(fmaf(z[i][r], a.scale_log2, -cm[i]));
+            if (edge) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const float e = __builtin_amdgcn_exp2f((z[u][r] - base) * a.scale_log2);
-                    sum += e;
-                    p[i][4 * u + r] = (__bf16)e;
+                    const bool see = sees(seen[i], sink, j0 + r);
+                    e[r] = see ? e[r] : 0.f;
+                    met[i] |= see;
                 }
-            l[i] += sum;
+            } else {
+                met[i] = true;
+            }
+            l[i] += (e[0] + e[1]) + (e[2] + e[3]);
+            if (mine(i)) ((uint2 *)mix)[(((t & 1) * MT + mt_of(i)) * 64 + lane) * 2 + kb] = pack4(e);
         }
+    };
+    // V^T of keys 4 g + 0..3 and + 16, 16 channels: the places of this lane's reads.
+    constexpr int D = SHARED ? DQK : DV, CH = D / 8;
+    const int ka = 4 * g + (c >> 2);
+    auto value = [&](int t, int b) {
         const uint16_t *vt = tiles[t % 3] + (SHARED ? 0 : KT * DQK);
-        constexpr int D = SHARED ? DQK : DV, CH = D / 8;
-        const int ka = 4 * g + (c >> 2), kc = ka + 16;
+        const int ch = 2 * (w * C::NB + b) + ((c & 3) >> 1);
+        const bf16x4_t u = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t *)(vt + ka * D + place<CH, SHARED>(ka, ch) * 8 + 4 * (c & 1)));
+        const bf16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t *)(vt + (ka + 16) * D + place<CH, SHARED>(ka + 16, ch) * 8 + 4 * (c & 1)));
+        return __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    auto values = [&](int t) {
+        bf16x8_t p[MT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) p[i] = frag(((const u32x4 *)mix)[((t & 1) * MT + i) * 64 + lane]);
 #pragma unroll
         for (int b = 0; b < C::NB; ++b) {
-            const int ch = 2 * (w * C::NB + b) + ((c & 3) >> 1);
-            const bf16x4_t u = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t *)(vt + ka * D + place<CH, SHARED>(ka, ch) * 8 + 4 * (c & 1)));
-            const bf16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t *)(vt + kc * D + place<CH, SHARED>(kc, ch) * 8 + 4 * (c & 1)));
-            bf16x8_t f = __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7);
-            if (CAREFUL) f = frag(finite_only(__builtin_bit_cast(u32x4, f)));
+            const bf16x8_t f = value(t, b);
 #pragma unroll
             for (int i = 0; i < MT; ++i) o[i][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, p[i], o[i][b], 0, 0, 0);
         }
-        if (CAREFUL) {                           // (any weight leaves them as they are)
-#pragma unroll 1
-            for (int k = 0; k < KT; ++k) {
-#pragma unroll
-                for (int b = 0; b < C::NB; ++b) {
-                    const uint2 v = *(const uint2 *)(vt + k * D + place<CH, SHARED>(k, 2 * (w * C::NB + b) + (g >> 1)) * 8 + 4 * (g & 1));
-                    const f32x4_t add = {special_only(v.x & 0xffffu), special_only(v.x >> 16), special_only(v.y & 0xffffu), special_only(v.y >> 16)};
-#pragma unroll
-                    for (int i = 0; i < MT; ++i)
-                        if (sees(seen[i], sink, j0 + k)) o[i][b] += add;
-                }
-            }
-        }
     };
 
-    auto walk = [&](auto careful) {
+    float m_row[MT], l_row[MT];                  // of rows 16 t + c, in every wave
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        m_row[t] = neg_inf();
+        l_row[t] = 0.f;
+    }
+    if (tb < te) {
         int next = rows_of(tb);
         load(next);
         next = rows_of(tb + 1);
@@ -266,49 +241,160 @@ __global__ __launch_bounds__(64 * NW) void paged_attn_kernel(PagedArgs a) {
         if (tb + 1 < te) store(tb + 1);
         if (tb + 2 < te) load(next);
         next = rows_of(tb + 3);
+#pragma unroll
+        for (int i = 0; i < C::PER; ++i) {       // (masked keys too: any score is a reference)
+            float top = fmaxf(fmaxf(z[i][0], z[i][1]), fmaxf(z[i][2], z[i][3]));
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            if (g == 0 && mine(i)) ends[0][mt_of(i)][kb][c] = top;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < C::PER; ++i) {
+            const int mt = mine(i) ? mt_of(i) : 0;
+            ref[i] = fmaxf(ends[0][mt][0][c], ends[0][mt][1][c]);
+            ref[i] = fabsf(ref[i]) < __builtin_inff() ? ref[i] : 0.f;
+            cm[i] = ref[i] * a.scale_log2;
+            // below kFar the rounding of cm is 2^-14 log2 units at most; beyond, scores are subtracted before they
+            // are scaled (of nearby scores the difference is exact)
+            far |= __ballot(!(fabsf(cm[i]) < kFar)) != 0;
+            l[i] = 0.f;
+            met[i] = false;
+        }
+#pragma unroll
+        for (int i = 0; i < C::PER; ++i) cm[i] = far ? 0.f : cm[i];
+        probabilities(tb);
         __syncthreads();
         for (int t = tb; t < te; ++t) {
             if (t + 1 < te) score(t + 1);
-            if (t + 2 < te) store(t + 2);         // (over tile t - 1, which every wave has weighted)
+            if (t + 2 < te) store(t + 2);        // (over tile t - 1, which every wave has weighted)
             if (t + 3 < te) load(next);
             next = rows_of(t + 4);
-            values(t, careful);
+            if (t + 1 < te) probabilities(t + 1);
+            values(t);
             __syncthreads();
         }
-    };
-    if (tb < te) {
-        walk(std::false_type{});
-        if (t_last > t_first && any_of(odd, (int *)tiles)) {
-            clear();
-            walk(std::true_type{});
+#pragma unroll
+        for (int i = 0; i < C::PER; ++i) {
+            l[i] += __shfl_xor(l[i], 16);
+            l[i] += __shfl_xor(l[i], 32);
+            const uint64_t any = __ballot(met[i]);
+            if (g == 0 && mine(i)) {
+                ends[1][mt_of(i)][kb][c] = l[i];
+                ends[2][mt_of(i)][kb][c] = (any >> c | any >> (16 + c) | any >> (32 + c) | any >> (48 + c)) & 1 ? 1.f : 0.f;
+            }
+        }
+        __syncthreads();
+        bool again = odd && t_last > t_first;
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            const float top = fmaxf(ends[0][t][0][c], ends[0][t][1][c]);
+            m_row[t] = fabsf(top) < __builtin_inff() ? top : 0.f;
+            l_row[t] = ends[1][t][0][c] + ends[1][t][1][c];
+            if (16 * t + c >= rows) continue;
+            if (ends[2][t][0][c] + ends[2][t][1][c] == 0.f) {
+                m_row[t] = neg_inf();            // (no key of the part's)
+                continue;
+            }
+            again |= !(l_row[t] > 0x1p-100f && l_row[t] < 0x1p100f);
+#pragma unroll
+            for (int b = 0; b < C::NB; ++b)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) again |= !(fabsf(o[t][b][r]) < __builtin_inff());
+        }
+        if (any_of(again, (int *)tiles)) {
+            // Tile by tile: every wave forms the probabilities of all rows, with a running maximum.
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                m_row[t] = neg_inf();
+                l_row[t] = 0.f;
+#pragma unroll
+                for (int b = 0; b < C::NB; ++b) o[t][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            }
+#pragma unroll 1
+            for (int t = tb; t < te; ++t) {
+                const int j0 = x.key(t, KT);
+                load(rows_of(t));
+                store(t);
+                __syncthreads();
+                score(t);
+#pragma unroll
+                for (int i = 0; i < C::PER; ++i)
+                    if (mine(i)) *(f32x4_t *)(mix + (16 * mt_of(i) + c) * C::SS + 16 * kb + 4 * g) = z[i];
+                __syncthreads();
+                const uint16_t *vt = tiles[t % 3] + (SHARED ? 0 : KT * DQK);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    const Sight see = sight(a, s, recent, row_of(16 * i + c) / a.group);
+                    float e[8], top = neg_inf(), sum = 0.f;
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) {
+                        const int k = 16 * (r >> 2) + 4 * g + (r & 3);
+                        e[r] = sees(see, sink, j0 + k) ? mix[(16 * i + c) * C::SS + k] : neg_inf();
+                        top = fmaxf(top, e[r]);
+                    }
+                    top = fmaxf(top, __shfl_xor(top, 16));
+                    top = fmaxf(top, __shfl_xor(top, 32));
+                    const float up = fmaxf(m_row[i], top), base = up == neg_inf() ? 0.f : up;
+                    const float alpha = up == m_row[i] ? 1.f : __builtin_amdgcn_exp2f((m_row[i] - up) * a.scale_log2);
+                    m_row[i] = up;
+                    bf16x8_t p;
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) {
+                        const float v = __builtin_amdgcn_exp2f((e[r] - base) * a.scale_log2);
+                        sum += v;
+                        p[r] = (__bf16)v;
+                    }
+                    l_row[i] = l_row[i] * alpha + sum;
+#pragma unroll
+                    for (int b = 0; b < C::NB; ++b) {
+                        o[i][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(finite_only(__builtin_bit_cast(u32x4, value(t, b)))), p,
+                                                                          o[i][b] * alpha, 0, 0, 0);
+                    }
+                    // infinities and NaNs for the rows that see them (any weight leaves them as they are)
+#pragma unroll 1
+                    for (int k = 0; k < KT; ++k) {
+                        if (!sees(see, sink, j0 + k)) continue;
+#pragma unroll
+                        for (int b = 0; b < C::NB; ++b) {
+                            const uint2 v = *(const uint2 *)(vt + k * D + place<CH, SHARED>(k, 2 * (w * C::NB + b) + (g >> 1)) * 8 + 4 * (g & 1));
+                            o[i][b] += f32x4_t{special_only(v.x & 0xffffu), special_only(v.x >> 16), special_only(v.y & 0xffffu), special_only(v.y >> 16)};
+                        }
+                    }
+                }
+                __syncthreads();
+            }
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                l_row[t] += __shfl_xor(l_row[t], 16);
+                l_row[t] += __shfl_xor(l_row[t], 32);
+            }
         }
     }
 
     // Results: to the output, or to the part's slot.
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-        l[t] += __shfl_xor(l[t], 16);
-        l[t] += __shfl_xor(l[t], 32);
         const int r = 16 * t + c;
         if (r >= rows) continue;
         if (item.parts == 1) {
-            const bool none = seen[t].end <= 0;
-            const float inv = none ? 0.f : 1.f / l[t];
+            const int tok = (r0 + r) / a.group, head = y * a.group + r0 + r - tok * a.group;
+            const bool none = sight(a, s, recent, tok).end <= 0;
+            const float inv = none ? 0.f : 1.f / l_row[t];
+            uint16_t *to = a.O + (int64_t)(s.start + tok) * a.o_tok + (int64_t)head * a.o_head;
 #pragma unroll
-            for (int b = 0; b < C::NB; ++b)
-                *(uint2 *)(a.O + o_at[t] + 16 * (w * C::NB + b) + 4 * g) = pack4(o[t][b] * inv);
-            if (a.lse && w == 0 && g == 0) {
-                const int tok = (r0 + r) / a.group, head = y * a.group + r0 + r - tok * a.group;
+            for (int b = 0; b < C::NB; ++b) *(uint2 *)(to + 16 * (w * C::NB + b) + 4 * g) = pack4(o[t][b] * inv);
+            if (a.lse && w == 0 && g == 0)
                 a.lse[(int64_t)head * a.n_tokens + s.start + tok] =
-                    none ? neg_inf() : fmaf(m[t] * kLn2, a.scale_log2, logf(l[t]));
-            }
+                    none ? neg_inf() : fmaf(m_row[t] * kLn2, a.scale_log2, logf(l_row[t]));
         } else {
             float *slot = a.part + (int64_t)(item.slot + item.part * item.step) * (C::ROWS * (DV + 2));
+            const float by = moderate(&m_row[t], &l_row[t], a.scale_log2);
 #pragma unroll
-            for (int b = 0; b < C::NB; ++b) *(f32x4_t *)(slot + r * DV + 16 * (w * C::NB + b) + 4 * g) = o[t][b];
+            for (int b = 0; b < C::NB; ++b) *(f32x4_t *)(slot + r * DV + 16 * (w * C::NB + b) + 4 * g) = o[t][b] * by;
             if (w == 0 && g == 0) {
-                slot[C::ROWS * DV + r] = m[t];
-                slot[C::ROWS * DV + C::ROWS + r] = l[t];
+                slot[C::ROWS * DV + r] = m_row[t];
+                slot[C::ROWS * DV + C::ROWS + r] = l_row[t];
             }
         }
     }
@@ -319,10 +405,11 @@ void launch_rows(const PagedArgs &a, int rows, hipStream_t s) {
     auto go = [&](auto mt) {
         constexpr int MT = decltype(mt)::value;
         hipLaunchKernelGGL((paged_attn_kernel<DQK, DV, SHARED, MT, NW>), dim3((unsigned)a.n_work), dim3(64 * NW), 0, s, a);
-        if (a.target > 0) launch_join<DV, 16 * MT, KT>(a, s);
+        if (a.target > 0) launch_join<DV, 16 * MT, KT, false>(a, s);
     };
     if (rows <= 16) go(std::integral_constant<int, 1>{});
     else if (rows <= 32) go(std::integral_constant<int, 2>{});
+    else if (rows <= 48) go(std::integral_constant<int, 3>{});
     else go(std::integral_constant<int, 4>{});
 }
 

@@ -40,14 +40,14 @@ struct PagedArgs {
 
 constexpr int kLatentRot = FKV_LATENT_ROT;
 
-// Attention of rows-per-tile (16, 32, 64) query rows, its parts joined (k_paged_attn.hip).
+// Attention of rows-per-tile (16, 32, 48, 64) query rows, its parts joined (k_paged_attn.hip).
 hipError_t launch_paged_attention(const PagedArgs &a, int head_dim, int rows, hipStream_t s);
 hipError_t launch_latent_rows(const PagedArgs &a, int latent_dim, int rows, hipStream_t s);
 // Attention of tiles of kPagedTileRows query rows, its parts joined (k_paged_tile.hip).
 constexpr int kPagedTileRows = 128;
 hipError_t launch_paged_tiles(const PagedArgs &a, int head_dim, hipStream_t s);
 hipError_t launch_expanded_tiles(const PagedArgs &a, int head_dim, hipStream_t s);
-inline int paged_row_tile(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 64; }
+inline int paged_row_tile(int rows) { return rows <= 64 ? (rows + 15) / 16 * 16 : 64; }
 
 // Rows into the pages (k_paged_append.hip).
 struct PagedAppendArgs {
@@ -146,13 +146,17 @@ struct Work {
     int slot;                       // of the item's part 0; the next part's is `step` further
     int step;
     int64_t base;                   // the sequence's first row in the expanded copies
+    int next;                       // by token, not found: the next row that may be
     bool ok;
 };
 
-// The launch's split: keys are dealt in parts of at least part_tiles tiles, about `target`
-// parts in all; where there are as many items as that, only items of more than twice the
-// share are cut.  A sequence's items are all cut alike, its parts dealt evenly over each item's tiles.
+// The launch's split: keys are dealt in parts of part_tiles tiles.  That is the least size, from
+// an equal share of all tiles for `target` workgroups up to twice the share, in kSizes steps, with which
+// the parts are no more than `target`: a workgroup too many would start when the others have ended.  Where
+// there are more items than that, only those of more than twice the share are cut.  A sequence's items are all
+// cut alike, its parts dealt evenly over each item's tiles.
 struct Split {
+    static constexpr int kSizes = 8;
     float part_tiles;
     template <int ROWS, int KT>
     static __device__ __forceinline__ void counts(const PagedArgs &a, const Seq &s, int *rts, int *tiles) {
@@ -161,23 +165,38 @@ struct Split {
         const int64_t keys = a.wide < 0 ? s.len : min((int64_t)s.len, (int64_t)a.wide + s.n + 2 * KT);
         *tiles = max((int)((keys + KT - 1) / KT), 1);
     }
+    static __device__ __forceinline__ float sum_of(float v) {
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+        return v;
+    }
     template <int ROWS, int KT>
     static __device__ __forceinline__ Split make(const PagedArgs &a) {
         const int lane = threadIdx.x & 63;
-        float sum = 0.f, items = 0.f;
+        float sum = 0.f;
         for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
             int rts, tiles;
             counts<ROWS, KT>(a, sequence(a, i0 + lane), &rts, &tiles);
             sum += (float)rts * (float)tiles;
-            items += (float)rts;
         }
+        const float share = sum_of(sum) * (float)a.kv / (float)a.target;
+        float size[kSizes], parts[kSizes];
 #pragma unroll
-        for (int d = 32; d > 0; d >>= 1) {
-            sum += __shfl_xor(sum, d);
-            items += __shfl_xor(items, d);
+        for (int k = 0; k < kSizes; ++k) {
+            size[k] = fmaxf((float)a.min_tiles, ceilf(share * (1.f + (float)(k * k) / ((kSizes - 1) * (kSizes - 1)))));
+            parts[k] = 0.f;
         }
-        const float share = ceilf(sum * (float)a.kv / (float)a.target);
-        return Split{fmaxf((float)a.min_tiles, items * (float)a.kv >= (float)a.target ? 2.f * share : share)};
+        for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
+            int rts, tiles;
+            counts<ROWS, KT>(a, sequence(a, i0 + lane), &rts, &tiles);
+#pragma unroll
+            for (int k = 0; k < kSizes; ++k) parts[k] += (float)rts * ceilf((float)tiles / size[k]);
+        }
+        float best = size[kSizes - 1];
+#pragma unroll
+        for (int k = kSizes - 2; k >= 0; --k)
+            if (sum_of(parts[k]) * (float)a.kv <= (float)a.target) best = size[k];
+        return Split{best};
     }
     __device__ __forceinline__ int parts(const PagedArgs &a, int tiles) const {
         return a.target > 0 ? max((int)ceilf((float)tiles / part_tiles), 1) : 1;
@@ -192,12 +211,13 @@ __device__ __forceinline__ Work locate(const PagedArgs &a, int want, int token) 
     const Split split = a.target > 0 ? Split::make<ROWS, KT>(a) : Split{0.f};
     Work w;
     w.ok = false;
-    int done = 0, slots = 0;
+    int done = 0, slots = 0, after = a.n_tokens;
     int64_t rows = 0;
     for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
         const Seq s = sequence(a, i0 + lane);
         int rts, tiles;
         Split::counts<ROWS, KT>(a, s, &rts, &tiles);
+        if (rts > 0 && s.start > token) after = min(after, s.start);
         const int parts = split.parts(a, tiles), c = a.kv * rts * parts, cut = parts > 1 ? c : 0;
         const int blocks = rts > 0 ? (s.len + kSeqRows - 1) / kSeqRows : 0;
         int ic = c, is = cut, ib = blocks;
@@ -241,6 +261,11 @@ __device__ __forceinline__ Work locate(const PagedArgs &a, int want, int token) 
         slots += __builtin_amdgcn_readlane(is, 63);
         rows += __builtin_amdgcn_readlane(ib, 63);
     }
+    if (token >= 0) {
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) after = min(after, __shfl_xor(after, d));
+    }
+    w.next = after;
     return w;
 }
 
@@ -324,6 +349,17 @@ __device__ __forceinline__ u32x4 finite_only(u32x4 v) {
     return v;
 }
 __device__ __forceinline__ float special_only(uint32_t bits) { return (bits & 0x7f80u) == 0x7f80u ? __uint_as_float(bits << 16) : 0.f; }
+
+// A part's sum far from 1 (its reference far from its largest score) moves into its reference by a power of two,
+// so that joining it with other parts' loses nothing; the factor for its outputs.
+__device__ __forceinline__ float moderate(float *m, float *l, float scale_log2) {
+    if (!(*l > 0.f) || (*l > 0x1p-20f && *l < 0x1p20f) || !(*l < __builtin_inff())) return 1.f;
+    const int k = __builtin_amdgcn_frexp_expf(*l);
+    *m += (float)k / scale_log2;
+    const float by = __builtin_amdgcn_ldexpf(1.f, -k);
+    *l *= by;
+    return by;
+}
 
 // Whether any thread of the workgroup says so; every thread calls it.  flag: LDS that is otherwise free
 // (__syncthreads_or takes LDS of its own, with which two workgroups no longer share a CU).
