@@ -154,6 +154,9 @@ size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
 constexpr int kFewRows = 64;        // query rows of a sequence and key head up to which the launch for few rows takes it
 
+// Query rows of a tile of the launch for many rows, by the most rows of a sequence and key head.
+int tile_rows(int64_t rows) { return rows > 512 ? 256 : 128; }
+
 struct AttendPlan {
     bool few, many;
     Launch f, m;
@@ -170,7 +173,8 @@ AttendPlan attend_plan(const fkv_batch *b, int n_heads, int kv, int head_dim, in
     if (p.few)
         p.f = plan(b, kv, group, 1, edge, fkv::paged_row_tile(std::min(most, edge) * group), (head_dim == 64 ? 4 : 2) * cus, 4, head_dim);
     if (p.many)
-        p.m = plan(b, kv, group, p.few ? edge + 1 : 1, std::numeric_limits<int32_t>::max(), fkv::kPagedTileRows, 2 * cus, 8, head_dim);
+        p.m = plan(b, kv, group, p.few ? edge + 1 : 1, std::numeric_limits<int32_t>::max(), tile_rows((int64_t)most * group), tile_rows((int64_t)most * group) == 256 ? cus : 2 * cus, 8,
+                   head_dim);
     p.bytes = std::max(p.f.part_bytes, p.m.part_bytes);
     return p;
 }
@@ -204,7 +208,7 @@ LatentPlan latent_plan(const fkv_batch *b, int n_heads, int d, int R, int form, 
         p.o_at = take(rows * R * 2);
     }
     if (p.expanded) {
-        p.m = plan(b, n_heads, 1, p.absorbed ? FKV_LATENT_FEW : 1, all, fkv::kPagedTileRows, 2 * cus, 8, d);
+        p.m = plan(b, n_heads, 1, p.absorbed ? FKV_LATENT_FEW : 1, all, 256, cus, 8, d);
         const int64_t block = fkv::paged::kSeqRows;
         p.head_rows = ((b->sum_len + block - 1) / block + b->n_seqs) * block;
         p.k_at = take((size_t)n_heads * p.head_rows * (d + FKV_LATENT_ROT) * 2);
@@ -335,7 +339,7 @@ fkv_status fkv_paged_attention(const fkv_batch *batch, int32_t n_heads, int32_t 
     }
     if (e == hipSuccess && p.many) {
         set_launch(&a, p.m, workspace, workspace != nullptr);
-        e = fkv::launch_paged_tiles(a, head_dim, (hipStream_t)stream);
+        e = fkv::launch_paged_tiles(a, head_dim, p.m.rows, (hipStream_t)stream);
     }
     return done(e, "fkv_paged_attention launch");
 }

@@ -9,6 +9,7 @@
 //                  score passes it by kSlack,
 //   O^T += V^T P^T (A = V^T through the LDS transpose read, P straight from S^T).
 #include <type_traits>
+#include <utility>
 
 #include "paged_join.h"
 
@@ -17,13 +18,16 @@ namespace {
 
 using namespace paged;
 
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef short short2_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) bf16x4_t lds_bf16x4_t;
 
-constexpr int KT = 64, ROWS = kPagedTileRows, NT = 256;
+constexpr int KT = 64;
 constexpr float kFar = 0x1p10f;     // log2 units from which scores are subtracted before they are scaled
 constexpr float kLn2 = 0.69314718055994530942f;
 
@@ -38,11 +42,25 @@ __device__ __forceinline__ uint2 pack4(float x0, float x1, float x2, float x3) {
 // The larger of a value and that of the lane 32 further.
 __device__ __forceinline__ float across_max(float v) { return fmaxf(v, __shfl_xor(v, 32)); }
 
-template <int DQK, int DV, bool EXPANDED>
-__global__ __launch_bounds__(NT, 2) void paged_tile_kernel(PagedArgs a) {
+// f(0), f(1), ... with constants.
+template <int... I, class F>
+__device__ __forceinline__ void each(std::integer_sequence<int, I...>, F &&f) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+
+template <int DQK, int DV, bool EXPANDED, int NW, bool LSE>
+__global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(PagedArgs a) {
+    constexpr int ROWS = 32 * NW, NT = 64 * NW;
     constexpr int CK = DQK / 8, CV = DV / 8, KS = DQK / 16, MB = DV / 32;
     constexpr int NK = KT * CK / NT, NV = KT * CV / NT;
-    __shared__ __attribute__((aligned(16))) uint16_t kts[2][KT * DQK], vts[2][KT * DV];
+    // Key tiles t and t + 1 are read while t + 2 is written: more than two buffers, or two and another
+    // barrier (NW 4: two workgroups share a CU's LDS).
+    constexpr int KB = NW == 8 ? 3 : 2;
+    // Rows in LDS are padded: 16 keys' chunks (the score operand), and the 8 rows of 64 bytes that a
+    // transpose read covers, then fall into distinct banks, and every read of a tile is one address
+    // and a constant.
+    constexpr int SK = DQK + 8, SV = DV + 32;
+    __shared__ __attribute__((aligned(16))) uint16_t kts[KB * KT * SK], vts[2 * KT * SV];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), hh = lane >> 5, c = lane & 31;
 
     Work item = locate<ROWS, KT>(a, blockIdx.x, -1);
@@ -69,7 +87,7 @@ __global__ __launch_bounds__(NT, 2) void paged_tile_kernel(PagedArgs a) {
     f32x16_t o[MB];
     float m, l;
 
-    // Rows of a tile's keys, one to a lane (past the part's last tile, that one's).
+    // Rows of a tile's keys, one to a lane (past the part's last tile, that one's); EXPANDED: the first one's.
     const int j_last = x.most.end - 1;
     const uint16_t *K = a.K, *V = a.V;
     if (EXPANDED) {
@@ -77,37 +95,59 @@ __global__ __launch_bounds__(NT, 2) void paged_tile_kernel(PagedArgs a) {
         V += (y * a.head_rows + item.base) * DV;
     }
     auto rows_of = [&](int t) {
-        const int j = min(x.key(min(t, te - 1), KT) + lane, j_last);
-        return EXPANDED ? j : pool_row(a, pages, y, j);
+        const int j = x.key(min(t, te - 1), KT);
+        return EXPANDED ? j : pool_row(a, pages, y, min(j + lane, j_last));
     };
     u32x4 kr[NK], vr[NV];
     bool odd = false;                             // an infinity or a NaN among values that not every row sees
-    auto load_k = [&](int row_of_lane) {
+    // EXPANDED: a tile's rows lie together; a row past the sequence's last is read as zeros.
+    auto rsrc = [](const uint16_t *p, int64_t bytes) {
+        return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)(uint32_t)bytes, 0x00020000);
+    };
+    const auto k_buf = rsrc(K, EXPANDED ? (int64_t)s.len * DQK * 2 : 0), v_buf = rsrc(V, EXPANDED ? (int64_t)s.len * DV * 2 : 0);
+    // N chunks of the rows of a pool; rows that follow one another are read from one address.
+    auto load = [&](const uint16_t *pool, int row_of_lane, auto width, auto &to) __attribute__((always_inline)) {
+        constexpr int W = width, CH = W / 8, N = KT * CH / NT;
+        const int first = __builtin_amdgcn_readfirstlane(row_of_lane);
+        if (__ballot(row_of_lane == first + lane) == ~0ull) {
+            const char *at = (const char *)(pool + (int64_t)first * W);
+#pragma unroll
+            for (int i = 0; i < N; ++i) to[i] = *(const u32x4 *)(at + i * (NT * 16) + (uint32_t)(tid * 16));
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int id = tid + i * NT, k = id / CH;
+                to[i] = *(const u32x4 *)(pool + (int64_t)__shfl(row_of_lane, k) * W + (id - k * CH) * 8);
+            }
+        }
+    };
+    auto load_k = [&](int row_of_lane) __attribute__((always_inline)) {
+        if constexpr (EXPANDED) {
+#pragma unroll
+            for (int i = 0; i < NK; ++i)
+                kr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(k_buf, (tid + i * NT) * 16, row_of_lane * (DQK * 2), 0));
+        } else {
+            load(K, row_of_lane, std::integral_constant<int, DQK>{}, kr);
+        }
+    };
+    auto load_v = [&](int row_of_lane) __attribute__((always_inline)) {
+        if constexpr (EXPANDED) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                vr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(v_buf, (tid + i * NT) * 16, row_of_lane * (DV * 2), 0));
+        } else {
+            load(V, row_of_lane, std::integral_constant<int, DV>{}, vr);
+        }
+    };
+    auto store_k = [&](uint16_t *kt) {
 #pragma unroll
         for (int i = 0; i < NK; ++i) {
             const int id = tid + i * NT, k = id / CK;
-            kr[i] = *(const u32x4 *)(K + (int64_t)__shfl(row_of_lane, k) * DQK + (id - k * CK) * 8);
+            *(u32x4 *)(kt + k * SK + (id - k * CK) * 8) = kr[i];
         }
     };
-    auto load_v = [&](int row_of_lane) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int id = tid + i * NT, k = id / CV;
-            vr[i] = *(const u32x4 *)(V + (int64_t)__shfl(row_of_lane, k) * DV + (id - k * CV) * 8);
-        }
-    };
-    auto store_k = [&](int t) {
-        uint16_t *kt = kts[t & 1];
-#pragma unroll
-        for (int i = 0; i < NK; ++i) {
-            const int id = tid + i * NT, k = id / CK;
-            *(u32x4 *)(kt + k * DQK + place<CK, true>(k, id - k * CK) * 8) = kr[i];
-        }
-    };
-    auto store_v = [&](int t) {
-        const int j0 = x.key(min(t, te - 1), KT);
-        uint16_t *vt = vts[t & 1];
-        if (!all_seen<KT>(x, sink, j0)) {
+    auto store_v = [&](uint16_t *vt, int j0, bool edge) {
+        if (edge) {
             // (values of keys that no row sees are cleared: a probability of zero would not silence a NaN)
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
@@ -118,25 +158,14 @@ __global__ __launch_bounds__(NT, 2) void paged_tile_kernel(PagedArgs a) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int id = tid + i * NT, k = id / CV;
-            *(u32x4 *)(vt + k * DV + place<CV, false>(k, id - k * CV) * 8) = vr[i];
+            *(u32x4 *)(vt + k * SV + (id - k * CV) * 8) = vr[i];
         }
     };
+    // Where this lane reads a tile: key c, chunk hh of K (then + 32 kb keys, + 2 k chunks); keys 4 hh + 0..3
+    // of V (+ 8, + 16 k), channels 16 (lane / 16 % 2) + 4 (lane % 4) (+ 32 b).
+    const uint16_t *k_lane = kts + c * SK + 8 * hh;
+    const uint16_t *v_lane = vts + (4 * hh + ((lane & 15) >> 2)) * SV + 16 * (lane >> 4 & 1) + 4 * (lane & 3);
 
-    // Where this lane reads the tiles: key c (and c + 32) of K, chunk 2 k + hh (the pattern of
-    // place() repeats every GK steps); keys 4 hh + 0..3 (and
-    // + 8) of V, channels 32 b + 16 (lane / 16 % 2) + 4 (lane % 4) of each four.
-    constexpr int GK = (CK % 16 == 0 ? 16 : 8) / 2;
-    int ka[GK], va[MB], vb[MB];
-    {
-        const int vk = 4 * hh + ((lane & 15) >> 2), vc = 2 * (lane >> 4 & 1) + ((lane & 3) >> 1), vh = 4 * (lane & 1);
-#pragma unroll
-        for (int k = 0; k < GK; ++k) ka[k] = c * DQK + place<CK, true>(c, 2 * k + hh) * 8;
-#pragma unroll
-        for (int b = 0; b < MB; ++b) {
-            va[b] = vk * DV + place<CV, false>(vk, 4 * b + vc) * 8 + vh;
-            vb[b] = (vk + 8) * DV + place<CV, false>(vk + 8, 4 * b + vc) * 8 + vh;
-        }
-    }
     auto clear = [&]() {
         l = 0.f;
 #pragma unroll
@@ -150,7 +179,7 @@ __global__ __launch_bounds__(NT, 2) void paged_tile_kernel(PagedArgs a) {
         for (int r = 0; r < 16; ++r) z[r] = 0.f;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-            const bf16x8_t f = frag(*(const u32x4 *)(kt + 32 * kb * DQK + ka[k % GK] + k / GK * GK * 16));
+            const bf16x8_t f = frag(*(const u32x4 *)(kt + 32 * kb * SK + 16 * k));
             z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, q[k], z, 0, 0, 0);
         }
     };
@@ -164,33 +193,36 @@ __global__ __launch_bounds__(NT, 2) void paged_tile_kernel(PagedArgs a) {
     };
     // V^T of keys 16 k + 4 hh + 0..3 and + 8, channels 32 b + (lane % 32).
     auto value = [&](const uint16_t *vt, int k, int b) {
-        const uint16_t *at = vt + 16 * k * DV;
-        const bf16x4_t u = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t *)(at + va[b]));
-        const bf16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t *)(at + vb[b]));
+        const uint16_t *at = vt + 16 * k * SV + 32 * b;
+        const bf16x4_t u = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t *)at);
+        const bf16x4_t v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_t *)(at + 8 * SV));
         return __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7);
     };
 
     m = neg_inf();
     clear();
     if (tb < te) {
-        int next_v = rows_of(tb), next_k = rows_of(tb + 1);   // pool rows of the tiles to load next
+        int next_v = rows_of(tb + 1), next_k = rows_of(tb + 2);   // pool rows of the tiles to load next
+        int j0 = x.key(tb, KT);
+        bool edge = !all_seen<KT>(x, sink, j0);   // not every row sees every key of the tile
+        {
+            const int first = rows_of(tb);
+            load_k(first);
+            load_v(first);
+        }
+        store_k(kts);
         load_k(next_v);
+        store_v(vts, j0, edge);
         load_v(next_v);
-        store_k(tb);
-        load_k(next_k);
-        store_v(tb);
-        next_v = next_k;
-        next_k = rows_of(tb + 2);
+        store_k(kts + KT * SK);
         __syncthreads();
+        f32x16_t z[2];
+        score(k_lane, 0, z[0]);
         {                                         // the reference: the row's largest score in the first tile, masked keys too
+            score(k_lane, 1, z[1]);
             float top = neg_inf();
-#pragma unroll 1
-            for (int kb = 0; kb < 2; ++kb) {
-                f32x16_t z;
-                score(kts[tb & 1], kb, z);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) top = fmaxf(top, z[r]);
-            }
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, fmaxf(z[0][r], z[1][r]));
             top = across_max(top);
             m = fabsf(top) < __builtin_inff() ? top : 0.f;
         }
@@ -199,46 +231,108 @@ __global__ __launch_bounds__(NT, 2) void paged_tile_kernel(PagedArgs a) {
         const bool far = __ballot(!(fabsf(m * a.scale_log2) < kFar)) != 0;
         const float cm = far ? 0.f : m * a.scale_log2;
         bool met = false;
-        for (int t = tb; t < te; ++t) {
-            if (t > tb) __syncthreads();
-            // the next tile's keys, then its values: over tile t - 1, which every wave has weighted (past the
-            // end the last tile again)
-            store_k(t + 1);
-            load_v(next_v);
-            const int j0 = x.key(t, KT);
-            const uint16_t *kt = kts[t & 1], *vt = vts[t & 1];
-            f32x16_t z[2];
-            score(kt, 0, z[0]);
-            score(kt, 1, z[1]);
-            if (far || !all_seen<KT>(x, sink, j0)) {
+        float sum[2] = {0.f, 0.f}, v[2];
+        u32x4 p[2][2];                            // probabilities, two bf16 a word: key block, 16 keys
+        auto ready = [&](int j, int kb) {         // a key block's scores are complete, and not those of an ordinary tile
+            hide(j, kb, z[kb]);
+            if (far) z[kb] -= m;
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                    hide(j0, kb, z[kb]);
-                    if (far) z[kb] -= m;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) met |= z[kb][r] != neg_inf();
-                }
+            for (int r = 0; r < 16; ++r) met |= z[kb][r] != neg_inf();
+        };
+        // Half of the work on scores 2 i and 2 i + 1 of key block kb.  The sum is of the probabilities as they
+        // are, or, without LSE, of the rounded ones that weight the values, two at a time.
+        auto step = [&](int kb, int i, int half) __attribute__((always_inline)) {
+            if (half == 0) {
+                v[0] = fmaf(z[kb][2 * i], a.scale_log2, -cm);
+                v[1] = fmaf(z[kb][2 * i + 1], a.scale_log2, -cm);
+                v[0] = __builtin_amdgcn_exp2f(v[0]);
             } else {
-                met = true;
+                v[1] = __builtin_amdgcn_exp2f(v[1]);
+                if (LSE) {
+                    sum[0] += v[0];
+                    sum[1] += v[1];
+                }
+                uint32_t word = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{v[0], v[1]}, bf16x2_t));
+                asm volatile("" : "+v"(word));     // (not moved to its use)
+                if (!LSE)
+                    sum[i & 1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(short2_t, word), __builtin_bit_cast(short2_t, 0x3f803f80), sum[i & 1], false);
+                p[kb][i >> 2][i & 3] = word;
             }
-            store_v(t + 1);
+        };
+        edge |= far;
+        if (edge) ready(j0, 0);
+        else met = true;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            step(0, i, 0);
+            step(0, i, 1);
+        }
+        // One pinned stream a tile: (C) the scores of its second key block, (D) the values of its first, (A)
+        // the scores of the next tile's first, (B) the values of its second; the exponentials of a key block run
+        // behind the 16 and more products after its scores, operands are read kAhead products ahead.
+        constexpr int kAhead = 4, NV4 = 2 * MB, kD = KS, kA = KS + NV4, kB = 2 * KS + NV4, kN = 2 * KS + 2 * NV4;
+        int k_this = 0, k_next = KT * SK, k_free = KB == 3 ? 2 * KT * SK : 0, v_this = 0;   // the buffers
+#pragma unroll 1
+        for (int t = tb; t < te; ++t) {
+            const uint16_t *k0 = k_lane + k_this, *k1 = k_lane + k_next, *vt = v_lane + v_this;
+            const int jn = x.key(min(t + 1, te - 1), KT);
+            const bool edge_n = !all_seen<KT>(x, sink, jn);
+            // over tile t - 1, which every wave has weighted; past the part's last tile that one again
+            store_v(vts + (KT * SV - v_this), jn, edge_n);
             load_k(next_k);
             next_v = next_k;
             next_k = rows_of(t + 3);
-            float sum[2] = {0.f, 0.f};
+            bf16x8_t f[kAhead];
+            auto fetch = [&](auto index) __attribute__((always_inline)) {
+                constexpr int i = index;
+                if constexpr (i < kD) f[i % kAhead] = frag(*(const u32x4 *)(k0 + 32 * SK + 16 * i));
+                else if constexpr (i < kA) f[i % kAhead] = value(vt, (i - kD) / MB, (i - kD) % MB);
+                else if constexpr (i < kB) f[i % kAhead] = frag(*(const u32x4 *)(k1 + 16 * (i - kA)));
+                else if constexpr (i < kN) f[i % kAhead] = value(vt, 2 + (i - kB) / MB, (i - kB) % MB);
+            };
+            each(std::make_integer_sequence<int, kAhead>{}, fetch);
+            each(std::make_integer_sequence<int, kN>{}, [&](auto index) __attribute__((always_inline)) {
+                constexpr int i = index;
+                constexpr bool scores = i < kD || (i >= kA && i < kB);
+                constexpr int kb = i < kD || i >= kB ? 1 : 0;                 // key block of the product
+                constexpr int at = i < kD ? i : i < kA ? i - kD : i < kB ? i - kA : i - kB, n = scores ? KS : NV4;
+                if constexpr (scores) {
+                    if constexpr (at == 0) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                bf16x8_t p;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float v = __builtin_amdgcn_exp2f(fmaf(z[k >> 1][8 * (k & 1) + e], a.scale_log2, -cm));
-                    sum[e & 1] += v;
-                    p[e] = (__bf16)v;
+                        for (int r = 0; r < 16; ++r) z[kb][r] = 0.f;
+                    }
+                    z[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % kAhead], q[at], z[kb], 0, 0, 0);
+                } else {
+                    o[at % MB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % kAhead], frag(p[kb][at / MB]), o[at % MB], 0, 0, 0);
                 }
+                fetch(std::integral_constant<int, i + kAhead>{});
+                // behind (C) and (B) key block 0, behind (D) and (A) key block 1; the first 8 scores behind values
+                constexpr int h0 = 8 * at / n, h1 = 8 * (at + 1) / n, of = i < kD || i >= kB ? 0 : 1, first = scores ? 4 : 0;
 #pragma unroll
-                for (int b = 0; b < MB; ++b) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value(vt, k, b), p, o[b], 0, 0, 0);
-            }
-            l += sum[0] + sum[1];
+                for (int h = h0; h < h1; ++h) step(of, first + h / 2, h & 1);
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (i == kD - 1) {
+                    if (edge) ready(j0, 1);
+                    if (KB == 2) __syncthreads();  // (every wave has read tile t's keys)
+                }
+                if constexpr (i == kA - 1) {
+                    store_k(kts + k_free);
+                    load_v(next_v);
+                }
+                if constexpr (i == kB - 1) {
+                    l = sum[0] + sum[1];           // (the last time without the tile after the last)
+                    j0 = jn;
+                    edge = edge_n || far;
+                    if (edge) ready(j0, 0);
+                    else met = true;
+                }
+            });
+            __syncthreads();
+            const int used = k_this;
+            k_this = k_next;
+            k_next = k_free;
+            k_free = KB == 3 ? used : k_this;
+            v_this = KT * SV - v_this;
         }
         met = (__ballot(met) >> c | __ballot(met) >> (32 + c)) & 1;
         const float all = l + __shfl_xor(l, 32);
@@ -258,18 +352,18 @@ __global__ __launch_bounds__(NT, 2) void paged_tile_kernel(PagedArgs a) {
             clear();
 #pragma unroll 1
             for (int t = tb; t < te; ++t) {
-                const int j0 = x.key(t, KT);
+                const int j = x.key(t, KT);
+                const uint16_t *kt = k_lane, *vt = v_lane;
                 load_k(rows_of(t));
                 load_v(rows_of(t));
-                store_k(t);
-                store_v(t);
+                store_k(kts);
+                store_v(vts, j, !all_seen<KT>(x, sink, j));
                 __syncthreads();
-                const uint16_t *kt = kts[t & 1], *vt = vts[t & 1];
 #pragma unroll 1
                 for (int kb = 0; kb < 2; ++kb) {
                     f32x16_t z;
                     score(kt, kb, z);
-                    hide(j0, kb, z);
+                    hide(j, kb, z);
                     float top = neg_inf(), sum = 0.f;
 #pragma unroll
                     for (int r = 0; r < 16; ++r) top = fmaxf(top, z[r]);
@@ -289,15 +383,15 @@ __global__ __launch_bounds__(NT, 2) void paged_tile_kernel(PagedArgs a) {
                         o[b] *= alpha;
 #pragma unroll
                         for (int k = 0; k < 2; ++k)
-                            o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(finite_only(__builtin_bit_cast(u32x4, value(vt + 32 * kb * DV, k, b)))),
+                            o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(finite_only(__builtin_bit_cast(u32x4, value(vt + 32 * kb * SV, k, b)))),
                                                                            p[k], o[b], 0, 0, 0);
                     }
 #pragma unroll 1
                     for (int k = 32 * kb; k < 32 * kb + 32; ++k) {    // (any weight leaves them as they are)
-                        if (!sees(seen, sink, j0 + k)) continue;
+                        if (!sees(seen, sink, j + k)) continue;
 #pragma unroll
                         for (int u = 0; u < 4 * MB; ++u) {            // channels 8 u + 4 hh + 0..3
-                            const uint2 v = *(const uint2 *)(vt + k * DV + place<CV, false>(k, u) * 8 + 4 * hh);
+                            const uint2 v = *(const uint2 *)(vts + k * SV + 8 * u + 4 * hh);
                             o[u >> 2][4 * (u & 3) + 0] += special_only(v.x & 0xffffu);
                             o[u >> 2][4 * (u & 3) + 1] += special_only(v.x >> 16);
                             o[u >> 2][4 * (u & 3) + 2] += special_only(v.y & 0xffffu);
@@ -339,23 +433,29 @@ __global__ __launch_bounds__(NT, 2) void paged_tile_kernel(PagedArgs a) {
     }
 }
 
-template <int DQK, int DV, bool EXPANDED>
+template <int DQK, int DV, bool EXPANDED, int NW>
 void launch(const PagedArgs &a, hipStream_t s) {
-    hipLaunchKernelGGL((paged_tile_kernel<DQK, DV, EXPANDED>), dim3((unsigned)a.n_work), dim3(NT), 0, s, a);
-    if (a.target > 0) launch_join<DV, ROWS, KT, true>(a, s);
+    if (!EXPANDED && a.lse) hipLaunchKernelGGL((paged_tile_kernel<DQK, DV, EXPANDED, NW, !EXPANDED>), dim3((unsigned)a.n_work), dim3(64 * NW), 0, s, a);
+    else hipLaunchKernelGGL((paged_tile_kernel<DQK, DV, EXPANDED, NW, false>), dim3((unsigned)a.n_work), dim3(64 * NW), 0, s, a);
+    if (a.target > 0) launch_join<DV, 32 * NW, KT, true>(a, s);
 }
 
 }  // namespace
 
-hipError_t launch_paged_tiles(const PagedArgs &a, int head_dim, hipStream_t s) {
-    if (head_dim == 64) launch<64, 64, false>(a, s);
-    else launch<128, 128, false>(a, s);
+hipError_t launch_paged_tiles(const PagedArgs &a, int head_dim, int rows, hipStream_t s) {
+    if (head_dim == 64) {
+        if (rows == 128) launch<64, 64, false, 4>(a, s);
+        else launch<64, 64, false, 8>(a, s);
+    } else {
+        if (rows == 128) launch<128, 128, false, 4>(a, s);
+        else launch<128, 128, false, 8>(a, s);
+    }
     return hipGetLastError();
 }
 
 hipError_t launch_expanded_tiles(const PagedArgs &a, int head_dim, hipStream_t s) {
-    if (head_dim == 64) launch<64 + kLatentRot, 64, true>(a, s);
-    else launch<128 + kLatentRot, 128, true>(a, s);
+    if (head_dim == 64) launch<64 + kLatentRot, 64, true, 8>(a, s);
+    else launch<128 + kLatentRot, 128, true, 8>(a, s);
     return hipGetLastError();
 }
 

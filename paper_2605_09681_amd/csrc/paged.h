@@ -43,10 +43,9 @@ constexpr int kLatentRot = FKV_LATENT_ROT;
 // Attention of rows-per-tile (16, 32, 48, 64) query rows, its parts joined (k_paged_attn.hip).
 hipError_t launch_paged_attention(const PagedArgs &a, int head_dim, int rows, hipStream_t s);
 hipError_t launch_latent_rows(const PagedArgs &a, int latent_dim, int rows, hipStream_t s);
-// Attention of tiles of kPagedTileRows query rows, its parts joined (k_paged_tile.hip).
-constexpr int kPagedTileRows = 128;
-hipError_t launch_paged_tiles(const PagedArgs &a, int head_dim, hipStream_t s);
-hipError_t launch_expanded_tiles(const PagedArgs &a, int head_dim, hipStream_t s);
+// Attention of tiles of 128 or 256 query rows, its parts joined (k_paged_tile.hip).
+hipError_t launch_paged_tiles(const PagedArgs &a, int head_dim, int rows, hipStream_t s);
+hipError_t launch_expanded_tiles(const PagedArgs &a, int head_dim, hipStream_t s);   // 256
 inline int paged_row_tile(int rows) { return rows <= 64 ? (rows + 15) / 16 * 16 : 64; }
 
 // Rows into the pages (k_paged_append.hip).
