@@ -121,7 +121,10 @@ struct Launch {
     size_t part_bytes;
 };
 
-Launch plan(const fkv_batch *b, int kv, int group, int32_t lo, int32_t hi, int rows, int target, int min_tiles, int width) {
+// few: of the launch for few rows (see few_groups), 0: of the other.
+Launch plan(const fkv_batch *b, int kv, int group, int32_t lo, int32_t hi, int rows, int cus, int few, int width) {
+    // the workgroups that the device holds at once; a part is worth 128 keys, or 512 to the larger tiles
+    const int target = cus * (few ? fkv::few_groups(few, rows) : rows == 256 ? 1 : 2), min_tiles = few ? 4 : 8;
     Launch l;
     l.lo = lo;
     l.hi = hi;
@@ -146,6 +149,7 @@ void set_launch(PagedArgs *a, const Launch &l, void *part, bool split) {
     a->n_work = (int32_t)l.n_work;
     a->n_slots = (int32_t)l.n_slots;
     a->part = (float *)part;
+    magic_of(a->group, &a->g_hi, &a->g_lo);
     // the join: some 2000 workgroups, whole tokens each
     a->join_tokens = (int32_t)(((int64_t)a->n_tokens * a->n_heads + 2047) / 2048);
 }
@@ -171,10 +175,9 @@ AttendPlan attend_plan(const fkv_batch *b, int n_heads, int kv, int head_dim, in
     p.many = most > edge;
     p.few = !p.many || b->n_seqs > 1;
     if (p.few)
-        p.f = plan(b, kv, group, 1, edge, fkv::paged_row_tile(std::min(most, edge) * group), (head_dim == 64 ? 4 : 2) * cus, 4, head_dim);
+        p.f = plan(b, kv, group, 1, edge, fkv::paged_row_tile(std::min(most, edge) * group), cus, -head_dim, head_dim);
     if (p.many)
-        p.m = plan(b, kv, group, p.few ? edge + 1 : 1, std::numeric_limits<int32_t>::max(), tile_rows((int64_t)most * group), tile_rows((int64_t)most * group) == 256 ? cus : 2 * cus, 8,
-                   head_dim);
+        p.m = plan(b, kv, group, p.few ? edge + 1 : 1, std::numeric_limits<int32_t>::max(), tile_rows((int64_t)most * group), cus, 0, head_dim);
     p.bytes = std::max(p.f.part_bytes, p.m.part_bytes);
     return p;
 }
@@ -201,14 +204,13 @@ LatentPlan latent_plan(const fkv_batch *b, int n_heads, int d, int R, int form, 
     const size_t rows = (size_t)b->n_tokens * n_heads;
     if (p.absorbed) {
         const int hi = p.expanded ? FKV_LATENT_FEW - 1 : all;
-        p.f = plan(b, 1, n_heads, 1, hi, fkv::paged_row_tile((int)std::min<int64_t>((int64_t)std::min(most, hi) * n_heads, 64)),
-                   (R == 256 ? 2 : 1) * cus, 4, R);
+        p.f = plan(b, 1, n_heads, 1, hi, fkv::paged_row_tile((int)std::min<int64_t>((int64_t)std::min(most, hi) * n_heads, 64)), cus, R, R);
         p.owned_at = take((size_t)b->n_tokens * 4);
         p.q_at = take(rows * (R + FKV_LATENT_ROT) * 2);
         p.o_at = take(rows * R * 2);
     }
     if (p.expanded) {
-        p.m = plan(b, n_heads, 1, p.absorbed ? FKV_LATENT_FEW : 1, all, 256, cus, 8, d);
+        p.m = plan(b, n_heads, 1, p.absorbed ? FKV_LATENT_FEW : 1, all, 256, cus, 0, d);
         const int64_t block = fkv::paged::kSeqRows;
         p.head_rows = ((b->sum_len + block - 1) / block + b->n_seqs) * block;
         p.k_at = take((size_t)n_heads * p.head_rows * (d + FKV_LATENT_ROT) * 2);
@@ -423,6 +425,7 @@ fkv_status fkv_latent_attention(const fkv_batch *batch, int32_t n_heads, int32_t
         tiles.V = a.V_exp;
         tiles.kv = n_heads;
         tiles.group = 1;
+        magic_of(1, &tiles.g_hi, &tiles.g_lo);
         set_span(&tiles, span, n_heads, true);
         if (e == hipSuccess) e = fkv::launch_expanded_tiles(tiles, head_dim, s);
     }

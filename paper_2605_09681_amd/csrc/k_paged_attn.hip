@@ -66,7 +66,7 @@ struct Cfg {
 };
 
 template <int DQK, int DV, bool SHARED, int MT, int NW>
-__global__ __launch_bounds__(64 * NW) void paged_attn_kernel(PagedArgs a) {
+__global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) void paged_attn_kernel(PagedArgs a) {
     using C = Cfg<DQK, DV, SHARED, MT, NW>;
     __shared__ __attribute__((aligned(16))) uint16_t tiles[3][C::TILE];
     // probabilities [2][MT][lane][key block] x 4 bf16; careful: scores [row][SS]
@@ -75,12 +75,12 @@ __global__ __launch_bounds__(64 * NW) void paged_attn_kernel(PagedArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
     static_assert(2 * MT * 64 * 16 <= sizeof mix, "two tiles' probabilities fit");
 
-    const Work item = locate<C::ROWS, KT>(a, blockIdx.x, -1);
+    const Work item = Split<C::ROWS, KT>(a).locate(a, blockIdx.x, -1, 0);
     if (!item.ok) return;
     const Seq s = item.s;
     const int y = item.y, r0 = item.rt * C::ROWS, rows = min(C::ROWS, s.n * a.group - r0);
     const int sink = a.sink[y], recent = a.recent[y];
-    const int t_first = r0 / a.group, t_last = (r0 + rows - 1) / a.group;
+    const int t_first = token_of(a, r0), t_last = token_of(a, r0 + rows - 1);
     const Tiles x = tiles_of<KT>(a, s, sink, recent, t_first, t_last);
     const int tb = (int)((int64_t)x.n * item.part / item.parts), te = (int)((int64_t)x.n * (item.part + 1) / item.parts);
     const int32_t *pages = a.table + (int64_t)item.i * a.max_pages;
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(64 * NW) void paged_attn_kernel(PagedArgs a) {
     Sight seen[C::PER];
 #pragma unroll
     for (int i = 0; i < C::PER; ++i) {
-        const int r = row_of(16 * mt_of(i) + c), tok = r / a.group, head = y * a.group + r - tok * a.group;
+        const int r = row_of(16 * mt_of(i) + c), tok = token_of(a, r), head = y * a.group + r - tok * a.group;
         const uint16_t *from = a.Q + (int64_t)(s.start + tok) * a.q_tok + (int64_t)head * a.q_head + 8 * g;
         seen[i] = sight(a, s, recent, tok);
 #pragma unroll
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(64 * NW) void paged_attn_kernel(PagedArgs a) {
     const int j_last = x.most.end - 1;
     auto rows_of = [&](int t) { return t < te ? pool_row(a, pages, y, min(x.key(t, KT) + (lane & 31), j_last)) : 0; };
     u32x4 kr[C::NK], vr[C::NV > 0 ? C::NV : 1];
-    auto load = [&](int row_of_lane) {
+    auto load_to = [&](int row_of_lane, auto &kr, auto &vr) {
 #pragma unroll
         for (int i = 0; i < C::NK; ++i) {
             const int id = min(tid + i * C::NT, KT * C::CK - 1), k = id / C::CK;
@@ -124,8 +124,9 @@ __global__ __launch_bounds__(64 * NW) void paged_attn_kernel(PagedArgs a) {
             vr[i] = *(const u32x4 *)(a.V + (int64_t)__shfl(row_of_lane, k) * DV + (id - k * C::CV) * 8);
         }
     };
+    auto load = [&](int row_of_lane) { load_to(row_of_lane, kr, vr); };
     bool odd = false;                            // an infinity or a NaN among values that not every row sees
-    auto store = [&](int t) {
+    auto store_from = [&](int t, auto &kr, auto &vr) {
         const int j0 = x.key(t, KT);
         uint16_t *kt = tiles[t % 3], *vt = kt + KT * DQK;
         if (!all_seen<KT>(x, sink, j0)) {
@@ -154,6 +155,7 @@ __global__ __launch_bounds__(64 * NW) void paged_attn_kernel(PagedArgs a) {
             *(u32x4 *)(vt + k * DV + place<C::CV, false>(k, id - k * C::CV) * 8) = vr[i];
         }
     };
+    auto store = [&](int t) { store_from(t, kr, vr); };
     // This wave's blocks of a tile's scores, two sums each so that half as many products wait for one another.
     f32x4_t z[C::PER];
     const bool busy = C::BLOCKS >= NW || w < C::BLOCKS;
@@ -230,17 +232,20 @@ __global__ __launch_bounds__(64 * NW) void paged_attn_kernel(PagedArgs a) {
         l_row[t] = 0.f;
     }
     if (tb < te) {
-        int next = rows_of(tb);
-        load(next);
-        next = rows_of(tb + 1);
-        store(tb);
-        if (tb + 1 < te) load(next);
-        next = rows_of(tb + 2);
+        int next;
+        {                                        // the first two tiles in flight together
+            const int at0 = rows_of(tb), at1 = rows_of(tb + 1);
+            u32x4 k2[C::NK], v2[C::NV > 0 ? C::NV : 1];
+            next = rows_of(tb + 2);
+            load(at0);
+            if (tb + 1 < te) load_to(at1, k2, v2);
+            store(tb);
+            if (tb + 2 < te) load(next);
+            next = rows_of(tb + 3);
+            if (tb + 1 < te) store_from(tb + 1, k2, v2);
+        }
         __syncthreads();
         score(tb);
-        if (tb + 1 < te) store(tb + 1);
-        if (tb + 2 < te) load(next);
-        next = rows_of(tb + 3);
 #pragma unroll
         for (int i = 0; i < C::PER; ++i) {       // (masked keys too: any score is a reference)
             float top = fmaxf(fmaxf(z[i][0], z[i][1]), fmaxf(z[i][2], z[i][3]));
@@ -325,7 +330,7 @@ __global__ __launch_bounds__(64 * NW) void paged_attn_kernel(PagedArgs a) {
                 const uint16_t *vt = tiles[t % 3] + (SHARED ? 0 : KT * DQK);
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
-                    const Sight see = sight(a, s, recent, row_of(16 * i + c) / a.group);
+                    const Sight see = sight(a, s, recent, token_of(a, row_of(16 * i + c)));
                     float e[8], top = neg_inf(), sum = 0.f;
 #pragma unroll
                     for (int r = 0; r < 8; ++r) {
@@ -378,7 +383,7 @@ __global__ __launch_bounds__(64 * NW) void paged_attn_kernel(PagedArgs a) {
         const int r = 16 * t + c;
         if (r >= rows) continue;
         if (item.parts == 1) {
-            const int tok = (r0 + r) / a.group, head = y * a.group + r0 + r - tok * a.group;
+            const int tok = token_of(a, r0 + r), head = y * a.group + r0 + r - tok * a.group;
             const bool none = sight(a, s, recent, tok).end <= 0;
             const float inv = none ? 0.f : 1.f / l_row[t];
             uint16_t *to = a.O + (int64_t)(s.start + tok) * a.o_tok + (int64_t)head * a.o_head;

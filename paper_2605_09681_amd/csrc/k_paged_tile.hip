@@ -63,19 +63,19 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
     __shared__ __attribute__((aligned(16))) uint16_t kts[KB * KT * SK], vts[2 * KT * SV];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), hh = lane >> 5, c = lane & 31;
 
-    Work item = locate<ROWS, KT>(a, blockIdx.x, -1);
+    Work item = Split<ROWS, KT>(a).locate(a, blockIdx.x, -1, 0);
     if (!item.ok) return;
     Seq s = item.s;
     if (EXPANDED) s.len = (int)min((int64_t)s.len, max(a.head_rows - item.base, (int64_t)0));
     const int y = item.y, r0 = item.rt * ROWS, rows = min(ROWS, s.n * a.group - r0);
     const int sink = a.sink[y], recent = a.recent[y];
-    const int t_first = r0 / a.group, t_last = (r0 + rows - 1) / a.group;
+    const int t_first = token_of(a, r0), t_last = token_of(a, r0 + rows - 1);
     const Tiles x = tiles_of<KT>(a, s, sink, recent, t_first, t_last);
     const int tb = (int)((int64_t)x.n * item.part / item.parts), te = (int)((int64_t)x.n * (item.part + 1) / item.parts);
     const int32_t *pages = a.table + (int64_t)item.i * a.max_pages;
 
     // This lane's query row.
-    const int row = min(32 * w + c, rows - 1) + r0, tok = row / a.group, head = y * a.group + row - tok * a.group;
+    const int row = min(32 * w + c, rows - 1) + r0, tok = token_of(a, row), head = y * a.group + row - tok * a.group;
     const bool live = 32 * w + c < rows;
     const Sight seen = sight(a, s, recent, tok);
     bf16x8_t q[KS];
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
             }
         }
     };
-    auto load_k = [&](int row_of_lane) __attribute__((always_inline)) {
+    auto load_k_to = [&](int row_of_lane, auto &kr) __attribute__((always_inline)) {
         if constexpr (EXPANDED) {
 #pragma unroll
             for (int i = 0; i < NK; ++i)
@@ -130,6 +130,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
             load(K, row_of_lane, std::integral_constant<int, DQK>{}, kr);
         }
     };
+    auto load_k = [&](int row_of_lane) __attribute__((always_inline)) { load_k_to(row_of_lane, kr); };
     auto load_v = [&](int row_of_lane) __attribute__((always_inline)) {
         if constexpr (EXPANDED) {
 #pragma unroll
@@ -139,13 +140,14 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
             load(V, row_of_lane, std::integral_constant<int, DV>{}, vr);
         }
     };
-    auto store_k = [&](uint16_t *kt) {
+    auto store_k_from = [&](uint16_t *kt, const auto &kr) {
 #pragma unroll
         for (int i = 0; i < NK; ++i) {
             const int id = tid + i * NT, k = id / CK;
             *(u32x4 *)(kt + k * SK + (id - k * CK) * 8) = kr[i];
         }
     };
+    auto store_k = [&](uint16_t *kt) { store_k_from(kt, kr); };
     auto store_v = [&](uint16_t *vt, int j0, bool edge) {
         if (edge) {
             // (values of keys that no row sees are cleared: a probability of zero would not silence a NaN)
@@ -207,14 +209,15 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
         bool edge = !all_seen<KT>(x, sink, j0);   // not every row sees every key of the tile
         {
             const int first = rows_of(tb);
+            u32x4 k2[NK];
             load_k(first);
             load_v(first);
+            load_k_to(next_v, k2);
+            store_k(kts);
+            store_v(vts, j0, edge);
+            load_v(next_v);
+            store_k_from(kts + KT * SK, k2);
         }
-        store_k(kts);
-        load_k(next_v);
-        store_v(vts, j0, edge);
-        load_v(next_v);
-        store_k(kts + KT * SK);
         __syncthreads();
         f32x16_t z[2];
         score(k_lane, 0, z[0]);

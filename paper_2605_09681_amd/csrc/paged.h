@@ -24,6 +24,7 @@ struct PagedArgs {
     int32_t n_seqs, max_pages, page_tokens, n_pages, n_tokens, max_new, cap;   // cap: tokens that a table row holds
     uint32_t mp_hi, mp_lo;          // floor(2^64 / page_tokens) + 1 (0 for 1)
     int32_t n_heads, kv, group;
+    uint32_t g_hi, g_lo;            // magic of group
     int32_t causal;
     float scale_log2;               // scale * log2(e), finite
     // The launch takes the sequences with lo <= new tokens <= hi.
@@ -46,6 +47,11 @@ hipError_t launch_latent_rows(const PagedArgs &a, int latent_dim, int rows, hipS
 // Attention of tiles of 128 or 256 query rows, its parts joined (k_paged_tile.hip).
 hipError_t launch_paged_tiles(const PagedArgs &a, int head_dim, int rows, hipStream_t s);
 hipError_t launch_expanded_tiles(const PagedArgs &a, int head_dim, hipStream_t s);   // 256
+// Workgroups of that kernel that share a CU, by its registers and LDS: head_dim 64 or 128, negative, or latent_dim.
+constexpr int few_groups(int dim, int rows) {
+    return dim == -64 ? (rows <= 16 ? 5 : rows <= 32 ? 4 : 3) : dim == -128 ? (rows <= 32 ? 3 : 2) : dim == 256 && rows <= 32 ? 2 : 1;
+}
+constexpr int few_waves(int dim, int rows) { return few_groups(dim, rows) * (dim < 0 ? 1 : 2); }   // per SIMD
 inline int paged_row_tile(int rows) { return rows <= 64 ? (rows + 15) / 16 * 16 : 64; }
 
 // Rows into the pages (k_paged_append.hip).
@@ -86,6 +92,27 @@ __device__ __forceinline__ int div_magic(int j, uint32_t hi, uint32_t lo) {
     return (int)(((uint64_t)(uint32_t)j * hi + __umulhi((uint32_t)j, lo)) >> 32);
 }
 
+// Sums over the lanes of a wave before and at each (DPP: no trip through LDS); the last lane's is the sum of all.
+__device__ __forceinline__ int scan_sum(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr 1, 2, 4, 8
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast 15, 31
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
+}
+__device__ __forceinline__ float sum_of(float x) {
+    auto add = [&](float y, int bits) { return y + __int_as_float(bits); };
+    x = add(x, __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x111, 0xf, 0xf, false));
+    x = add(x, __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x112, 0xf, 0xf, false));
+    x = add(x, __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x114, 0xf, 0xf, false));
+    x = add(x, __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x118, 0xf, 0xf, false));
+    x = add(x, __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x142, 0xa, 0xf, false));
+    x = add(x, __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x143, 0xc, 0xf, false));
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+
 struct Seq {
     int len, start, n, first;       // first: position of the first new token (negative: more new tokens than tokens)
 };
@@ -101,6 +128,9 @@ __device__ __forceinline__ Seq sequence(const PagedArgs &a, int i) {
     }
     return s;
 }
+
+// Token of query row r (of a sequence and key head).
+__device__ __forceinline__ int token_of(const PagedArgs &a, int r) { return div_magic(r, a.g_hi, a.g_lo); }
 
 // Which keys of a sequence the query rows of a token see: j < end and (j < sink or j >= low).
 struct Sight {
@@ -142,131 +172,105 @@ struct Work {
     Seq s;
     int i;                          // the sequence
     int y, rt, part, parts;
-    int slot;                       // of the item's part 0; the next part's is `step` further
+    int slot;                       // of the item's part 0 (by token: of key head 0's last row tile); the next part's is `step` further
     int step;
     int64_t base;                   // the sequence's first row in the expanded copies
-    int next;                       // by token, not found: the next row that may be
     bool ok;
 };
 
-// The launch's split: keys are dealt in parts of part_tiles tiles.  That is the least size, from
-// an equal share of all tiles for `target` workgroups up to twice the share, in kSizes steps, with which
+// The launch's split: keys are dealt in parts of some tiles.  That is the least size, from an
+// equal share of all tiles for `target` workgroups up to twice the share, in kSizes steps, with which
 // the parts are no more than `target`: a workgroup too many would start when the others have ended.  Where
 // there are more items than that, only those of more than twice the share are cut.  A sequence's items are all
 // cut alike, its parts dealt evenly over each item's tiles.
+template <int ROWS, int KT>
 struct Split {
     static constexpr int kSizes = 8;
-    float part_tiles;
-    template <int ROWS, int KT>
+    float per_tile;                 // parts a tile; 0: nothing is cut
+    Seq first;                      // this lane's sequence of the first 64
+
+    // Row tiles of this lane's sequence, 0 if the launch does not take it; the most key tiles of an item.
     static __device__ __forceinline__ void counts(const PagedArgs &a, const Seq &s, int *rts, int *tiles) {
         const bool mine = s.n > 0 && s.n >= a.lo && s.n <= a.hi;
-        *rts = mine ? (int)(((int64_t)s.n * a.group + ROWS - 1) / ROWS) : 0;
-        const int64_t keys = a.wide < 0 ? s.len : min((int64_t)s.len, (int64_t)a.wide + s.n + 2 * KT);
-        *tiles = max((int)((keys + KT - 1) / KT), 1);
+        *rts = mine ? (int)(((uint32_t)s.n * (uint32_t)a.group + ROWS - 1) / ROWS) : 0;    // (n, group: 24 and 7 bits)
+        const int keys = a.wide < 0 ? s.len : (int)min((int64_t)s.len, (int64_t)a.wide + s.n + 2 * KT);
+        *tiles = max((keys + KT - 1) / KT, 1);
     }
-    static __device__ __forceinline__ float sum_of(float v) {
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
-        return v;
-    }
-    template <int ROWS, int KT>
-    static __device__ __forceinline__ Split make(const PagedArgs &a) {
-        const int lane = threadIdx.x & 63;
+    __device__ __forceinline__ Seq of(const PagedArgs &a, int i0) const { return i0 == 0 ? first : sequence(a, i0 + (threadIdx.x & 63)); }
+    __device__ __forceinline__ int parts(int tiles) const { return max((int)ceilf((float)tiles * per_tile), 1); }
+
+    __device__ __forceinline__ explicit Split(const PagedArgs &a) {
+        first = sequence(a, threadIdx.x & 63);
+        per_tile = 0.f;
+        if (a.target <= 0) return;
         float sum = 0.f;
         for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
             int rts, tiles;
-            counts<ROWS, KT>(a, sequence(a, i0 + lane), &rts, &tiles);
+            counts(a, of(a, i0), &rts, &tiles);
             sum += (float)rts * (float)tiles;
         }
         const float share = sum_of(sum) * (float)a.kv / (float)a.target;
-        float size[kSizes], parts[kSizes];
+        float per[kSizes], total[kSizes];
 #pragma unroll
         for (int k = 0; k < kSizes; ++k) {
-            size[k] = fmaxf((float)a.min_tiles, ceilf(share * (1.f + (float)(k * k) / ((kSizes - 1) * (kSizes - 1)))));
-            parts[k] = 0.f;
+            per[k] = __builtin_amdgcn_rcpf(fmaxf((float)a.min_tiles, ceilf(share * (1.f + (float)(k * k) / ((kSizes - 1) * (kSizes - 1))))));
+            total[k] = 0.f;
         }
         for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
             int rts, tiles;
-            counts<ROWS, KT>(a, sequence(a, i0 + lane), &rts, &tiles);
+            counts(a, of(a, i0), &rts, &tiles);
 #pragma unroll
-            for (int k = 0; k < kSizes; ++k) parts[k] += (float)rts * ceilf((float)tiles / size[k]);
+            for (int k = 0; k < kSizes; ++k) total[k] += (float)rts * fmaxf(ceilf((float)tiles * per[k]), 1.f);
         }
-        float best = size[kSizes - 1];
+        per_tile = per[kSizes - 1];
 #pragma unroll
         for (int k = kSizes - 2; k >= 0; --k)
-            if (sum_of(parts[k]) * (float)a.kv <= (float)a.target) best = size[k];
-        return Split{best};
+            if (sum_of(total[k]) * (float)a.kv <= (float)a.target) per_tile = per[k];
     }
-    __device__ __forceinline__ int parts(const PagedArgs &a, int tiles) const {
-        return a.target > 0 ? max((int)ceilf((float)tiles / part_tiles), 1) : 1;
+
+    // Work item `want` (token < 0), or the first cut sequence with batch rows in token .. end - 1.  Every lane of a
+    // wave calls it; the result is the same in all.
+    __device__ __forceinline__ Work locate(const PagedArgs &a, int want, int token, int end) const {
+        Work w;
+        w.ok = false;
+        int done = 0, slots = 0, rows = 0;
+        for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
+            const Seq s = of(a, i0);
+            int rts, tiles;
+            counts(a, s, &rts, &tiles);
+            const int n = parts(tiles), c = a.kv * rts * n, cut = n > 1 ? c : 0;
+            const int blocks = rts > 0 ? (s.len + kSeqRows - 1) / kSeqRows : 0;
+            const int ic = scan_sum(c), is = scan_sum(cut), ib = scan_sum(blocks);
+            const uint64_t found = token < 0 ? __ballot(done + ic > want) : __ballot(cut > 0 && s.start < end && s.start + s.n > token);
+            if (found) {
+                const int l = __builtin_ctzll(found);
+                auto at = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+                w.i = i0 + l;
+                w.s = Seq{at(s.len), at(s.start), at(s.n), at(s.first)};
+                const int rt = at(rts), before = done + at(ic) - at(c);
+                w.parts = at(n);
+                w.step = a.kv * rt;
+                w.base = (int64_t)(rows + at(ib) - at(blocks)) * kSeqRows;
+                w.slot = slots + at(is) - at(cut);
+                w.part = w.y = w.rt = 0;
+                if (token < 0) {
+                    const int local = want - before;
+                    w.part = w.parts > 1 ? local / w.step : 0;
+                    const int u = local - w.part * w.step;
+                    w.y = u / rt;
+                    w.rt = rt - 1 - (u - w.y * rt);          // the longest rows of a causal chunk first
+                    w.slot += u;
+                }
+                w.ok = true;
+                return w;
+            }
+            done += __builtin_amdgcn_readlane(ic, 63);
+            slots += __builtin_amdgcn_readlane(is, 63);
+            rows += __builtin_amdgcn_readlane(ib, 63);
+        }
+        return w;
     }
 };
-
-// Looks for work item `want` (token < 0), or for the sequence that holds batch row `token`.
-// Every lane of a wave calls it; the result is the same in all.
-template <int ROWS, int KT>
-__device__ __forceinline__ Work locate(const PagedArgs &a, int want, int token) {
-    const int lane = threadIdx.x & 63;
-    const Split split = a.target > 0 ? Split::make<ROWS, KT>(a) : Split{0.f};
-    Work w;
-    w.ok = false;
-    int done = 0, slots = 0, after = a.n_tokens;
-    int64_t rows = 0;
-    for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
-        const Seq s = sequence(a, i0 + lane);
-        int rts, tiles;
-        Split::counts<ROWS, KT>(a, s, &rts, &tiles);
-        if (rts > 0 && s.start > token) after = min(after, s.start);
-        const int parts = split.parts(a, tiles), c = a.kv * rts * parts, cut = parts > 1 ? c : 0;
-        const int blocks = rts > 0 ? (s.len + kSeqRows - 1) / kSeqRows : 0;
-        int ic = c, is = cut, ib = blocks;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int uc = __shfl_up(ic, d), us = __shfl_up(is, d), ub = __shfl_up(ib, d);
-            if (lane >= d) {
-                ic += uc;
-                is += us;
-                ib += ub;
-            }
-        }
-        const uint64_t found = token < 0 ? __ballot(done + ic > want)
-                                         : __ballot(rts > 0 && token >= s.start && token - s.start < s.n);
-        if (found) {
-            const int l = __builtin_ctzll(found);
-            auto at = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
-            w.i = i0 + l;
-            w.s = Seq{at(s.len), at(s.start), at(s.n), at(s.first)};
-            const int rt = at(rts), first = done + at(ic) - at(c);
-            w.parts = at(parts);
-            w.step = a.kv * rt;
-            w.base = (rows + at(ib) - at(blocks)) * kSeqRows;
-            const int slot = slots + at(is) - at(cut);
-            if (token < 0) {
-                const int local = want - first;
-                w.part = local / w.step;
-                const int u = local - w.part * w.step;
-                w.y = u / rt;
-                w.rt = rt - 1 - (u - w.y * rt);          // the longest rows of a causal chunk first
-                w.slot = slot + u;
-            } else {
-                w.part = 0;
-                w.y = w.rt = 0;
-                w.slot = slot;                           // of key head 0's last row tile
-            }
-            w.ok = true;
-            return w;
-        }
-        done += __builtin_amdgcn_readlane(ic, 63);
-        slots += __builtin_amdgcn_readlane(is, 63);
-        rows += __builtin_amdgcn_readlane(ib, 63);
-    }
-    if (token >= 0) {
-#pragma unroll
-        for (int d = 32; d > 0; d >>= 1) after = min(after, __shfl_xor(after, d));
-    }
-    w.next = after;
-    return w;
-}
 
 // The sequence that holds this lane's batch row `token` (-1: none, or not one of the launch's), and the
 // sequence.  Every lane of a wave calls it.
@@ -295,12 +299,7 @@ __device__ __forceinline__ int locate_block(const PagedArgs &a, int want, Seq *h
     for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
         const Seq s = sequence(a, i0 + lane);
         const int blocks = s.n > 0 && s.n >= a.lo && s.n <= a.hi ? (s.len + kSeqRows - 1) / kSeqRows : 0;
-        int ib = blocks;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int u = __shfl_up(ib, d);
-            if (lane >= d) ib += u;
-        }
+        const int ib = scan_sum(blocks);
         const uint64_t found = __ballot(done + ib > want);
         if (found) {
             const int l = __builtin_ctzll(found);

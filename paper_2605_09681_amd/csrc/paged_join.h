@@ -25,20 +25,14 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedArgs a) {
     __shared__ float top[kLanes], total[kLanes];
     const int head = blockIdx.y, y = head / a.group, d = threadIdx.x % (D / 4), lane = threadIdx.x / (D / 4);
     const int end = min((int)(blockIdx.x + 1) * a.join_tokens, a.n_tokens);
+    const Split<ROWS, KT> split(a);
     for (int token = blockIdx.x * a.join_tokens; token < end;) {
-        const Work w = locate<ROWS, KT>(a, 0, token);    // (the same in the whole workgroup)
-        if (!w.ok) {
-            token = w.next;
-            continue;
-        }
-        const int last = min(end, w.s.start + w.s.n);    // the sequence's tokens of the workgroup
-        if (w.parts == 1) {
-            token = last;
-            continue;
-        }
+        const Work w = split.locate(a, 0, token, end);   // (the same in the whole workgroup)
+        if (!w.ok) return;
+        const int from = max(token, w.s.start), last = min(end, w.s.start + w.s.n);   // the sequence's tokens of the workgroup
         const int rts = w.step / a.kv;
         const int64_t step = w.step * kSlot;
-        for (int t = token + (WIDE ? lane : 0); t < last; t += WIDE ? kLanes : 1) {
+        for (int t = from + (WIDE ? lane : 0); t < last; t += WIDE ? kLanes : 1) {
             const int tok = t - w.s.start, r = tok * a.group + head - y * a.group, rt = r / ROWS;
             const float *p = a.part + (int64_t)(w.slot + y * rts + rts - 1 - rt) * kSlot;
             const float *po = p + (r - rt * ROWS) * D + 4 * d, *pm = p + ROWS * D + r - rt * ROWS, *pl = pm + ROWS;
