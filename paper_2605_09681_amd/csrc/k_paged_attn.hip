@@ -92,15 +92,6 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
     auto mine = [&](int i) { return C::BLOCKS % NW == 0 || w + NW * i < C::BLOCKS; };
     bf16x8_t q[C::PER][C::KS];
     Sight seen[C::PER];
-#pragma unroll
-    for (int i = 0; i < C::PER; ++i) {
-        const int r = row_of(16 * mt_of(i) + c), tok = token_of(a, r), head = y * a.group + r - tok * a.group;
-        const uint16_t *from = a.Q + (int64_t)(s.start + tok) * a.q_tok + (int64_t)head * a.q_head + 8 * g;
-        seen[i] = sight(a, s, recent, tok);
-#pragma unroll
-        for (int k = 0; k < C::KS; ++k)
-            q[i][k] = frag(mine(i) && 16 * mt_of(i) + c < rows ? *(const u32x4 *)(from + 32 * k) : u32x4{0, 0, 0, 0});
-    }
     f32x4_t o[MT][C::NB];
 #pragma unroll
     for (int t = 0; t < MT; ++t)
@@ -239,6 +230,15 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
             next = rows_of(tb + 2);
             load(at0);
             if (tb + 1 < te) load_to(at1, k2, v2);
+#pragma unroll
+            for (int i = 0; i < C::PER; ++i) {
+                const int r = row_of(16 * mt_of(i) + c), tok = token_of(a, r), head = y * a.group + r - tok * a.group;
+                const uint16_t *from = a.Q + (int64_t)(s.start + tok) * a.q_tok + (int64_t)head * a.q_head + 8 * g;
+                seen[i] = sight(a, s, recent, tok);
+#pragma unroll
+                for (int k = 0; k < C::KS; ++k)
+                    q[i][k] = frag(mine(i) && 16 * mt_of(i) + c < rows ? *(const u32x4 *)(from + 32 * k) : u32x4{0, 0, 0, 0});
+            }
             store(tb);
             if (tb + 2 < te) load(next);
             next = rows_of(tb + 3);

@@ -79,11 +79,6 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
     const bool live = 32 * w + c < rows;
     const Sight seen = sight(a, s, recent, tok);
     bf16x8_t q[KS];
-    {
-        const uint16_t *from = a.Q + (int64_t)(s.start + tok) * a.q_tok + (int64_t)head * a.q_head + 8 * hh;
-#pragma unroll
-        for (int k = 0; k < KS; ++k) q[k] = frag(live ? *(const u32x4 *)(from + 16 * k) : u32x4{0, 0, 0, 0});
-    }
     f32x16_t o[MB];
     float m, l;
 
@@ -213,6 +208,11 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
             load_k(first);
             load_v(first);
             load_k_to(next_v, k2);
+            {
+                const uint16_t *from = a.Q + (int64_t)(s.start + tok) * a.q_tok + (int64_t)head * a.q_head + 8 * hh;
+#pragma unroll
+                for (int k = 0; k < KS; ++k) q[k] = frag(live ? *(const u32x4 *)(from + 16 * k) : u32x4{0, 0, 0, 0});
+            }
             store_k(kts);
             store_v(vts, j0, edge);
             load_v(next_v);

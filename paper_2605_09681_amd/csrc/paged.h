@@ -178,6 +178,12 @@ struct Work {
     bool ok;
 };
 
+// a / b for 0 <= a < 2^24, b >= 1 (an integer division is some 40 instructions).
+__device__ __forceinline__ int quotient(int a, int b) {
+    const int q = (int)((float)a * __builtin_amdgcn_rcpf((float)b)), r = a - q * b;
+    return q + (r >= b) - (r < 0);
+}
+
 // The launch's split: keys are dealt in parts of some tiles.  That is the least size, from an
 // equal share of all tiles for `target` workgroups up to twice the share, in kSizes steps, with which
 // the parts are no more than `target`: a workgroup too many would start when the others have ended.  Where
@@ -255,9 +261,9 @@ struct Split {
                 w.part = w.y = w.rt = 0;
                 if (token < 0) {
                     const int local = want - before;
-                    w.part = w.parts > 1 ? local / w.step : 0;
+                    w.part = w.parts > 1 ? quotient(local, w.step) : 0;
                     const int u = local - w.part * w.step;
-                    w.y = u / rt;
+                    w.y = quotient(u, rt);
                     w.rt = rt - 1 - (u - w.y * rt);          // the longest rows of a causal chunk first
                     w.slot += u;
                 }

@@ -1,10 +1,10 @@
 // paged_join.h -- joins the parts of split items: M = max_j m_j,
 // L = sum_j 2^(c (m_j - M)) l_j, O = sum_j 2^(c (m_j - M)) o_j / L.  A launch of its own: the
 // parts cross as ordinary stores and loads, and the workspace holds no counters.
-// A workgroup takes join_tokens tokens of a query head; D / 4 threads take 4 channels of a
-// row each.  WIDE (few parts of many rows): every such group of threads takes rows of its
-// own; otherwise the groups share a row, each taking every kLanes'th part, and their
-// sums meet in LDS in a fixed order.  Tokens of items that were not split are left alone.
+// A workgroup takes 64 channels of join_tokens tokens of a query head, 16 threads 4 channels
+// each.  WIDE (few parts of many rows): every 16 threads take rows of their own; otherwise
+// they share a row, each taking every kLanes'th part, and their sums meet in LDS in a fixed
+// order.  Tokens of items that were not split are left alone.
 #pragma once
 
 #include "paged.h"
@@ -16,14 +16,15 @@ constexpr int kJoinThreads = 256, kJoin = 4;   // threads of a workgroup, parts 
 typedef float join_f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 join_bf16x4 __attribute__((ext_vector_type(4)));
 
-// grid: x = tokens, y = query head.  ROWS, KT: of the kernel that wrote the parts.
+// grid: x = tokens, y = query head, z = 64 channels.  ROWS, KT: of the kernel that wrote the parts.
 template <int D, int ROWS, int KT, bool WIDE>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedArgs a) {
-    constexpr int kLanes = kJoinThreads / (D / 4);
+    constexpr int kLanes = kJoinThreads / 16;
     constexpr int64_t kSlot = ROWS * (D + 2);
-    __shared__ join_f32x4 sum[kLanes][D / 4];
+    __shared__ join_f32x4 sum[kLanes][16];
     __shared__ float top[kLanes], total[kLanes];
-    const int head = blockIdx.y, y = head / a.group, d = threadIdx.x % (D / 4), lane = threadIdx.x / (D / 4);
+    const int head = blockIdx.y, y = head / a.group, d = threadIdx.x % 16, lane = threadIdx.x / 16;
+    const int ch = 64 * blockIdx.z + 4 * d;
     const int end = min((int)(blockIdx.x + 1) * a.join_tokens, a.n_tokens);
     const Split<ROWS, KT> split(a);
     for (int token = blockIdx.x * a.join_tokens; token < end;) {
@@ -35,7 +36,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedArgs a) {
         for (int t = from + (WIDE ? lane : 0); t < last; t += WIDE ? kLanes : 1) {
             const int tok = t - w.s.start, r = tok * a.group + head - y * a.group, rt = r / ROWS;
             const float *p = a.part + (int64_t)(w.slot + y * rts + rts - 1 - rt) * kSlot;
-            const float *po = p + (r - rt * ROWS) * D + 4 * d, *pm = p + ROWS * D + r - rt * ROWS, *pl = pm + ROWS;
+            const float *po = p + (r - rt * ROWS) * D + ch, *pm = p + ROWS * D + r - rt * ROWS, *pl = pm + ROWS;
             float M = neg_inf(), L = 0.f;
             join_f32x4 acc = {0.f, 0.f, 0.f, 0.f};
             auto add = [&](float m, float l, const join_f32x4 &o) {
@@ -78,8 +79,8 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedArgs a) {
             join_bf16x4 out;
 #pragma unroll
             for (int k = 0; k < 4; ++k) out[k] = (__bf16)(acc[k] * inv);
-            *(join_bf16x4 *)(a.O + (int64_t)t * a.o_tok + (int64_t)head * a.o_head + 4 * d) = out;
-            if (a.lse && d == 0)
+            *(join_bf16x4 *)(a.O + (int64_t)t * a.o_tok + (int64_t)head * a.o_head + ch) = out;
+            if (a.lse && ch == 0)
                 a.lse[(int64_t)head * a.n_tokens + t] = none ? neg_inf() : fmaf(M * 0.69314718055994530942f, a.scale_log2, logf(L));
         }
         token = last;
@@ -88,7 +89,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedArgs a) {
 
 template <int D, int ROWS, int KT, bool WIDE>
 inline void launch_join(const PagedArgs &a, hipStream_t s) {
-    const dim3 grid((unsigned)((a.n_tokens + a.join_tokens - 1) / a.join_tokens), (unsigned)a.n_heads);
+    const dim3 grid((unsigned)((a.n_tokens + a.join_tokens - 1) / a.join_tokens), (unsigned)a.n_heads, D / 64);
     hipLaunchKernelGGL((paged_join_kernel<D, ROWS, KT, WIDE>), grid, dim3(kJoinThreads), 0, s, a);
 }
 
