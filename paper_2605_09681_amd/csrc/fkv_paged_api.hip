@@ -104,6 +104,9 @@ void set_batch(PagedArgs *a, const fkv_batch *b) {
 void set_span(PagedArgs *a, const fkv_span *spans, int n, bool one) {
     const int32_t most = 1 << 30;
     a->wide = 0;
+    a->one_span = 1;
+    for (int y = 1; spans && !one && y < n; ++y)
+        if (spans[y].sink_tokens != spans[0].sink_tokens || spans[y].recent_tokens != spans[0].recent_tokens) a->one_span = 0;
     for (int y = 0; y < n; ++y) {
         a->sink[y] = spans ? std::min(spans[one ? 0 : y].sink_tokens, most) : 0;
         a->recent[y] = spans ? std::min(spans[one ? 0 : y].recent_tokens, most) : -1;
@@ -116,8 +119,7 @@ void set_span(PagedArgs *a, const fkv_span *spans, int n, bool one) {
 // them to a sequence and key head), split for `target` workgroups.
 struct Launch {
     int32_t lo, hi, rows, target, min_tiles;
-    int64_t n_work;
-    int64_t n_slots;
+    int64_t n_items, n_work, n_slots, n_joins;   // items at the most; workgroups, slots, cut items where items are cut
     size_t part_bytes;
 };
 
@@ -135,10 +137,13 @@ Launch plan(const fkv_batch *b, int kv, int group, int32_t lo, int32_t hi, int r
     // row tiles: a sequence has one beside every `rows` rows of its own
     const int64_t most = std::min(std::min(b->max_new, b->n_tokens), hi), seqs = std::min(b->n_seqs, b->n_tokens);
     const int64_t tiles = most * group <= rows ? seqs : (int64_t)b->n_tokens * group / rows + seqs;
-    l.n_work = tiles * kv + (target > 0 ? target + 8 : 0);
-    // a sequence is cut only if its tiles are more than one part's: at most twice the target
-    l.n_slots = target > 0 ? 2 * (int64_t)target + 64 : 0;
-    l.part_bytes = (size_t)l.n_slots * rows * (width + 2) * 4;
+    // few rows: the items, and the parts that cuts add; a sequence is cut only if its tiles are more than one
+    // part's, so parts of cut ones are at most twice the target.  Many rows: a share and two slots to a workgroup.
+    l.n_items = tiles * kv;
+    l.n_work = few ? l.n_items + target + 8 : target;
+    l.n_slots = 2 * (int64_t)target + (few ? 64 : 0);
+    l.n_joins = few ? std::min(l.n_items, l.n_slots / 2) : target;
+    l.part_bytes = l.n_joins * sizeof(fkv::JoinItem) + (size_t)l.n_slots * rows * (width + 2) * 4;
     return l;
 }
 
@@ -147,12 +152,12 @@ void set_launch(PagedArgs *a, const Launch &l, void *part, bool split) {
     a->hi = l.hi;
     a->target = split ? l.target : 0;
     a->min_tiles = l.min_tiles;
-    a->n_work = (int32_t)l.n_work;
+    a->n_work = (int32_t)(split ? l.n_work : l.n_items);
     a->n_slots = (int32_t)l.n_slots;
-    a->part = (float *)part;
+    a->joins = (fkv::JoinItem *)part;
+    a->n_joins = (int32_t)l.n_joins;
+    a->part = (float *)((char *)part + l.n_joins * sizeof(fkv::JoinItem));
     magic_of(a->group, &a->g_hi, &a->g_lo);
-    // the join: some 2000 workgroups, whole tokens each
-    a->join_tokens = (int32_t)(((int64_t)a->n_tokens * a->n_heads + 2047) / 2048);
 }
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
@@ -224,7 +229,7 @@ LatentPlan latent_plan(const fkv_batch *b, int n_heads, int d, int R, int form, 
 
 fkv_status check_work(const Launch &l) {
     // (a launch holds fewer than 2^32 threads, at most 512 in a workgroup)
-    return l.n_work >= (int64_t)1 << 22 ? fail(FKV_ERR_SHAPE, "%lld tiles of query rows are too many for one call", (long long)l.n_work)
+    return l.n_items >= (int64_t)1 << 22 ? fail(FKV_ERR_SHAPE, "%lld tiles of query rows are too many for one call", (long long)l.n_items)
                                         : FKV_OK;
 }
 

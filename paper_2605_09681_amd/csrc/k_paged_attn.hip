@@ -75,7 +75,12 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
     static_assert(2 * MT * 64 * 16 <= sizeof mix, "two tiles' probabilities fit");
 
-    const Work item = Split<C::ROWS, KT>(a).locate(a, blockIdx.x, -1, 0);
+    const Split<C::ROWS, KT> split(a);
+    const Work item = split.locate(a, blockIdx.x);
+    if (blockIdx.x == 0 && a.target > 0) {
+        const int n = split.cut_items(a);
+        if (tid == 0) a.joins[0].count = n;
+    }
     if (!item.ok) return;
     const Seq s = item.s;
     const int y = item.y, r0 = item.rt * C::ROWS, rows = min(C::ROWS, s.n * a.group - r0);
@@ -84,6 +89,18 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
     const Tiles x = tiles_of<KT>(a, s, sink, recent, t_first, t_last);
     const int tb = (int)((int64_t)x.n * item.part / item.parts), te = (int)((int64_t)x.n * (item.part + 1) / item.parts);
     const int32_t *pages = a.table + (int64_t)item.i * a.max_pages;
+    if (item.parts > 1 && item.part == 0 && tid == 0 && item.join < a.n_joins) {
+        JoinItem &j = a.joins[item.join];
+        j.rows = rows;
+        j.start = s.start;
+        j.len = s.len;
+        j.first = s.first;
+        j.y = y;
+        j.row0 = r0;
+        j.parts = item.parts;
+        j.slot = item.slot;
+        j.step = item.step;
+    }
     auto row_of = [&](int r) { return min(r, rows - 1) + r0; };
 
     // Score blocks of this wave: key block kb of row tiles mt_of(0), mt_of(1).
@@ -405,12 +422,53 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
     }
 }
 
+// One workgroup joins a row of a cut item: D / 4 threads take 4 channels each, kLanes of them every
+// kLanes'th part, and their sums meet in LDS in a fixed order.  grid: x = cut item, y = row.
+template <int D, int ROWS>
+__global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedArgs a) {
+    constexpr int kLanes = kJoinThreads / (D / 4), kAtOnce = 4;
+    __shared__ join_f32x4 sum[kLanes][D / 4];
+    __shared__ float top[kLanes], total[kLanes];
+    if ((int)blockIdx.x >= a.joins[0].count) return;
+    const JoinItem j = a.joins[blockIdx.x];
+    const int r = blockIdx.y, d = threadIdx.x % (D / 4), lane = threadIdx.x / (D / 4);
+    if (r >= j.rows) return;
+    const int64_t step = (int64_t)j.step * (ROWS * (D + 2));
+    const float *p = a.part + (int64_t)j.slot * (ROWS * (D + 2)), *po = p + r * D + 4 * d, *pm = p + ROWS * D + r, *pl = pm + ROWS;
+    Joined x;
+    for (int k0 = lane; k0 < j.parts; k0 += kAtOnce * kLanes) {
+        float m[kAtOnce], l[kAtOnce];
+        join_f32x4 o[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const int64_t at = min(k0 + k * kLanes, j.parts - 1) * step;
+            m[k] = pm[at];
+            l[k] = pl[at];
+            o[k] = *(const join_f32x4 *)(po + at);
+        }
+        // (all loads before the first use: one memory latency, not one each)
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
+            if (k0 + k * kLanes < j.parts) x.add(m[k], l[k], o[k], a.scale_log2);
+    }
+    sum[lane][d] = x.acc;
+    if (d == 0) {
+        top[lane] = x.M;
+        total[lane] = x.L;
+    }
+    __syncthreads();
+    if (lane > 0) return;
+    for (int i = 1; i < kLanes; ++i) x.add(top[i], total[i], sum[i][d], a.scale_log2);
+    x.put(a, j, r, 4 * d);
+}
+
 template <int DQK, int DV, bool SHARED, int NW>
 void launch_rows(const PagedArgs &a, int rows, hipStream_t s) {
     auto go = [&](auto mt) {
         constexpr int MT = decltype(mt)::value;
         hipLaunchKernelGGL((paged_attn_kernel<DQK, DV, SHARED, MT, NW>), dim3((unsigned)a.n_work), dim3(64 * NW), 0, s, a);
-        if (a.target > 0) launch_join<DV, 16 * MT, KT, false>(a, s);
+        if (a.target > 0) hipLaunchKernelGGL((paged_join_kernel<DV, 16 * MT>), dim3((unsigned)a.n_joins, 16 * MT), dim3(kJoinThreads), 0, s, a);
     };
     if (rows <= 16) go(std::integral_constant<int, 1>{});
     else if (rows <= 32) go(std::integral_constant<int, 2>{});

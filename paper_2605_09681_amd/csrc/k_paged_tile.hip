@@ -19,7 +19,6 @@ namespace {
 using namespace paged;
 
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-typedef short short2_t __attribute__((ext_vector_type(2)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
@@ -63,16 +62,49 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
     __shared__ __attribute__((aligned(16))) uint16_t kts[KB * KT * SK], vts[2 * KT * SV];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), hh = lane >> 5, c = lane & 31;
 
-    Work item = Split<ROWS, KT>(a).locate(a, blockIdx.x, -1, 0);
-    if (!item.ok) return;
-    Seq s = item.s;
-    if (EXPANDED) s.len = (int)min((int64_t)s.len, max(a.head_rows - item.base, (int64_t)0));
-    const int y = item.y, r0 = item.rt * ROWS, rows = min(ROWS, s.n * a.group - r0);
+    // A share of the line of all items, or (no workspace) one item.
+    using Line = Shares<ROWS, KT>;
+    const bool shared = a.target > 0;
+    const int number = shared ? (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3) : blockIdx.x;   // (neighbours on one XCD)
+    typename Line::Place at;
+    int rt = 0;
+    int64_t base = 0;                             // the sequence's first row in the expanded copies
+    double from = 0., until = 0., stride = 0.;
+    if (shared) {
+        if (tid == 0) {
+            a.joins[number].rows = 0;
+            a.joins[number].goes_on = 0;
+        }
+        const Line line(a);
+        if (number >= line.groups || line.total == 0.) return;
+        from = line.start(number);
+        until = line.start(number + 1);
+        stride = line.each;
+        at = line.find(a, from);
+        if (!at.ok) return;
+        while (at.y + 1 < a.kv && at.y_begin + at.y_long <= from) Line::next_head(a, &at);
+        rt = Line::row_tile_at(a, at, from);
+    } else {
+        const Work item = Split<ROWS, KT>(a).locate(a, number);
+        if (!item.ok) return;
+        at.s = item.s;
+        at.i = item.i;
+        at.y = item.y;
+        rt = item.rt;
+    }
+    if (EXPANDED) base = first_row(a, at.i);
+#pragma unroll 1
+    for (;;) {                                    // (the body ends with the workgroup past its reads of LDS)
+    Seq s = at.s;
+    if (EXPANDED) s.len = (int)min((int64_t)s.len, max(a.head_rows - base, (int64_t)0));
+    const int y = at.y, r0 = rt * ROWS, rows = min(ROWS, s.n * a.group - r0);
     const int sink = a.sink[y], recent = a.recent[y];
     const int t_first = token_of(a, r0), t_last = token_of(a, r0 + rows - 1);
     const Tiles x = tiles_of<KT>(a, s, sink, recent, t_first, t_last);
-    const int tb = (int)((int64_t)x.n * item.part / item.parts), te = (int)((int64_t)x.n * (item.part + 1) / item.parts);
-    const int32_t *pages = a.table + (int64_t)item.i * a.max_pages;
+    const double item_at = shared ? Line::at(a, at, rt) : 0., item_end = shared ? Line::at(a, at, rt + 1) : 0.;
+    const int tb = shared ? Line::cut(from, item_at, item_end, x.n) : 0, te = shared ? Line::cut(until, item_at, item_end, x.n) : x.n;
+    const bool whole = tb == 0 && te == x.n;
+    const int32_t *pages = a.table + (int64_t)at.i * a.max_pages;
 
     // This lane's query row.
     const int row = min(32 * w + c, rows - 1) + r0, tok = token_of(a, row), head = y * a.group + row - tok * a.group;
@@ -86,8 +118,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
     const int j_last = x.most.end - 1;
     const uint16_t *K = a.K, *V = a.V;
     if (EXPANDED) {
-        K += (y * a.head_rows + item.base) * DQK;
-        V += (y * a.head_rows + item.base) * DV;
+        K += (y * a.head_rows + base) * DQK;
+        V += (y * a.head_rows + base) * DV;
     }
     auto rows_of = [&](int t) {
         const int j = x.key(min(t, te - 1), KT);
@@ -258,7 +290,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
                 uint32_t word = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{v[0], v[1]}, bf16x2_t));
                 asm volatile("" : "+v"(word));     // (not moved to its use)
                 if (!LSE)
-                    sum[i & 1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(short2_t, word), __builtin_bit_cast(short2_t, 0x3f803f80), sum[i & 1], false);
+                    sum[i & 1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, word), __builtin_bit_cast(bf16x2_t, 0x3f803f80), sum[i & 1], false);
                 p[kb][i >> 2][i & 3] = word;
             }
         };
@@ -408,8 +440,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
     }
 
     l += __shfl_xor(l, 32);
-    if (!live) return;
-    if (item.parts == 1) {
+    if (live && whole && (tb < te || !shared || (item_at >= from && item_at < until))) {   // (no key: who has the item's begin)
         const bool none = seen.end <= 0;
         const float inv = none ? 0.f : 1.f / l;
         uint16_t *to = a.O + (int64_t)(s.start + tok) * a.o_tok + (int64_t)head * a.o_head + 4 * hh;
@@ -418,10 +449,28 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
 #pragma unroll
             for (int u = 0; u < 4; ++u)
                 *(uint2 *)(to + 32 * b + 8 * u) = pack4(o[b][4 * u] * inv, o[b][4 * u + 1] * inv, o[b][4 * u + 2] * inv, o[b][4 * u + 3] * inv);
-        if (a.lse && hh == 0)
+        if (LSE && hh == 0)
             a.lse[(int64_t)head * a.n_tokens + s.start + tok] = none ? neg_inf() : fmaf(m * kLn2, a.scale_log2, logf(l));
-    } else {
-        float *slot = a.part + (int64_t)(item.slot + item.part * item.step) * (ROWS * (DV + 2));
+    } else if (live && !whole && tb < te) {
+        if (tid == 0) {
+            JoinItem &j = a.joins[number];
+            if (tb > 0) {
+                j.goes_on = 1;
+            } else {
+                j.rows = rows;
+                j.start = s.start;
+                j.len = s.len;
+                j.first = s.first;
+                j.y = y;
+                j.row0 = r0;
+                // the workgroups whose shares begin before the item ends
+                int n = min((int)((item_end - from) / stride), (int)gridDim.x - 1 - number);
+                while (n > 0 && stride * (double)(number + n) >= item_end) --n;
+                while (number + n + 1 < (int)gridDim.x && stride * (double)(number + n + 1) < item_end) ++n;
+                j.parts = n + 1;
+            }
+        }
+        float *slot = a.part + (int64_t)(2 * number + (tb == 0)) * (ROWS * (DV + 2));
         float *to = slot + (32 * w + c) * DV + 4 * hh;
         const float by = moderate(&m, &l, a.scale_log2);
 #pragma unroll
@@ -434,13 +483,55 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
             slot[ROWS * DV + ROWS + 32 * w + c] = l;
         }
     }
+    // The next item of the share.
+    if (!shared || item_end >= until) return;
+    if (++rt == at.rts) {
+        rt = 0;
+        if (at.y + 1 < a.kv) {
+            Line::next_head(a, &at);
+        } else {
+            const Line line(a);
+            at = line.find(a, at.end);
+            if (!at.ok) return;
+            if (EXPANDED) base = first_row(a, at.i);
+        }
+    }
+    }
+}
+
+// One workgroup joins kJoinRows rows of the cut item that workgroup x's share ends in: its own part lies in slot
+// 2 x + 1, those of the workgroups after it in slots 2 g, of some that have none in no slot.  D / 4 threads take 4
+// channels each of a row.  grid: x = workgroup, y = rows.
+constexpr int kJoinRows = 32;
+template <int D, int ROWS>
+__global__ __launch_bounds__(kJoinThreads) void paged_share_join_kernel(PagedArgs a) {
+    constexpr int kLanes = kJoinThreads / (D / 4);
+    constexpr int64_t kSlot = ROWS * (D + 2);
+    const JoinItem j = a.joins[blockIdx.x];
+    const int d = threadIdx.x % (D / 4), r0 = blockIdx.y * kJoinRows;
+    for (int r = r0 + threadIdx.x / (D / 4); r < min(r0 + kJoinRows, j.rows); r += kLanes) {
+        Joined x;
+        for (int k = 0; k < j.parts; ++k) {
+            const int g = blockIdx.x + k;
+            if (k > 0 && !a.joins[g].goes_on) continue;
+            const float *p = a.part + (2 * g + (k == 0)) * kSlot;
+            x.add(p[ROWS * D + r], p[ROWS * D + ROWS + r], *(const join_f32x4 *)(p + r * D + 4 * d), a.scale_log2);
+        }
+        x.put(a, j, r, 4 * d);
+    }
+}
+
+template <int DQK, int DV, bool EXPANDED, int NW, bool LSE>
+void launch_as(const PagedArgs &a, hipStream_t s) {
+    hipLaunchKernelGGL((paged_tile_kernel<DQK, DV, EXPANDED, NW, LSE>), dim3((unsigned)a.n_work), dim3(64 * NW), 0, s, a);
+    if (a.target == 0) return;
+    hipLaunchKernelGGL((paged_share_join_kernel<DV, 32 * NW>), dim3((unsigned)a.n_work, 32 * NW / kJoinRows), dim3(kJoinThreads), 0, s, a);
 }
 
 template <int DQK, int DV, bool EXPANDED, int NW>
 void launch(const PagedArgs &a, hipStream_t s) {
-    if (!EXPANDED && a.lse) hipLaunchKernelGGL((paged_tile_kernel<DQK, DV, EXPANDED, NW, !EXPANDED>), dim3((unsigned)a.n_work), dim3(64 * NW), 0, s, a);
-    else hipLaunchKernelGGL((paged_tile_kernel<DQK, DV, EXPANDED, NW, false>), dim3((unsigned)a.n_work), dim3(64 * NW), 0, s, a);
-    if (a.target > 0) launch_join<DV, 32 * NW, KT, true>(a, s);
+    if (!EXPANDED && a.lse) launch_as<DQK, DV, EXPANDED, NW, !EXPANDED>(a, s);
+    else launch_as<DQK, DV, EXPANDED, NW, false>(a, s);
 }
 
 }  // namespace

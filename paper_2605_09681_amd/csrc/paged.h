@@ -14,6 +14,17 @@
 
 namespace fkv {
 
+// A cut item, as the launch that computes its parts leaves it for the one that joins them.
+struct JoinItem {
+    int32_t rows;                   // query rows; 0: none
+    int32_t start, len, first;      // of its sequence
+    int32_t y, row0;                // key head, first query row
+    int32_t parts, slot, step;      // few rows: slots slot + step * part; many rows: `parts` workgroups from slot's on
+    int32_t goes_on;                // many rows: this workgroup's share begins with a part of an item (its slot 2 r)
+    int32_t count;                  // few rows, in the first: cut items of the launch
+    int32_t pad[5];
+};
+
 // Every tensor that the paged kernels take; also the launch's plan.
 struct PagedArgs {
     const uint16_t *Q, *K, *V;      // rows; page pools [n_pages][kv][page_tokens][d] (or the expanded copies)
@@ -33,7 +44,9 @@ struct PagedArgs {
     int32_t min_tiles;              // key tiles that a part is worth
     int32_t n_work, n_slots;        // workgroups launched, slots in `part`
     float *part;
-    int32_t join_tokens;            // tokens per workgroup of the join
+    JoinItem *joins;                // few rows: [n_joins] cut items; many rows: one a workgroup
+    int32_t n_joins;
+    int32_t one_span;               // every key head has the same span
     int32_t wide;                   // the most keys outside the new tokens that a head sees; < 0: all
     int64_t head_rows;              // expanded copies: rows per head
     int32_t sink[FKV_MAX_HEADS], recent[FKV_MAX_HEADS];   // per key head; recent < 0: every key
@@ -172,9 +185,9 @@ struct Work {
     Seq s;
     int i;                          // the sequence
     int y, rt, part, parts;
-    int slot;                       // of the item's part 0 (by token: of key head 0's last row tile); the next part's is `step` further
+    int slot;                       // of the item's part 0; the next part's is `step` further
     int step;
-    int64_t base;                   // the sequence's first row in the expanded copies
+    int join;                       // number of the item among the cut ones
     bool ok;
 };
 
@@ -234,47 +247,185 @@ struct Split {
             if (sum_of(total[k]) * (float)a.kv <= (float)a.target) per_tile = per[k];
     }
 
-    // Work item `want` (token < 0), or the first cut sequence with batch rows in token .. end - 1.  Every lane of a
-    // wave calls it; the result is the same in all.
-    __device__ __forceinline__ Work locate(const PagedArgs &a, int want, int token, int end) const {
+    // Work item `want`.  Every lane of a wave calls it; the result is the same in all.
+    __device__ __forceinline__ Work locate(const PagedArgs &a, int want) const {
         Work w;
         w.ok = false;
-        int done = 0, slots = 0, rows = 0;
+        int done = 0, slots = 0, joins = 0;
         for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
             const Seq s = of(a, i0);
             int rts, tiles;
             counts(a, s, &rts, &tiles);
-            const int n = parts(tiles), c = a.kv * rts * n, cut = n > 1 ? c : 0;
-            const int blocks = rts > 0 ? (s.len + kSeqRows - 1) / kSeqRows : 0;
-            const int ic = scan_sum(c), is = scan_sum(cut), ib = scan_sum(blocks);
-            const uint64_t found = token < 0 ? __ballot(done + ic > want) : __ballot(cut > 0 && s.start < end && s.start + s.n > token);
+            const int n = parts(tiles), c = a.kv * rts * n, cut = n > 1 ? c : 0, items = n > 1 ? a.kv * rts : 0;
+            const int ic = scan_sum(c), is = scan_sum(cut), ij = scan_sum(items);
+            const uint64_t found = __ballot(done + ic > want);
             if (found) {
                 const int l = __builtin_ctzll(found);
                 auto at = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
                 w.i = i0 + l;
                 w.s = Seq{at(s.len), at(s.start), at(s.n), at(s.first)};
-                const int rt = at(rts), before = done + at(ic) - at(c);
+                const int rt = at(rts), local = want - (done + at(ic) - at(c));
                 w.parts = at(n);
                 w.step = a.kv * rt;
-                w.base = (int64_t)(rows + at(ib) - at(blocks)) * kSeqRows;
-                w.slot = slots + at(is) - at(cut);
-                w.part = w.y = w.rt = 0;
-                if (token < 0) {
-                    const int local = want - before;
-                    w.part = w.parts > 1 ? quotient(local, w.step) : 0;
-                    const int u = local - w.part * w.step;
-                    w.y = quotient(u, rt);
-                    w.rt = rt - 1 - (u - w.y * rt);          // the longest rows of a causal chunk first
-                    w.slot += u;
-                }
+                w.part = w.parts > 1 ? quotient(local, w.step) : 0;
+                const int u = local - w.part * w.step;
+                w.y = quotient(u, rt);
+                w.rt = rt - 1 - (u - w.y * rt);              // the longest rows of a causal chunk first
+                w.slot = slots + at(is) - at(cut) + u;
+                w.join = joins + at(ij) - at(items) + u;
                 w.ok = true;
                 return w;
             }
             done += __builtin_amdgcn_readlane(ic, 63);
             slots += __builtin_amdgcn_readlane(is, 63);
-            rows += __builtin_amdgcn_readlane(ib, 63);
+            joins += __builtin_amdgcn_readlane(ij, 63);
         }
         return w;
+    }
+    // Cut items of the launch.
+    __device__ __forceinline__ int cut_items(const PagedArgs &a) const {
+        int sum = 0;
+        for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
+            int rts, tiles;
+            counts(a, of(a, i0), &rts, &tiles);
+            sum += __builtin_amdgcn_readlane(scan_sum(parts(tiles) > 1 ? a.kv * rts : 0), 63);
+        }
+        return sum;
+    }
+};
+
+// Equal shares for launches of many rows: all items (sequence, key head, row tile, in this order) lie on a line,
+// each as long as its key tiles, and workgroup r takes what lies in [r, r + 1) shares, so that a device full of workgroups
+// ends at once whatever the lengths.  The tiles of a head's row tiles are taken to grow evenly from the first
+// to the last row tile's, which makes every place on the line a closed form (in 64 bits; that they are not quite so
+// costs balance alone), and an item costs kFixed tiles beside its own (the first loads, the first tile's references, the
+// output: 10 us, a tile 2).  An item whose stretch a share ends in is cut there: workgroup r's first part of a cut item
+// lies in slot 2 r if the item began before it, in slot 2 r + 1 otherwise.
+template <int ROWS, int KT>
+struct Shares {
+    static constexpr int kFixed = 5;
+    double total, each;             // of the line
+    int groups;                     // workgroups that have a share
+    Seq lane_seq;                   // this lane's sequence of the first 64
+
+    // A sequence on the line, and a key head of it; uniform.
+    struct Place {
+        Seq s;
+        int i, rts, y;
+        double begin, end;          // of the sequence
+        double y_begin, y_long;     // of the key head: begin and length
+        double first, grow;         // its first row tile's length, growth from one to the next
+        bool ok;
+    };
+
+    static __device__ __forceinline__ int row_tiles(const PagedArgs &a, const Seq &s) {
+        return s.n > 0 && s.n >= a.lo && s.n <= a.hi ? (int)(((uint32_t)s.n * (uint32_t)a.group + ROWS - 1) / ROWS) : 0;
+    }
+    static __device__ __forceinline__ void lengths(const PagedArgs &a, const Seq &s, int rts, int y, double *first, double *grow, double *all) {
+        const int last = (rts - 1) * ROWS, rows = s.n * a.group;
+        const int f = max(tiles_of<KT>(a, s, a.sink[y], a.recent[y], 0, token_of(a, min(ROWS, rows) - 1)).n, 1) + kFixed;
+        const int l = max(tiles_of<KT>(a, s, a.sink[y], a.recent[y], token_of(a, last), token_of(a, rows - 1)).n, 1) + kFixed;
+        *first = f;
+        *grow = rts > 1 ? (double)(l - f) / (double)(rts - 1) : 0.;
+        *all = 0.5 * (double)rts * (double)(f + l);
+    }
+    static __device__ __forceinline__ double length(const PagedArgs &a, const Seq &s, int rts) {
+        if (rts == 0) return 0.;
+        double f, g, all, sum = 0.;
+        if (a.one_span) {
+            lengths(a, s, rts, 0, &f, &g, &all);
+            return all * (double)a.kv;
+        }
+        for (int y = 0; y < a.kv; ++y) {
+            lengths(a, s, rts, y, &f, &g, &all);
+            sum += all;
+        }
+        return sum;
+    }
+    template <int CTRL, int MASK>
+    static __device__ __forceinline__ double moved(double v) {
+        const uint64_t u = __builtin_bit_cast(uint64_t, v);
+        const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, MASK, 0xf, false);
+        const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, MASK, 0xf, false);
+        return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+    }
+    static __device__ __forceinline__ double scan(double x) {     // as scan_sum
+        x += moved<0x111, 0xf>(x);
+        x += moved<0x112, 0xf>(x);
+        x += moved<0x114, 0xf>(x);
+        x += moved<0x118, 0xf>(x);
+        x += moved<0x142, 0xa>(x);
+        x += moved<0x143, 0xc>(x);
+        return x;
+    }
+    static __device__ __forceinline__ double lane_of(double v, int l) {
+        const uint64_t u = __builtin_bit_cast(uint64_t, v);
+        const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)u, l), hi = __builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), l);
+        return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+    }
+    __device__ __forceinline__ Seq of(const PagedArgs &a, int i0) const { return i0 == 0 ? lane_seq : sequence(a, i0 + (threadIdx.x & 63)); }
+
+    __device__ __forceinline__ explicit Shares(const PagedArgs &a) {
+        lane_seq = sequence(a, threadIdx.x & 63);
+        total = 0.;
+        for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
+            const Seq s = of(a, i0);
+            total += lane_of(scan(length(a, s, row_tiles(a, s))), 63);
+        }
+        groups = max((int)fmin((double)a.target, total / (double)a.min_tiles), 1);
+        each = total / (double)groups;
+    }
+    __device__ __forceinline__ double start(int r) const { return r >= groups ? total : each * (double)r; }
+
+    static __device__ __forceinline__ void set_head(const PagedArgs &a, Place *p, int y, double begin) {
+        p->y = y;
+        p->y_begin = begin;
+        lengths(a, p->s, p->rts, y, &p->first, &p->grow, &p->y_long);
+    }
+    static __device__ __forceinline__ void next_head(const PagedArgs &a, Place *p) { set_head(a, p, p->y + 1, p->y_begin + p->y_long); }
+    // Where row tile k of the place's head begins (k = rts: where the head ends).
+    static __device__ __forceinline__ double at(const PagedArgs &a, const Place &p, int k) {
+        if (k == p.rts) return p.y + 1 == a.kv ? p.end : p.y_begin + p.y_long;
+        return p.y_begin + (double)k * (p.first + 0.5 * p.grow * (double)(k - 1));
+    }
+    // The key tile at which x cuts an item of n tiles that lies in [from, to).
+    static __device__ __forceinline__ int cut(double x, double from, double to, int n) {
+        return x <= from ? 0 : x >= to ? n : min(max((int)((x - from) / (to - from) * (double)(n + kFixed) + 0.5) - kFixed, 0), n);
+    }
+    // The sequence at x of the line; key head 0.
+    __device__ __forceinline__ Place find(const PagedArgs &a, double x) const {
+        Place p;
+        p.ok = false;
+        double done = 0.;
+        for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
+            const Seq s = of(a, i0);
+            const int rts = row_tiles(a, s);
+            const double sum = scan(length(a, s, rts));
+            const uint64_t found = __ballot(rts > 0 && done + sum > x);
+            if (found) {
+                const int l = __builtin_ctzll(found);
+                auto at = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+                p.i = i0 + l;
+                p.s = Seq{at(s.len), at(s.start), at(s.n), at(s.first)};
+                p.rts = at(rts);
+                p.begin = l > 0 ? done + lane_of(sum, l - 1) : done;
+                p.end = done + lane_of(sum, l);
+                set_head(a, &p, 0, p.begin);
+                p.ok = true;
+                return p;
+            }
+            done += lane_of(sum, 63);
+        }
+        return p;
+    }
+    // Row tile of the place's head in which x lies.
+    static __device__ __forceinline__ int row_tile_at(const PagedArgs &a, const Place &p, double x) {
+        const double u = x - p.y_begin, b = p.first - 0.5 * p.grow;        // u = b k + grow / 2 k^2
+        double k = p.grow == 0. ? u / p.first : (sqrt(fmax(b * b + 2. * p.grow * u, 0.)) - b) / p.grow;
+        int i = (int)fmin(fmax(k, 0.), (double)(p.rts - 1));
+        while (i > 0 && at(a, p, i) > x) --i;
+        while (i + 1 < p.rts && at(a, p, i + 1) <= x) ++i;
+        return i;
     }
 };
 
@@ -295,6 +446,18 @@ __device__ __forceinline__ int owner_of(const PagedArgs &a, int token, Seq *held
         }
     }
     return owner;
+}
+
+// First row of sequence i in the expanded copies.
+__device__ __forceinline__ int64_t first_row(const PagedArgs &a, int i) {
+    const int lane = threadIdx.x & 63;
+    int done = 0;
+    for (int i0 = 0; i0 < i; i0 += 64) {
+        const Seq s = sequence(a, i0 + lane);
+        const bool mine = i0 + lane < i && s.n > 0 && s.n >= a.lo && s.n <= a.hi;
+        done += __builtin_amdgcn_readlane(scan_sum(mine ? (s.len + kSeqRows - 1) / kSeqRows : 0), 63);
+    }
+    return (int64_t)done * kSeqRows;
 }
 
 // Block `want` of kSeqRows rows of the expanded copies: the sequence, its number in *seq, and the
