@@ -752,7 +752,7 @@ fkv_status fkv_paged_attention(const fkv_batch *batch, int32_t n_heads, int32_t 
  * and values) is rounded to bf16.  The workspace (fkv_latent_attention_workspace_size bytes
  * for the same batch sizes and form, no initialisation, shared in turn) is
  * needed.  FKV_ERR_SHAPE also for a sum_len above 2^30 and an expanded form of more
- * than 65535 blocks of 128 tokens (one more a sequence than sum_len needs). */
+ * than 65535 blocks of 256 tokens (one more a sequence than sum_len needs). */
 #define FKV_LATENT_ROT 64
 #define FKV_LATENT_FEW 128
 typedef enum { FKV_LATENT_AUTO = 0, FKV_LATENT_ABSORBED = 1, FKV_LATENT_EXPANDED = 2 } fkv_latent_form;

@@ -125,9 +125,8 @@ struct Launch {
 
 // few: of the launch for few rows (see few_groups), 0: of the other.
 Launch plan(const fkv_batch *b, int kv, int group, int32_t lo, int32_t hi, int rows, int cus, int few, int width) {
-    // the workgroups that the device holds at once; a part is worth 128 keys, 256 latent ones (their parts' sums are
-    // wide), or 512 to the larger tiles
-    const int target = cus * (few ? fkv::few_groups(few, rows) : rows == 256 ? 1 : 2), min_tiles = few < 0 ? 4 : 8;
+    // the workgroups that the device holds at once; a part is worth 128 keys, or 512 to the larger tiles
+    const int target = cus * (few ? fkv::few_groups(few, rows) : rows == 256 ? 1 : 2), min_tiles = few ? 4 : 8;
     Launch l;
     l.lo = lo;
     l.hi = hi;

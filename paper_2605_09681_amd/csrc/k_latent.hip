@@ -4,6 +4,8 @@
 // are rounded to bf16 for the matrix units, as the queries and outputs themselves are.
 // Expanded form: k_h = W_k,h c and v_h = W_v,h c of every cached token, rounded to bf16
 // as a cache of its own keys and values would hold them.
+#include <algorithm>
+
 #include "paged.h"
 
 namespace fkv {
@@ -120,13 +122,16 @@ __global__ __launch_bounds__(NT) void latent_unabsorb_kernel(LatentArgs a, int D
     }
 }
 
-// Keys and values of 128 cached tokens of a sequence: 128 of the heads' 2 D channels a
-// workgroup, 64 x 64 a wave, latent channels 64 at a time through two LDS buffers.  The last column
-// block copies the tokens' rotated keys to every head.  grid: x = column block, y = token block.
+// Keys and values of 256 cached tokens of a sequence, blocks of 256 of the heads' 2 D channels in turn: 8
+// waves of 64 channels and 128 tokens, latent channels 64 at a time through two LDS buffers; the next block's
+// first operands are on their way while a block's results are stored.  The first workgroup of a token block copies its
+// rotated keys to every head.  A block of 128 x 128 reads twice as much for a product, from L2, and was bound by that.
+// grid: x = every gridDim.x'th channel block, y = token block.
 template <int D, int R>
-__global__ __launch_bounds__(NT, 2) void latent_expand_kernel(LatentArgs a) {
-    constexpr int STEP = 64, N = 128 * STEP / 8 / NT;      // chunks per thread and operand
-    __shared__ __attribute__((aligned(16))) uint16_t lat[2][128 * STEP], wts[2][128 * STEP];
+__global__ __launch_bounds__(512, 2) void latent_expand_kernel(LatentArgs a) {
+    constexpr int NT = 512, STEP = 64, N = 256 * STEP / 8 / NT;      // chunks per thread and operand
+    constexpr int HEADS = 128 / D;                         // heads per channel block
+    __shared__ __attribute__((aligned(16))) uint16_t lat[2][256 * STEP], wts[2][256 * STEP];
     const PagedArgs &p = a.p;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, hh = lane >> 5, c = lane & 31;
     Seq s;
@@ -141,90 +146,107 @@ __global__ __launch_bounds__(NT, 2) void latent_expand_kernel(LatentArgs a) {
     const int32_t *pages = p.table + (int64_t)i * p.max_pages;
     const int width = R + kLatentRot;
     constexpr int W = D + kLatentRot;
-    const int cols = p.n_heads * 2 * D / 128;
-    // this lane's two of the block's rows
-    const int row_a = pool_row(p, pages, 0, min(j0 + lane, j0 + n - 1)), row_b = pool_row(p, pages, 0, min(j0 + 64 + lane, j0 + n - 1));
-    if ((int)blockIdx.x == cols) {
-        for (int k0 = 0; k0 < 128; k0 += NT / 8) {
-            const int k = k0 + tid / 8, r = __shfl(k & 64 ? row_b : row_a, k & 63);
-            const u32x4 v = *(const u32x4 *)(p.K + (int64_t)r * width + R + tid % 8 * 8);
+    const int cols = (p.n_heads + HEADS - 1) / HEADS;
+    // Where this thread's N chunks of a token row come from: tokens tid / 8 + 64 u.
+    const uint16_t *from_l[N];
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+        from_l[u] = p.K + (int64_t)pool_row(p, pages, 0, min(j0 + tid / 8 + 64 * u, j0 + n - 1)) * width + tid % 8 * 8;
+    if (blockIdx.x == 0) {
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int k = tid / 8 + 64 * u;
+            const u32x4 v = *(const u32x4 *)(from_l[u] + R);
             if (k >= n) continue;
             for (int h = 0; h < p.n_heads; ++h) *(u32x4 *)(a.K_exp + (h * p.head_rows + base + k) * W + D + tid % 8 * 8) = v;
         }
-        return;
     }
-    // Channel rows of the block: K's or V's of one head, or (D = 64) K's and V's.
-    const int h = blockIdx.x * 128 / (2 * D), second = blockIdx.x * 128 % (2 * D);   // second: first channel among the head's 2 D
-    const uint16_t *w0 = second ? a.W_v + (int64_t)h * D * R : a.W_k + (int64_t)h * D * R;
-    const uint16_t *w1 = D == 64 ? a.W_v + (int64_t)h * D * R : w0 + (int64_t)64 * R;
-    const uint16_t *from_l[N], *from_w[N];
-#pragma unroll
-    for (int u = 0; u < N; ++u) {
-        const int id = tid + u * NT, k = id / 8;
-        from_l[u] = p.K + (int64_t)__shfl(k & 64 ? row_b : row_a, k & 63) * width + id % 8 * 8;
-        from_w[u] = (k < 64 ? w0 : w1) + (int64_t)(k & 63) * R + id % 8 * 8;
-    }
+    // Channel rows of a block, 64 at a time: of head h its keys', then its values', (D = 64) then the next head's.
+    auto channels = [&](int x, int u) {                    // u: which 64
+        const int h = min(x * HEADS + (D == 64 ? u >> 1 : 0), p.n_heads - 1);
+        const bool value = D == 64 ? u & 1 : u >> 1;
+        return (value ? a.W_v : a.W_k) + ((int64_t)h * D + (D == 64 ? 0 : 64 * (u & 1))) * R;
+    };
     u32x4 lr[N], wr[N];
-    auto load = [&](int k) {
+    auto load = [&](int x, int k) {
 #pragma unroll
         for (int u = 0; u < N; ++u) {
             lr[u] = *(const u32x4 *)(from_l[u] + k * STEP);
-            wr[u] = *(const u32x4 *)(from_w[u] + k * STEP);
+            wr[u] = *(const u32x4 *)(channels(x, u) + (uint32_t)((tid / 8) * R + tid % 8 * 8) + k * STEP);
         }
     };
     auto store = [&](int buf) {
 #pragma unroll
         for (int u = 0; u < N; ++u) {
-            const int id = tid + u * NT, k = id / 8, at = k * STEP + place<8, true>(k, id % 8) * 8;
+            const int k = tid / 8 + 64 * u, at = k * STEP + place<8, true>(k, tid % 8) * 8;
             *(u32x4 *)(lat[buf] + at) = lr[u];
             *(u32x4 *)(wts[buf] + at) = wr[u];
         }
     };
-    f32x16_t acc[2][2];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int v = 0; v < 2; ++v)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[u][v][r] = 0.f;
-    const int wc = w & 1, wk = w >> 1;                     // this wave's 64 channels and 64 tokens
-    load(0);
-    store(0);
-    load(1);
+    const int wc = w & 3, wk = w >> 2;                     // this wave's 64 channels and 128 tokens
+    load(blockIdx.x, 0);
 #pragma unroll 1
-    for (int k = 0; k < R / STEP; ++k) {
-        __syncthreads();
-        const int buf = k & 1;
-        if (k + 1 < R / STEP) store(buf ^ 1);
-        if (k + 2 < R / STEP) load(k + 2);
+    for (int x = blockIdx.x; x < cols; x += gridDim.x) {
+        f32x16_t acc[2][4];
 #pragma unroll
-        for (int u = 0; u < STEP / 16; ++u) {
-            bf16x8_t fa[2], fb[2];
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int v = 0; v < 2; ++v) {
-                fa[v] = frag(*(const u32x4 *)(wts[buf] + (64 * wc + 32 * v + c) * STEP + place<8, true>(c, 2 * u + hh) * 8));
-                fb[v] = frag(*(const u32x4 *)(lat[buf] + (64 * wk + 32 * v + c) * STEP + place<8, true>(c, 2 * u + hh) * 8));
+            for (int v = 0; v < 4; ++v)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[u][v][r] = 0.f;
+        store(0);
+        load(x, 1);
+#pragma unroll 1
+        for (int k = 0; k < R / STEP; ++k) {
+            __syncthreads();
+            const int buf = k & 1;
+            if (k + 1 < R / STEP) store(buf ^ 1);
+            if (k + 2 < R / STEP) load(x, k + 2);
+#pragma unroll
+            for (int u = 0; u < STEP / 16; ++u) {
+                bf16x8_t fa[2], fb[4];
+#pragma unroll
+                for (int v = 0; v < 2; ++v)
+                    fa[v] = frag(*(const u32x4 *)(wts[buf] + (64 * wc + 32 * v + c) * STEP + place<8, true>(c, 2 * u + hh) * 8));
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+                    fb[v] = frag(*(const u32x4 *)(lat[buf] + (128 * wk + 32 * v + c) * STEP + place<8, true>(c, 2 * u + hh) * 8));
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) acc[y][v] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[y], fb[v], acc[y][v], 0, 0, 0);
             }
+        }
+        static_assert(R / STEP % 2 == 0, "the last step reads buffer 1, the next block's first goes to buffer 0");
+        if (x + (int)gridDim.x < cols) load(x + gridDim.x, 0);
+        const int h = x * HEADS + (D == 64 ? wc >> 1 : 0);
+        const bool value = D == 64 ? wc & 1 : wc >> 1;
+        uint16_t *out = value ? a.V_exp : a.K_exp;
+        const int stride = value ? D : W, c0 = D == 64 ? 0 : 64 * (wc & 1);
+        // Through LDS (buffer 0, which every wave has read; 64 tokens at a time, 8 KB a wave), so that 8 lanes store a
+        // token's 64 channels together.
+        uint16_t *mine = (w < 4 ? lat[0] : wts[0]) + (w & 3) * 4096;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // (a wave's LDS operations finish in order)
 #pragma unroll
             for (int v = 0; v < 2; ++v)
 #pragma unroll
-                for (int x = 0; x < 2; ++x) acc[v][x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[v], fb[x], acc[v][x], 0, 0, 0);
+                for (int y = 0; y < 2; ++y)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        *(uint2 *)(mine + (32 * v + c) * 64 + ((4 * y + u) ^ (c & 7)) * 8 + 4 * hh) =
+                            pack4(acc[y][2 * half + v][4 * u], acc[y][2 * half + v][4 * u + 1], acc[y][2 * half + v][4 * u + 2],
+                                  acc[y][2 * half + v][4 * u + 3]);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int row = 8 * u + (lane >> 3), k = 128 * wk + 64 * half + row;
+                const u32x4 v = *(const u32x4 *)(mine + row * 64 + ((lane & 7) ^ (row & 7)) * 8);
+                if (k < n && h < p.n_heads) *(u32x4 *)(out + (h * p.head_rows + base + k) * stride + c0 + (lane & 7) * 8) = v;
+            }
         }
-    }
-    const bool value = D == 64 ? wc == 1 : second != 0;
-    uint16_t *out = value ? a.V_exp : a.K_exp;
-    const int stride = value ? D : W, c0 = D == 64 ? 0 : 64 * wc;
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        const int k = 64 * wk + 32 * x + c;
-        if (k >= n) continue;
-        uint16_t *to = out + (h * p.head_rows + base + k) * stride + c0 + 4 * hh;
-#pragma unroll
-        for (int v = 0; v < 2; ++v)
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                *(uint2 *)(to + 32 * v + 8 * u) =
-                    pack4(acc[v][x][4 * u], acc[v][x][4 * u + 1], acc[v][x][4 * u + 2], acc[v][x][4 * u + 3]);
+        __syncthreads();                                   // (the next block's first operands go there)
     }
 }
 
@@ -259,13 +281,15 @@ hipError_t launch_latent_unabsorb(const LatentArgs &a, int head_dim, hipStream_t
 }
 
 hipError_t launch_latent_expand(const LatentArgs &a, int head_dim, hipStream_t s) {
-    const dim3 grid((unsigned)(a.p.n_heads * 2 * head_dim / 128 + 1), (unsigned)(a.p.head_rows / kSeqRows));
+    // a round of workgroups: each pays for its first loads and its place in the batch once
+    const int cols = (a.p.n_heads * head_dim + 127) / 128, blocks = (int)(a.p.head_rows / kSeqRows);
+    const dim3 grid((unsigned)std::min(std::max(256 / blocks, 1), cols), (unsigned)blocks), threads(512);
     if (head_dim == 64) {
-        if (a.R == 256) hipLaunchKernelGGL((latent_expand_kernel<64, 256>), grid, dim3(NT), 0, s, a);
-        else hipLaunchKernelGGL((latent_expand_kernel<64, 512>), grid, dim3(NT), 0, s, a);
+        if (a.R == 256) hipLaunchKernelGGL((latent_expand_kernel<64, 256>), grid, threads, 0, s, a);
+        else hipLaunchKernelGGL((latent_expand_kernel<64, 512>), grid, threads, 0, s, a);
     } else {
-        if (a.R == 256) hipLaunchKernelGGL((latent_expand_kernel<128, 256>), grid, dim3(NT), 0, s, a);
-        else hipLaunchKernelGGL((latent_expand_kernel<128, 512>), grid, dim3(NT), 0, s, a);
+        if (a.R == 256) hipLaunchKernelGGL((latent_expand_kernel<128, 256>), grid, threads, 0, s, a);
+        else hipLaunchKernelGGL((latent_expand_kernel<128, 512>), grid, threads, 0, s, a);
     }
     return hipGetLastError();
 }

@@ -511,11 +511,24 @@ __global__ __launch_bounds__(kJoinThreads) void paged_share_join_kernel(PagedArg
     const int d = threadIdx.x % (D / 4), r0 = blockIdx.y * kJoinRows;
     for (int r = r0 + threadIdx.x / (D / 4); r < min(r0 + kJoinRows, j.rows); r += kLanes) {
         Joined x;
-        for (int k = 0; k < j.parts; ++k) {
-            const int g = blockIdx.x + k;
-            if (k > 0 && !a.joins[g].goes_on) continue;
-            const float *p = a.part + (2 * g + (k == 0)) * kSlot;
-            x.add(p[ROWS * D + r], p[ROWS * D + ROWS + r], *(const join_f32x4 *)(p + r * D + 4 * d), a.scale_log2);
+        constexpr int kAtOnce = 4;
+        for (int k0 = 0; k0 < j.parts; k0 += kAtOnce) {
+            float m[kAtOnce], l[kAtOnce];
+            join_f32x4 o[kAtOnce];
+            int on[kAtOnce];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {           // (a slot that nobody wrote is read and left out)
+                const int g = blockIdx.x + min(k0 + k, j.parts - 1);
+                const float *p = a.part + (2 * g + (k0 + k == 0)) * kSlot;
+                on[k] = a.joins[g].goes_on;
+                m[k] = p[ROWS * D + r];
+                l[k] = p[ROWS * D + ROWS + r];
+                o[k] = *(const join_f32x4 *)(p + r * D + 4 * d);
+            }
+            __builtin_amdgcn_sched_barrier(0);            // (all loads before the first use)
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k)
+                if (k0 + k == 0 || (k0 + k < j.parts && on[k])) x.add(m[k], l[k], o[k], a.scale_log2);
         }
         x.put(a, j, r, 4 * d);
     }

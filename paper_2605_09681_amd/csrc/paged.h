@@ -95,7 +95,7 @@ hipError_t launch_latent_expand(const LatentArgs &a, int head_dim, hipStream_t s
 
 namespace paged {
 
-constexpr int kSeqRows = 128;       // rows of the expanded copies are dealt to sequences in these
+constexpr int kSeqRows = 256;       // rows of the expanded copies are dealt to sequences in these
 
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
 
