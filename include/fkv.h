@@ -748,8 +748,8 @@ fkv_status fkv_paged_attention(const fkv_batch *batch, int32_t n_heads, int32_t 
  *                        made first (in the workspace), then attended;
  *   FKV_LATENT_AUTO      each sequence by its new tokens: absorbed up to
  *                        FKV_LATENT_FEW - 1 of them, expanded from there on.
- * What lies between the products (absorbed queries and outputs, expanded keys
- * and values) is rounded to bf16.  The workspace (fkv_latent_attention_workspace_size bytes
+ * Absorbed queries, expanded keys and values, and the expanded form's probabilities are
+ * rounded to bf16; the absorbed form's probabilities and latent outputs are not.  The workspace (fkv_latent_attention_workspace_size bytes
  * for the same batch sizes and form, no initialisation, shared in turn) is
  * needed.  FKV_ERR_SHAPE also for a sum_len above 2^30 and an expanded form of more
  * than 65535 blocks of 256 tokens (one more a sequence than sum_len needs). */

@@ -212,7 +212,7 @@ LatentPlan latent_plan(const fkv_batch *b, int n_heads, int d, int R, int form, 
         p.f = plan(b, 1, n_heads, 1, hi, fkv::paged_row_tile((int)std::min<int64_t>((int64_t)std::min(most, hi) * n_heads, 64)), cus, R, R);
         p.owned_at = take((size_t)b->n_tokens * 4);
         p.q_at = take(rows * (R + FKV_LATENT_ROT) * 2);
-        p.o_at = take(rows * R * 2);
+        p.o_at = take(rows * R * 4);
     }
     if (p.expanded) {
         p.m = plan(b, n_heads, 1, p.absorbed ? FKV_LATENT_FEW : 1, all, 256, cus, 0, d);
@@ -406,13 +406,13 @@ fkv_status fkv_latent_attention(const fkv_batch *batch, int32_t n_heads, int32_t
     if (p.absorbed) {
         a.owned = (int32_t *)(ws + p.owned_at);
         a.q_abs = (uint16_t *)(ws + p.q_at);
-        a.o_abs = (uint16_t *)(ws + p.o_at);
+        a.o_abs = (float *)(ws + p.o_at);
         set_launch(&a.p, p.f, ws + p.part_at, true);
         PagedArgs rows = a.p;
         rows.Q = a.q_abs;
         rows.q_head = latent_dim + FKV_LATENT_ROT;
         rows.q_tok = n_heads * rows.q_head;
-        rows.O = a.o_abs;
+        rows.O = (uint16_t *)a.o_abs;                      // (fp32 rows)
         rows.o_head = latent_dim;
         rows.o_tok = (int64_t)n_heads * latent_dim;
         e = fkv::launch_latent_absorb(a, head_dim, s);

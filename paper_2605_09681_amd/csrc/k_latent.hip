@@ -1,7 +1,7 @@
 // k_latent.hip -- the matrix products around attention over latent rows, gfx950 MFMA.
 //
-// Absorbed form: q'_h = W_k,h^T q_h before the attention, o_h = W_v,h o'_h after it; both
-// are rounded to bf16 for the matrix units, as the queries and outputs themselves are.
+// Absorbed form: q'_h = W_k,h^T q_h before the attention, rounded to bf16 for the matrix units as the
+// queries themselves are, and o_h = W_v,h o'_h after it, o' in fp32 as the sum of two bf16.
 // Expanded form: k_h = W_k,h c and v_h = W_v,h c of every cached token, rounded to bf16
 // as a cache of its own keys and values would hold them.
 #include <algorithm>
@@ -99,20 +99,32 @@ __global__ __launch_bounds__(NT) void latent_unabsorb_kernel(LatentArgs a, int D
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, c = lane & 15;
     const int h = blockIdx.y, t0 = blockIdx.x * (16 * TM), c0 = 64 * blockIdx.z + 16 * w;
     const uint16_t *W = a.W_v + ((int64_t)h * D + c0 + c) * R + 8 * g;
-    const uint16_t *row[TM];
+    const float *row[TM];
     f32x4_t acc[TM];
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
         row[i] = a.o_abs + ((int64_t)min(t0 + 16 * i + c, p.n_tokens - 1) * p.n_heads + h) * R + 8 * g;
         acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-    constexpr int kAhead = TM == 1 ? 16 : 4;
+    constexpr int kAhead = TM == 1 ? 8 : 2;
 #pragma unroll kAhead
     for (int k = 0; k < R / 32; ++k) {
         const bf16x8_t f = frag(*(const u32x4 *)(W + 32 * k));
 #pragma unroll
-        for (int i = 0; i < TM; ++i)
-            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, frag(*(const u32x4 *)(row[i] + 32 * k)), acc[i], 0, 0, 0);
+        for (int i = 0; i < TM; ++i) {
+            bf16x8_t hi, lo;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const f32x4_t v = *(const f32x4_t *)(row[i] + 32 * k + 4 * h);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    hi[4 * h + e] = (__bf16)v[e];
+                    lo[4 * h + e] = (__bf16)(v[e] - (float)hi[4 * h + e]);
+                }
+            }
+            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, hi, acc[i], 0, 0, 0);
+            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, lo, acc[i], 0, 0, 0);
+        }
     }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {

@@ -13,7 +13,7 @@
 //            and 16 rows are dealt to the waves, which turn theirs into probabilities
 //            and put those into LDS (bf16; the sum adds them before they are rounded);
 //   values   O^T += V^T P^T: each wave owns DV / NW output channels of all rows (V^T
-//            through the LDS transpose read).
+//            through the LDS transpose read).  SHARED leaves its outputs in fp32 to the product that follows.
 // The scores of tile t + 1 and the values of tile t run in the same stretch between two
 // barriers, one barrier a tile; tile t + 3 is on its way from HBM meanwhile.
 //
@@ -61,6 +61,10 @@ struct Cfg {
     static constexpr int NB = DV / 16 / NW;                          // 16-channel blocks of a wave's output
     static constexpr int NK = (KT * CK + NT - 1) / NT, NV = SHARED ? 0 : (KT * CV + NT - 1) / NT;   // chunks per thread
     static constexpr int TILE = KT * (DQK + (SHARED ? 0 : DV));      // elements
+    // Probabilities as one bf16, or (SHARED: the queries were rounded to bf16 once more, and the outputs go through
+    // another product) as the sum of two, of which nothing is lost.
+    static constexpr int PL = SHARED ? 2 : 1;
+    static constexpr int P_FLOATS = 2 * PL * MT * 64 * 4;            // [2][PL][MT][lane][key block] x 4 bf16
     static constexpr int SS = KT + 4;                                // careful: floats per row of scores (16 rows in distinct banks)
     static_assert(DV % (16 * NW) == 0 && KT * CV % NT == 0 && NW % 2 == 0, "whole blocks and chunks");
 };
@@ -69,11 +73,10 @@ template <int DQK, int DV, bool SHARED, int MT, int NW>
 __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) void paged_attn_kernel(PagedArgs a) {
     using C = Cfg<DQK, DV, SHARED, MT, NW>;
     __shared__ __attribute__((aligned(16))) uint16_t tiles[3][C::TILE];
-    // probabilities [2][MT][lane][key block] x 4 bf16; careful: scores [row][SS]
-    __shared__ __attribute__((aligned(16))) float mix[C::ROWS * C::SS];
+    // probabilities; careful: scores [row][SS]
+    __shared__ __attribute__((aligned(16))) float mix[C::P_FLOATS > C::ROWS * C::SS ? C::P_FLOATS : C::ROWS * C::SS];
     __shared__ float ends[3][MT][2][16];         // per row and key block: first tile's largest scores, sums, whether a key was seen
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
-    static_assert(2 * MT * 64 * 16 <= sizeof mix, "two tiles' probabilities fit");
 
     const Split<C::ROWS, KT> split(a);
     const Work item = split.locate(a, blockIdx.x);
@@ -208,7 +211,14 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
                 met[i] = true;
             }
             l[i] += (e[0] + e[1]) + (e[2] + e[3]);
-            if (mine(i)) ((uint2 *)mix)[(((t & 1) * MT + mt_of(i)) * 64 + lane) * 2 + kb] = pack4(e);
+            if (!mine(i)) continue;
+            const uint2 hi = pack4(e);
+            ((uint2 *)mix)[(((t & 1) * C::PL * MT + mt_of(i)) * 64 + lane) * 2 + kb] = hi;
+            if (C::PL == 2) {
+                const f32x4_t rest = {e[0] - __uint_as_float(hi.x << 16), e[1] - __uint_as_float(hi.x & 0xffff0000u),
+                                      e[2] - __uint_as_float(hi.y << 16), e[3] - __uint_as_float(hi.y & 0xffff0000u)};
+                ((uint2 *)mix)[((((t & 1) * C::PL + 1) * MT + mt_of(i)) * 64 + lane) * 2 + kb] = pack4(rest);
+            }
         }
     };
     // V^T of keys 4 g + 0..3 and + 16, 16 channels: the places of this lane's reads.
@@ -222,14 +232,14 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
         return __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7);
     };
     auto values = [&](int t) {
-        bf16x8_t p[MT];
+        bf16x8_t p[C::PL * MT];
 #pragma unroll
-        for (int i = 0; i < MT; ++i) p[i] = frag(((const u32x4 *)mix)[((t & 1) * MT + i) * 64 + lane]);
+        for (int i = 0; i < C::PL * MT; ++i) p[i] = frag(((const u32x4 *)mix)[((t & 1) * C::PL * MT + i) * 64 + lane]);
 #pragma unroll
         for (int b = 0; b < C::NB; ++b) {
             const bf16x8_t f = value(t, b);
 #pragma unroll
-            for (int i = 0; i < MT; ++i) o[i][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, p[i], o[i][b], 0, 0, 0);
+            for (int i = 0; i < C::PL * MT; ++i) o[i % MT][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, p[i], o[i % MT][b], 0, 0, 0);
         }
     };
 
@@ -360,18 +370,20 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
                     const float up = fmaxf(m_row[i], top), base = up == neg_inf() ? 0.f : up;
                     const float alpha = up == m_row[i] ? 1.f : __builtin_amdgcn_exp2f((m_row[i] - up) * a.scale_log2);
                     m_row[i] = up;
-                    bf16x8_t p;
+                    bf16x8_t p, rest;
 #pragma unroll
                     for (int r = 0; r < 8; ++r) {
                         const float v = __builtin_amdgcn_exp2f((e[r] - base) * a.scale_log2);
                         sum += v;
                         p[r] = (__bf16)v;
+                        rest[r] = (__bf16)(v - (float)p[r]);
                     }
                     l_row[i] = l_row[i] * alpha + sum;
 #pragma unroll
                     for (int b = 0; b < C::NB; ++b) {
-                        o[i][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(finite_only(__builtin_bit_cast(u32x4, value(t, b)))), p,
-                                                                          o[i][b] * alpha, 0, 0, 0);
+                        const bf16x8_t f = frag(finite_only(__builtin_bit_cast(u32x4, value(t, b))));
+                        o[i][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, p, o[i][b] * alpha, 0, 0, 0);
+                        if (C::PL == 2) o[i][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, rest, o[i][b], 0, 0, 0);
                     }
                     // infinities and NaNs for the rows that see them (any weight leaves them as they are)
 #pragma unroll 1
@@ -403,9 +415,12 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
             const int tok = token_of(a, r0 + r), head = y * a.group + r0 + r - tok * a.group;
             const bool none = sight(a, s, recent, tok).end <= 0;
             const float inv = none ? 0.f : 1.f / l_row[t];
-            uint16_t *to = a.O + (int64_t)(s.start + tok) * a.o_tok + (int64_t)head * a.o_head;
+            const int64_t to = (int64_t)(s.start + tok) * a.o_tok + (int64_t)head * a.o_head + 4 * g;
 #pragma unroll
-            for (int b = 0; b < C::NB; ++b) *(uint2 *)(to + 16 * (w * C::NB + b) + 4 * g) = pack4(o[t][b] * inv);
+            for (int b = 0; b < C::NB; ++b) {
+                if (SHARED) *(f32x4_t *)((float *)a.O + to + 16 * (w * C::NB + b)) = o[t][b] * inv;
+                else *(uint2 *)(a.O + to + 16 * (w * C::NB + b)) = pack4(o[t][b] * inv);
+            }
             if (a.lse && w == 0 && g == 0)
                 a.lse[(int64_t)head * a.n_tokens + s.start + tok] =
                     none ? neg_inf() : fmaf(m_row[t] * kLn2, a.scale_log2, logf(l_row[t]));
@@ -423,8 +438,8 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
 }
 
 // One workgroup joins a row of a cut item: D / 4 threads take 4 channels each, kLanes of them every
-// kLanes'th part, and their sums meet in LDS in a fixed order.  grid: x = cut item, y = row.
-template <int D, int ROWS>
+// kLanes'th part, and their sums meet in LDS in a fixed order.  WIDE: the output is fp32.  grid: x = cut item, y = row.
+template <int D, int ROWS, bool WIDE>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedArgs a) {
     constexpr int kLanes = kJoinThreads / (D / 4), kAtOnce = 4;
     __shared__ join_f32x4 sum[kLanes][D / 4];
@@ -460,7 +475,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedArgs a) {
     __syncthreads();
     if (lane > 0) return;
     for (int i = 1; i < kLanes; ++i) x.add(top[i], total[i], sum[i][d], a.scale_log2);
-    x.put(a, j, r, 4 * d);
+    x.put<WIDE>(a, j, r, 4 * d);
 }
 
 template <int DQK, int DV, bool SHARED, int NW>
@@ -468,7 +483,7 @@ void launch_rows(const PagedArgs &a, int rows, hipStream_t s) {
     auto go = [&](auto mt) {
         constexpr int MT = decltype(mt)::value;
         hipLaunchKernelGGL((paged_attn_kernel<DQK, DV, SHARED, MT, NW>), dim3((unsigned)a.n_work), dim3(64 * NW), 0, s, a);
-        if (a.target > 0) hipLaunchKernelGGL((paged_join_kernel<DV, 16 * MT>), dim3((unsigned)a.n_joins, 16 * MT), dim3(kJoinThreads), 0, s, a);
+        if (a.target > 0) hipLaunchKernelGGL((paged_join_kernel<DV, 16 * MT, SHARED>), dim3((unsigned)a.n_joins, 16 * MT), dim3(kJoinThreads), 0, s, a);
     };
     if (rows <= 16) go(std::integral_constant<int, 1>{});
     else if (rows <= 32) go(std::integral_constant<int, 2>{});

@@ -85,7 +85,7 @@ struct LatentArgs {
     const uint16_t *W_k, *W_v;      // [n_heads][d][R]
     int32_t R;
     uint16_t *q_abs;                // absorbed: [n_tokens][n_heads][R + 64]
-    uint16_t *o_abs;                // absorbed: [n_tokens][n_heads][R]
+    float *o_abs;                   // absorbed: [n_tokens][n_heads][R]
     int32_t *owned;                 // absorbed: [n_tokens], 1 where a sequence of the launch holds the token
     uint16_t *K_exp, *V_exp;        // expanded: [n_heads][head_rows][d + 64], [n_heads][head_rows][d]
 };

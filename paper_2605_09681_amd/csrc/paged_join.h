@@ -25,7 +25,8 @@ struct Joined {
         L = L * so + l * sn;
         acc = acc * so + o * sn;
     }
-    // Channels ch .. ch + 3 of the item's row r.
+    // Channels ch .. ch + 3 of the item's row r.  WIDE: of fp32.
+    template <bool WIDE = false>
     __device__ __forceinline__ void put(const PagedArgs &a, const JoinItem &j, int r, int ch) const {
         const int row = j.row0 + r, tok = token_of(a, row), head = j.y * a.group + row - tok * a.group, t = j.start + tok;
         const bool none = sight(a, Seq{j.len, j.start, 0, j.first}, a.recent[j.y], tok).end <= 0;
@@ -33,7 +34,9 @@ struct Joined {
         join_bf16x4 out;
 #pragma unroll
         for (int k = 0; k < 4; ++k) out[k] = (__bf16)(acc[k] * inv);
-        *(join_bf16x4 *)(a.O + (int64_t)t * a.o_tok + (int64_t)head * a.o_head + ch) = out;
+        const int64_t to = (int64_t)t * a.o_tok + (int64_t)head * a.o_head + ch;
+        if (WIDE) *(join_f32x4 *)((float *)a.O + to) = acc * inv;
+        else *(join_bf16x4 *)(a.O + to) = out;
         if (a.lse && ch == 0)
             a.lse[(int64_t)head * a.n_tokens + t] = none ? neg_inf() : fmaf(M * 0.69314718055994530942f, a.scale_log2, logf(L));
     }
