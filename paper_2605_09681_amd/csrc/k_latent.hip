@@ -106,10 +106,17 @@ __global__ __launch_bounds__(NT) void latent_unabsorb_kernel(LatentArgs a, int D
         row[i] = a.o_abs + ((int64_t)min(t0 + 16 * i + c, p.n_tokens - 1) * p.n_heads + h) * R + 8 * g;
         acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-    constexpr int kAhead = TM == 1 ? 8 : 2;
+    // (few tokens: every weight on its way before the first product)
+    constexpr int kSteps = R / 32, kHeld = TM == 1 ? kSteps : 1, kAhead = TM == 1 ? kSteps : 2;
+    u32x4 held[kHeld];
+    if (TM == 1) {
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k) held[k] = *(const u32x4 *)(W + 32 * k);
+        __builtin_amdgcn_sched_barrier(0);
+    }
 #pragma unroll kAhead
     for (int k = 0; k < R / 32; ++k) {
-        const bf16x8_t f = frag(*(const u32x4 *)(W + 32 * k));
+        const bf16x8_t f = frag(TM == 1 ? held[k % kHeld] : *(const u32x4 *)(W + 32 * k));
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             bf16x8_t hi, lo;

@@ -437,19 +437,19 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
     }
 }
 
-// One workgroup joins a row of a cut item: D / 4 threads take 4 channels each, kLanes of them every
-// kLanes'th part, and their sums meet in LDS in a fixed order.  WIDE: the output is fp32.  grid: x = cut item, y = row.
-template <int D, int ROWS, bool WIDE>
+// One workgroup joins CH channels of a row of a cut item: CH / 4 threads take 4 each, kLanes of them every
+// kLanes'th part, and their sums meet in LDS in a fixed order.  WIDE: the output is fp32.  grid: x = cut item, y = row, z = channels.
+template <int D, int ROWS, bool WIDE, int CH>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedArgs a) {
-    constexpr int kLanes = kJoinThreads / (D / 4), kAtOnce = 4;
-    __shared__ join_f32x4 sum[kLanes][D / 4];
+    constexpr int kLanes = kJoinThreads / (CH / 4), kAtOnce = 4;
+    __shared__ join_f32x4 sum[kLanes][CH / 4];
     __shared__ float top[kLanes], total[kLanes];
     if ((int)blockIdx.x >= a.joins[0].count) return;
     const JoinItem j = a.joins[blockIdx.x];
-    const int r = blockIdx.y, d = threadIdx.x % (D / 4), lane = threadIdx.x / (D / 4);
+    const int r = blockIdx.y, d = threadIdx.x % (CH / 4), lane = threadIdx.x / (CH / 4), ch = CH * blockIdx.z + 4 * d;
     if (r >= j.rows) return;
     const int64_t step = (int64_t)j.step * (ROWS * (D + 2));
-    const float *p = a.part + (int64_t)j.slot * (ROWS * (D + 2)), *po = p + r * D + 4 * d, *pm = p + ROWS * D + r, *pl = pm + ROWS;
+    const float *p = a.part + (int64_t)j.slot * (ROWS * (D + 2)), *po = p + r * D + ch, *pm = p + ROWS * D + r, *pl = pm + ROWS;
     Joined x;
     for (int k0 = lane; k0 < j.parts; k0 += kAtOnce * kLanes) {
         float m[kAtOnce], l[kAtOnce];
@@ -475,15 +475,15 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedArgs a) {
     __syncthreads();
     if (lane > 0) return;
     for (int i = 1; i < kLanes; ++i) x.add(top[i], total[i], sum[i][d], a.scale_log2);
-    x.put<WIDE>(a, j, r, 4 * d);
+    x.put<WIDE>(a, j, r, ch);
 }
 
 template <int DQK, int DV, bool SHARED, int NW>
 void launch_rows(const PagedArgs &a, int rows, hipStream_t s) {
     auto go = [&](auto mt) {
-        constexpr int MT = decltype(mt)::value;
+        constexpr int MT = decltype(mt)::value, kCh = DV == 512 ? 128 : DV == 256 ? 64 : DV;
         hipLaunchKernelGGL((paged_attn_kernel<DQK, DV, SHARED, MT, NW>), dim3((unsigned)a.n_work), dim3(64 * NW), 0, s, a);
-        if (a.target > 0) hipLaunchKernelGGL((paged_join_kernel<DV, 16 * MT, SHARED>), dim3((unsigned)a.n_joins, 16 * MT), dim3(kJoinThreads), 0, s, a);
+        if (a.target > 0) hipLaunchKernelGGL((paged_join_kernel<DV, 16 * MT, SHARED, kCh>), dim3((unsigned)a.n_joins, 16 * MT, DV / kCh), dim3(kJoinThreads), 0, s, a);
     };
     if (rows <= 16) go(std::integral_constant<int, 1>{});
     else if (rows <= 32) go(std::integral_constant<int, 2>{});
