@@ -34,7 +34,9 @@ from typing import Optional, Sequence, Union
 
 import torch
 
-from . import (Cache8, FKV_DYNAMIC, FKV_STATIC, fkv_append_frames, fkv_append_frames_q8,
+from . import (Cache8, FKV_DYNAMIC, FKV_LATENT_ROT, FKV_STATIC, PagedBatch, fkv_append_frames, fkv_append_paged,
+               fkv_latent_attention, fkv_latent_attention_workspace_size, fkv_paged_attention,
+               fkv_paged_attention_workspace_size, fkv_append_frames_q8,
                fkv_append_frames_rotated, fkv_attention_mass, fkv_chunk_attention_q8,
                fkv_chunk_attention_q8_workspace_size, fkv_rope, fkv_rotate_chunk, fkv_score_select_q8,
                fkv_attention_workspace_size, fkv_chunk_attention, fkv_chunk_attention_heads,
@@ -646,6 +648,97 @@ class RolloutStack:
                                       self.V_hist[layer])
         else:
             fkv_append_frames(self.shape(0), K_new, V_new, dst_slots, self.K_hist[layer], self.V_hist[layer])
+
+
+class PagedStreams:
+    """The caches of many streams in one pool of pages, for a stack of attention layers.
+
+    Streams of any lengths share ``n_pages`` pages of ``page_tokens`` tokens (the
+    same page numbers in every layer): :meth:`open` starts one, :meth:`step` gives
+    streams room for their next tokens and returns the :class:`PagedBatch` that
+    :meth:`append` and :meth:`attend` of every layer take, :meth:`close` gives a
+    stream's pages back.  A page is held by one stream at a time.  ``latent_dim`` > 0:
+    the layers cache latent rows (one of latent_dim + 64 channels a token, for all
+    heads), and :meth:`attend` takes the layer's up-projections.
+
+    Layers run one after another and share one workspace, which grows with the
+    batches (one that a captured graph may still use is kept).  Calls enqueue on
+    the current stream; :meth:`step` copies the batch's tables to the device."""
+
+    def __init__(self, n_layers: int, n_heads: int, head_dim: int, n_pages: int, page_tokens: int,
+                 n_kv_heads: Optional[int] = None, latent_dim: int = 0, device="cuda"):
+        if latent_dim and n_kv_heads not in (None, 1):
+            raise ValueError("a latent cache has one row for all heads")
+        self.n_layers, self.n_heads, self.d, self.latent_dim = n_layers, n_heads, head_dim, latent_dim
+        self.kv = 1 if latent_dim else (n_heads if n_kv_heads is None else n_kv_heads)
+        self.page_tokens, self.device = page_tokens, torch.device(device)
+        size = (n_pages, self.kv, page_tokens, latent_dim + FKV_LATENT_ROT if latent_dim else head_dim)
+        pool = lambda: [torch.zeros(size, dtype=torch.bfloat16, device=self.device) for _ in range(n_layers)]  # noqa: E731
+        self.K_pages, self.V_pages = pool(), None if latent_dim else pool()
+        self.scale = 1.0 / math.sqrt(head_dim + (FKV_LATENT_ROT if latent_dim else 0))
+        self._free = list(range(n_pages))[::-1]
+        self._pages, self._len, self._next = {}, {}, 0
+        self._ws, self._kept = None, []
+
+    def open(self) -> int:
+        """A new stream without tokens."""
+        self._next += 1
+        self._pages[self._next], self._len[self._next] = [], 0
+        return self._next
+
+    def close(self, stream: int):
+        """Ends a stream: its pages serve others from the next :meth:`step` on."""
+        self._free += self._pages.pop(stream)[::-1]
+        del self._len[stream]
+
+    def length(self, stream: int) -> int:
+        return self._len[stream]
+
+    def step(self, new: Sequence) -> PagedBatch:
+        """Room for the next tokens of streams, [(stream, tokens), ...], whose rows follow one another in this
+        order in the batch's tensors.  Raises RuntimeError, and changes nothing, if the pool has too few pages."""
+        if len({s for s, _ in new}) != len(new) or any(n < 1 for _, n in new) or not new:
+            raise ValueError("a step takes each stream once, with a token at least")
+        P = self.page_tokens
+        need = {s: -(-(self._len[s] + n) // P) - len(self._pages[s]) for s, n in new}
+        if sum(need.values()) > len(self._free):
+            raise RuntimeError(f"{sum(need.values())} pages needed, {len(self._free)} free")
+        starts = [0]
+        for s, n in new:
+            self._pages[s] += [self._free.pop() for _ in range(need[s])]
+            self._len[s] += n
+            starts.append(starts[-1] + n)
+        lens = [self._len[s] for s, _ in new]
+        width = max(len(self._pages[s]) for s, _ in new)
+        table = [self._pages[s] + [-1] * (width - len(self._pages[s])) for s, _ in new]
+        dev = lambda v: torch.tensor(v, dtype=torch.int32, device=self.device)  # noqa: E731
+        return PagedBatch(dev(table), dev(lens), dev(starts), P, starts[-1], max(n for _, n in new), sum(lens))
+
+    def append(self, layer: int, batch: PagedBatch, K_new, V_new=None):
+        """The batch's new keys and values (latent rows: K_new alone), [n_kv_heads][n_tokens][d] views, into the layer's pages."""
+        fkv_append_paged(batch, K_new, V_new, self.K_pages[layer], None if self.latent_dim else self.V_pages[layer])
+
+    def attend(self, layer: int, batch: PagedBatch, Q, O, causal: bool = True, spans=None, lse=None, W_k=None, W_v=None,
+               form: str = "auto"):
+        """Attention of the batch's new tokens, appended before, over their streams: Q, O [n_heads][n_tokens][d]
+        views (Q [..][d + 64] and the layer's W_k, W_v over latent rows; spans then one pair)."""
+        if self.latent_dim:
+            if lse is not None:
+                raise ValueError("no lse over a latent cache")
+            with torch.cuda.device(self.device):
+                n = fkv_latent_attention_workspace_size(batch, self.n_heads, self.d, self.latent_dim, form)
+            fkv_latent_attention(batch, Q, self.K_pages[layer], W_k, W_v, self.scale, O, causal, spans, form, self._workspace(n))
+        else:
+            n = fkv_paged_attention_workspace_size(batch, self.n_heads, self.kv, self.d)
+            fkv_paged_attention(batch, Q, self.K_pages[layer], self.V_pages[layer], self.scale, O, causal, spans, lse,
+                                self._workspace(n))
+
+    def _workspace(self, n: int):
+        if self._ws is None or self._ws.numel() < n:
+            if self._ws is not None:
+                self._kept.append(self._ws)
+            self._ws = torch.empty(max(n, 1), dtype=torch.uint8, device=self.device)
+        return self._ws
 
 
 class _Budget:
