@@ -661,8 +661,9 @@ fkv_status fkv_chunk_attention_q8(const fkv_shape *shape, const fkv_head *heads,
  *               are left as they are
  *   max_new     >= every n_i: of a sequence with more new tokens only the first
  *               max_new are served
- *   sum_len     >= the sum of seq_len (read by the expanded latent form alone,
- *               which has room for that many tokens and leaves out those beyond)
+ *   sum_len     >= the sum of seq_len; the expanded latent form has room for that
+ *               many tokens and leaves out those beyond.  Elsewhere it may be 0 (not
+ *               known); where it is small, chunks of few tokens are split more finely
  * Lengths, starts and pages are read on the device when the call runs, so a
  * captured graph serves other values later; values outside their range are held
  * to it (a key on a page outside the pool is read from another page, a new
@@ -747,14 +748,15 @@ fkv_status fkv_paged_attention(const fkv_batch *batch, int32_t n_heads, int32_t 
  *   FKV_LATENT_EXPANDED  every head's keys and values of all cached tokens are
  *                        made first (in the workspace), then attended;
  *   FKV_LATENT_AUTO      each sequence by its new tokens: absorbed up to
- *                        FKV_LATENT_FEW - 1 of them, expanded from there on.
+ *                        FKV_LATENT_FEW - 1 of them, expanded from there on (512
+ *                        channels: the times cross at 45 to 80 tokens, 256: at 100).
  * Absorbed queries, expanded keys and values, and the expanded form's probabilities are
  * rounded to bf16; the absorbed form's probabilities and latent outputs are not.  The workspace (fkv_latent_attention_workspace_size bytes
  * for the same batch sizes and form, no initialisation, shared in turn) is
  * needed.  FKV_ERR_SHAPE also for a sum_len above 2^30 and an expanded form of more
  * than 65535 blocks of 256 tokens (one more a sequence than sum_len needs). */
 #define FKV_LATENT_ROT 64
-#define FKV_LATENT_FEW 128
+#define FKV_LATENT_FEW 64
 typedef enum { FKV_LATENT_AUTO = 0, FKV_LATENT_ABSORBED = 1, FKV_LATENT_EXPANDED = 2 } fkv_latent_form;
 fkv_status fkv_latent_attention_workspace_size(const fkv_batch *batch, int32_t n_heads, int32_t head_dim,
                                                int32_t latent_dim, int32_t form, size_t *bytes);

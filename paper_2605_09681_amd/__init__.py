@@ -54,7 +54,7 @@ FKV_PAIR_ADJACENT, FKV_PAIR_HALVES = 0, 1
 FKV_MAX_HEADS, FKV_MAX_FRAMES, FKV_MAX_SEGMENTS = 64, 256, 4096
 FKV_MAX_POSITION = 1 << 24
 FKV_LATENT_AUTO, FKV_LATENT_ABSORBED, FKV_LATENT_EXPANDED = 0, 1, 2
-FKV_LATENT_ROT, FKV_LATENT_FEW, FKV_MAX_SEQS = 64, 128, 4096
+FKV_LATENT_ROT, FKV_LATENT_FEW, FKV_MAX_SEQS = 64, 64, 4096
 
 EXPORTED = ("fkv_num_segments", "fkv_kept_tokens_max", "fkv_compress_static",
             "fkv_score_workspace_size", "fkv_score_segments", "fkv_select_compact",
@@ -984,7 +984,7 @@ class PagedBatch:
     new tokens) lie on the GPU and may be written between calls.  ``n_tokens``
     rows have the batch's tensors; ``max_new`` is at least every sequence's new
     tokens, ``sum_len`` at least the sum of ``seq_len`` (the expanded latent form
-    needs it)."""
+    needs it; elsewhere 0 for unknown)."""
 
     def __init__(self, page_table, seq_len, q_start, page_tokens: int, n_tokens: int, max_new: int, sum_len: int = 0):
         self.device = _device_of(page_table, "page_table")

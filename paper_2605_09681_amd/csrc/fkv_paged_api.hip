@@ -161,7 +161,11 @@ void set_launch(PagedArgs *a, const Launch &l, void *part, bool split) {
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
-constexpr int kFewRows = 64;        // query rows of a sequence and key head up to which the launch for few rows takes it
+// Query rows of a sequence and key head up to which the launch for few rows takes it: a tile of its own, or, where the
+// batch's keys are known to be few, four.  The other launch reaches three times its rate, once there is work for the
+// device (us, few / many): 12 heads of 128, 3000 tokens, 128 new 26 / 50; 20000 tokens, 192 new 80 / 101, 384 new 137 /
+// 106; 16 heads over 4, 20000 tokens, 48 new 40 / 83; 16 sequences of 4000 tokens, 12 heads, 128 new 204 / 144.
+int few_rows(const fkv_batch *b, int kv) { return b->sum_len > 0 && b->sum_len <= ((int64_t)1 << 18) / kv ? 256 : 64; }
 
 // Query rows of a tile of the launch for many rows, by the most rows of a sequence and key head.
 int tile_rows(int64_t rows) { return rows > 512 ? 256 : 128; }
@@ -175,12 +179,12 @@ struct AttendPlan {
 AttendPlan attend_plan(const fkv_batch *b, int n_heads, int kv, int head_dim, int cus) {
     AttendPlan p;
     memset(&p, 0, sizeof p);
-    const int group = n_heads / kv, edge = kFewRows / group;   // new tokens of a sequence: few up to edge
+    const int group = n_heads / kv, edge = few_rows(b, kv) / group;   // new tokens of a sequence: few up to edge
     const int most = std::min(b->max_new, std::max(b->n_tokens, 1));
     p.many = most > edge;
     p.few = !p.many || b->n_seqs > 1;
     if (p.few)
-        p.f = plan(b, kv, group, 1, edge, fkv::paged_row_tile(std::min(most, edge) * group), cus, -head_dim, head_dim);
+        p.f = plan(b, kv, group, 1, edge, fkv::paged_row_tile((int)std::min((int64_t)std::min(most, edge) * group, (int64_t)64)), cus, -head_dim, head_dim);
     if (p.many)
         p.m = plan(b, kv, group, p.few ? edge + 1 : 1, std::numeric_limits<int32_t>::max(), tile_rows((int64_t)most * group), cus, 0, head_dim);
     p.bytes = std::max(p.f.part_bytes, p.m.part_bytes);

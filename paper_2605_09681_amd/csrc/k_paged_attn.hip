@@ -23,6 +23,15 @@
 // [2^-100, 2^100] or an output is not finite, and where an infinity or a NaN lies among
 // values that only some rows see, the part is computed again, tile by tile with a running
 // maximum (`careful`).
+//
+// Why so: few rows are bound by the bytes of their keys, so the keys of a sequence are split
+// over the device (Split), a tile is read once for all rows, and each CU has 16 to 48 KB of them
+// on their way.  480P, one token over 32761 keys of 12 heads (201 MB): 34 us and 4 for the
+// join; 16 sequences of up to 7800 tokens, 16 heads over 4 key heads (76 MB): 18.5 and 4 us, 4.1
+// TB/s; the same over latent rows of 576, 40 heads (54 MB): 25 and 8.5 us.  Of the last, 2 us are the
+// split, 6 the first two tiles and the queries, 6 five tiles, 3 the output (82 KB a workgroup).
+// Measured beside it: every wave forming all probabilities from scores in LDS (40 heads 67 us), parts of
+// 256 keys instead of 128 (latent rows: 16.2 against 12.9 us for one token).
 #include <type_traits>
 
 #include "paged_join.h"

@@ -1,13 +1,35 @@
 // k_paged_tile.hip -- attention of chunks and prompts of many sequences over paged caches
 // (or, EXPANDED, over the keys and values made from latent rows), gfx950 MFMA.
 //
-// A workgroup of 4 waves takes one part of an item (sequence, key head, tile of 128 query
-// rows; the query heads of a key head share a tile) and walks its keys 64 at a time
-// through two LDS buffers.  Per wave, 32 query rows and v_mfma_f32_32x32x16_bf16:
+// An item is a sequence, a key head and a tile of 32 NW query rows (the query heads of a key
+// head share a tile).  A workgroup of NW waves computes its share of the line of all items
+// (Shares), walking the keys of each 64 at a time.  Per wave, 32 query rows and
+// v_mfma_f32_32x32x16_bf16:
 //   S^T = K Q^T    (A = K rows from LDS, B = the wave's queries in registers),
-//   softmax        per query column, fp32, a running maximum that moves only where a
-//                  score passes it by kSlack,
+//   softmax        per query column, fp32, with a reference that is not the maximum but the
+//                  largest score of the part's first tile: any reference cancels in the
+//                  quotient, and probabilities above one are as exact as those below,
 //   O^T += V^T P^T (A = V^T through the LDS transpose read, P straight from S^T).
+// Where a row's sum leaves [2^-100, 2^100] or an output is not finite, and where an infinity
+// or a NaN lies among values that only some rows see, the part is computed again, tile by
+// tile with a running maximum.  The sum adds the probabilities as they are; where no lse is
+// asked for, the rounded ones that weight the values, two at a time.
+//
+// The matrix units bound it, so everything is arranged around their stream: the products of a
+// tile are one pinned sequence (scores of key block 1, values of block 0, scores of the next
+// tile's block 0, values of block 1) with the exponentials of a block spread over the 16 products behind its scores, a few
+// VALU instructions each, and operands read four products ahead.  LDS rows are padded so that
+// every read is one address and a constant (with chunks placed by exclusive-or instead, 24
+// VALU instructions a tile more).  At 480P (12 heads of 128, 4680 rows over 37440 keys, 1.08
+// TFLOP) 1.03 to 1.24 ms as the card is cool or hot, 0.87 to 1.05 PFLOP/s; products in 59% of
+// the cycles.  Steps: running maxima and 128 rows, two workgroups a CU 1510 us; the pinned
+// stream with 256 rows 1250; padded rows, rotating buffers, contiguous rows read from one
+// address 1210; equal shares 1130 (228 items leave 28 CUs idle otherwise; with 14 heads, 266
+// items, 1970 without and 1270 with).  An item costs 10 us beside its tiles (4 the first
+// loads, 1 the reference, 3 the output); prompts of 1700 to 3500 tokens, five items a
+// workgroup, reach 0.68 PFLOP/s for that.  Measured beside it, slower: 128 rows and two
+// workgroups a CU in the same stream (1270 us, prompts 490 against 440), tiles loaded through
+// four unrolled buffers (spills).
 #include <type_traits>
 #include <utility>
 

@@ -56,41 +56,42 @@ LONG = [(300, 300), (61, 61), (1000, 129), (128, 128), (129, 1), (450, 65)]
 
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("heads,kv", [(4, 4), (6, 2), (16, 1)])
-@pytest.mark.parametrize("seqs,page", [(ONES, 16), (SHORT, 48), (LONG, 64)])
-def test_causal(fkv, d, heads, kv, seqs, page):
+@pytest.mark.parametrize("seqs,page,sum_len", [(ONES, 16, None), (SHORT, 48, None), (LONG, 64, None), (LONG, 64, 0)])
+def test_causal(fkv, d, heads, kv, seqs, page, sum_len):
     x = Paged(seqs, page, kv, d, seed=d + heads, spare=3, before=2)
     Q = x.rows(heads, d)
-    O, lse = run_attend(fkv, x, Q)
+    O, lse = run_attend(fkv, x, Q, sum_len=sum_len)
     check(x, Q, O, lse, True, None)
 
 
+@pytest.mark.parametrize("sum_len", [None, 0])
 @pytest.mark.parametrize("workspace", [True, False])
 @pytest.mark.parametrize("d,heads,kv,seqs,page,layout", [
     (128, 3, 3, [(1560, 390)], 390, "head"), (64, 2, 1, [(515, 130), (40, 40)], 7, "token"), (128, 2, 2, [(2000, 1)], 1, "head"),
     (64, 5, 1, [(333, 20), (1, 1), (2, 2)], 333, "head")])
-def test_chunk(fkv, workspace, d, heads, kv, seqs, page, layout):
+def test_chunk(fkv, sum_len, workspace, d, heads, kv, seqs, page, layout):
     x = Paged(seqs, page, kv, d, seed=3)
     Q = x.rows(heads, d)
-    O, lse = run_attend(fkv, x, Q, causal=False, layout=layout, workspace=workspace)
+    O, lse = run_attend(fkv, x, Q, causal=False, layout=layout, workspace=workspace, sum_len=sum_len)
     check(x, Q, O, lse, False, None)
 
 
 @pytest.mark.parametrize("causal", [True, False])
-@pytest.mark.parametrize("d,seqs", [(128, ONES), (64, SHORT), (128, LONG), (64, LONG)])
-def test_spans(fkv, causal, d, seqs):
+@pytest.mark.parametrize("d,seqs,sum_len", [(128, ONES, None), (64, SHORT, None), (128, LONG, None), (64, LONG, None), (128, LONG, 0), (64, LONG, 0)])
+def test_spans(fkv, causal, d, seqs, sum_len):
     x = Paged(seqs, 32, 4, d, seed=5, spare=1)
     Q = x.rows(8, d)
     spans = [(0, 0), (33, 100), (0, -1), (1, 40)]
-    O, lse = run_attend(fkv, x, Q, causal=causal, spans=spans)
+    O, lse = run_attend(fkv, x, Q, causal=causal, spans=spans, sum_len=sum_len)
     check(x, Q, O, lse, causal, spans)
     tight = [(4, 64)] * 4                     # no head sees everything
-    O, lse = run_attend(fkv, x, Q, causal=causal, spans=tight)
+    O, lse = run_attend(fkv, x, Q, causal=causal, spans=tight, sum_len=sum_len)
     check(x, Q, O, lse, causal, tight)
 
 
 @pytest.mark.parametrize("causal,key", [(True, True), (False, True), (False, False)])
-@pytest.mark.parametrize("d,seqs", [(64, [(90, 20), (40, 3)]), (128, [(300, 200), (70, 70)])])
-def test_odd_values_where_not_seen(fkv, causal, key, d, seqs):
+@pytest.mark.parametrize("d,seqs,sum_len", [(64, [(90, 20), (40, 3)], None), (128, [(300, 200), (70, 70)], None), (128, [(300, 200), (70, 70)], 0)])
+def test_odd_values_where_not_seen(fkv, causal, key, d, seqs, sum_len):
     """Infinities and NaNs at keys that a row does not see, behind the last token and in other pages."""
     x = Paged(seqs, 16, 2, d, seed=9)
     spans = [(5, 30), (0, -1)]
@@ -104,7 +105,7 @@ def test_odd_values_where_not_seen(fkv, causal, key, d, seqs):
             page, row = x.place(i, length - 1)
             x.K[page, y, row + 1:], x.V[page, y, row + 1:] = math.nan, math.inf
     Q = x.rows(4, d)
-    O, lse = run_attend(fkv, x, Q, causal=causal, spans=spans)
+    O, lse = run_attend(fkv, x, Q, causal=causal, spans=spans, sum_len=sum_len)
     ref, rl, A, top = attend(x, Q, 1 / math.sqrt(d), causal, spans)
     ref = torch.where(torch.isnan(rl)[..., None], math.nan, ref)
     odd = ~torch.isfinite(ref)

@@ -31,14 +31,15 @@ def along(x, Q, levels):
     return Q
 
 
+@pytest.mark.parametrize("sum_len", [None, 0])
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("d,heads,seqs", [(128, 2, [(700, 3)]), (64, 4, [(400, 1), (300, 20)]), (128, 3, [(900, 300)]), (64, 2, [(700, 600)])])
 @pytest.mark.parametrize("first,later", [(0.0, 150.0), (150.0, 0.0), (0.0, -400.0), (-300.0, 90.0)])
-def test_first_tile_is_a_poor_reference(fkv, causal, d, heads, seqs, first, later):
+def test_first_tile_is_a_poor_reference(fkv, sum_len, causal, d, heads, seqs, first, later):
     """Scores that rise or fall by hundreds of log2 units after a part's first tile."""
     x = Paged(seqs, 32, heads, d, seed=1)
     Q = along(x, x.rows(heads, d), [[first if j < 100 else later + 0.05 * (j % 9) for j in range(n)] for n, _ in seqs])
-    O, lse = run_attend(fkv, x, Q, causal=causal)
+    O, lse = run_attend(fkv, x, Q, causal=causal, sum_len=sum_len)
     check(x, Q, O, lse, causal, None)
 
 
@@ -81,8 +82,9 @@ def test_many_sequences(fkv, d, kv, heads):
     seqs = [((37 * i) % 400 + n, n) for i, n in enumerate([1, 3, 17, 1, 70, 0, 2, 130] * 17)]
     x = Paged(seqs, 16, kv, d, seed=4, spare=5, before=3)
     Q = x.rows(heads, d)
-    O, lse = run_attend(fkv, x, Q)
-    check(x, Q, O, lse, True, None)
+    for sum_len in (None, 0):
+        O, lse = run_attend(fkv, x, Q, sum_len=sum_len)
+        check(x, Q, O, lse, True, None)
 
 
 @pytest.mark.parametrize("group", [1, 2, 3, 5, 7, 12, 16, 21, 32, 33, 48, 64])
