@@ -133,9 +133,9 @@ Launch plan(const fkv_batch *b, int kv, int group, int32_t lo, int32_t hi, int r
     l.rows = rows;
     l.target = target;
     l.min_tiles = min_tiles;
-    // row tiles: a sequence has one beside every `rows` rows of its own
+    // row tiles: one for every `rows` rows of the batch, and one more a sequence; no more than the longest sequence's of each
     const int64_t most = std::min(std::min(b->max_new, b->n_tokens), hi), seqs = std::min(b->n_seqs, b->n_tokens);
-    const int64_t tiles = most * group <= rows ? seqs : (int64_t)b->n_tokens * group / rows + seqs;
+    const int64_t tiles = std::min((int64_t)b->n_tokens * group / rows + seqs, seqs * ((most * group + rows - 1) / rows));
     // few rows: the items, and the parts that cuts add; a sequence is cut only if its tiles are more than one
     // part's, so parts of cut ones are at most twice the target.  Many rows: a share and two slots to a workgroup.
     l.n_items = tiles * kv;

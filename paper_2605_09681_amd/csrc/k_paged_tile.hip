@@ -115,6 +115,45 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
         rt = item.rt;
     }
     if (EXPANDED) base = first_row(a, at.i);
+    f32x16_t o[MB];
+    float m = neg_inf(), l = 0.f;
+    // This lane's row of the item before, whose results are stored while the next one's first tiles are on their way.
+    int pending = 0;                              // 1: an output row, 2: a part of one
+    bool none = false;                            // the row sees no key
+    int64_t out_at = 0, lse_at = 0;               // where it goes: in O and lse, or (a part) in `part`
+    auto clear = [&]() {
+        m = neg_inf();
+        l = 0.f;
+#pragma unroll
+        for (int b = 0; b < MB; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[b][r] = 0.f;
+    };
+    auto flush = [&]() {
+        if (pending == 1) {
+            const float inv = none ? 0.f : 1.f / l;
+            uint16_t *to = a.O + out_at;
+#pragma unroll
+            for (int b = 0; b < MB; ++b)
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    *(uint2 *)(to + 32 * b + 8 * u) = pack4(o[b][4 * u] * inv, o[b][4 * u + 1] * inv, o[b][4 * u + 2] * inv, o[b][4 * u + 3] * inv);
+            if (LSE && hh == 0) a.lse[lse_at] = none ? neg_inf() : fmaf(m * kLn2, a.scale_log2, logf(l));
+        } else if (pending == 2) {
+            float *to = a.part + out_at;
+            const float by = moderate(&m, &l, a.scale_log2);
+#pragma unroll
+            for (int b = 0; b < MB; ++b)
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    *(f32x4_t *)(to + 32 * b + 8 * u) = f32x4_t{o[b][4 * u], o[b][4 * u + 1], o[b][4 * u + 2], o[b][4 * u + 3]} * by;
+            if (hh == 0) {
+                a.part[lse_at] = m;
+                a.part[lse_at + ROWS] = l;
+            }
+        }
+        pending = 0;
+    };
 #pragma unroll 1
     for (;;) {                                    // (the body ends with the workgroup past its reads of LDS)
     Seq s = at.s;
@@ -133,9 +172,6 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
     const bool live = 32 * w + c < rows;
     const Sight seen = sight(a, s, recent, tok);
     bf16x8_t q[KS];
-    f32x16_t o[MB];
-    float m, l;
-
     // Rows of a tile's keys, one to a lane (past the part's last tile, that one's); EXPANDED: the first one's.
     const int j_last = x.most.end - 1;
     const uint16_t *K = a.K, *V = a.V;
@@ -217,13 +253,6 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
     const uint16_t *k_lane = kts + c * SK + 8 * hh;
     const uint16_t *v_lane = vts + (4 * hh + ((lane & 15) >> 2)) * SV + 16 * (lane >> 4 & 1) + 4 * (lane & 3);
 
-    auto clear = [&]() {
-        l = 0.f;
-#pragma unroll
-        for (int b = 0; b < MB; ++b)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[b][r] = 0.f;
-    };
     // Scores of key block kb (32 keys).
     auto score = [&](const uint16_t *kt, int kb, f32x16_t &z) {
 #pragma unroll
@@ -250,9 +279,10 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
         return __builtin_shufflevector(u, v, 0, 1, 2, 3, 4, 5, 6, 7);
     };
 
-    m = neg_inf();
-    clear();
-    if (tb < te) {
+    if (tb >= te) {
+        flush();
+        clear();
+    } else {
         int next_v = rows_of(tb + 1), next_k = rows_of(tb + 2);   // pool rows of the tiles to load next
         int j0 = x.key(tb, KT);
         bool edge = !all_seen<KT>(x, sink, j0);   // not every row sees every key of the tile
@@ -267,6 +297,9 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
 #pragma unroll
                 for (int k = 0; k < KS; ++k) q[k] = frag(live ? *(const u32x4 *)(from + 16 * k) : u32x4{0, 0, 0, 0});
             }
+            __builtin_amdgcn_sched_barrier(0);
+            flush();
+            clear();
             store_k(kts);
             store_v(vts, j0, edge);
             load_v(next_v);
@@ -405,7 +438,6 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
         if (any_of(again, (int *)kts)) {
             // Tile by tile with a running maximum; an infinity or a NaN among the values goes to the rows that
             // see it alone.
-            m = neg_inf();
             clear();
 #pragma unroll 1
             for (int t = tb; t < te; ++t) {
@@ -462,17 +494,11 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
     }
 
     l += __shfl_xor(l, 32);
+    none = seen.end <= 0;
     if (live && whole && (tb < te || !shared || (item_at >= from && item_at < until))) {   // (no key: who has the item's begin)
-        const bool none = seen.end <= 0;
-        const float inv = none ? 0.f : 1.f / l;
-        uint16_t *to = a.O + (int64_t)(s.start + tok) * a.o_tok + (int64_t)head * a.o_head + 4 * hh;
-#pragma unroll
-        for (int b = 0; b < MB; ++b)
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                *(uint2 *)(to + 32 * b + 8 * u) = pack4(o[b][4 * u] * inv, o[b][4 * u + 1] * inv, o[b][4 * u + 2] * inv, o[b][4 * u + 3] * inv);
-        if (LSE && hh == 0)
-            a.lse[(int64_t)head * a.n_tokens + s.start + tok] = none ? neg_inf() : fmaf(m * kLn2, a.scale_log2, logf(l));
+        pending = 1;
+        out_at = (int64_t)(s.start + tok) * a.o_tok + (int64_t)head * a.o_head + 4 * hh;
+        lse_at = (int64_t)head * a.n_tokens + s.start + tok;
     } else if (live && !whole && tb < te) {
         if (tid == 0) {
             JoinItem &j = a.joins[number];
@@ -492,21 +518,13 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
                 j.parts = n + 1;
             }
         }
-        float *slot = a.part + (int64_t)(2 * number + (tb == 0)) * (ROWS * (DV + 2));
-        float *to = slot + (32 * w + c) * DV + 4 * hh;
-        const float by = moderate(&m, &l, a.scale_log2);
-#pragma unroll
-        for (int b = 0; b < MB; ++b)
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                *(f32x4_t *)(to + 32 * b + 8 * u) = f32x4_t{o[b][4 * u], o[b][4 * u + 1], o[b][4 * u + 2], o[b][4 * u + 3]} * by;
-        if (hh == 0) {
-            slot[ROWS * DV + 32 * w + c] = m;
-            slot[ROWS * DV + ROWS + 32 * w + c] = l;
-        }
+        pending = 2;
+        const int64_t slot = (int64_t)(2 * number + (tb == 0)) * (ROWS * (DV + 2));
+        out_at = slot + (32 * w + c) * DV + 4 * hh;
+        lse_at = slot + ROWS * DV + 32 * w + c;
     }
     // The next item of the share.
-    if (!shared || item_end >= until) return;
+    if (!shared || item_end >= until) break;
     if (++rt == at.rts) {
         rt = 0;
         if (at.y + 1 < a.kv) {
@@ -514,11 +532,12 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
         } else {
             const Line line(a);
             at = line.find(a, at.end);
-            if (!at.ok) return;
+            if (!at.ok) break;
             if (EXPANDED) base = first_row(a, at.i);
         }
     }
     }
+    flush();
 }
 
 // One workgroup joins kJoinRows rows of the cut item that workgroup x's share ends in: its own part lies in slot
