@@ -673,8 +673,9 @@ fkv_status fkv_chunk_attention_q8(const fkv_shape *shape, const fkv_head *heads,
  *
  * Limits (FKV_ERR_SHAPE): n_seqs up to FKV_MAX_SEQS, n_tokens up to 2^24,
  * page_tokens 1 to 2^20, n_pages * n_kv_heads * page_tokens below 2^31; a
- * sequence's tokens beyond 2^30 are not seen. */
-#define FKV_MAX_SEQS 4096
+ * sequence's tokens beyond 2^30 are not seen; an attention call has at most 2^22 tiles
+ * of query rows (64 or more rows of a sequence and key head, or its rest). */
+#define FKV_MAX_SEQS 1024
 typedef struct {
     int32_t n_seqs, max_pages, page_tokens, n_pages, n_tokens, max_new;
     int64_t sum_len;

@@ -54,7 +54,7 @@ FKV_PAIR_ADJACENT, FKV_PAIR_HALVES = 0, 1
 FKV_MAX_HEADS, FKV_MAX_FRAMES, FKV_MAX_SEGMENTS = 64, 256, 4096
 FKV_MAX_POSITION = 1 << 24
 FKV_LATENT_AUTO, FKV_LATENT_ABSORBED, FKV_LATENT_EXPANDED = 0, 1, 2
-FKV_LATENT_ROT, FKV_LATENT_FEW, FKV_MAX_SEQS = 64, 64, 4096
+FKV_LATENT_ROT, FKV_LATENT_FEW, FKV_MAX_SEQS = 64, 64, 1024
 
 EXPORTED = ("fkv_num_segments", "fkv_kept_tokens_max", "fkv_compress_static",
             "fkv_score_workspace_size", "fkv_score_segments", "fkv_select_compact",

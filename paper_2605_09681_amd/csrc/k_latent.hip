@@ -42,7 +42,7 @@ __global__ __launch_bounds__(NT) void latent_absorb_kernel(LatentArgs a) {
     uint16_t *out = a.q_abs + (int64_t)h * width + 64 * x;
     if (x == 0 && h == 0 && w == 0) {
         Seq s;
-        const bool mine = owner_of(p, lane < 16 * TM && t0 + lane < p.n_tokens ? t0 + lane : -1, &s) >= 0;
+        const bool mine = owner_of(p, lane < 16 * TM && t0 + lane < p.n_tokens ? t0 + lane : -1, t0, t0 + 16 * TM, &s) >= 0;
         if (lane < 16 * TM && t0 + lane < p.n_tokens) a.owned[t0 + lane] = mine;
     }
     if (64 * x == a.R) {

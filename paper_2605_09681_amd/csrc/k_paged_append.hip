@@ -19,7 +19,7 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(PagedAppendArgs 
     if (threadIdx.x < 64) {
         const int lane = threadIdx.x;
         Seq s = {0, 0, 0, 0};
-        const int i = owner_of(b, lane < n ? t0 + lane : -1, &s);
+        const int i = owner_of(b, lane < n ? t0 + lane : -1, t0, t0 + n, &s);
         int page = -1, row = 0;
         if (i >= 0) {
             const int p = s.first + t0 + lane - s.start;

@@ -6,8 +6,8 @@
 // query rows of one key head are r = token * group + (head within the group), so heads
 // that share keys share tiles.  Lengths, starts and the page table are device data that
 // a captured graph may change between replays: every value is held to its range here, and
-// the split over workgroups is worked out from them by every wave (two short passes over
-// the sequences, 64 a step), not on the host.
+// the split over workgroups is worked out from them by every wave (two or three passes over
+// the sequences, 64 a step: 2 us for up to 64 of them, some 20 for 1024), not on the host.
 #pragma once
 
 #include "fkv_internal.h"
@@ -235,13 +235,14 @@ struct Split {
             per[k] = __builtin_amdgcn_rcpf(fmaxf((float)a.min_tiles, ceilf(share * (1.f + (float)(k * k) / ((kSizes - 1) * (kSizes - 1))))));
             total[k] = 0.f;
         }
+        per_tile = per[kSizes - 1];
+        if ((int64_t)a.n_seqs * a.kv > a.target) return;      // (more items than that, or sequences that take no part)
         for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
             int rts, tiles;
             counts(a, of(a, i0), &rts, &tiles);
 #pragma unroll
             for (int k = 0; k < kSizes; ++k) total[k] += (float)rts * fmaxf(ceilf((float)tiles * per[k]), 1.f);
         }
-        per_tile = per[kSizes - 1];
 #pragma unroll
         for (int k = kSizes - 2; k >= 0; --k)
             if (sum_of(total[k]) * (float)a.kv <= (float)a.target) per_tile = per[k];
@@ -429,15 +430,16 @@ struct Shares {
     }
 };
 
-// The sequence that holds this lane's batch row `token` (-1: none, or not one of the launch's), and the
-// sequence.  Every lane of a wave calls it.
-__device__ __forceinline__ int owner_of(const PagedArgs &a, int token, Seq *held) {
+// The sequence that holds this lane's batch row `token`, one of t0 .. t1 - 1 (-1: none, or not one of the
+// launch's), and in *held what is known of it.  Every lane of a wave calls it.
+__device__ __forceinline__ int owner_of(const PagedArgs &a, int token, int t0, int t1, Seq *held) {
     const int lane = threadIdx.x & 63;
     int owner = -1;
     for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
         const Seq s = sequence(a, i0 + lane);
-        const int n = s.n >= a.lo && s.n <= a.hi ? s.n : 0, count = min(64, a.n_seqs - i0);
-        for (int l = 0; l < count; ++l) {
+        const int n = s.n >= a.lo && s.n <= a.hi ? s.n : 0;
+        for (uint64_t some = __ballot(n > 0 && s.start < t1 && s.start + n > t0); some; some &= some - 1) {
+            const int l = __builtin_ctzll(some);
             const int start = __builtin_amdgcn_readlane(s.start, l), m = __builtin_amdgcn_readlane(n, l);
             if (owner < 0 && token >= start && token - start < m) {
                 owner = i0 + l;

@@ -59,7 +59,7 @@ def _latent(fkv, batch="default", heads=4, d=128, R=256, Q="default", pages=FAKE
 @pytest.mark.parametrize("call", [_append, _attend, _latent])
 def test_batches(fkv, call):
     assert call(fkv, batch=None) == ARG and "batch" in fkv.fkv_last_error()
-    for kw in (dict(n_seqs=0), dict(n_seqs=4097), dict(n_tokens=-1), dict(n_tokens=(1 << 24) + 1), dict(page_tokens=0),
+    for kw in (dict(n_seqs=0), dict(n_seqs=1025), dict(n_tokens=-1), dict(n_tokens=(1 << 24) + 1), dict(page_tokens=0),
                dict(page_tokens=(1 << 20) + 1), dict(n_pages=0), dict(max_pages=0), dict(n_pages=1 << 30)):
         assert call(fkv, batch=_batch(fkv, **kw)) == SHAPE, kw
     for kw in (dict(max_new=0), dict(sum_len=-1), dict(page_table=None), dict(seq_len=None), dict(q_start=None),
@@ -108,7 +108,7 @@ def test_latent(fkv):
     assert _latent(fkv, ws=FAKE + 128) == ARG
     assert _latent(fkv, Q=_rows(fkv, token=100)) == ARG and _latent(fkv, O=_rows(fkv, token=64)) == ARG
     assert _latent(fkv, batch=_batch(fkv, sum_len=(1 << 30) + 1)) == SHAPE
-    assert _latent(fkv, batch=_batch(fkv, sum_len=1 << 25), form=2) == SHAPE      # 2^18 blocks of 128 tokens
+    assert _latent(fkv, batch=_batch(fkv, sum_len=1 << 25), form=2) == SHAPE      # 2^17 blocks of 256 tokens
 
 
 def test_sizes_without_a_device_are_checked_first(fkv):

@@ -360,3 +360,35 @@ def test_streams(fkv, latent):
         p.step([(ids["e"], 10000)])
     with pytest.raises(ValueError):
         p.step([(ids["e"], 1), (ids["e"], 1)])
+
+
+@pytest.mark.parametrize("new,sum_len", [(1, None), (90, 0)])
+def test_pages_past_2_31_elements(fkv, new, sum_len):
+    """Pages whose offsets pass 32 bits in elements and in bytes: written, then attended."""
+    n_pages, kv, page, d = 22100, 12, 64, 128            # 2.17e9 elements a pool
+    seqs = [(150, new)]
+    x = Paged(seqs, page, kv, d, seed=70)
+    kp, vp = (torch.zeros((n_pages, kv, page, d), dtype=BF, device="cuda") for _ in range(2))
+    far = torch.tensor([n_pages - 1, 5, n_pages - 2], dtype=torch.int32)
+    for at, to in zip(x.table[0, :3].tolist(), far.tolist()):
+        kp[to], vp[to] = x.K[at].cuda(), x.V[at].cuda()
+    K, V, Q = x.rows(kv, d), x.rows(kv, d), x.rows(kv, d)
+    for t in range(new):
+        at, row = x.place(0, 150 - new + t)
+        x.K[at, :, row], x.V[at, :, row] = K[:, t], V[:, t]
+    b = x.batch(fkv, sum_len=sum_len)
+    b.page_table[0, :3] = far.cuda()
+    O, lse = torch.zeros((kv, new, d), dtype=BF, device="cuda"), torch.zeros((kv, new), device="cuda")
+    ws = torch.empty(fkv.fkv_paged_attention_workspace_size(b, kv, kv, d), dtype=torch.uint8, device="cuda")
+    fkv.fkv_append_paged(b, K.cuda(), V.cuda(), kp, vp)
+    fkv.fkv_paged_attention(b, Q.cuda(), kp, vp, 1 / math.sqrt(d), O, lse=lse, workspace=ws)
+    check(x, Q, O.cpu(), lse.cpu(), True, None)
+
+
+@pytest.mark.parametrize("seqs", [[(300001, 1)], [(100003, 70)]])
+def test_long_sequences(fkv, seqs):
+    x = Paged(seqs, 100, 1, 64, seed=71)
+    Q = x.rows(2, 64)
+    for sum_len in (None, 0):
+        O, lse = run_attend(fkv, x, Q, sum_len=sum_len)
+        check(x, Q, O, lse, True, None)
