@@ -248,7 +248,7 @@ fkv_status check_latent(const fkv_batch *b, int32_t n_heads, int32_t head_dim, i
     if ((st = check_batch(b, 1, sizes)) != FKV_OK) return st;
     if (b->sum_len > (int64_t)1 << 30) return fail(FKV_ERR_SHAPE, "sum_len %lld above 2^30", (long long)b->sum_len);
     const LatentPlan p = latent_plan(b, n_heads, head_dim, latent_dim, form, 8);
-    if (p.head_rows / fkv::paged::kSeqRows > 65535)
+    if (p.head_rows / fkv::paged::kSeqRows > 65535 || p.head_rows * (head_dim + FKV_LATENT_ROT) * 2 >= (int64_t)1 << 32)
         return fail(FKV_ERR_SHAPE, "sum_len %lld is too large for the expanded form", (long long)b->sum_len);
     return FKV_OK;
 }

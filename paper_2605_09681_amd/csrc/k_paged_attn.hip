@@ -422,7 +422,7 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
         if (r >= rows) continue;
         if (item.parts == 1) {
             const int tok = token_of(a, r0 + r), head = y * a.group + r0 + r - tok * a.group;
-            const bool none = sight(a, s, recent, tok).end <= 0;
+            const bool none = blind(sight(a, s, recent, tok), sink);
             const float inv = none ? 0.f : 1.f / l_row[t];
             const int64_t to = (int64_t)(s.start + tok) * a.o_tok + (int64_t)head * a.o_head + 4 * g;
 #pragma unroll

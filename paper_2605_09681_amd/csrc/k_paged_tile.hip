@@ -185,7 +185,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
     };
     u32x4 kr[NK], vr[NV];
     bool odd = false;                             // an infinity or a NaN among values that not every row sees
-    // EXPANDED: a tile's rows lie together; a row past the sequence's last is read as zeros.
+    // EXPANDED: a tile's rows lie together; a row past the sequence's last is read as zeros.  (Offsets are unsigned: a
+    // head's copies have fewer than 2^32 bytes.  A buffer of its own for every tile: 620 us against 600 at 480P.)
     auto rsrc = [](const uint16_t *p, int64_t bytes) {
         return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)(uint32_t)bytes, 0x00020000);
     };
@@ -210,7 +211,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
         if constexpr (EXPANDED) {
 #pragma unroll
             for (int i = 0; i < NK; ++i)
-                kr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(k_buf, (tid + i * NT) * 16, row_of_lane * (DQK * 2), 0));
+                kr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(k_buf, (tid + i * NT) * 16, (int)((uint32_t)row_of_lane * (DQK * 2)), 0));
         } else {
             load(K, row_of_lane, std::integral_constant<int, DQK>{}, kr);
         }
@@ -220,7 +221,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
         if constexpr (EXPANDED) {
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                vr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(v_buf, (tid + i * NT) * 16, row_of_lane * (DV * 2), 0));
+                vr[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(v_buf, (tid + i * NT) * 16, (int)((uint32_t)row_of_lane * (DV * 2)), 0));
         } else {
             load(V, row_of_lane, std::integral_constant<int, DV>{}, vr);
         }
@@ -494,7 +495,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
     }
 
     l += __shfl_xor(l, 32);
-    none = seen.end <= 0;
+    none = blind(seen, sink);
     if (live && whole && (tb < te || !shared || (item_at >= from && item_at < until))) {   // (no key: who has the item's begin)
         pending = 1;
         out_at = (int64_t)(s.start + tok) * a.o_tok + (int64_t)head * a.o_head + 4 * hh;

@@ -154,6 +154,8 @@ __device__ __forceinline__ Sight sight(const PagedArgs &a, const Seq &s, int rec
     return Sight{a.causal ? min(p + 1, s.len) : s.len, recent < 0 ? 0 : p - recent};
 }
 __device__ __forceinline__ bool sees(const Sight &v, int sink, int j) { return j < v.end && (j < sink || j >= v.low); }
+// No key at all (a sequence without tokens, a position before 0, or an expanded copy that ends before what the row sees).
+__device__ __forceinline__ bool blind(const Sight &v, int sink) { return v.end <= 0 || (sink <= 0 && v.low >= v.end); }
 
 // The key tiles that tokens t0 .. t1 of a sequence visit: [0, a_tiles) and, from tile
 // b_first on, the others; KT keys each.
@@ -520,9 +522,10 @@ __device__ __forceinline__ u32x4 finite_only(u32x4 v) {
 __device__ __forceinline__ float special_only(uint32_t bits) { return (bits & 0x7f80u) == 0x7f80u ? __uint_as_float(bits << 16) : 0.f; }
 
 // A part's sum far from 1 (its reference far from its largest score) moves into its reference by a power of two,
-// so that joining it with other parts' loses nothing; the factor for its outputs.
+// so that joining it with other parts' loses nothing; the factor for its outputs.  (Where that power would leave the
+// range of a score the parts' references are too near one another to need it.)
 __device__ __forceinline__ float moderate(float *m, float *l, float scale_log2) {
-    if (!(*l > 0.f) || (*l > 0x1p-20f && *l < 0x1p20f) || !(*l < __builtin_inff())) return 1.f;
+    if (!(*l > 0.f) || (*l > 0x1p-20f && *l < 0x1p20f) || !(*l < __builtin_inff()) || scale_log2 < 0x1p-100f) return 1.f;
     const int k = __builtin_amdgcn_frexp_expf(*l);
     *m += (float)k / scale_log2;
     const float by = __builtin_amdgcn_ldexpf(1.f, -k);

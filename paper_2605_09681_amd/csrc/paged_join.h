@@ -29,7 +29,7 @@ struct Joined {
     template <bool WIDE = false>
     __device__ __forceinline__ void put(const PagedArgs &a, const JoinItem &j, int r, int ch) const {
         const int row = j.row0 + r, tok = token_of(a, row), head = j.y * a.group + row - tok * a.group, t = j.start + tok;
-        const bool none = sight(a, Seq{j.len, j.start, 0, j.first}, a.recent[j.y], tok).end <= 0;
+        const bool none = blind(sight(a, Seq{j.len, j.start, 0, j.first}, a.recent[j.y], tok), a.sink[j.y]);
         const float inv = none ? 0.f : 1.f / L;
         join_bf16x4 out;
 #pragma unroll

@@ -34,7 +34,7 @@ from typing import Optional, Sequence, Union
 
 import torch
 
-from . import (Cache8, FKV_DYNAMIC, FKV_LATENT_ROT, FKV_STATIC, PagedBatch, fkv_append_frames, fkv_append_paged,
+from . import (Cache8, FKV_DYNAMIC, FKV_LATENT_ROT, FKV_MAX_SEQS, FKV_STATIC, PagedBatch, fkv_append_frames, fkv_append_paged,
                fkv_latent_attention, fkv_latent_attention_workspace_size, fkv_paged_attention,
                fkv_paged_attention_workspace_size, fkv_append_frames_q8,
                fkv_append_frames_rotated, fkv_attention_mass, fkv_chunk_attention_q8,
@@ -699,6 +699,8 @@ class PagedStreams:
         order in the batch's tensors.  Raises RuntimeError, and changes nothing, if the pool has too few pages."""
         if len({s for s, _ in new}) != len(new) or any(n < 1 for _, n in new) or not new:
             raise ValueError("a step takes each stream once, with a token at least")
+        if len(new) > FKV_MAX_SEQS:
+            raise ValueError(f"a step takes up to {FKV_MAX_SEQS} streams (got {len(new)})")
         P = self.page_tokens
         need = {s: -(-(self._len[s] + n) // P) - len(self._pages[s]) for s, n in new}
         if sum(need.values()) > len(self._free):

@@ -111,6 +111,11 @@ def test_latent(fkv):
     assert _latent(fkv, batch=_batch(fkv, sum_len=1 << 25), form=2) == SHAPE      # 2^17 blocks of 256 tokens
 
 
+def test_latent_keys_of_4_gib(fkv):
+    """2^32 / 384 = 11184810.7 tokens of 192 channels, and the blocks that the sequences may leave unfilled."""
+    assert _latent(fkv, d=128, batch=_batch(fkv, sum_len=11_184_800), form=2) == SHAPE
+
+
 def test_sizes_without_a_device_are_checked_first(fkv):
     out = ctypes.c_size_t(0)
     L = fkv.lib()
@@ -135,3 +140,15 @@ def test_binding(fkv):
         fkv._spans([(0, 1 << 40)], 1)
     with pytest.raises(ValueError):
         fkv._form("both")
+
+
+def test_streams_in_a_step(fkv):
+    from paper_2605_09681_amd.layer import PagedStreams
+    p = PagedStreams(1, 1, 64, n_pages=4, page_tokens=16, device="cpu")
+    streams = [p.open() for _ in range(fkv.FKV_MAX_SEQS + 1)]
+    for new in ([], [(streams[0], 0)], [(streams[0], 1)] * 2, [(s, 1) for s in streams]):
+        with pytest.raises(ValueError):
+            p.step(new)
+    with pytest.raises(RuntimeError):
+        p.step([(streams[0], 65)])
+    assert all(p.length(s) == 0 for s in streams) and len(p._free) == 4

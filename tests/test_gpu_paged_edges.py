@@ -392,3 +392,40 @@ def test_long_sequences(fkv, seqs):
     for sum_len in (None, 0):
         O, lse = run_attend(fkv, x, Q, sum_len=sum_len)
         check(x, Q, O, lse, True, None)
+
+
+@pytest.mark.parametrize("d,sum_len", [(128, 5_800_001), (64, 9_000_001)])
+def test_expanded_copies_past_2_31_bytes(fkv, d, sum_len):
+    """A sequence whose expanded keys pass 32 bits of offset; rows see its first and its last tokens."""
+    R, page, span = 256, 1000, (100, 500)
+    pages = -(-sum_len // page)
+    near = sum_len - (pages - 3) * page                  # the same last tokens, and the first, of a short sequence
+    x, Q, W_k, W_v = latent_case([(page + near, 70)], page, 1, d, R, 72)
+    ref, _ = attend_latent(x, Q, W_k, W_v, 1 / math.sqrt(d + ROT), True, span)
+    short = x.table[0]
+    x.seqs = [(sum_len, 70)]
+    x.table = torch.full((1, pages), int(short[0]), dtype=torch.int32)
+    x.table[0, -3:] = short[1:4]
+    O = run_latent(fkv, x, Q, W_k, W_v, span=span, form="expanded")
+    a, b = x.starts
+    assert rel2(O[:, a:b], ref[:, a:b]) <= 2.0 ** -7
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_latent_room_ends_before_what_a_row_sees(fkv, causal):
+    """Rows that only see tokens beyond the room of the expanded form see no key."""
+    x, Q, W_k, W_v = latent_case([(900, 200)], 64, 2, 64, 256, 14)
+    b = x.batch(fkv, sum_len=0)                          # (256 tokens)
+    O = torch.full((2, x.n_tokens, 64), 7, dtype=BF, device="cuda")
+    fkv.fkv_latent_attention(b, Q.cuda(), x.K.cuda(), W_k.cuda(), W_v.cuda(), 0.1, O, causal=causal, span=(0, 50), form="expanded")
+    assert bool((O[:, x.starts[0]:x.starts[1]] == 0).all())
+
+
+def test_small_scale(fkv):
+    """A scale that makes every probability one: plain means."""
+    x = Paged([(2000, 1), (700, 90)], 64, 1, 64, seed=73)
+    Q = x.rows(2, 64)
+    for sum_len in (None, 0):
+        O, lse = run_attend(fkv, x, Q, sum_len=sum_len, scale=1e-42)
+        ref, rl, A, top = attend(x, Q, 1e-42)
+        assert close(O, ref, A, top, 64, 2000) and close_lse(lse, rl, top, 64, 2000)
