@@ -91,8 +91,18 @@ __global__ __launch_bounds__(NT) void latent_absorb_kernel(LatentArgs a) {
     }
 }
 
+// fp32 values as the sum of two bf16.
+__device__ __forceinline__ void two_bf16(const f32x4_t &v0, const f32x4_t &v1, bf16x8_t *hi, bf16x8_t *lo) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float v = e < 4 ? v0[e] : v1[e - 4];
+        (*hi)[e] = (__bf16)v;
+        (*lo)[e] = (__bf16)(v - (float)(*hi)[e]);
+    }
+}
+
 // o[t][h][c] = sum_r W_v[h][c][r] o'[t][h][r], for the tokens that a sequence of the launch holds:
-// 16 channels a wave, both operands straight from memory.  grid: x = token tile, y = head, z = 64 channels.
+// 16 channels a wave and 16 TM tokens, both operands straight from memory.  grid: x = token tile, y = head, z = 64 channels.
 template <int R, int TM>
 __global__ __launch_bounds__(NT) void latent_unabsorb_kernel(LatentArgs a, int D) {
     const PagedArgs &p = a.p;
@@ -106,29 +116,13 @@ __global__ __launch_bounds__(NT) void latent_unabsorb_kernel(LatentArgs a, int D
         row[i] = a.o_abs + ((int64_t)min(t0 + 16 * i + c, p.n_tokens - 1) * p.n_heads + h) * R + 8 * g;
         acc[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-    // (few tokens: every weight on its way before the first product)
-    constexpr int kSteps = R / 32, kHeld = TM == 1 ? kSteps : 1, kAhead = TM == 1 ? kSteps : 2;
-    u32x4 held[kHeld];
-    if (TM == 1) {
-#pragma unroll
-        for (int k = 0; k < kHeld; ++k) held[k] = *(const u32x4 *)(W + 32 * k);
-        __builtin_amdgcn_sched_barrier(0);
-    }
-#pragma unroll kAhead
+#pragma unroll 2
     for (int k = 0; k < R / 32; ++k) {
-        const bf16x8_t f = frag(TM == 1 ? held[k % kHeld] : *(const u32x4 *)(W + 32 * k));
+        const bf16x8_t f = frag(*(const u32x4 *)(W + 32 * k));
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
             bf16x8_t hi, lo;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const f32x4_t v = *(const f32x4_t *)(row[i] + 32 * k + 4 * h);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    hi[4 * h + e] = (__bf16)v[e];
-                    lo[4 * h + e] = (__bf16)(v[e] - (float)hi[4 * h + e]);
-                }
-            }
+            two_bf16(*(const f32x4_t *)(row[i] + 32 * k), *(const f32x4_t *)(row[i] + 32 * k + 4), &hi, &lo);
             acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, hi, acc[i], 0, 0, 0);
             acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, lo, acc[i], 0, 0, 0);
         }
@@ -139,6 +133,45 @@ __global__ __launch_bounds__(NT) void latent_unabsorb_kernel(LatentArgs a, int D
         if (t < p.n_tokens && a.owned[t])
             *(uint2 *)(p.O + (int64_t)t * p.o_tok + (int64_t)h * p.o_head + c0 + 4 * g) = pack4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
     }
+}
+
+// The same for few tokens, bound by the latency of its loads and by how many CUs read the weights: 16 channels and 16
+// tokens a workgroup, the latent channels dealt to its 4 waves, whose every load is on its way before the first product;
+// their sums meet in LDS in order.  16 tokens of 40 heads, 512 latent channels (10.5 MB of weights) 5.0 us; a wave to all latent
+// channels, 64 channels a workgroup, 7.4.  grid: x = token tile, y = head, z = 16 channels.
+template <int R>
+__global__ __launch_bounds__(NT) void latent_unabsorb_few_kernel(LatentArgs a, int D) {
+    constexpr int S = R / 128;
+    __shared__ f32x4_t sums[3][64];
+    const PagedArgs &p = a.p;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, c = lane & 15;
+    const int h = blockIdx.y, t = blockIdx.x * 16 + c, c0 = 16 * blockIdx.z, r0 = w * (R / 4) + 8 * g;
+    const uint16_t *W = a.W_v + ((int64_t)h * D + c0 + c) * R + r0;
+    const float *row = a.o_abs + ((int64_t)min(t, p.n_tokens - 1) * p.n_heads + h) * R + r0;
+    u32x4 f[S];
+    f32x4_t v[S][2];
+#pragma unroll
+    for (int k = 0; k < S; ++k) {
+        f[k] = *(const u32x4 *)(W + 32 * k);
+        v[k][0] = *(const f32x4_t *)(row + 32 * k);
+        v[k][1] = *(const f32x4_t *)(row + 32 * k + 4);
+    }
+    const bool owned = w == 0 && t < p.n_tokens && a.owned[t];
+    __builtin_amdgcn_sched_barrier(0);
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < S; ++k) {
+        bf16x8_t hi, lo;
+        two_bf16(v[k][0], v[k][1], &hi, &lo);
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(f[k]), hi, acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(f[k]), lo, acc, 0, 0, 0);
+    }
+    if (w > 0) sums[w - 1][lane] = acc;
+    __syncthreads();
+    if (!owned) return;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) acc += sums[i][lane];
+    *(uint2 *)(p.O + (int64_t)t * p.o_tok + (int64_t)h * p.o_head + c0 + 4 * g) = pack4(acc[0], acc[1], acc[2], acc[3]);
 }
 
 // Keys and values of 256 cached tokens of a sequence, blocks of 256 of the heads' 2 D channels in turn: 8
@@ -287,14 +320,13 @@ hipError_t launch_latent_absorb(const LatentArgs &a, int head_dim, hipStream_t s
 }
 
 hipError_t launch_latent_unabsorb(const LatentArgs &a, int head_dim, hipStream_t s) {
-    const bool few = a.p.n_tokens <= 32;
-    const int tile = few ? 16 : 64;
-    const dim3 grid((a.p.n_tokens + tile - 1) / tile, a.p.n_heads, head_dim / 64);
-    if (a.R == 256) {
-        if (few) hipLaunchKernelGGL((latent_unabsorb_kernel<256, 1>), grid, dim3(NT), 0, s, a, head_dim);
-        else hipLaunchKernelGGL((latent_unabsorb_kernel<256, 4>), grid, dim3(NT), 0, s, a, head_dim);
+    if (a.p.n_tokens <= 32) {
+        const dim3 grid((a.p.n_tokens + 15) / 16, a.p.n_heads, head_dim / 16);
+        if (a.R == 256) hipLaunchKernelGGL((latent_unabsorb_few_kernel<256>), grid, dim3(NT), 0, s, a, head_dim);
+        else hipLaunchKernelGGL((latent_unabsorb_few_kernel<512>), grid, dim3(NT), 0, s, a, head_dim);
     } else {
-        if (few) hipLaunchKernelGGL((latent_unabsorb_kernel<512, 1>), grid, dim3(NT), 0, s, a, head_dim);
+        const dim3 grid((a.p.n_tokens + 63) / 64, a.p.n_heads, head_dim / 64);
+        if (a.R == 256) hipLaunchKernelGGL((latent_unabsorb_kernel<256, 4>), grid, dim3(NT), 0, s, a, head_dim);
         else hipLaunchKernelGGL((latent_unabsorb_kernel<512, 4>), grid, dim3(NT), 0, s, a, head_dim);
     }
     return hipGetLastError();
