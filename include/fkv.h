@@ -655,7 +655,8 @@ fkv_status fkv_chunk_attention_q8(const fkv_shape *shape, const fkv_head *heads,
  *   page_table  device int32 [n_seqs][max_pages]; entries behind a sequence's
  *               last page are not read
  *   seq_len     device int32 [n_seqs]: tokens of the sequence, new ones included
- *   q_start     device int32 [n_seqs + 1], not falling
+ *   q_start     device int32 [n_seqs + 1], not falling (each is held to the largest
+ *               before it: a row belongs to one sequence at most)
  *   n_tokens    rows of the batch's tensors (0 enqueues nothing); rows before
  *               q_start[0] and from q_start[n_seqs] on belong to no sequence and
  *               are left as they are

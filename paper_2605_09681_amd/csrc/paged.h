@@ -115,6 +115,16 @@ __device__ __forceinline__ int scan_sum(int x) {
     x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
     return x;
 }
+// The largest of the lanes before and at each, of values >= 0.
+__device__ __forceinline__ int scan_max(int x) {
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));
+    x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
+    return x;
+}
 __device__ __forceinline__ float sum_of(float x) {
     auto add = [&](float y, int bits) { return y + __int_as_float(bits); };
     x = add(x, __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x111, 0xf, 0xf, false));
@@ -130,14 +140,22 @@ struct Seq {
     int len, start, n, first;       // first: position of the first new token (negative: more new tokens than tokens)
 };
 
-__device__ __forceinline__ Seq sequence(const PagedArgs &a, int i) {
+// This lane's of the sequences i0 .. i0 + 63; every lane of a wave calls it, for i0 = 0, 64, ... in turn.  *held: the
+// largest start before i0 (0 at first), then the largest before i0 + 64.  A start is held to the largest before
+// it, so that a row belongs to one sequence at most and all sequences' rows are no more than the batch has, which
+// the host's bounds on items, slots and joins rest on.
+__device__ __forceinline__ Seq sequence(const PagedArgs &a, int i0, int *held) {
+    const int i = i0 + (threadIdx.x & 63);
+    const bool mine = i < a.n_seqs;
+    auto row = [&](int k) { return min(max(a.q_start[k], 0), a.n_tokens); };
+    const int start = max(scan_max(mine ? row(i) : 0), *held), end = mine ? max(row(i + 1), start) : start;
+    *held = __builtin_amdgcn_readlane(end, 63);
     Seq s = {0, 0, 0, 0};
-    if (i < a.n_seqs) {
+    if (mine) {
         s.len = min(max(a.seq_len[i], 0), a.cap);
-        s.start = min(max(a.q_start[i], 0), a.n_tokens);
-        const int n = min(max(a.q_start[i + 1], s.start), a.n_tokens) - s.start;
-        s.n = min(n, a.max_new);
-        s.first = s.len - n;
+        s.start = start;
+        s.n = min(end - start, a.max_new);
+        s.first = s.len - (end - start);
     }
     return s;
 }
@@ -209,6 +227,7 @@ struct Split {
     static constexpr int kSizes = 8;
     float per_tile;                 // parts a tile; 0: nothing is cut
     Seq first;                      // this lane's sequence of the first 64
+    int first_held;                 // the largest start of those (see sequence)
 
     // Row tiles of this lane's sequence, 0 if the launch does not take it; the most key tiles of an item.
     static __device__ __forceinline__ void counts(const PagedArgs &a, const Seq &s, int *rts, int *tiles) {
@@ -217,17 +236,22 @@ struct Split {
         const int keys = a.wide < 0 ? s.len : (int)min((int64_t)s.len, (int64_t)a.wide + s.n + 2 * KT);
         *tiles = max((keys + KT - 1) / KT, 1);
     }
-    __device__ __forceinline__ Seq of(const PagedArgs &a, int i0) const { return i0 == 0 ? first : sequence(a, i0 + (threadIdx.x & 63)); }
+    __device__ __forceinline__ Seq of(const PagedArgs &a, int i0, int *held) const {
+        if (i0 > 0) return sequence(a, i0, held);
+        *held = first_held;
+        return first;
+    }
     __device__ __forceinline__ int parts(int tiles) const { return max((int)ceilf((float)tiles * per_tile), 1); }
 
     __device__ __forceinline__ explicit Split(const PagedArgs &a) {
-        first = sequence(a, threadIdx.x & 63);
+        first_held = 0;
+        first = sequence(a, 0, &first_held);
         per_tile = 0.f;
         if (a.target <= 0) return;
         float sum = 0.f;
-        for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
+        for (int i0 = 0, held = 0; i0 < a.n_seqs; i0 += 64) {
             int rts, tiles;
-            counts(a, of(a, i0), &rts, &tiles);
+            counts(a, of(a, i0, &held), &rts, &tiles);
             sum += (float)rts * (float)tiles;
         }
         const float share = sum_of(sum) * (float)a.kv / (float)a.target;
@@ -239,9 +263,9 @@ struct Split {
         }
         per_tile = per[kSizes - 1];
         if ((int64_t)a.n_seqs * a.kv > a.target) return;      // (more items than that, or sequences that take no part)
-        for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
+        for (int i0 = 0, held = 0; i0 < a.n_seqs; i0 += 64) {
             int rts, tiles;
-            counts(a, of(a, i0), &rts, &tiles);
+            counts(a, of(a, i0, &held), &rts, &tiles);
 #pragma unroll
             for (int k = 0; k < kSizes; ++k) total[k] += (float)rts * fmaxf(ceilf((float)tiles * per[k]), 1.f);
         }
@@ -255,8 +279,8 @@ struct Split {
         Work w;
         w.ok = false;
         int done = 0, slots = 0, joins = 0;
-        for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
-            const Seq s = of(a, i0);
+        for (int i0 = 0, held = 0; i0 < a.n_seqs; i0 += 64) {
+            const Seq s = of(a, i0, &held);
             int rts, tiles;
             counts(a, s, &rts, &tiles);
             const int n = parts(tiles), c = a.kv * rts * n, cut = n > 1 ? c : 0, items = n > 1 ? a.kv * rts : 0;
@@ -288,9 +312,9 @@ struct Split {
     // Cut items of the launch.
     __device__ __forceinline__ int cut_items(const PagedArgs &a) const {
         int sum = 0;
-        for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
+        for (int i0 = 0, held = 0; i0 < a.n_seqs; i0 += 64) {
             int rts, tiles;
-            counts(a, of(a, i0), &rts, &tiles);
+            counts(a, of(a, i0, &held), &rts, &tiles);
             sum += __builtin_amdgcn_readlane(scan_sum(parts(tiles) > 1 ? a.kv * rts : 0), 63);
         }
         return sum;
@@ -310,6 +334,7 @@ struct Shares {
     double total, each;             // of the line
     int groups;                     // workgroups that have a share
     Seq lane_seq;                   // this lane's sequence of the first 64
+    int lane_held;                  // the largest start of those (see sequence)
 
     // A sequence on the line, and a key head of it; uniform.
     struct Place {
@@ -366,13 +391,18 @@ struct Shares {
         const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)u, l), hi = __builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), l);
         return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
     }
-    __device__ __forceinline__ Seq of(const PagedArgs &a, int i0) const { return i0 == 0 ? lane_seq : sequence(a, i0 + (threadIdx.x & 63)); }
+    __device__ __forceinline__ Seq of(const PagedArgs &a, int i0, int *held) const {
+        if (i0 > 0) return sequence(a, i0, held);
+        *held = lane_held;
+        return lane_seq;
+    }
 
     __device__ __forceinline__ explicit Shares(const PagedArgs &a) {
-        lane_seq = sequence(a, threadIdx.x & 63);
+        lane_held = 0;
+        lane_seq = sequence(a, 0, &lane_held);
         total = 0.;
-        for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
-            const Seq s = of(a, i0);
+        for (int i0 = 0, held = 0; i0 < a.n_seqs; i0 += 64) {
+            const Seq s = of(a, i0, &held);
             total += lane_of(scan(length(a, s, row_tiles(a, s))), 63);
         }
         groups = max((int)fmin((double)a.target, total / (double)a.min_tiles), 1);
@@ -400,8 +430,8 @@ struct Shares {
         Place p;
         p.ok = false;
         double done = 0.;
-        for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
-            const Seq s = of(a, i0);
+        for (int i0 = 0, held = 0; i0 < a.n_seqs; i0 += 64) {
+            const Seq s = of(a, i0, &held);
             const int rts = row_tiles(a, s);
             const double sum = scan(length(a, s, rts));
             const uint64_t found = __ballot(rts > 0 && done + sum > x);
@@ -435,10 +465,9 @@ struct Shares {
 // The sequence that holds this lane's batch row `token`, one of t0 .. t1 - 1 (-1: none, or not one of the
 // launch's), and in *held what is known of it.  Every lane of a wave calls it.
 __device__ __forceinline__ int owner_of(const PagedArgs &a, int token, int t0, int t1, Seq *held) {
-    const int lane = threadIdx.x & 63;
     int owner = -1;
-    for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
-        const Seq s = sequence(a, i0 + lane);
+    for (int i0 = 0, before = 0; i0 < a.n_seqs; i0 += 64) {
+        const Seq s = sequence(a, i0, &before);
         const int n = s.n >= a.lo && s.n <= a.hi ? s.n : 0;
         for (uint64_t some = __ballot(n > 0 && s.start < t1 && s.start + n > t0); some; some &= some - 1) {
             const int l = __builtin_ctzll(some);
@@ -456,8 +485,8 @@ __device__ __forceinline__ int owner_of(const PagedArgs &a, int token, int t0, i
 __device__ __forceinline__ int64_t first_row(const PagedArgs &a, int i) {
     const int lane = threadIdx.x & 63;
     int done = 0;
-    for (int i0 = 0; i0 < i; i0 += 64) {
-        const Seq s = sequence(a, i0 + lane);
+    for (int i0 = 0, held = 0; i0 < i; i0 += 64) {
+        const Seq s = sequence(a, i0, &held);
         const bool mine = i0 + lane < i && s.n > 0 && s.n >= a.lo && s.n <= a.hi;
         done += __builtin_amdgcn_readlane(scan_sum(mine ? (s.len + kSeqRows - 1) / kSeqRows : 0), 63);
     }
@@ -467,10 +496,9 @@ __device__ __forceinline__ int64_t first_row(const PagedArgs &a, int i) {
 // Block `want` of kSeqRows rows of the expanded copies: the sequence, its number in *seq, and the
 // block's first key (-1: no such block).
 __device__ __forceinline__ int locate_block(const PagedArgs &a, int want, Seq *held, int *seq) {
-    const int lane = threadIdx.x & 63;
     int done = 0;
-    for (int i0 = 0; i0 < a.n_seqs; i0 += 64) {
-        const Seq s = sequence(a, i0 + lane);
+    for (int i0 = 0, before = 0; i0 < a.n_seqs; i0 += 64) {
+        const Seq s = sequence(a, i0, &before);
         const int blocks = s.n > 0 && s.n >= a.lo && s.n <= a.hi ? (s.len + kSeqRows - 1) / kSeqRows : 0;
         const int ib = scan_sum(blocks);
         const uint64_t found = __ballot(done + ib > want);
