@@ -471,10 +471,12 @@ __device__ __forceinline__ int owner_of(const PagedArgs &a, int token, int t0, i
         const int n = s.n >= a.lo && s.n <= a.hi ? s.n : 0;
         for (uint64_t some = __ballot(n > 0 && s.start < t1 && s.start + n > t0); some; some &= some - 1) {
             const int l = __builtin_ctzll(some);
-            const int start = __builtin_amdgcn_readlane(s.start, l), m = __builtin_amdgcn_readlane(n, l);
-            if (owner < 0 && token >= start && token - start < m) {
+            auto at = [&](int v) { return __builtin_amdgcn_readlane(v, l); };
+            // (read by all lanes: within the branch, lane l may take no part, nor have worked its values out)
+            const Seq x = {at(s.len), at(s.start), at(n), at(s.first)};
+            if (owner < 0 && token >= x.start && token - x.start < x.n) {
                 owner = i0 + l;
-                *held = Seq{__builtin_amdgcn_readlane(s.len, l), start, m, __builtin_amdgcn_readlane(s.first, l)};
+                *held = x;
             }
         }
     }

@@ -131,6 +131,16 @@ def test_starts_that_fall(host, n_tokens, lens, starts, heads, kv):
 
 
 @pytest.mark.parametrize("n_tokens,lens,starts", FALLING)
+def test_a_row_has_one_owner(host, n_tokens, lens, starts):
+    case = Case(lens, starts, n_tokens)
+    want = [-1] * n_tokens
+    for i, (start, n, _) in enumerate(case.rows()):
+        want[start:start + n] = [i] * n
+    assert host.host_append(ctypes.byref(case.c), 4, 64) == 0
+    assert read(host.host_owners, I32) == want
+
+
+@pytest.mark.parametrize("n_tokens,lens,starts", FALLING)
 def test_latent_rows(host, n_tokens, lens, starts):
     case = Case(lens, starts, n_tokens, sum_len=sum(max(n, 0) for n in lens) % (1 << 22))
     assert host.host_latent(ctypes.byref(case.c), 5, 64, 256, 1) == 0
