@@ -664,7 +664,8 @@ fkv_status fkv_chunk_attention_q8(const fkv_shape *shape, const fkv_head *heads,
  *               max_new are served
  *   sum_len     >= the sum of seq_len; the expanded latent form has room for that
  *               many tokens and leaves out those beyond.  Elsewhere it may be 0 (not
- *               known); where it is small, chunks of few tokens are split more finely
+ *               known: latent attention that chooses its form stays absorbed); where
+ *               it is small, chunks of few tokens are split more finely
  * Lengths, starts and pages are read on the device when the call runs, so a
  * captured graph serves other values later; values outside their range are held
  * to it (a key on a page outside the pool is read from another page, a new
@@ -751,7 +752,8 @@ fkv_status fkv_paged_attention(const fkv_batch *batch, int32_t n_heads, int32_t 
  *                        made first (in the workspace), then attended;
  *   FKV_LATENT_AUTO      each sequence by its new tokens: absorbed up to
  *                        FKV_LATENT_FEW - 1 of them, expanded from there on (512
- *                        channels: the times cross at 45 to 80 tokens, 256: at 100).
+ *                        channels: the times cross at 45 to 80 tokens, 256: at 100);
+ *                        all absorbed where sum_len is 0.
  * Absorbed queries, expanded keys and values, and the expanded form's probabilities are
  * rounded to bf16; the absorbed form's probabilities and latent outputs are not (off by
  * 2.9e-3 and 2.3e-3 from 64 bits in relative 2-norm, a bf16 output alone by 1.7e-3).  The

@@ -984,7 +984,7 @@ class PagedBatch:
     new tokens) lie on the GPU and may be written between calls.  ``n_tokens``
     rows have the batch's tensors; ``max_new`` is at least every sequence's new
     tokens, ``sum_len`` at least the sum of ``seq_len`` (the expanded latent form
-    needs it; elsewhere 0 for unknown)."""
+    needs it; elsewhere 0 for unknown, with which form "auto" stays absorbed)."""
 
     def __init__(self, page_table, seq_len, q_start, page_tokens: int, n_tokens: int, max_new: int, sum_len: int = 0):
         self.device = _device_of(page_table, "page_table")

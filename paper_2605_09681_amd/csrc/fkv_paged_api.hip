@@ -202,7 +202,8 @@ LatentPlan latent_plan(const fkv_batch *b, int n_heads, int d, int R, int form, 
     LatentPlan p;
     memset(&p, 0, sizeof p);
     const int most = std::min(b->max_new, std::max(b->n_tokens, 1)), all = std::numeric_limits<int32_t>::max();
-    p.expanded = form == FKV_LATENT_EXPANDED || (form == FKV_LATENT_AUTO && most >= FKV_LATENT_FEW);
+    // (expanded copies have room for sum_len tokens: where that is not known, the other form serves them all)
+    p.expanded = form == FKV_LATENT_EXPANDED || (form == FKV_LATENT_AUTO && most >= FKV_LATENT_FEW && b->sum_len > 0);
     p.absorbed = form == FKV_LATENT_ABSORBED || (form == FKV_LATENT_AUTO && (!p.expanded || b->n_seqs > 1));
     size_t at = 0;
     auto take = [&](size_t n) {

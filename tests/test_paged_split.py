@@ -166,3 +166,13 @@ def test_any_batch(host, seed):
     spans = (Span * kv)(*[Span(rng.randint(0, 50), rng.choice([-1, rng.randint(0, 3000)])) for _ in range(kv)])
     assert host.host_attend(ctypes.byref(case.c), kv * group, kv, 64, rng.choice([None, spans]), 1) == 0
     check(host, case, group, kv)
+
+
+@pytest.mark.parametrize("form,sum_len,tiles,hi", [(0, 0, 0, 2 ** 31 - 1), (0, 1100, 256, 63), (1, 1100, 0, 2 ** 31 - 1), (1, 0, 0, 2 ** 31 - 1)])
+def test_form(host, form, sum_len, tiles, hi):
+    """The form that is chosen expands a sequence's tokens only where their number is known."""
+    case = Case([900, 200], [0, 200, 201], 201, sum_len=sum_len)
+    assert host.host_latent(ctypes.byref(case.c), 3, 64, 256, form) == 0
+    p = host.host_plan().contents
+    assert (p.tiles, p.lo, p.hi) == (tiles, 1, hi)
+    check(host, case, 3, 1)
