@@ -440,7 +440,7 @@ class RolloutStack:
         if cache == "e4m3":
             self.step_mode = "q8"
             self.cache8 = [Cache8.zeros(full, block_tokens, dev) for _ in range(n_layers)]
-            self._q8_bytes, self._q8_ws, self._q8_stream, self._q8_captured = {}, None, None, []
+            self._q8_bytes, self._q8_ws = {}, _Workspace(self.device)
             return
         hist = (n_heads, window, frame_tokens, head_dim)
         self.K_hist = [torch.zeros(hist, dtype=dt, device=dev) for _ in range(n_layers)]
@@ -608,24 +608,13 @@ class RolloutStack:
             raise ValueError(f"{what}: not available for an 8-bit cache")
 
     def _q8_workspace(self, heads, key):
-        """The 8-bit attention's workspace: the largest so far, sized for the full
-        window, so that a window that fills up does not replace it chunk by chunk.  A
-        smaller one stays allocated only if a graph was captured with it, which still
-        writes to it."""
+        """The 8-bit attention's workspace, sized for the full window, so that a window
+        that fills up does not replace it chunk by chunk."""
         with torch.cuda.device(self.device):
             if key not in self._q8_bytes:
                 self._q8_bytes[key] = max(fkv_chunk_attention_q8_workspace_size(self.shape(H), heads, key[2], key[3])
                                           for H in {key[1], self.window})
-            stream = torch.cuda.current_stream()
-            if self._q8_ws is None or self._q8_bytes[key] > self._q8_ws.numel():
-                self._q8_ws = torch.empty(max(self._q8_bytes[key], 1), dtype=torch.uint8, device=self.device)
-                self._q8_stream = stream
-            if torch.cuda.is_current_stream_capturing():
-                if not any(w is self._q8_ws for w in self._q8_captured):
-                    self._q8_captured.append(self._q8_ws)
-            elif stream != self._q8_stream:
-                self._q8_ws.record_stream(stream)      # freed only after this stream's use of it
-        return self._q8_ws
+        return self._q8_ws.get(self._q8_bytes[key])
 
     def rotate(self, frame_pos, Q, K, V, Qr, Kr, Vr):
         """The chunk's Q and K turned by ``rope`` and its V as it is, from any strided
@@ -650,6 +639,34 @@ class RolloutStack:
             fkv_append_frames(self.shape(0), K_new, V_new, dst_slots, self.K_hist[layer], self.V_hist[layer])
 
 
+class _Workspace:
+    """The workspace of calls that run one after another: the largest so far.  A smaller
+    one stays allocated only if a graph was captured with it, which still writes to it."""
+
+    def __init__(self, device):
+        self.device, self.held, self.stream, self.captured = device, None, None, []
+
+    def get(self, n: int, room: int = 0) -> torch.Tensor:
+        """At least n bytes on the current stream; one that has to be replaced is made of room bytes if those are more."""
+        with torch.cuda.device(self.device):
+            stream = torch.cuda.current_stream()
+            if self.held is None or n > self.held.numel():
+                self.held = None
+                try:
+                    self.held = torch.empty(max(n, room, 1), dtype=torch.uint8, device=self.device)
+                except torch.cuda.OutOfMemoryError:
+                    if room <= n:
+                        raise
+                    self.held = torch.empty(max(n, 1), dtype=torch.uint8, device=self.device)
+                self.stream = stream
+            if torch.cuda.is_current_stream_capturing():
+                if not any(w is self.held for w in self.captured):
+                    self.captured.append(self.held)
+            elif stream != self.stream:
+                self.held.record_stream(stream)            # freed only after this stream's use of it
+            return self.held
+
+
 class PagedStreams:
     """The caches of many streams in one pool of pages, for a stack of attention layers.
 
@@ -662,8 +679,10 @@ class PagedStreams:
     heads), and :meth:`attend` takes the layer's up-projections.
 
     Layers run one after another and share one workspace, which grows with the
-    batches (one that a captured graph may still use is kept).  Calls enqueue on
-    the current stream; :meth:`step` copies the batch's tables to the device."""
+    batches, by half at least (one that a graph was captured with is kept).  Calls
+    enqueue on the current stream; :meth:`step` copies the batch's tables to the
+    device: a graph captured over a batch's calls reads that batch's tensors on
+    replay, which have to be kept, and serves other streams if those are written."""
 
     def __init__(self, n_layers: int, n_heads: int, head_dim: int, n_pages: int, page_tokens: int,
                  n_kv_heads: Optional[int] = None, latent_dim: int = 0, device="cuda"):
@@ -678,7 +697,7 @@ class PagedStreams:
         self.scale = 1.0 / math.sqrt(head_dim + (FKV_LATENT_ROT if latent_dim else 0))
         self._free = list(range(n_pages))[::-1]
         self._pages, self._len, self._next = {}, {}, 0
-        self._ws, self._kept = None, []
+        self._ws = _Workspace(self.device)
 
     def open(self) -> int:
         """A new stream without tokens."""
@@ -736,11 +755,9 @@ class PagedStreams:
                                 self._workspace(n))
 
     def _workspace(self, n: int):
-        if self._ws is None or self._ws.numel() < n:
-            if self._ws is not None:
-                self._kept.append(self._ws)
-            self._ws = torch.empty(max(n, 1), dtype=torch.uint8, device=self.device)
-        return self._ws
+        # (streams that grow by chunks need a little more at every step)
+        held = self._ws.held
+        return self._ws.get(n, 0 if held is None else held.numel() * 3 // 2)
 
 
 class _Budget:
