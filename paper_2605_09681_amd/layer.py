@@ -30,6 +30,7 @@ synchronises with the host.
 from __future__ import annotations
 
 import math
+from operator import index
 from typing import Optional, Sequence, Union
 
 import torch
@@ -715,25 +716,31 @@ class PagedStreams:
 
     def step(self, new: Sequence) -> PagedBatch:
         """Room for the next tokens of streams, [(stream, tokens), ...], whose rows follow one another in this
-        order in the batch's tensors.  Raises RuntimeError, and changes nothing, if the pool has too few pages."""
+        order in the batch's tensors.  Raises RuntimeError if the pool has too few pages; a step that raises changes nothing."""
+        new = [(s, index(n)) for s, n in new]
         if len({s for s, _ in new}) != len(new) or any(n < 1 for _, n in new) or not new:
             raise ValueError("a step takes each stream once, with a token at least")
         if len(new) > FKV_MAX_SEQS:
             raise ValueError(f"a step takes up to {FKV_MAX_SEQS} streams (got {len(new)})")
-        P = self.page_tokens
-        need = {s: -(-(self._len[s] + n) // P) - len(self._pages[s]) for s, n in new}
-        if sum(need.values()) > len(self._free):
-            raise RuntimeError(f"{sum(need.values())} pages needed, {len(self._free)} free")
-        starts = [0]
-        for s, n in new:
-            self._pages[s] += [self._free.pop() for _ in range(need[s])]
-            self._len[s] += n
+        P, pages, used = self.page_tokens, {}, 0
+        lens = [self._len[s] + n for s, n in new]
+        need = [-(-length // P) - len(self._pages[s]) for (s, _), length in zip(new, lens)]
+        if sum(need) > len(self._free):
+            raise RuntimeError(f"{sum(need)} pages needed, {len(self._free)} free")
+        left = len(self._free) - sum(need)
+        starts, fresh = [0], self._free[left:][::-1]
+        for (s, n), k in zip(new, need):
+            pages[s] = self._pages[s] + fresh[used:used + k]
+            used += k
             starts.append(starts[-1] + n)
-        lens = [self._len[s] for s, _ in new]
-        width = max(len(self._pages[s]) for s, _ in new)
-        table = [self._pages[s] + [-1] * (width - len(self._pages[s])) for s, _ in new]
+        width = max(len(pages[s]) for s, _ in new)
+        table = [pages[s] + [-1] * (width - len(pages[s])) for s, _ in new]
         dev = lambda v: torch.tensor(v, dtype=torch.int32, device=self.device)  # noqa: E731
-        return PagedBatch(dev(table), dev(lens), dev(starts), P, starts[-1], max(n for _, n in new), sum(lens))
+        batch = PagedBatch(dev(table), dev(lens), dev(starts), P, starts[-1], max(n for _, n in new), sum(lens))
+        del self._free[left:]
+        self._pages.update(pages)
+        self._len.update((s, length) for (s, _), length in zip(new, lens))
+        return batch
 
     def append(self, layer: int, batch: PagedBatch, K_new, V_new=None):
         """The batch's new keys and values (latent rows: K_new alone), [n_kv_heads][n_tokens][d] views, into the layer's pages."""
