@@ -486,13 +486,13 @@ __device__ __forceinline__ int owner_of(const PagedArgs &a, int token, int t0, i
 // First row of sequence i in the expanded copies.
 __device__ __forceinline__ int64_t first_row(const PagedArgs &a, int i) {
     const int lane = threadIdx.x & 63;
-    int done = 0;
+    int64_t done = 0;                // (lengths may say more than the copies have room for)
     for (int i0 = 0, held = 0; i0 < i; i0 += 64) {
         const Seq s = sequence(a, i0, &held);
         const bool mine = i0 + lane < i && s.n > 0 && s.n >= a.lo && s.n <= a.hi;
         done += __builtin_amdgcn_readlane(scan_sum(mine ? (s.len + kSeqRows - 1) / kSeqRows : 0), 63);
     }
-    return (int64_t)done * kSeqRows;
+    return done * kSeqRows;
 }
 
 // Block `want` of kSeqRows rows of the expanded copies: the sequence, its number in *seq, and the

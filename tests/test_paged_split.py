@@ -176,3 +176,19 @@ def test_form(host, form, sum_len, tiles, hi):
     p = host.host_plan().contents
     assert (p.tiles, p.lo, p.hi) == (tiles, 1, hi)
     check(host, case, 3, 1)
+
+
+@pytest.mark.parametrize("lens,pages,page,sum_len", [
+    ([300, 0, 256, 257, 1, 5000] * 30, 512, 16, 30 * 6000), ([300, 5, 0, 700], 512, 16, 100),
+    ([1 << 30] * 1024, 1024, 1 << 20, 1000),               # 2^40 tokens where 1000 are said to be
+    ([2 ** 31 - 1, 5, -3] * 300, 1024, 1 << 20, 1 << 20)])
+def test_rows_of_expanded_copies(host, lens, pages, page, sum_len):
+    """Sequences follow one another in whole blocks, those beyond the room of the copies behind it."""
+    case = Case(lens, list(range(len(lens) + 1)), len(lens), sum_len=sum_len, pages=pages, page=page)
+    assert host.host_latent(ctypes.byref(case.c), 2, 64, 256, 2) == 0
+    blocks = [-(-min(max(n, 0), pages * page) // 256) for n in lens]
+    assert read(host.host_first_rows, ctypes.c_int64) == [256 * sum(blocks[:i]) for i in range(len(lens))]
+    owned, room = [], -(-sum_len // 256) + len(lens)
+    for i, n in enumerate(blocks):
+        owned += [v for k in range(min(n, room - len(owned) // 2)) for v in (i, 256 * k)]
+    assert read(host.host_blocks, I32, 2) == owned + [-1, -1] * (room - len(owned) // 2)
