@@ -19,8 +19,9 @@
 //
 // m is not the maximum but the largest score of the part's first tile: any reference
 // cancels in the quotient, and probabilities above one are as exact in fp32 and bf16 as
-// those below, so nothing waits for other waves' scores.  Where a row's sum leaves
-// [2^-100, 2^100] or an output is not finite, and where an infinity or a NaN lies among
+// those below (down to 2^-126: what a sum of 2^-64 and more loses with each weight below it is under
+// 2^-62 of it), so nothing waits for other waves' scores.  Where a row's sum leaves
+// [2^-64, 2^100] or an output is not finite, and where an infinity or a NaN lies among
 // values that only some rows see, the part is computed again, tile by tile with a running
 // maximum (`careful`).
 //
@@ -337,7 +338,7 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
                 m_row[t] = neg_inf();            // (no key of the part's)
                 continue;
             }
-            again |= !(l_row[t] > 0x1p-100f && l_row[t] < 0x1p100f);
+            again |= !(l_row[t] > 0x1p-64f && l_row[t] < 0x1p100f);
 #pragma unroll
             for (int b = 0; b < C::NB; ++b)
 #pragma unroll

@@ -10,10 +10,10 @@
 //                  largest score of the part's first tile: any reference cancels in the
 //                  quotient, and probabilities above one are as exact as those below,
 //   O^T += V^T P^T (A = V^T through the LDS transpose read, P straight from S^T).
-// Where a row's sum leaves [2^-100, 2^100] or an output is not finite, and where an infinity
-// or a NaN lies among values that only some rows see, the part is computed again, tile by
-// tile with a running maximum.  The sum adds the probabilities as they are; where no lse is
-// asked for, the rounded ones that weight the values, two at a time.
+// Where a row's sum leaves [2^-64, 2^100] (weights below 2^-126 are lost, and would count) or an output is not
+// finite, and where an infinity or a NaN lies among values that only some rows see, the part is
+// computed again, tile by tile with a running maximum.  The sum adds the probabilities as they
+// are; where no lse is asked for, the rounded ones that weight the values, two at a time.
 //
 // The matrix units bound it, so everything is arranged around their stream: the products of a
 // tile are one pinned sequence (scores of key block 1, values of block 0, scores of the next
@@ -430,7 +430,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
             const float all = l + __shfl_xor(l, 32);
             bool again = odd;
             if (live && met) {
-                again |= !(all > 0x1p-100f && all < 0x1p100f);
+                again |= !(all > 0x1p-64f && all < 0x1p100f);
 #pragma unroll
                 for (int b = 0; b < MB; ++b)
 #pragma unroll
