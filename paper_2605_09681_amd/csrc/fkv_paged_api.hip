@@ -289,7 +289,8 @@ fkv_status fkv_append_paged(const fkv_batch *batch, int32_t n_heads, int32_t hea
     a.chunks = head_dim * es / 16;
     magic_of(a.chunks, &a.chunks_hi, &a.chunks_lo);
     magic_of(a.heads, &a.heads_hi, &a.heads_lo);
-    a.block_tokens = std::max(1, std::min(64, 1024 / (a.heads * a.chunks)));
+    // (a launch holds fewer than 2^32 threads)
+    a.block_tokens = std::max(batch->n_tokens < 1 << 23 ? 1 : 2, std::min(64, 1024 / (a.heads * a.chunks)));
     (void)hipGetLastError();
     return done(fkv::launch_paged_append(a, (hipStream_t)stream), "fkv_append_paged launch");
 }

@@ -40,6 +40,7 @@ hipError_t split(const fkv::PagedArgs &a, int rows) {
 }
 
 std::vector<int32_t> owners, blocks;
+int32_t block_tokens;
 std::vector<int64_t> first_rows;
 
 }  // namespace
@@ -81,6 +82,8 @@ hipError_t launch_expanded_tiles(const PagedArgs &a, int, hipStream_t) {
     return hipSuccess;
 }
 hipError_t launch_paged_append(const PagedAppendArgs &a, hipStream_t) {
+    block_tokens = a.block_tokens;
+    if (owners.empty()) return hipSuccess;
     for (int t0 = 0; t0 < a.batch.n_tokens; t0 += wave::kLanes)
         wave::run([&](int lane) {
             paged::Seq s;
@@ -117,11 +120,12 @@ int host_latent(const fkv_batch *b, int heads, int d, int R, int form) {
     const fkv_rows q = rows_of(heads, d + FKV_LATENT_ROT), o = rows_of(heads, d);
     return fkv_latent_attention(b, heads, d, R, &q, kAny, kAny, kAny, 1, nullptr, 0.1f, &o, form, kAny, (size_t)1 << 50, nullptr);
 }
-int host_append(const fkv_batch *b, int heads, int d) {
-    owners.assign(b->n_tokens, -2);
+int host_append(const fkv_batch *b, int heads, int d, int dtype, int owned) {
+    owners.assign(owned ? b->n_tokens : 0, -2);
     const fkv_rows r = rows_of(heads, d);
-    return fkv_append_paged(b, heads, d, FKV_BF16, &r, &r, kAny, kAny, nullptr);
+    return fkv_append_paged(b, heads, d, dtype, &r, &r, kAny, kAny, nullptr);
 }
+int host_block_tokens() { return block_tokens; }
 const Plan *host_plan() { return &plan_out; }
 int host_items(const Item **p) {
     *p = items.data();

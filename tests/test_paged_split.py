@@ -51,7 +51,7 @@ def host(tmp_path_factory):
     B = ctypes.POINTER(Batch)
     L.host_attend.argtypes = [B, I32, I32, I32, ctypes.POINTER(Span), I32]
     L.host_latent.argtypes = [B, I32, I32, I32, I32]
-    L.host_append.argtypes = [B, I32, I32]
+    L.host_append.argtypes = [B, I32, I32, I32, I32]
     L.host_plan.restype = ctypes.POINTER(Plan)
     return L
 
@@ -136,7 +136,7 @@ def test_a_row_has_one_owner(host, n_tokens, lens, starts):
     want = [-1] * n_tokens
     for i, (start, n, _) in enumerate(case.rows()):
         want[start:start + n] = [i] * n
-    assert host.host_append(ctypes.byref(case.c), 4, 64) == 0
+    assert host.host_append(ctypes.byref(case.c), 4, 64, 0, 1) == 0
     assert read(host.host_owners, I32) == want
 
 
@@ -192,3 +192,13 @@ def test_rows_of_expanded_copies(host, lens, pages, page, sum_len):
     for i, n in enumerate(blocks):
         owned += [v for k in range(min(n, room - len(owned) // 2)) for v in (i, 256 * k)]
     assert read(host.host_blocks, I32, 2) == owned + [-1, -1] * (room - len(owned) // 2)
+
+
+@pytest.mark.parametrize("heads,d,dtype", [(1, 8, 0), (12, 128, 0), (64, 64, 0), (64, 128, 0), (12, 128, 1), (64, 4096, 1), (3, 8192, 0)])
+@pytest.mark.parametrize("n_tokens", [1, 7, 4680, (1 << 23) - 1, (1 << 23) + 1, 1 << 24])
+def test_append_launches(host, heads, d, dtype, n_tokens):
+    """Workgroups of 256 threads for at most 64 tokens each, fewer than 2^32 threads in all, whatever the rows' width."""
+    case = Case([1], [0, 1], n_tokens)
+    assert host.host_append(ctypes.byref(case.c), heads, d, dtype, 0) == 0
+    tokens = host.host_block_tokens()
+    assert 1 <= tokens <= 64 and -(-n_tokens // tokens) * 256 < 1 << 32
