@@ -719,7 +719,8 @@ fkv_status fkv_append_paged(const fkv_batch *batch, int32_t n_heads, int32_t hea
  * effect on it, infinities and NaNs included.  head_dim 64 or 128, n_heads a
  * multiple of n_kv_heads, both up to FKV_MAX_HEADS.  Products are bf16 with
  * fp32 accumulation, softmax and sums fp32; probabilities are rounded to bf16
- * for the value product.
+ * for the value product, which the sum of the rounded ones divides (a row that
+ * sees one key has its value exactly); lse takes the sum of them as they are.
  *
  * With a workspace of fkv_paged_attention_workspace_size bytes (for the same
  * batch sizes, on the same device; no initialisation; calls may share one in

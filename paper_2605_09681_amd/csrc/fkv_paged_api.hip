@@ -142,7 +142,7 @@ Launch plan(const fkv_batch *b, int kv, int group, int32_t lo, int32_t hi, int r
     l.n_work = few ? l.n_items + target + 8 : target;
     l.n_slots = 2 * (int64_t)target + (few ? 64 : 0);
     l.n_joins = few ? std::min(l.n_items, l.n_slots / 2) : target;
-    l.part_bytes = l.n_joins * sizeof(fkv::JoinItem) + (size_t)l.n_slots * rows * (width + 2) * 4;
+    l.part_bytes = l.n_joins * sizeof(fkv::JoinItem) + (size_t)l.n_slots * rows * fkv::part_width(width) * 4;
     return l;
 }
 

@@ -85,7 +85,9 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
     __shared__ __attribute__((aligned(16))) uint16_t tiles[3][C::TILE];
     // probabilities; careful: scores [row][SS]
     __shared__ __attribute__((aligned(16))) float mix[C::P_FLOATS > C::ROWS * C::SS ? C::P_FLOATS : C::ROWS * C::SS];
-    __shared__ float ends[3][MT][2][16];         // per row and key block: first tile's largest scores, sums, whether a key was seen
+    // per row and key block: first tile's largest scores, sums of the weights as they weigh the values, and as they are (-1: no
+    // key was seen)
+    __shared__ float ends[3][MT][2][16];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, c = lane & 15;
 
     const Split<C::ROWS, KT> split(a);
@@ -198,7 +200,9 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
 #pragma unroll
         for (int i = 0; i < C::PER; ++i) z[i] += u[i];
     };
-    float ref[C::PER], cm[C::PER], l[C::PER];    // the reference, times scale_log2 (0: taken from the scores before), the sums
+    // The reference, times scale_log2 (0: taken from the scores before); the sums of the weights as they weigh the values, and,
+    // where those are rounded, as they are.
+    float ref[C::PER], cm[C::PER], l[C::PER], exact[C::PER];
     bool far = false, met[C::PER];               // met: a key of the row's was seen
     auto probabilities = [&](int t) {
         if (!busy) return;
@@ -220,9 +224,14 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
             } else {
                 met[i] = true;
             }
-            l[i] += (e[0] + e[1]) + (e[2] + e[3]);
-            if (!mine(i)) continue;
             const uint2 hi = pack4(e);
+            const float four = (e[0] + e[1]) + (e[2] + e[3]);
+            if (C::PL == 2) l[i] += four;
+            else {
+                l[i] = add_two(hi.y, add_two(hi.x, l[i]));
+                exact[i] += four;
+            }
+            if (!mine(i)) continue;
             ((uint2 *)mix)[(((t & 1) * C::PL * MT + mt_of(i)) * 64 + lane) * 2 + kb] = hi;
             if (C::PL == 2) {
                 const f32x4_t rest = {e[0] - __uint_as_float(hi.x << 16), e[1] - __uint_as_float(hi.x & 0xffff0000u),
@@ -253,11 +262,11 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
         }
     };
 
-    float m_row[MT], l_row[MT];                  // of rows 16 t + c, in every wave
+    float m_row[MT], l_row[MT], exact_row[MT];   // of rows 16 t + c, in every wave
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
         m_row[t] = neg_inf();
-        l_row[t] = 0.f;
+        l_row[t] = exact_row[t] = 0.f;
     }
     if (tb < te) {
         int next;
@@ -300,7 +309,7 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
             // below kFar the rounding of cm is 2^-14 log2 units at most; beyond, scores are subtracted before they
             // are scaled (of nearby scores the difference is exact)
             far |= __ballot(!(fabsf(cm[i]) < kFar)) != 0;
-            l[i] = 0.f;
+            l[i] = exact[i] = 0.f;
             met[i] = false;
         }
 #pragma unroll
@@ -320,10 +329,12 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
         for (int i = 0; i < C::PER; ++i) {
             l[i] += __shfl_xor(l[i], 16);
             l[i] += __shfl_xor(l[i], 32);
+            exact[i] += __shfl_xor(exact[i], 16);
+            exact[i] += __shfl_xor(exact[i], 32);
             const uint64_t any = __ballot(met[i]);
             if (g == 0 && mine(i)) {
                 ends[1][mt_of(i)][kb][c] = l[i];
-                ends[2][mt_of(i)][kb][c] = (any >> c | any >> (16 + c) | any >> (32 + c) | any >> (48 + c)) & 1 ? 1.f : 0.f;
+                ends[2][mt_of(i)][kb][c] = (any >> c | any >> (16 + c) | any >> (32 + c) | any >> (48 + c)) & 1 ? exact[i] : -1.f;
             }
         }
         __syncthreads();
@@ -333,8 +344,10 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
             const float top = fmaxf(ends[0][t][0][c], ends[0][t][1][c]);
             m_row[t] = fabsf(top) < __builtin_inff() ? top : 0.f;
             l_row[t] = ends[1][t][0][c] + ends[1][t][1][c];
+            const float exact0 = ends[2][t][0][c], exact1 = ends[2][t][1][c];
+            exact_row[t] = (exact0 < 0.f ? 0.f : exact0) + (exact1 < 0.f ? 0.f : exact1);
             if (16 * t + c >= rows) continue;
-            if (ends[2][t][0][c] + ends[2][t][1][c] == 0.f) {
+            if (exact0 < 0.f && exact1 < 0.f) {
                 m_row[t] = neg_inf();            // (no key of the part's)
                 continue;
             }
@@ -349,7 +362,7 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
                 m_row[t] = neg_inf();
-                l_row[t] = 0.f;
+                l_row[t] = exact_row[t] = 0.f;
 #pragma unroll
                 for (int b = 0; b < C::NB; ++b) o[t][b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
             }
@@ -368,7 +381,7 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
                     const Sight see = sight(a, s, recent, token_of(a, row_of(16 * i + c)));
-                    float e[8], top = neg_inf(), sum = 0.f;
+                    float e[8], top = neg_inf(), sum = 0.f, rounded = 0.f;
 #pragma unroll
                     for (int r = 0; r < 8; ++r) {
                         const int k = 16 * (r >> 2) + 4 * g + (r & 3);
@@ -387,8 +400,10 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
                         sum += v;
                         p[r] = (__bf16)v;
                         rest[r] = (__bf16)(v - (float)p[r]);
+                        rounded += (float)p[r];
                     }
-                    l_row[i] = l_row[i] * alpha + sum;
+                    l_row[i] = l_row[i] * alpha + (C::PL == 2 ? sum : rounded);
+                    exact_row[i] = exact_row[i] * alpha + sum;
 #pragma unroll
                     for (int b = 0; b < C::NB; ++b) {
                         const bf16x8_t f = frag(finite_only(__builtin_bit_cast(u32x4, value(t, b))));
@@ -412,6 +427,8 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
             for (int t = 0; t < MT; ++t) {
                 l_row[t] += __shfl_xor(l_row[t], 16);
                 l_row[t] += __shfl_xor(l_row[t], 32);
+                exact_row[t] += __shfl_xor(exact_row[t], 16);
+                exact_row[t] += __shfl_xor(exact_row[t], 32);
             }
         }
     }
@@ -433,15 +450,16 @@ __global__ __launch_bounds__(64 * NW, few_waves(SHARED ? DV : -DV, 16 * MT)) voi
             }
             if (a.lse && w == 0 && g == 0)
                 a.lse[(int64_t)head * a.n_tokens + s.start + tok] =
-                    none ? neg_inf() : fmaf(m_row[t] * kLn2, a.scale_log2, logf(l_row[t]));
+                    none ? neg_inf() : fmaf(m_row[t] * kLn2, a.scale_log2, logf(exact_row[t]));
         } else {
-            float *slot = a.part + (int64_t)(item.slot + item.part * item.step) * (C::ROWS * (DV + 2));
-            const float by = moderate(&m_row[t], &l_row[t], a.scale_log2);
+            float *slot = a.part + (int64_t)(item.slot + item.part * item.step) * (C::ROWS * part_width(DV));
+            const float by = moderate(&m_row[t], &l_row[t], &exact_row[t], a.scale_log2);
 #pragma unroll
             for (int b = 0; b < C::NB; ++b) *(f32x4_t *)(slot + r * DV + 16 * (w * C::NB + b) + 4 * g) = o[t][b] * by;
             if (w == 0 && g == 0) {
                 slot[C::ROWS * DV + r] = m_row[t];
                 slot[C::ROWS * DV + C::ROWS + r] = l_row[t];
+                if (!SHARED) slot[C::ROWS * DV + 2 * C::ROWS + r] = exact_row[t];
             }
         }
     }
@@ -453,38 +471,40 @@ template <int D, int ROWS, bool WIDE, int CH>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedArgs a) {
     constexpr int kLanes = kJoinThreads / (CH / 4), kAtOnce = 4;
     __shared__ join_f32x4 sum[kLanes][CH / 4];
-    __shared__ float top[kLanes], total[kLanes];
+    __shared__ float top[kLanes], total[kLanes], exact[kLanes];
     if ((int)blockIdx.x >= a.joins[0].count) return;
     const JoinItem j = a.joins[blockIdx.x];
     const int r = blockIdx.y, d = threadIdx.x % (CH / 4), lane = threadIdx.x / (CH / 4), ch = CH * blockIdx.z + 4 * d;
     if (r >= j.rows) return;
-    const int64_t step = (int64_t)j.step * (ROWS * (D + 2));
-    const float *p = a.part + (int64_t)j.slot * (ROWS * (D + 2)), *po = p + r * D + ch, *pm = p + ROWS * D + r, *pl = pm + ROWS;
+    const int64_t step = (int64_t)j.step * (ROWS * part_width(D));
+    const float *p = a.part + (int64_t)j.slot * (ROWS * part_width(D)), *po = p + r * D + ch, *pm = p + ROWS * D + r, *pl = pm + ROWS;
     Joined x;
     for (int k0 = lane; k0 < j.parts; k0 += kAtOnce * kLanes) {
-        float m[kAtOnce], l[kAtOnce];
+        float m[kAtOnce], l[kAtOnce], e[kAtOnce];
         join_f32x4 o[kAtOnce];
 #pragma unroll
         for (int k = 0; k < kAtOnce; ++k) {
             const int64_t at = min(k0 + k * kLanes, j.parts - 1) * step;
             m[k] = pm[at];
             l[k] = pl[at];
+            e[k] = WIDE ? 0.f : pl[at + ROWS];
             o[k] = *(const join_f32x4 *)(po + at);
         }
         // (all loads before the first use: one memory latency, not one each)
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int k = 0; k < kAtOnce; ++k)
-            if (k0 + k * kLanes < j.parts) x.add(m[k], l[k], o[k], a.scale_log2);
+            if (k0 + k * kLanes < j.parts) x.add(m[k], l[k], e[k], o[k], a.scale_log2);
     }
     sum[lane][d] = x.acc;
     if (d == 0) {
         top[lane] = x.M;
         total[lane] = x.L;
+        exact[lane] = x.E;
     }
     __syncthreads();
     if (lane > 0) return;
-    for (int i = 1; i < kLanes; ++i) x.add(top[i], total[i], sum[i][d], a.scale_log2);
+    for (int i = 1; i < kLanes; ++i) x.add(top[i], total[i], exact[i], sum[i][d], a.scale_log2);
     x.put<WIDE>(a, j, r, ch);
 }
 

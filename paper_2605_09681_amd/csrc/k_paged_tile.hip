@@ -12,8 +12,8 @@
 //   O^T += V^T P^T (A = V^T through the LDS transpose read, P straight from S^T).
 // Where a row's sum leaves [2^-64, 2^100] (weights below 2^-126 are lost, and would count) or an output is not
 // finite, and where an infinity or a NaN lies among values that only some rows see, the part is
-// computed again, tile by tile with a running maximum.  The sum adds the probabilities as they
-// are; where no lse is asked for, the rounded ones that weight the values, two at a time.
+// computed again, tile by tile with a running maximum.  The sum adds the rounded probabilities that
+// weight the values, two at a time; lse takes another one of the probabilities as they are.
 //
 // The matrix units bound it, so everything is arranged around their stream: the products of a
 // tile are one pinned sequence (scores of key block 1, values of block 0, scores of the next
@@ -117,14 +117,14 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
     }
     if (EXPANDED) base = first_row(a, at.i);
     f32x16_t o[MB];
-    float m = neg_inf(), l = 0.f;
+    float m = neg_inf(), l = 0.f, exact = 0.f;    // exact (LSE): the sum of the weights as they are, not as they are rounded
     // This lane's row of the item before, whose results are stored while the next one's first tiles are on their way.
     int pending = 0;                              // 1: an output row, 2: a part of one
     bool none = false;                            // the row sees no key
     int64_t out_at = 0, lse_at = 0;               // where it goes: in O and lse, or (a part) in `part`
     auto clear = [&]() {
         m = neg_inf();
-        l = 0.f;
+        l = exact = 0.f;
 #pragma unroll
         for (int b = 0; b < MB; ++b)
 #pragma unroll
@@ -139,10 +139,10 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
                     *(uint2 *)(to + 32 * b + 8 * u) = pack4(o[b][4 * u] * inv, o[b][4 * u + 1] * inv, o[b][4 * u + 2] * inv, o[b][4 * u + 3] * inv);
-            if (LSE && hh == 0) a.lse[lse_at] = none ? neg_inf() : fmaf(m * kLn2, a.scale_log2, logf(l));
+            if (LSE && hh == 0) a.lse[lse_at] = none ? neg_inf() : fmaf(m * kLn2, a.scale_log2, logf(exact));
         } else if (pending == 2) {
             float *to = a.part + out_at;
-            const float by = moderate(&m, &l, a.scale_log2);
+            const float by = moderate(&m, &l, &exact, a.scale_log2);
 #pragma unroll
             for (int b = 0; b < MB; ++b)
 #pragma unroll
@@ -151,6 +151,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
             if (hh == 0) {
                 a.part[lse_at] = m;
                 a.part[lse_at + ROWS] = l;
+                if (LSE) a.part[lse_at + 2 * ROWS] = exact;
             }
         }
         pending = 0;
@@ -323,7 +324,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
             const bool far = __ballot(!(fabsf(m * a.scale_log2) < kFar)) != 0;
             const float cm = far ? 0.f : m * a.scale_log2;
             bool met = false;
-            float sum[2] = {0.f, 0.f}, v[2];
+            float sum[2] = {0.f, 0.f}, all_sum[2] = {0.f, 0.f}, v[2];
             u32x4 p[2][2];                            // probabilities, two bf16 a word: key block, 16 keys
             auto ready = [&](int j, int kb) {         // a key block's scores are complete, and not those of an ordinary tile
                 hide(j, kb, z[kb]);
@@ -331,8 +332,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
 #pragma unroll
                 for (int r = 0; r < 16; ++r) met |= z[kb][r] != neg_inf();
             };
-            // Half of the work on scores 2 i and 2 i + 1 of key block kb.  The sum is of the probabilities as they
-            // are, or, without LSE, of the rounded ones that weight the values, two at a time.
+            // Half of the work on scores 2 i and 2 i + 1 of key block kb.
             auto step = [&](int kb, int i, int half) __attribute__((always_inline)) {
                 if (half == 0) {
                     v[0] = fmaf(z[kb][2 * i], a.scale_log2, -cm);
@@ -341,13 +341,12 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
                 } else {
                     v[1] = __builtin_amdgcn_exp2f(v[1]);
                     if (LSE) {
-                        sum[0] += v[0];
-                        sum[1] += v[1];
+                        all_sum[0] += v[0];
+                        all_sum[1] += v[1];
                     }
                     uint32_t word = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{v[0], v[1]}, bf16x2_t));
                     asm volatile("" : "+v"(word));     // (not moved to its use)
-                    if (!LSE)
-                        sum[i & 1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, word), __builtin_bit_cast(bf16x2_t, 0x3f803f80), sum[i & 1], false);
+                    sum[i & 1] = add_two(word, sum[i & 1]);
                     p[kb][i >> 2][i & 3] = word;
                 }
             };
@@ -413,6 +412,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
                     }
                     if constexpr (i == kB - 1) {
                         l = sum[0] + sum[1];           // (the last time without the tile after the last)
+                        if (LSE) exact = all_sum[0] + all_sum[1];
                         j0 = jn;
                         edge = edge_n || far;
                         if (edge) ready(j0, 0);
@@ -455,7 +455,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
                         f32x16_t z;
                         score(kt, kb, z);
                         hide(j, kb, z);
-                        float top = neg_inf(), sum = 0.f;
+                        float top = neg_inf(), sum = 0.f, rounded = 0.f;
 #pragma unroll
                         for (int r = 0; r < 16; ++r) top = fmaxf(top, z[r]);
                         const float up = fmaxf(m, across_max(top)), base = up == neg_inf() ? 0.f : up;
@@ -467,8 +467,10 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
                             const float v = __builtin_amdgcn_exp2f((z[r] - base) * a.scale_log2);
                             sum += v;
                             p[r >> 3][r & 7] = (__bf16)v;
+                            rounded += (float)p[r >> 3][r & 7];
                         }
-                        l = l * alpha + sum;
+                        l = l * alpha + rounded;
+                        exact = exact * alpha + sum;
 #pragma unroll
                         for (int b = 0; b < MB; ++b) {
                             o[b] *= alpha;
@@ -496,6 +498,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
         }
 
         l += __shfl_xor(l, 32);
+        if (LSE) exact += __shfl_xor(exact, 32);
         none = blind(seen, sink);
         if (live && whole && (tb < te || !shared || (item_at >= from && item_at < until))) {   // (no key: who has the item's begin)
             pending = 1;
@@ -521,7 +524,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_tile_kernel(Pa
                 }
             }
             pending = 2;
-            const int64_t slot = (int64_t)(2 * number + (tb == 0)) * (ROWS * (DV + 2));
+            const int64_t slot = (int64_t)(2 * number + (tb == 0)) * (ROWS * part_width(DV));
             out_at = slot + (32 * w + c) * DV + 4 * hh;
             lse_at = slot + ROWS * DV + 32 * w + c;
         }
@@ -551,14 +554,14 @@ constexpr int join_rows() { return kJoinThreads / (D / 4); }
 
 template <int D, int ROWS>
 __global__ __launch_bounds__(kJoinThreads) void paged_share_join_kernel(PagedArgs a) {
-    constexpr int64_t kSlot = ROWS * (D + 2);
+    constexpr int64_t kSlot = ROWS * part_width(D);
     const JoinItem j = a.joins[blockIdx.x];
     const int d = threadIdx.x % (D / 4), r = blockIdx.y * join_rows<D>() + threadIdx.x / (D / 4);
     if (r >= j.rows) return;
     Joined x;
     constexpr int kAtOnce = 4;
     for (int k0 = 0; k0 < j.parts; k0 += kAtOnce) {
-        float m[kAtOnce], l[kAtOnce];
+        float m[kAtOnce], l[kAtOnce], e[kAtOnce];
         join_f32x4 o[kAtOnce];
         int on[kAtOnce];
 #pragma unroll
@@ -568,12 +571,13 @@ __global__ __launch_bounds__(kJoinThreads) void paged_share_join_kernel(PagedArg
             on[k] = a.joins[g].goes_on;
             m[k] = p[ROWS * D + r];
             l[k] = p[ROWS * D + ROWS + r];
+            e[k] = p[ROWS * D + 2 * ROWS + r];            // (only written and used for lse)
             o[k] = *(const join_f32x4 *)(p + r * D + 4 * d);
         }
         __builtin_amdgcn_sched_barrier(0);                // (all loads before the first use)
 #pragma unroll
         for (int k = 0; k < kAtOnce; ++k)
-            if (k0 + k == 0 || (k0 + k < j.parts && on[k])) x.add(m[k], l[k], o[k], a.scale_log2);
+            if (k0 + k == 0 || (k0 + k < j.parts && on[k])) x.add(m[k], l[k], e[k], o[k], a.scale_log2);
     }
     x.put(a, j, r, 4 * d);
 }

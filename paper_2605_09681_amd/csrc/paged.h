@@ -65,6 +65,9 @@ constexpr int few_groups(int dim, int rows) {
     return dim == -64 ? (rows <= 16 ? 5 : rows <= 32 ? 4 : 3) : dim == -128 ? (rows <= 32 ? 3 : 2) : dim == 256 && rows <= 32 ? 2 : 1;
 }
 constexpr int few_waves(int dim, int rows) { return few_groups(dim, rows) * (dim < 0 ? 1 : 2); }   // per SIMD
+// Floats of a row of a part's slot: its output, its reference, the sum of its weights as they weigh the values, and as
+// they are (for lse).  A slot holds all rows' outputs, then their references and sums.
+constexpr int part_width(int d) { return d + 3; }
 inline int paged_row_tile(int rows) { return rows <= 64 ? (rows + 15) / 16 * 16 : 64; }
 
 // Rows into the pages (k_paged_append.hip).
@@ -534,6 +537,12 @@ __device__ __forceinline__ int place(int k, int c) {
     return c ^ (KEYS ? (k >> 1 & 7) : ((k >> 1 & 1) << 2 | (k >> 2 & 3)));
 }
 
+// sum + the two bf16 of a word, one rounding.
+__device__ __forceinline__ float add_two(uint32_t word, float sum) {
+    typedef __bf16 pair_t __attribute__((ext_vector_type(2)));
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pair_t, word), __builtin_bit_cast(pair_t, 0x3f803f80), sum, false);
+}
+
 // Any of the 8 bf16 of v is an infinity or a NaN.
 __device__ __forceinline__ bool special(const u32x4 &v) {
     bool s = false;
@@ -554,12 +563,13 @@ __device__ __forceinline__ float special_only(uint32_t bits) { return (bits & 0x
 // A part's sum far from 1 (its reference far from its largest score) moves into its reference by a power of two,
 // so that joining it with other parts' loses nothing; the factor for its outputs.  (Where that power would leave the
 // range of a score the parts' references are too near one another to need it.)
-__device__ __forceinline__ float moderate(float *m, float *l, float scale_log2) {
+__device__ __forceinline__ float moderate(float *m, float *l, float *exact, float scale_log2) {
     if (!(*l > 0.f) || (*l > 0x1p-20f && *l < 0x1p20f) || !(*l < __builtin_inff()) || scale_log2 < 0x1p-100f) return 1.f;
     const int k = __builtin_amdgcn_frexp_expf(*l);
     *m += (float)k / scale_log2;
     const float by = __builtin_amdgcn_ldexpf(1.f, -k);
     *l *= by;
+    *exact *= by;
     return by;
 }
 
