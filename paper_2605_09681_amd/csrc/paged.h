@@ -148,14 +148,20 @@ struct Seq {
 // it, so that a row belongs to one sequence at most and all sequences' rows are no more than the batch has, which
 // the host's bounds on items, slots and joins rest on.
 __device__ __forceinline__ Seq sequence(const PagedArgs &a, int i0, int *held) {
-    const int i = i0 + (threadIdx.x & 63);
-    const bool mine = i < a.n_seqs;
-    auto row = [&](int k) { return min(max(a.q_start[k], 0), a.n_tokens); };
-    const int start = max(scan_max(mine ? row(i) : 0), *held), end = mine ? max(row(i + 1), start) : start;
+    const int i = i0 + (threadIdx.x & 63), k = min(i, a.n_seqs - 1);
+    const int len = a.seq_len[k], from = a.q_start[k], to = a.q_start[k + 1];
+    // (lanes behind the last sequence: its end)
+    int end = min(max(to, 0), a.n_tokens), start = i < a.n_seqs ? min(max(from, 0), a.n_tokens) : end;
+    // A branch: with the maximum taken in any case and loads between its steps, attention of one token each of 1024
+    // sequences of 100 took 147 us instead of 103.
+    if (__ballot(end < start || start < *held) != 0) {
+        start = max(scan_max(start), *held);
+        end = max(end, start);
+    }
     *held = __builtin_amdgcn_readlane(end, 63);
     Seq s = {0, 0, 0, 0};
-    if (mine) {
-        s.len = min(max(a.seq_len[i], 0), a.cap);
+    if (i < a.n_seqs) {
+        s.len = min(max(len, 0), a.cap);
         s.start = start;
         s.n = min(end - start, a.max_new);
         s.first = s.len - (end - start);

@@ -115,6 +115,10 @@ inline int __builtin_amdgcn_frexp_expf(float x) {
     frexpf(x, &e);
     return e;
 }
+template <class T>
+inline float __builtin_amdgcn_fdot2_f32_bf16(T a, T b, float c, bool) {
+    return (float)((double)(float)a[0] * (float)b[0] + (double)(float)a[1] * (float)b[1] + c);
+}
 inline float __builtin_amdgcn_ldexpf(float x, int e) { return ldexpf(x, e); }
 inline float __builtin_amdgcn_exp2f(float x) { return exp2f(x); }
 inline int __float_as_int(float x) { return __builtin_bit_cast(int, x); }
