@@ -3,6 +3,7 @@
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
+#include <stdlib.h>
 #include <string.h>
 
 #include <algorithm>
@@ -60,7 +61,17 @@ fkv_status check_heads(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim) {
     return FKV_OK;
 }
 
-// out: rows that are written, of `width` elements.
+// Whether rows h * head + t * token of `width` elements share some.
+bool overlap(int64_t heads, int64_t tokens, int64_t head, int64_t token, int64_t width) {
+    if ((heads > 1 && head < width) || (tokens > 1 && token < width)) return true;
+    if (heads == 1 || tokens == 1 || head >= (tokens - 1) * token + width || token >= (heads - 1) * head + width) return false;
+    for (int64_t h = 1; h < heads; ++h)                   // the nearest of the tokens before and after
+        for (int64_t t = h * head / token; t <= h * head / token + 1; ++t)
+            if (t < tokens && std::abs(h * head - t * token) < width) return true;
+    return false;
+}
+
+// out_width: of rows that are written.
 fkv_status check_rows(const fkv_rows *r, int elem, const char *name, int n_heads, int n_tokens, int out_width = 0) {
     if (!r || !r->data) return fail(FKV_ERR_ARG, "%s: NULL tensor pointer", name);
     if (!aligned(r->data, 16)) return fail(FKV_ERR_ARG, "%s is not 16-byte aligned", name);
@@ -69,7 +80,7 @@ fkv_status check_rows(const fkv_rows *r, int elem, const char *name, int n_heads
         r->token_stride > most)
         return fail(FKV_ERR_ARG, "%s: strides %lld and %lld must be multiples of %lld elements in [0, 2^36]", name,
                     (long long)r->head_stride, (long long)r->token_stride, (long long)per);
-    if (out_width && ((n_heads > 1 && r->head_stride < out_width) || (n_tokens > 1 && r->token_stride < out_width)))
+    if (out_width && overlap(n_heads, n_tokens, r->head_stride, r->token_stride, out_width))
         return fail(FKV_ERR_ARG, "%s: rows of %d elements overlap at strides %lld and %lld", name, out_width,
                     (long long)r->head_stride, (long long)r->token_stride);
     return FKV_OK;

@@ -202,3 +202,35 @@ def test_append_launches(host, heads, d, dtype, n_tokens):
     assert host.host_append(ctypes.byref(case.c), heads, d, dtype, 0) == 0
     tokens = host.host_block_tokens()
     assert 1 <= tokens <= 64 and -(-n_tokens // tokens) * 256 < 1 << 32
+
+
+def overlapping(heads, tokens, width, head, token):
+    rows = sorted(h * head + t * token for h in range(heads) for t in range(tokens))
+    return any(b - a < width for a, b in zip(rows, rows[1:]))
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_outputs_that_overlap(seed):
+    """Rows of an output that share elements are refused, whatever the strides of heads and tokens; others are not (that
+    call then stops at its workspace)."""
+    import paper_2605_09681_amd as fkv
+    if not os.path.exists(fkv.LIB_PATH):
+        build.build()
+    rng = random.Random(seed)
+    seen = set()
+    cases = [(4, 6, 128, 128), (4, 6, 768, 128), (4, 6, 128, 512), (2, 3, 384, 256), (2, 50, 128, 256), (3, 2, 256, 384)]
+    for k in range(400):
+        heads, tokens = rng.choice([1, 2, 3, 5, 64]), rng.choice([1, 2, 3, 7, 40])
+        head, token = (8 * rng.choice([0, 16, rng.randint(1, 40), rng.randint(1, 800), 16 * rng.randint(1, 100)]) for _ in range(2))
+        cases.append((heads, tokens, head, token))
+    for heads, tokens, head, token in cases:
+        batch = fkv.fkv_batch(n_seqs=1, max_pages=4, page_tokens=16, n_pages=9, n_tokens=tokens, max_new=4, sum_len=70,
+                              page_table=0x1000, seq_len=0x1000, q_start=0x1000)
+        rows = lambda h, t: ctypes.byref(fkv.fkv_rows(0x1000, h, t))  # noqa: E731
+        st = fkv.lib().fkv_latent_attention(ctypes.byref(batch), heads, 128, 256, rows(192, 12288), 0x1000, 0x1000, 0x1000, 1, None, 0.1,
+                                            rows(head, token), 0, None, 0, None)
+        assert st == 1
+        bad = overlapping(heads, tokens, 128, head, token)
+        assert ("overlap" in fkv.fkv_last_error()) == bad, (heads, tokens, head, token, fkv.fkv_last_error())
+        seen.add(bad)
+    assert seen == {True, False}
