@@ -182,7 +182,8 @@ __global__ __launch_bounds__(NT) void latent_unabsorb_few_kernel(LatentArgs a, i
 // first operands are on their way while a block's results are stored.  The first workgroup of a token block copies its
 // rotated keys to every head.  Bound by latency between its few steps and by its 120 MB of results: 15600 tokens, 12 heads of
 // 128, 512 latent channels (49 GFLOP) 75 to 95 us; with blocks of 128 x 128 95 to 120, stored 8 bytes a token and lane 90 to
-// 114.  grid: x = every gridDim.x'th channel block, y = token block.
+// 114.  Two registers (14 at D 64) do not fit and are stored outside the products.  grid: x = every gridDim.x'th channel
+// block, y = token block.
 template <int D, int R>
 __global__ __launch_bounds__(512, 2) void latent_expand_kernel(LatentArgs a) {
     constexpr int NT = 512, STEP = 64, N = 256 * STEP / 8 / NT;      // chunks per thread and operand

@@ -1,17 +1,18 @@
 // k_paged_attn.hip -- attention of few new tokens of many sequences over paged caches,
 // gfx950 MFMA: single tokens and short chunks (up to 64 query rows of a sequence and key
-// head, or any number over latent rows), with keys and values of their own or, SHARED,
-// with values that are the first DV channels of the key rows (latent rows: all heads
-// read one row).
+// head, 256 where the batch's keys are known to be few, or any number over latent rows), with
+// keys and values of their own or, SHARED, with values that are the first DV channels of the
+// key rows (latent rows: all heads read one row).
 //
 //   o = sum_j 2^(c (s_j - m)) v_j / sum_j 2^(c (s_j - m)),  s_j = q . k_j,  c = scale log2 e
 //
 // A workgroup takes one part of an item (sequence, key head, tile of 16 MT query rows)
 // and walks its keys 32 at a time.  The NW waves share each tile of keys, which is read
-// from HBM once and lies in LDS, three tiles deep:
+// once for the item's up to 64 rows and lies in LDS, three tiles deep:
 //   scores   S^T = K Q^T (v_mfma_f32_16x16x32_bf16): the tile's 2 x MT blocks of 16 keys
 //            and 16 rows are dealt to the waves, which turn theirs into probabilities
-//            and put those into LDS (bf16; the sum adds them before they are rounded);
+//            and put those into LDS (bf16; the sum that divides the output adds them as they
+//            are rounded, lse's as they are);
 //   values   O^T += V^T P^T: each wave owns DV / NW output channels of all rows (V^T
 //            through the LDS transpose read).  SHARED leaves its outputs in fp32 to the product that follows.
 // The scores of tile t + 1 and the values of tile t run in the same stretch between two
@@ -26,13 +27,16 @@
 // maximum (`careful`).
 //
 // Why so: few rows are bound by the bytes of their keys, so the keys of a sequence are split
-// over the device (Split), a tile is read once for all rows, and each CU has 16 to 48 KB of them
+// over the device (Split), a tile is read once for 64 rows (more rows are more items, each of which
+// reads the keys again, from the caches where they are few), and each CU has 16 to 48 KB of them
 // on their way.  480P, one token over 32761 keys of 12 heads (201 MB): 34 us and 4 for the
 // join; 16 sequences of up to 7800 tokens, 16 heads over 4 key heads (76 MB): 18.5 and 4 us, 4.1
 // TB/s; the same over latent rows of 576, 40 heads (54 MB): 25 and 8.5 us.  Of the last, 2 us are the
 // split, 6 the first two tiles and the queries, 6 five tiles, 3 the output (82 KB a workgroup).
 // Measured beside it: every wave forming all probabilities from scores in LDS (40 heads 67 us), parts of
 // 256 keys instead of 128 (latent rows: 16.2 against 12.9 us for one token).
+// Registers: latent rows of 320 channels with 16 and 32 query rows have 18 and 59 fewer than they would use in the
+// 128 that two workgroups a CU leave (2 and 7 reloads a tile), those of 576 with 64 rows 31.
 #include <type_traits>
 
 #include "paged_join.h"

@@ -21,16 +21,20 @@
 // VALU instructions each, and operands read four products ahead.  LDS rows are padded so that
 // every read is one address and a constant (with chunks placed by exclusive-or instead, 24
 // VALU instructions a tile more).  At 480P (12 heads of 128, 4680 rows over 37440 keys, 1.08
-// TFLOP) 1.04 to 1.20 ms as the card is cool or hot, 0.9 to 1.04 PFLOP/s; products in 59% of
-// the cycles.  Steps: running maxima and 128 rows, two workgroups a CU 1510 us; the pinned
+// TFLOP) 1.04 to 1.20 ms as the card is cool or hot, 0.9 to 1.04 PFLOP/s; products in 57% of
+// the cycles.  Attention over one history in place (k_attn.hip) does the same sums in 0.97 ms where this takes
+// 1.07, in turn on one card: it transposes values on their way into LDS, this reads two transposed halves for
+// each value product (1.6 LDS instructions a product in place of 1.2).  Steps: running maxima and 128 rows, two workgroups a CU 1510 us; the pinned
 // stream with 256 rows 1250; padded rows, rotating buffers, contiguous rows read from one
 // address 1210; equal shares 1130 (228 items leave 28 CUs idle otherwise; with 14 heads, 266
 // items, 1970 without and 1270 with); results stored under the next item's first loads 1070.  An item
 // costs some 10 us beside its tiles (4 the first loads, 1 the reference, 3 the output);
 // prompts of 1700 to 3500 tokens, 40 heads over 8, five items a workgroup, reach 0.73 PFLOP/s
-// for that (242 GFLOP, 333 us), one prompt of 8192 tokens and 16 heads 0.85.  Measured beside it,
+// for that (242 GFLOP, 347 us, 0.70 on a hot card), one prompt of 8192 tokens and 16 heads 0.83.  Measured beside it,
 // slower: 128 rows and two workgroups a CU in the same stream (1270 us, prompts 490 against
-// 440), tiles loaded through four unrolled buffers (spills).
+// 440), tiles loaded through four unrolled buffers (spills in the loop over tiles).  Registers: at head_dim 128
+// 24 values and more do not fit (41 with lse, 32 over expanded copies, 52 and 68 with 128 rows).  They are stored and
+// loaded in an item's setup and output; in the loop over tiles 3 are, with 128 rows and lse.
 #include <type_traits>
 #include <utility>
 
