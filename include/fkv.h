@@ -757,7 +757,7 @@ fkv_status fkv_paged_attention(const fkv_batch *batch, int32_t n_heads, int32_t 
  *                        all absorbed where sum_len is 0.
  * Absorbed queries, expanded keys and values, and the expanded form's probabilities are
  * rounded to bf16; the absorbed form's probabilities and latent outputs are not (off by
- * 2.9e-3 and 2.3e-3 from 64 bits in relative 2-norm, a bf16 output alone by 1.7e-3).  The
+ * 3.1e-3 and 2.3e-3 at most from 64 bits in relative 2-norm, a bf16 output alone by 1.7e-3).  The
  * workspace (fkv_latent_attention_workspace_size bytes for the same batch sizes and form,
  * no initialisation, shared in turn) is needed.  FKV_ERR_SHAPE also for a sum_len above 2^30 and an expanded form of more
  * than 65535 blocks of 256 tokens (one more a sequence than sum_len needs) or of 4 GiB

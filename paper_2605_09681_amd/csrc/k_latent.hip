@@ -4,9 +4,10 @@
 // queries themselves are, and o_h = W_v,h o'_h after it, o' in fp32 as the sum of two bf16.
 // Expanded form: k_h = W_k,h c and v_h = W_v,h c of every cached token, rounded to bf16
 // as a cache of its own keys and values would hold them.  With the probabilities and the output that
-// makes four roundings to bf16 of 1.4e-3 to 1.7e-3 each, 2.9e-3 together at the most (relative 2-norm against 64
-// bits), where the absorbed form has 2.3e-3.  Keys, values or probabilities as the sum of two bf16 would take 1.4 to 1.6
-// times the products each and save one of the four; fp16 has the digits but not the range of the latent rows.
+// makes four roundings to bf16 of 1.4e-3 to 1.7e-3 each, 3.1e-3 together at the most (measured 1.9e-3 to
+// 3.0e-3, relative 2-norm against 64 bits), where the absorbed form has 2.3e-3.  Keys, values or
+// probabilities as the sum of two bf16 would take 1.4 to 1.6 times the products each and save one of the
+// four; fp16 has the digits but not the range of the latent rows.
 #include <algorithm>
 
 #include "paged.h"
